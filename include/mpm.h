@@ -392,6 +392,125 @@ typedef enum {
 MPM_API mpm_status mpm_trace_read(uint64_t* out);
 MPM_API mpm_status mpm_trace_reset(void);
 
+/*
+ * Encoder-block operators (the paper has no counterpart: it leaves the
+ * blocks between two insertions to the model).  They work on the packed
+ * ragged rows that mpm_merge writes, so that what surrounds a merge in an
+ * encoder can stay in this library: the norms, gate and residual addition
+ * around a block in one pass, and linear layers on 4-bit operands.
+ *
+ * Unlike the entry points above they take rows of any width and alignment:
+ * `..._stride` is the distance of two rows in elements (>= dim where there are
+ * several rows), buffers need only the alignment of their elements, and
+ * outputs without a stride are contiguous.  Whole 16-byte rows are fastest.
+ */
+typedef enum mpm_norm_kind {
+  MPM_NORM_RMS = 0,   /* v / sqrt(mean(v^2) + eps) */
+  MPM_NORM_LAYER = 1  /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) */
+} mpm_norm_kind;
+
+/*
+ * The norm after a block, its gate, the scaled residual stream and the norm
+ * before the next block.  For every row, with N the normalisation above:
+ *   u            = N(y) * post_weight + post_bias
+ *   residual_out = residual_scale * residual + gate * u
+ *   h            = N(residual_out) * pre_weight + pre_bias
+ * All arithmetic is fp32; h is taken from residual_out before that is rounded.
+ *
+ *   y             [rows, dim] the block's output (dtype)
+ *   residual      [rows, dim] the residual stream (stream_dtype: dtype, or
+ *                 MPM_F32 with bf16 blocks; otherwise MPM_ERR_UNSUPPORTED)
+ *   offsets       int64 [batch + 1] device offsets of the images, or NULL:
+ *                 every row is taken, and batch only has to be >= 1.  With
+ *                 offsets, rows from offsets[batch] on are neither read nor
+ *                 written.
+ *   post_weight   float [dim], or NULL: u = y.  post_bias: float [dim] or NULL.
+ *   gate          float [dim], float [batch, dim] when gate_per_image != 0
+ *                 (needs offsets), or NULL: 1.
+ *   pre_weight    float [dim], or NULL (then h is NULL too: only the stream is
+ *                 written).  pre_bias: float [dim] or NULL.
+ *   residual_out  [rows, dim] (stream_dtype); may be `residual` itself when
+ *                 that is contiguous
+ *   h             [rows, dim] (dtype)
+ *   stats         optional float [rows, 4], 16-byte aligned, for the backward
+ *                 pass: mean and 1 / deviation of both norms (0 and 1 for one
+ *                 that is absent)
+ *   device_status optional int32 [2] device word: offsets that are not
+ *                 0 = off[0] <= ... <= off[batch] <= rows are reported as
+ *                 MPM_ERR_DEVICE_CHECK (detail = index); no access leaves the
+ *                 buffers either way.
+ * eps >= 0.  An image may be empty.  Other overlaps of an output with an
+ * input or another output: MPM_ERR_ALIASING.
+ */
+MPM_API mpm_status mpm_block_norm(const void* y, int64_t y_stride, const void* residual, int64_t residual_stride,
+                                  const int64_t* offsets, int32_t batch, int64_t rows, int32_t dim, mpm_dtype dtype,
+                                  mpm_dtype stream_dtype, mpm_norm_kind norm, float eps, float residual_scale,
+                                  const float* post_weight, const float* post_bias, const float* gate,
+                                  int32_t gate_per_image, const float* pre_weight, const float* pre_bias,
+                                  void* residual_out, void* h, float* stats, int32_t* device_status, void* stream);
+
+/* Bytes of device workspace of mpm_block_norm_backward (256-byte aligned); 0 for an invalid dim. */
+MPM_API size_t mpm_block_norm_workspace_size(int32_t dim);
+
+/*
+ * Gradients of mpm_block_norm, from the gradients of its outputs, its inputs
+ * and the statistics that it kept.
+ *   d_residual_out, d_h  gradients of residual_out and h; NULL: zero
+ *   d_y, d_residual      [rows, dim], written for the rows of images
+ *   d_post_weight, d_post_bias, d_gate, d_pre_weight, d_pre_bias
+ *                        float gradients of the parameters, NULL where not
+ *                        wanted; d_gate has the gate's shape.  Written whole
+ *                        (zeros for an empty image, or without rows).
+ *   workspace            mpm_block_norm_workspace_size(dim) bytes
+ * Sums are taken in fp32 in a fixed order: the same call gives the same bits.
+ */
+MPM_API mpm_status mpm_block_norm_backward(
+    const void* d_residual_out, int64_t d_residual_out_stride, const void* d_h, int64_t d_h_stride, const void* y,
+    int64_t y_stride, const void* residual, int64_t residual_stride, const float* stats, const int64_t* offsets,
+    int32_t batch, int64_t rows, int32_t dim, mpm_dtype dtype, mpm_dtype stream_dtype, mpm_norm_kind norm,
+    float residual_scale, const float* post_weight, const float* post_bias, const float* gate, int32_t gate_per_image,
+    const float* pre_weight, void* d_y, void* d_residual, float* d_post_weight, float* d_post_bias, float* d_gate,
+    float* d_pre_weight, float* d_pre_bias, void* workspace, size_t workspace_bytes, int32_t* device_status,
+    void* stream);
+
+/*
+ * MXFP4 (OCP Microscaling Formats 1.0): along a row, 32 neighbouring values
+ * share the scale 2^(c - 127), c = max(floor(log2(max |v|)) - 2 + 127, 0), and
+ * each is the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times it (ties to the
+ * even code; above 6: 6).  A block with a NaN or an infinity gets the scale
+ * code of NaN (255) and reads back as NaN.
+ *   codes   rows of 32 * ceil(dim / 64) bytes: element 2i in the low half of
+ *           byte i, 2i + 1 in the high half (sign, two exponent bits, one
+ *           mantissa bit); zeros after the row's own
+ *   scales  [ceil(rows / 128), ceil(dim / 128), 512] bytes: scale j of row r of
+ *           a tile of 128 rows x 4 blocks is byte 16 (r % 32) + 4 (r / 32) + j;
+ *           zeros where a tile reaches past the rows or the row
+ * Both are 16-byte aligned.  1 <= dim <= MPM_MXFP4_MAX_DIM.
+ */
+#define MPM_MXFP4_MAX_DIM (1 << 20)
+/* Bytes of the codes and of the scales of [rows, dim] values (0 for invalid sizes, or no rows). */
+MPM_API size_t mpm_mxfp4_code_bytes(int64_t rows, int32_t dim);
+MPM_API size_t mpm_mxfp4_scale_bytes(int64_t rows, int32_t dim);
+MPM_API mpm_status mpm_mxfp4_quantize(const void* tokens, int64_t stride, int64_t rows, int32_t dim, mpm_dtype dtype,
+                                      uint8_t* codes, uint8_t* scales, void* stream);
+/* out = the values that codes and scales stand for, rounded to dtype (exact but for fp32's and bf16's own range). */
+MPM_API mpm_status mpm_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t dim,
+                                        mpm_dtype dtype, void* out, int64_t out_stride, void* stream);
+
+/*
+ * A linear layer on MXFP4 operands: out[i, j] = sum_t a[i, t] b[j, t] + bias[j],
+ * summed in fp32 on the tensor cores and rounded once to dtype.
+ *   a  [m, k] tokens and b [n, k] weights, codes and scales as above
+ *   bias           float [n] or NULL
+ *   out            m rows of n values (dtype), out_stride elements apart
+ *   device_status  optional int32 [2] device word: a wait in the kernel that
+ *                  ran out is reported as MPM_ERR_DEVICE_TIMEOUT
+ * m, n <= 2^30.
+ */
+MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int64_t m, const uint8_t* b_codes,
+                                    const uint8_t* b_scales, int32_t n, int32_t k, const float* bias, mpm_dtype dtype,
+                                    void* out, int64_t out_stride, int32_t* device_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

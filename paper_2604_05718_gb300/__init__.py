@@ -2,9 +2,21 @@
 
 The compute path lives in ``libmpm.so`` (CUDA kernels for sm_103a, built by
 ``paper_2604_05718_gb300.build.build()``); ``paper_2604_05718_gb300.mpm``
-marshals torch tensors into its C entry points.
+(the merge) and ``paper_2604_05718_gb300.blocks`` (the encoder blocks around
+it: fused norms, 4-bit linear layers) marshal torch tensors into its C entry
+points.
 """
 
+from .blocks import (  # noqa: F401
+    MXFP4,
+    BlockNormGrads,
+    block_norm,
+    block_norm_backward,
+    block_norm_workspace,
+    dequantize_mxfp4,
+    matmul_mxfp4,
+    quantize_mxfp4,
+)
 from .mpm import (  # noqa: F401
     MPMError,
     compose_gather,

@@ -32,7 +32,9 @@ STATUS_NAMES = {
 EXPORTS = ("mpm_abi_version", "mpm_status_string", "mpm_merge_workspace_size", "mpm_merge", "mpm_merge_timed",
            "mpm_compose_maps", "mpm_unmerge_gather", "mpm_nearest_neighbors", "mpm_get_device_status",
            "mpm_merge_no_alloc", "mpm_no_alloc_get_device_status", "mpm_compose_gather", "mpm_pad_batch",
-           "mpm_unpad_batch", "mpm_merge_chunked", "mpm_nearest_neighbors_chunked")
+           "mpm_unpad_batch", "mpm_merge_chunked", "mpm_nearest_neighbors_chunked", "mpm_block_norm",
+           "mpm_block_norm_workspace_size", "mpm_block_norm_backward", "mpm_mxfp4_code_bytes", "mpm_mxfp4_scale_bytes",
+           "mpm_mxfp4_quantize", "mpm_mxfp4_dequantize", "mpm_mxfp4_matmul")
 
 _lib = None
 
@@ -46,7 +48,7 @@ class MPMError(RuntimeError):
 
 
 def _declare(lib: ctypes.CDLL) -> None:
-    P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    P, I32, I64, SZ, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     sigs = {
         "mpm_abi_version": (I32, []),
         "mpm_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -67,6 +69,17 @@ def _declare(lib: ctypes.CDLL) -> None:
         "mpm_nearest_neighbors_chunked": (ctypes.c_int, [P, P, I32, I64, I32, ctypes.c_int, ctypes.c_int, I64, P, P,
                                                          P, SZ, P]),
         "mpm_unpad_batch": (ctypes.c_int, [P, I32, I64, I32, ctypes.c_int, P, I64, P, P, P]),
+        "mpm_block_norm": (ctypes.c_int, [P, I64, P, I64, P, I32, I64, I32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                          F32, F32, P, P, P, I32, P, P, P, P, P, P, P]),
+        "mpm_block_norm_workspace_size": (SZ, [I32]),
+        "mpm_block_norm_backward": (ctypes.c_int, [P, I64, P, I64, P, I64, P, I64, P, P, I32, I64, I32, ctypes.c_int,
+                                                   ctypes.c_int, ctypes.c_int, F32, P, P, P, I32, P, P, P, P, P, P, P,
+                                                   P, P, SZ, P, P]),
+        "mpm_mxfp4_code_bytes": (SZ, [I64, I32]),
+        "mpm_mxfp4_scale_bytes": (SZ, [I64, I32]),
+        "mpm_mxfp4_quantize": (ctypes.c_int, [P, I64, I64, I32, ctypes.c_int, P, P, P]),
+        "mpm_mxfp4_dequantize": (ctypes.c_int, [P, P, I64, I32, ctypes.c_int, P, I64, P]),
+        "mpm_mxfp4_matmul": (ctypes.c_int, [P, P, I64, P, P, I32, I32, P, ctypes.c_int, P, I64, P, P]),
         "mpm_selftest_wait_timeout": (ctypes.c_int, [P, ctypes.c_uint32, P]),
         "mpm_trace_read": (ctypes.c_int, [P]),
         "mpm_trace_reset": (ctypes.c_int, []),
