@@ -43,9 +43,10 @@ constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kScaleCols = 2 * kTileN;                 // first column of the scales
 constexpr uint32_t kColsSA = 4, kColsSB = 8;                // columns of one scale tile of A, of two of B
 constexpr uint32_t kStageCols = kScaleTiles * (kColsSA + kColsSB);
-constexpr int kEpilogueWarps = 8;
+constexpr int kWarpCols = 64;                               // columns of the tile that an epilogue warp writes
+constexpr int kEpilogueWarps = 4 * (kTileN / kWarpCols);
 constexpr int kThreads = (2 + kEpilogueWarps) * 32;
-constexpr int kWarpCols = kTileN / 2;                       // columns of the tile that an epilogue warp writes
+constexpr int kBoxBytes = 32 * 128;                         // staged output: 32 rows of 128 bytes, swizzled
 constexpr uint64_t kWaitNs = 2000000000ull;
 static_assert(kScaleCols + kStages * kStageCols <= kTmemCols, "accumulators and scales share tensor memory");
 static_assert(kStageBytes % 1024 == 0 && kBytesA % 1024 == 0 && kBytesB % 1024 == 0, "swizzled tiles on 1024 bytes");
@@ -67,7 +68,7 @@ struct Control {
   int abort_flag;
 };
 
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + sizeof(Control) + 16;
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + kEpilogueWarps * kBoxBytes + sizeof(Control);
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -122,6 +123,16 @@ __device__ __forceinline__ void commit_local(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(ptx::smem_addr(bar))
                : "memory");
 }
+// Staged output box to global memory; what lies past the matrix is cut off.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(src), "r"(x), "r"(y)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void wait_box_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void wait_box_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
   ctl->abort_flag = 1;
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
@@ -131,10 +142,10 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 1)
     mxfp4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
-                        MxMatmulArgs a, int vec) {
+                        const __grid_constant__ CUtensorMap map_out, MxMatmulArgs a, bool tma_out, bool bias_vec) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
-  Control* ctl = reinterpret_cast<Control*>(smem + kStages * kStageBytes);
+  Control* ctl = reinterpret_cast<Control*>(smem + kStages * kStageBytes + kEpilogueWarps * kBoxBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
@@ -155,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::prefetch_tensor_map(&map_b);
     ptx::prefetch_tensor_map(&map_sa);
     ptx::prefetch_tensor_map(&map_sb);
+    if (tma_out) ptx::prefetch_tensor_map(&map_out);
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -279,22 +291,31 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ---------------- epilogue (both CTAs) ----------------
-    // Warp (q, part): rows 32 q .. + 31 of this CTA, columns kWarpCols part .. of the tile.
+    // Warp (q, part): rows 32 q .. + 31 of this CTA, columns 64 part .. + 63 of
+    // the tile, through a staged box of 32 rows x 128 bytes (64 bf16 or 32
+    // fp32): a lane writes its own row, 16-byte piece p at p ^ (row & 7), which
+    // is the 128-byte swizzle and free of bank conflicts; a TMA store takes the
+    // box to global memory in whole 128-byte runs.  Stores from registers,
+    // 16 bytes a row and instruction, took 144 us instead of the 75 that this
+    // takes for 54208 x 768 x 2304 to bf16.
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t empty0 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[0]), 0);
     const uint32_t empty1 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[1]), 0);
+    uint8_t* box = smem + kStages * kStageBytes + (warp - 2) * kBoxBytes;
+    constexpr int kBoxCols = 128 / static_cast<int>(sizeof(T));
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int64_t t = cluster; t < tiles; t += clusters) {
+      const int64_t row0 = t / tiles_n * kTileM + kHalf * rank + q * 32;
+      const int n0 = static_cast<int>(t % tiles_n) * kTileN + part * kWarpCols;
+      const bool live = row0 < a.m && n0 < a.n;
       if (!ptx::mbar_wait(&ctl->acc_full[acc], acc_phase, abort_flag, kWaitNs)) {
         fail(ctl, a.status, 24);
         break;
       }
       ptx::tc_fence_after_sync();
-      const int64_t row = t / tiles_n * kTileM + kHalf * rank + q * 32 + lane;
-      const int n0 = static_cast<int>(t % tiles_n) * kTileN + part * kWarpCols;
       const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * kTileN + part * kWarpCols);
-      T* out = static_cast<T*>(a.out) + row * a.stride;
+#pragma unroll
       for (int c = 0; c < kWarpCols; c += 32) {
         uint32_t r[32];
         ptx::tmem_ld_32x32b_x32(from + c, r);
@@ -304,39 +325,61 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) remote_arrive(acc == 0 ? empty0 : empty1);
         }
+        if (!live) continue;
         const int n = n0 + c;
-        if (row < a.m && n < a.n) {
-          if (a.bias != nullptr) {
+        if (a.bias != nullptr) {
+          if (n + 32 <= a.n && bias_vec) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + (n + i < a.n ? __ldg(a.bias + n + i) : 0.f));
-          }
-          if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              __nv_bfloat162 h[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                h[j] = __floats2bfloat162_rn(__uint_as_float(r[i + 2 * j]), __uint_as_float(r[i + 2 * j + 1]));
-              if (vec && n + i + 8 <= a.n) {
-                *reinterpret_cast<uint4*>(out + n + i) = *reinterpret_cast<const uint4*>(h);
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  if (n + i + j < a.n) out[n + i + j] = reinterpret_cast<const __nv_bfloat16*>(h)[j];
-              }
+            for (int i = 0; i < 32; i += 4) {
+              const float4 b = __ldg(reinterpret_cast<const float4*>(a.bias + n + i));
+              r[i] = __float_as_uint(__uint_as_float(r[i]) + b.x);
+              r[i + 1] = __float_as_uint(__uint_as_float(r[i + 1]) + b.y);
+              r[i + 2] = __float_as_uint(__uint_as_float(r[i + 2]) + b.z);
+              r[i + 3] = __float_as_uint(__uint_as_float(r[i + 3]) + b.w);
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              if (vec && n + i + 4 <= a.n) {
-                *reinterpret_cast<uint4*>(out + n + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (n + i + j < a.n) out[n + i + j] = __uint_as_float(r[i + j]);
-              }
-            }
+            for (int i = 0; i < 32; ++i)
+              if (n + i < a.n) r[i] = __float_as_uint(__uint_as_float(r[i]) + __ldg(a.bias + n + i));
           }
+        }
+        // The box that left from here last has been read.
+        if ((sizeof(T) == 4 || c == 0) && lane == 0) wait_box_read();
+        __syncwarp();
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            __nv_bfloat162 h[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              h[j] = __floats2bfloat162_rn(__uint_as_float(r[8 * p + 2 * j]), __uint_as_float(r[8 * p + 2 * j + 1]));
+            *reinterpret_cast<uint4*>(box + lane * 128 + (((c / 8 + p) ^ (lane & 7)) * 16)) = *reinterpret_cast<const uint4*>(h);
+          }
+        } else {
+#pragma unroll
+          for (int p = 0; p < 8; ++p)
+            *reinterpret_cast<uint4*>(box + lane * 128 + ((p ^ (lane & 7)) * 16)) =
+                make_uint4(r[4 * p], r[4 * p + 1], r[4 * p + 2], r[4 * p + 3]);
+        }
+        if (sizeof(T) == 2 && c + 32 < kWarpCols) continue;
+        const int first = sizeof(T) == 2 ? n0 : n;
+        if (tma_out) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && first < a.n) store_box(&map_out, ptx::smem_addr(box), first, static_cast<int32_t>(row0));
+        } else {
+          // Rows that are not 16-byte aligned: element by element, a warp along each row.
+          __syncwarp();
+          T* out = static_cast<T*>(a.out) + row0 * a.stride + first;
+          const int rows = a.m - row0 < 32 ? static_cast<int>(a.m - row0) : 32;
+          for (int i = 0; i < rows; ++i)
+#pragma unroll
+            for (int j = lane; j < kBoxCols; j += 32)
+              if (first + j < a.n)
+                out[i * a.stride + j] =
+                    *reinterpret_cast<const T*>(box + i * 128 + (((j * static_cast<int>(sizeof(T)) / 16) ^ (i & 7)) * 16) +
+                                                j * sizeof(T) % 16);
+          __syncwarp();
         }
       }
       if (++acc == 2) {
@@ -344,6 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         acc_phase ^= 1u;
       }
     }
+    if (lane == 0) wait_box_written();  // shared memory outlives the stores that read it
+    __syncwarp();
   }
 
   ptx::tc_fence_before_sync();
@@ -386,6 +431,17 @@ bool map_scales(CUtensorMap* map, const uint8_t* scales, int64_t rows, int k) {
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Output: boxes of 32 rows x 128 bytes, swizzled.
+template <typename T>
+bool map_output(CUtensorMap* map, const MxMatmulArgs& a) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.n), static_cast<cuuint64_t>(a.m)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.m > 1 ? a.stride : (a.n + 15) / 16 * 16) * sizeof(T)};
+  const cuuint32_t box[2] = {128 / sizeof(T), 32}, each[2] = {1, 1};
+  return encoder()(map, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, a.out,
+                   dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T>
 cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t stream) {
   if (encoder() == nullptr) return cudaErrorNotSupported;
@@ -406,7 +462,11 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   }
   const int64_t tiles = (a.m + kTileM - 1) / kTileM * ((a.n + kTileN - 1) / kTileN);
   const int64_t pairs = num_sms > 1 ? num_sms / 2 : 1;
-  const int vec = a.stride * static_cast<int64_t>(sizeof(T)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+  CUtensorMap map_out = map_a;
+  const bool tma_out = (a.m == 1 || a.stride * static_cast<int64_t>(sizeof(T)) % 16 == 0) &&
+                       reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+  if (tma_out && !map_output<T>(&map_out, a)) return cudaErrorInvalidValue;
+  const bool bias_vec = reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs)));
   cfg.blockDim = dim3(kThreads);
@@ -421,7 +481,8 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, mxfp4_matmul_kernel<T>, map_a, map_b, map_sa, map_sb, a, vec);
+  return cudaLaunchKernelEx(&cfg, mxfp4_matmul_kernel<T>, map_a, map_b, map_sa, map_sb, map_out, a, tma_out,
+                            bias_vec);
 }
 
 }  // namespace
