@@ -133,6 +133,16 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, 
 }
 __device__ __forceinline__ void wait_box_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void wait_box_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// True in one lane of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+// Bounded wait of a whole warp: one answer for all of its lanes, which go on converged.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
+}
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
   ctl->abort_flag = 1;
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
@@ -192,30 +202,37 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     // ---------------- TMA producer (both CTAs) ----------------
-    if (lane == 0) {
+    // The whole warp runs this loop and the next one; an elected lane issues.
+    // In a branch of one lane every operand of a copy or product first moves to
+    // a uniform register, about 70 cycles an instruction, which bound the
+    // kernel: 8192 x 8192 x 8192 took 316 us instead of 176.
+    {
       int stage = 0, issued = 0;
       uint32_t phase = 0, issued_phase = 0;
       bool ok = true;
+      const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
+      const uint32_t full0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full[0]), 0), 0);
       for (int64_t t = cluster; ok && t < tiles; t += clusters) {
         const int32_t m0 = static_cast<int32_t>(t / tiles_n) * kTileM + kHalf * static_cast<int32_t>(rank);
         const int32_t n0 = static_cast<int32_t>(t % tiles_n) * kTileN;
         for (int kb = 0; kb < stages_k; ++kb) {
-          if (!ptx::mbar_wait(&ctl->empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
+          if (!warp_wait(&ctl->empty[stage], phase ^ 1u, abort_flag)) {
             fail(ctl, a.status, 21);
             ok = false;
             break;
           }
-          const uint32_t at = ptx::smem_addr(smem + stage * kStageBytes);
-          const uint32_t full = map_to_rank(ptx::smem_addr(&ctl->full[stage]), 0);
-          if (leader) ptx::mbar_arrive_expect_tx(&ctl->full[stage], 2 * kStageBytes);
-          load_pair(at, &map_a, full, kb * 128, m0);
-          load_pair(at + kBytesA, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
+          const uint32_t at = smem0 + stage * kStageBytes, full = full0 + stage * 8;
           // A scale tile past the last one along K belongs to other rows, or reads as zeros: no product uses it.
-          const int32_t kt = kb * kScaleTiles;
-          load_pair(at + kBytesA + kBytesB, &map_sa, full, 0, m0 / mx::kTileRows * tiles_k + kt);
-          const int32_t nt = n0 / mx::kTileRows;
-          load_pair(at + kBytesA + kBytesB + kBytesSA, &map_sb, full, 0, nt * tiles_k + kt);
-          load_pair(at + kBytesA + kBytesB + 2 * kBytesSA, &map_sb, full, 0, (nt + 1) * tiles_k + kt);
+          const int32_t kt = kb * kScaleTiles, nt = n0 / mx::kTileRows;
+          if (elect_one()) {
+            if (leader) ptx::mbar_arrive_expect_tx(&ctl->full[stage], 2 * kStageBytes);
+            load_pair(at, &map_a, full, kb * 128, m0);
+            load_pair(at + kBytesA, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
+            load_pair(at + kBytesA + kBytesB, &map_sa, full, 0, m0 / mx::kTileRows * tiles_k + kt);
+            load_pair(at + kBytesA + kBytesB + kBytesSA, &map_sb, full, 0, nt * tiles_k + kt);
+            load_pair(at + kBytesA + kBytesB + 2 * kBytesSA, &map_sb, full, 0, (nt + 1) * tiles_k + kt);
+          }
+          __syncwarp();
           issued |= 1 << stage;
           issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
           if (++stage == kStages) {
@@ -232,23 +249,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ---------------- MMA issuer (leader) ----------------
-    if (leader && lane == 0) {
+    if (leader) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      const uint32_t smem0 = ptx::smem_addr(smem);
+      const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
+      const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
       const uint64_t desc0 = ptx::sdesc_k_sw128(smem0);
       for (int64_t t = cluster; ok && t < tiles; t += clusters) {
-        if (!ptx::mbar_wait(&ctl->acc_empty[acc], acc_phase ^ 1u, abort_flag, kWaitNs)) {
+        if (!warp_wait(&ctl->acc_empty[acc], acc_phase ^ 1u, abort_flag)) {
           fail(ctl, a.status, 22);
           break;
         }
         ptx::tc_fence_after_sync();
-        const uint32_t d = tmem + static_cast<uint32_t>(acc * kTileN);
+        const uint32_t d = tmem0 + static_cast<uint32_t>(acc * kTileN);
         // The tile's first row of B within its scale tile: a column of scales holds 32 rows.
         const uint32_t sb_shift = static_cast<uint32_t>(t % tiles_n) * kTileN % mx::kTileRows / 32;
         for (int kb = 0; kb < stages_k; ++kb) {
-          if (!ptx::mbar_wait(&ctl->full[stage], phase, abort_flag, kWaitNs)) {
+          if (!warp_wait(&ctl->full[stage], phase, abort_flag)) {
             fail(ctl, a.status, 23);
             ok = false;
             break;
@@ -256,36 +274,41 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tc_fence_after_sync();
           const uint64_t da = desc0 + static_cast<uint64_t>((stage * kStageBytes) >> 4), db = da + (kBytesA >> 4);
           const uint32_t scales = smem0 + stage * kStageBytes + kBytesA + kBytesB;
-          const uint32_t sa = tmem + kScaleCols + stage * kStageCols, sb = sa + kScaleTiles * kColsSA;
+          const uint32_t sa = tmem0 + kScaleCols + stage * kStageCols, sb = sa + kScaleTiles * kColsSA;
           const int products = min(kStageK / 64, (a.k - kb * kStageK + 63) / 64);
+          if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < kScaleTiles; ++j) {
-            if (2 * j < products) {
-              copy_scales(sa + j * kColsSA, scale_desc(scales + j * mx::kTileBytes));
-              copy_scales(sb + j * kColsSB, scale_desc(scales + kBytesSA + j * mx::kTileBytes));
-              copy_scales(sb + j * kColsSB + 4, scale_desc(scales + 2 * kBytesSA + j * mx::kTileBytes));
+            for (int j = 0; j < kScaleTiles; ++j) {
+              if (2 * j < products) {
+                copy_scales(sa + j * kColsSA, scale_desc(scales + j * mx::kTileBytes));
+                copy_scales(sb + j * kColsSB, scale_desc(scales + kBytesSA + j * mx::kTileBytes));
+                copy_scales(sb + j * kColsSB + 4, scale_desc(scales + 2 * kBytesSA + j * mx::kTileBytes));
+              }
             }
-          }
 #pragma unroll
-          for (int p = 0; p < kStageK / 64; ++p) {
-            if (p < products)
-              mma_mx(d, da + 2 * p, db + 2 * p, kIdesc | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
-                     sb + (p / 2) * kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
+            for (int p = 0; p < kStageK / 64; ++p) {
+              if (p < products)
+                mma_mx(d, da + 2 * p, db + 2 * p, kIdesc | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
+                       sb + (p / 2) * kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
+            }
+            commit_both(&ctl->empty[stage]);
           }
-          commit_both(&ctl->empty[stage]);
+          __syncwarp();
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
         }
         if (!ok) break;
-        commit_both(&ctl->acc_full[acc]);
+        if (elect_one()) commit_both(&ctl->acc_full[acc]);
+        __syncwarp();
         if (++acc == 2) {
           acc = 0;
           acc_phase ^= 1u;
         }
       }
-      commit_local(&ctl->drain);
+      if (elect_one()) commit_local(&ctl->drain);
+      __syncwarp();
       ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
     }
     __syncwarp();
@@ -309,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t row0 = t / tiles_n * kTileM + kHalf * rank + q * 32;
       const int n0 = static_cast<int>(t % tiles_n) * kTileN + part * kWarpCols;
       const bool live = row0 < a.m && n0 < a.n;
-      if (!ptx::mbar_wait(&ctl->acc_full[acc], acc_phase, abort_flag, kWaitNs)) {
+      if (!warp_wait(&ctl->acc_full[acc], acc_phase, abort_flag)) {
         fail(ctl, a.status, 24);
         break;
       }
