@@ -7,9 +7,14 @@
 // A block with a NaN or an infinity has no scale: it is stored as the scale
 // code of NaN, and all of its elements read back as NaN.
 //
-// Bound: HBM (bf16: 2 bytes an element in, 17/32 out).  A thread takes eight
-// elements of a row, four neighbouring lanes make up a block, and a thread
-// has four such loads in flight.
+// Bound: HBM (bf16: 2 bytes an element in, 17/32 out).  A block of threads
+// takes whole scale tiles (128 rows x 128 columns): half a warp spans the
+// tile's columns, eight elements a lane, and a thread has the loads of its
+// eight rows in flight.  Rows and columns of a thread are then constants of
+// the loop; walking all rows' elements with running indexes was bound by
+// those instructions (65536 x 768 bf16: 46 us; tiles 24).
+#include <string.h>
+
 #include "common.cuh"
 #include "mxfp4.cuh"
 
@@ -17,54 +22,59 @@ namespace mpm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnit = 8;      // elements a thread takes at a time
-constexpr int kUnroll = 4;
-// Units of one scale tile's columns: rows are walked in whole tiles, so that padding scales are written too.
-constexpr int kTileUnits = mx::kBlock * mx::kTileBlocks / kUnit;
+constexpr int kUnit = 8;                                           // elements a thread takes of a row
+constexpr int kTileCols = mx::kBlock * mx::kTileBlocks;
+constexpr int kLanes = kTileCols / kUnit;                          // lanes that span a tile's columns
+constexpr int kRowsAtOnce = kThreads / kLanes;
+constexpr int kRows = mx::kTileRows / kRowsAtOnce;                 // rows of a tile that a thread takes
+static_assert(kLanes == 16 && kRows == 8, "half a warp per row");
 
-// Place of a thread in the units of all rows, advanced without divisions.
-struct Walk {
-  int64_t row;
-  int unit;
-  __device__ __forceinline__ void advance(int64_t rows, int units, int per_row) {
-    row += rows;
-    unit += units;
-    if (unit >= per_row) {
-      unit -= per_row;
-      ++row;
-    }
-  }
+// Eight elements of a row, as they lie in memory.
+template <typename T>
+struct Unit {
+  uint4 w[sizeof(T) / 2];
 };
-
 template <typename T>
-__device__ __forceinline__ float as_f32(T v);
-template <>
-__device__ __forceinline__ float as_f32<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float as_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-template <typename T>
-__device__ __forceinline__ void load_unit(const T* p, int left, bool vec, float (&v)[kUnit]) {
+__device__ __forceinline__ Unit<T> load_unit(const T* p, int left, bool vec) {
+  Unit<T> u;
   if (vec && left >= kUnit) {
-    if constexpr (sizeof(T) == 2) {
-      const uint4 r = ld_stream(reinterpret_cast<const uint4*>(p));
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    } else {
-      const uint4 a = ld_stream(reinterpret_cast<const uint4*>(p)), b = ld_stream(reinterpret_cast<const uint4*>(p) + 1);
-      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    }
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) u.w[i] = ld_stream(reinterpret_cast<const uint4*>(p) + i);
   } else {
+    T e[kUnit];
 #pragma unroll
-    for (int i = 0; i < kUnit; ++i) v[i] = i < left ? as_f32(p[i]) : 0.f;
+    for (int i = 0; i < kUnit; ++i) e[i] = i < left ? p[i] : T(0.f);
+    memcpy(&u, e, sizeof(u));
+  }
+  return u;
+}
+// The largest magnitude's bits, as those of a float.
+__device__ __forceinline__ uint32_t top_bits(const Unit<__nv_bfloat16>& u) {
+  const uint32_t w[4] = {u.w[0].x, u.w[0].y, u.w[0].z, u.w[0].w};
+  uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+  return max(m << 16, m & 0xFFFF0000u);
+}
+__device__ __forceinline__ uint32_t top_bits(const Unit<float>& u) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w[4] = {u.w[i].x, u.w[i].y, u.w[i].z, u.w[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, w[j] & 0x7FFFFFFFu);
+  }
+  return m;
+}
+__device__ __forceinline__ void widen(const Unit<__nv_bfloat16>& u, float (&v)[kUnit]) {
+  const uint32_t w[4] = {u.w[0].x, u.w[0].y, u.w[0].z, u.w[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
+__device__ __forceinline__ void widen(const Unit<float>& u, float (&v)[kUnit]) { memcpy(v, &u, sizeof(u)); }
 
 // Eight E2M1 codes, the first in the lowest bits.
 __device__ __forceinline__ uint32_t encode8(const float (&v)[8]) {
@@ -80,151 +90,140 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8]) {
   return r;
 }
 
-__device__ __forceinline__ void decode8(uint32_t codes, float (&v)[8]) {
-  uint32_t h[4];
-  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-      "mov.b32 {a, b, c, d}, %4;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-      : "r"(codes));
+// Eight codes to bf16 pairs, times 2^(c - 127).  A code's exponent and
+// mantissa bits in the place of bf16's last exponent bits and first mantissa
+// bit are the value times 2^-126 (E2M1's subnormal 0.5 as bf16's), so one
+// multiplication makes it the value and another scales it: both are exact
+// (bf16 reaches down to 2^-133), or overflow as fp32 would.
+__device__ __forceinline__ void decode8(uint32_t codes, int c, __nv_bfloat162 (&v)[4]) {
+  const __nv_bfloat162 up = __bfloat162bfloat162(__ushort_as_bfloat16(253 << 7));  // 2^126
+  const uint16_t unit = c == mx::kNanScale ? 0x7FFF : c > 0 ? static_cast<uint16_t>(c << 7) : 0x0040;
+  const __nv_bfloat162 by = __bfloat162bfloat162(__ushort_as_bfloat16(unit));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
+    const uint32_t b = codes >> (8 * i);
+    const uint32_t t = (b & 0xFu) | ((b & 0xF0u) << 12);
+    const uint32_t bits = ((t & 0x00070007u) << 6) | ((t & 0x00080008u) << 12);
+    v[i] = __hmul2_rn(__hmul2_rn(*reinterpret_cast<const __nv_bfloat162*>(&bits), up), by);
   }
 }
 
-__device__ __forceinline__ float scale_value(int code) {
-  return __uint_as_float(code == mx::kNanScale ? 0x7FFFFFFFu : code > 0 ? static_cast<uint32_t>(code) << 23 : 0x00400000u);
-}
-
 template <typename T>
-__global__ void __launch_bounds__(kThreads) quantize_kernel(QuantizeArgs a, bool vec, int64_t padded_rows, int64_t step_rows,
-                                                            int step_units) {
+__global__ void __launch_bounds__(kThreads) quantize_kernel(QuantizeArgs a, bool vec, int64_t scale_tiles) {
   wait_for_previous_grid();
   allow_next_grid();
-  const int tiles = mx::scale_tiles(a.dim), per_row = tiles * kTileUnits, pitch = mx::code_pitch(a.dim);
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  Walk at{first / per_row, static_cast<int>(first % per_row)};
-  // Rows are whole numbers of 16 units: a block's four lanes leave the loop together.
-  while (at.row < padded_rows) {
-    Walk unit[kUnroll];
-    float v[kUnroll][kUnit];
+  const int tiles_k = mx::scale_tiles(a.dim), pitch = mx::code_pitch(a.dim);
+  const int lane = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
+  for (int64_t tile = blockIdx.x; tile < scale_tiles; tile += gridDim.x) {
+    const int64_t row_tile = tile / tiles_k;
+    const int col = static_cast<int>(tile - row_tile * tiles_k) * kTileCols + lane * kUnit;
+    const int64_t row0 = row_tile * mx::kTileRows + first;
+    const T* x = static_cast<const T*>(a.x) + row0 * a.stride + col;
+    Unit<T> u[kRows];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      unit[u] = at;
-      const int col = at.unit * kUnit;
-      load_unit(static_cast<const T*>(a.x) + (at.row < a.rows ? at.row * a.stride + col : 0),
-                at.row < a.rows ? a.dim - col : 0, vec, v[u]);
-      at.advance(step_rows, step_units, per_row);
-    }
+    for (int i = 0; i < kRows; ++i)
+      u[i] = load_unit(x + i * kRowsAtOnce * a.stride, row0 + i * kRowsAtOnce < a.rows ? a.dim - col : 0, vec);
+    uint8_t* codes = a.codes + row0 * pitch + col / 2;
+    uint8_t* scales = a.scales + tile * mx::kTileBytes + lane / 4;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < kRows; ++i) {
+      // The four lanes of a block.
+      uint32_t top = top_bits(u[i]);
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+      // What a block that is not finite holds as codes does not matter: its scale makes it NaN.
       const bool finite = top < 0x7F800000u;
-      const int exponent = static_cast<int>(top >> 23);
-      const int code = finite ? max(exponent - 2, 0) : mx::kNanScale;
+      const int code = finite ? max(static_cast<int>(top >> 23) - 2, 0) : mx::kNanScale;
       const float by = finite ? __uint_as_float(static_cast<uint32_t>(254 - code) << 23) : 0.f;
+      float v[kUnit];
+      widen(u[i], v);
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i) v[u][i] = finite ? v[u][i] * by : 0.f;
-      const Walk w = unit[u];
-      if (w.row < a.rows && w.unit * 4 < pitch)
-        *reinterpret_cast<uint32_t*>(a.codes + w.row * pitch + w.unit * 4) = encode8(v[u]);
-      if ((w.unit & 3) == 0 && w.row < padded_rows)
-        a.scales[mx::scale_byte(w.row, w.unit >> 2, tiles)] = static_cast<uint8_t>(code);
+      for (int j = 0; j < kUnit; ++j) v[j] *= by;
+      if (row0 + i * kRowsAtOnce < a.rows && col / 2 < pitch)
+        *reinterpret_cast<uint32_t*>(codes + i * kRowsAtOnce * static_cast<int64_t>(pitch)) = encode8(v);
+      const int r = first + i * kRowsAtOnce;
+      if (lane % 4 == 0) scales[(r % 32) * 16 + (r / 32) * 4] = static_cast<uint8_t>(code);
     }
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, bool vec, int64_t step_rows, int step_units) {
-  wait_for_previous_grid();
-  allow_next_grid();
-  const int tiles = mx::scale_tiles(a.dim), per_row = (a.dim + kUnit - 1) / kUnit, pitch = mx::code_pitch(a.dim);
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  Walk at{first / per_row, static_cast<int>(first % per_row)};
-  while (at.row < a.rows) {
-    Walk unit[kUnroll];
-    uint32_t codes[kUnroll];
-    int scale[kUnroll];
+__device__ __forceinline__ void store_unit(T* p, int left, bool vec, const __nv_bfloat162 (&v)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    if (vec && left >= kUnit) {
+      st_stream(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(v));
+    } else {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      unit[u] = at;
-      const bool in = at.row < a.rows;
-      codes[u] = in ? __ldcs(reinterpret_cast<const uint32_t*>(a.codes + at.row * pitch + at.unit * 4)) : 0u;
-      scale[u] = in ? __ldg(a.scales + mx::scale_byte(at.row, at.unit >> 2, tiles)) : 0;
-      at.advance(step_rows, step_units, per_row);
+      for (int i = 0; i < kUnit; ++i)
+        if (i < left) p[i] = i & 1 ? __high2bfloat16(v[i / 2]) : __low2bfloat16(v[i / 2]);
     }
+  } else {
+    float f[kUnit];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const Walk w = unit[u];
-      if (w.row >= a.rows) break;
-      float v[kUnit];
-      decode8(codes[u], v);
-      const float by = scale_value(scale[u]);
+    for (int i = 0; i < 4; ++i) {
+      const float2 w = __bfloat1622float2(v[i]);
+      f[2 * i] = w.x;
+      f[2 * i + 1] = w.y;
+    }
+    if (vec && left >= kUnit) {
+      __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
+      __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
+    } else {
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i) v[i] *= by;
-      const int col = w.unit * kUnit;
-      T* out = static_cast<T*>(a.out) + w.row * a.stride + col;
-      if (vec && col + kUnit <= a.dim) {
-        if constexpr (sizeof(T) == 2) {
-          uint4 r;
-          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-          st_stream(reinterpret_cast<uint4*>(out), r);
-        } else {
-          __stcs(reinterpret_cast<float4*>(out), make_float4(v[0], v[1], v[2], v[3]));
-          __stcs(reinterpret_cast<float4*>(out) + 1, make_float4(v[4], v[5], v[6], v[7]));
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i)
-          if (col + i < a.dim) {
-            if constexpr (sizeof(T) == 2) out[i] = __float2bfloat16_rn(v[i]);
-            else out[i] = v[i];
-          }
-      }
+      for (int i = 0; i < kUnit; ++i)
+        if (i < left) p[i] = f[i];
     }
   }
 }
 
-// Grid and the step of a grid-wide stride, in rows and units.
-struct Plan {
-  int grid;
-  int64_t step_rows;
-  int step_units;
-};
-Plan plan_of(int64_t rows, int per_row, int per_sm, int num_sms) {
-  const int64_t want = (rows * per_row + kThreads * kUnroll - 1) / (kThreads * kUnroll);
-  const int64_t most = static_cast<int64_t>(num_sms) * per_sm;
-  const int grid = static_cast<int>(want < most ? want : most);
-  const int64_t step = static_cast<int64_t>(grid) * kThreads;
-  return {grid, step / per_row, static_cast<int>(step % per_row)};
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, bool vec, int64_t scale_tiles) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int tiles_k = mx::scale_tiles(a.dim), pitch = mx::code_pitch(a.dim);
+  const int lane = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
+  for (int64_t tile = blockIdx.x; tile < scale_tiles; tile += gridDim.x) {
+    const int64_t row_tile = tile / tiles_k;
+    const int col = static_cast<int>(tile - row_tile * tiles_k) * kTileCols + lane * kUnit;
+    const int64_t row0 = row_tile * mx::kTileRows + first;
+    const uint8_t* codes = a.codes + row0 * pitch + col / 2;
+    const uint8_t* scales = a.scales + tile * mx::kTileBytes + lane / 4;
+    T* out = static_cast<T*>(a.out) + row0 * a.stride + col;
+    uint32_t code[kRows];
+    int scale[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int r = first + i * kRowsAtOnce;
+      const bool in = row0 + i * kRowsAtOnce < a.rows && col < a.dim;
+      code[i] = in ? __ldcs(reinterpret_cast<const uint32_t*>(codes + i * kRowsAtOnce * static_cast<int64_t>(pitch))) : 0u;
+      scale[i] = in ? __ldg(scales + (r % 32) * 16 + (r / 32) * 4) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      __nv_bfloat162 v[4];
+      decode8(code[i], scale[i], v);
+      if (row0 + i * kRowsAtOnce < a.rows) store_unit(out + i * kRowsAtOnce * a.stride, a.dim - col, vec, v);
+    }
+  }
+}
+
+template <typename Kernel, typename Args>
+cudaError_t launch_tiles(Kernel kernel, int per_sm, const Args& a, bool vec, int num_sms, cudaStream_t stream) {
+  const int64_t tiles = mx::row_tiles(a.rows) * mx::scale_tiles(a.dim), most = static_cast<int64_t>(num_sms) * per_sm;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(tiles < most ? tiles : most)), dim3(kThreads), 0, stream, a,
+                          vec, tiles);
 }
 
 template <typename T>
 cudaError_t quantize(const QuantizeArgs& a, bool vec, int num_sms, cudaStream_t stream) {
   static const int per_sm = resident_per_sm(quantize_kernel<T>, kThreads, 8);
-  const int64_t padded = mx::row_tiles(a.rows) * mx::kTileRows;
-  const Plan p = plan_of(padded, mx::scale_tiles(a.dim) * kTileUnits, per_sm, num_sms);
-  return launch_dependent(quantize_kernel<T>, dim3(p.grid), dim3(kThreads), 0, stream, a, vec, padded, p.step_rows,
-                          p.step_units);
+  return launch_tiles(quantize_kernel<T>, per_sm, a, vec, num_sms, stream);
 }
 
 template <typename T>
 cudaError_t dequantize(const DequantizeArgs& a, bool vec, int num_sms, cudaStream_t stream) {
   static const int per_sm = resident_per_sm(dequantize_kernel<T>, kThreads, 8);
-  const Plan p = plan_of(a.rows, (a.dim + kUnit - 1) / kUnit, per_sm, num_sms);
-  return launch_dependent(dequantize_kernel<T>, dim3(p.grid), dim3(kThreads), 0, stream, a, vec, p.step_rows, p.step_units);
+  return launch_tiles(dequantize_kernel<T>, per_sm, a, vec, num_sms, stream);
 }
 
 }  // namespace
