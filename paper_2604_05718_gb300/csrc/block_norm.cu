@@ -14,6 +14,12 @@
 // features take one warp, whose sums are shuffles; longer ones take a group
 // of warps that meet at a named barrier per sum.  The variance is a second
 // pass over the registers around the mean, not E[v^2] - m^2.
+//
+// A warp's parameters are as many bytes as several rows.  They lie in shared
+// memory in the order in which lanes take them (16 bytes a lane, no bank
+// conflicts), and a warp takes two rows of one image for each of their loads;
+// read through L1 for every row, they bound the kernel (54208 x 768 bf16, layer
+// norm on both sides: 85 us; now FWD1).
 #include "block_launch.h"
 #include "norm_rows.cuh"
 
@@ -24,12 +30,47 @@ using namespace norm;
 
 constexpr int kThreads = 256;
 
+// The parameters of one row in shared memory: vector v, chunk c, element i of
+// a lane.  Absent vectors stand there too (as ones or zeros).
+enum Vector : int { kPostWeight, kPostBias, kPreWeight, kPreBias, kVectors };
+template <int C, bool VEC>
+struct SharedParams {
+  float v[kVectors][C][2][32][4];
+  __device__ __forceinline__ void fill(Vector which, const float* p, float otherwise, int dim) {
+    for (int e = threadIdx.x; e < C * kNormWarpCols; e += blockDim.x) {
+      const int c = e / kNormWarpCols, k = e % kNormWarpCols;
+      const int lane = VEC ? k / 8 : k % 32, i = VEC ? k % 8 : k / 32;
+      v[which][c][i / 4][lane][i % 4] = p == nullptr ? otherwise : e < dim ? __ldg(p + e) : 0.f;
+    }
+  }
+  __device__ __forceinline__ F8 get(Vector which, int c, int lane) const {
+    return join(*reinterpret_cast<const float4*>(v[which][c][0][lane]), *reinterpret_cast<const float4*>(v[which][c][1][lane]));
+  }
+};
+
+// Rows that a warp takes at once.
+__host__ __device__ constexpr int rows_at_once(int chunks, bool multi) { return multi || chunks > 1 ? 1 : 2; }
+
 template <typename TY, typename TX, int C, bool VEC, bool MULTI>
-__global__ void __launch_bounds__(MULTI ? 512 : kThreads) block_norm_kernel(NormForward a, int row_warps) {
+__global__ void __launch_bounds__(MULTI ? 512 : kThreads, MULTI ? 1 : (VEC ? C < 4 : C < 3) ? 3 : 2) block_norm_kernel(NormForward a, int row_warps) {
+  constexpr int R = rows_at_once(C, MULTI);
+  __shared__ float2 sh[MULTI ? 32 : 1];
+  __shared__ SharedParams<MULTI ? 1 : C, VEC> shared;
   wait_for_previous_grid();
   allow_next_grid();
-  __shared__ float2 sh[MULTI ? 32 : 1];
   check_offsets(a.offsets, a.batch, a.rows, a.status);
+  const bool post = a.post_weight != nullptr, pre = a.pre_weight != nullptr;
+  if constexpr (!MULTI) {
+    if (post) {
+      shared.fill(kPostWeight, a.post_weight, 1.f, a.dim);
+      shared.fill(kPostBias, a.post_bias, 0.f, a.dim);
+    }
+    if (pre) {
+      shared.fill(kPreWeight, a.pre_weight, 1.f, a.dim);
+      shared.fill(kPreBias, a.pre_bias, 0.f, a.dim);
+    }
+    __syncthreads();
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
   const int groups = (blockDim.x >> 5) / w, group = warp / w, in_group = warp % w;
@@ -40,7 +81,6 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads) block_norm_kernel(Norm
   const int64_t per = total / all, extra = total % all;
   const int64_t begin = g * per + (g < extra ? g : extra), end = begin + per + (g < extra ? 1 : 0);
   const float inv_dim = 1.f / static_cast<float>(a.dim);
-  const bool post = a.post_weight != nullptr, pre = a.pre_weight != nullptr;
   const float* gate = a.gate;
   int image = 0;
   int64_t image_end = INT64_MAX;
@@ -52,76 +92,117 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads) block_norm_kernel(Norm
   int col[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) col[c] = first_column<VEC>(c * w + in_group, lane);
+  auto param = [&](Vector which, const float* p, int c, float otherwise) {
+    if constexpr (MULTI) return param8<VEC>(p, col[c], a.dim, otherwise);
+    else return shared.get(which, c, lane);
+  };
 
-  for (int64_t row = begin; row < end; ++row) {
+  for (int64_t row = begin; row < end;) {
     while (row >= image_end && image < a.batch - 1) {
       ++image;
       image_end = __ldg(a.offsets + image + 1);
       gate = a.gate + static_cast<int64_t>(image) * a.dim;
     }
-    float u[C][8], x[C][8];
-    const TY* yr = static_cast<const TY*>(a.y) + row * a.y_stride;
-    const TX* xr = static_cast<const TX*>(a.residual) + row * a.residual_stride;
+    // The last row stands in for one past the run's or the image's end, and is written once.
+    int64_t at[R];
+    int count = 1;
+    at[0] = row;
 #pragma unroll
-    for (int c = 0; c < C; ++c) load8<TY, VEC>(yr, col[c], a.dim, u[c]);
+    for (int r = 1; r < R; ++r) {
+      const bool more = row + r < end && (row + r < image_end || image == a.batch - 1);
+      at[r] = more ? row + r : row;
+      count += more ? 1 : 0;
+    }
+    row += count;
+    F8 u[R][C], x[R][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) load8<TX, VEC>(xr, col[c], a.dim, x[c]);
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        u[r][c] = load8<TY, VEC>(static_cast<const TY*>(a.y) + at[r] * a.y_stride, col[c], a.dim);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        x[r][c] = load8<TX, VEC>(static_cast<const TX*>(a.residual) + at[r] * a.residual_stride, col[c], a.dim);
+    }
 
-    // (mean, 1 / deviation) of a row in registers.
-    auto statistics = [&](const float(&v)[C][8]) {
-      float m = 0.f;
+    // Takes the mean out of rows in registers; 1 / deviation and the mean of each.
+    auto standardise = [&](F8(&v)[R][C], float2(&s)[R]) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r].x = 0.f;
       if (a.layer) {
-        float s = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float2 t = pair(0.f);
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t = add(t, v[r][c].p[k]);
+          s[r].x = t.x + t.y;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r].x = sum(s[r].x, 0.f).x * inv_dim;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const F8 in = mask8<VEC>(col[c], a.dim);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[r][c].p[k] = fma(in.p[k], pair(-s[r].x), v[r][c].p[k]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float2 t = pair(0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s += v[c][i];
-        m = sum(s, 0.f).x * inv_dim;
+          for (int k = 0; k < 4; ++k) t = fma(v[r][c].p[k], v[r][c].p[k], t);
+        s[r].y = t.x + t.y;
       }
-      float s = 0.f;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float d = inside<VEC>(col[c], i, a.dim) ? v[c][i] - m : 0.f;
-          s = fmaf(d, d, s);
-        }
-      return make_float2(m, 1.f / sqrtf(fmaf(sum(s, 0.f).x, inv_dim, a.eps)));
+      for (int r = 0; r < R; ++r) s[r].y = 1.f / sqrtf(fmaf(sum(s[r].y, 0.f).x, inv_dim, a.eps));
     };
 
-    float2 s1 = make_float2(0.f, 1.f), s2 = make_float2(0.f, 1.f);
-    if (post) s1 = statistics(u);
+    float2 s1[R], s2[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s1[r] = s2[r] = make_float2(0.f, 1.f);
+    if (post) standardise(u, s1);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (post) {
-        float wv[8], bv[8];
-        param8<VEC>(a.post_weight, col[c], a.dim, 1.f, wv);
-        param8<VEC>(a.post_bias, col[c], a.dim, 0.f, bv);
+        const F8 wv = param(kPostWeight, a.post_weight, c, 1.f), bv = param(kPostBias, a.post_bias, c, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] = fmaf((u[c][i] - s1.x) * s1.y, wv[i], bv[i]);
-      }
-      float gv[8];
-      param8<VEC>(gate, col[c], a.dim, 1.f, gv);
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[c][i] = fmaf(gv[i], u[c][i], a.alpha * x[c][i]);
-        if (!inside<VEC>(col[c], i, a.dim)) x[c][i] = 0.f;
+          for (int k = 0; k < 4; ++k) u[r][c].p[k] = fma(mul(u[r][c].p[k], pair(s1[r].y)), wv.p[k], bv.p[k]);
       }
-      store8<TX, VEC>(static_cast<TX*>(a.residual_out) + row * a.dim, col[c], a.dim, x[c]);
+      // Outside the row u and x are zeros, and so is x'.
+      const F8 gv = param8<VEC>(gate, col[c], a.dim, 1.f);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[r][c].p[k] = fma(gv.p[k], u[r][c].p[k], mul(pair(a.alpha), x[r][c].p[k]));
+        if (r < count) store8<TX, VEC>(static_cast<TX*>(a.residual_out) + at[r] * a.dim, col[c], a.dim, x[r][c]);
+      }
     }
     if (pre) {
-      s2 = statistics(x);
+      standardise(x, s2);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float wv[8], bv[8];
-        param8<VEC>(a.pre_weight, col[c], a.dim, 1.f, wv);
-        param8<VEC>(a.pre_bias, col[c], a.dim, 0.f, bv);
+        const F8 wv = param(kPreWeight, a.pre_weight, c, 1.f), bv = param(kPreBias, a.pre_bias, c, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[c][i] = fmaf((x[c][i] - s2.x) * s2.y, wv[i], bv[i]);
-        store8<TY, VEC>(static_cast<TY*>(a.h) + row * a.dim, col[c], a.dim, x[c]);
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[r][c].p[k] = fma(mul(x[r][c].p[k], pair(s2[r].y)), wv.p[k], bv.p[k]);
+          if (r < count) store8<TY, VEC>(static_cast<TY*>(a.h) + at[r] * a.dim, col[c], a.dim, x[r][c]);
+        }
       }
     }
-    if (a.stats != nullptr && in_group == 0 && lane == 0) a.stats[row] = make_float4(s1.x, s1.y, s2.x, s2.y);
+    if (a.stats != nullptr && in_group == 0 && lane == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (r < count) a.stats[at[r]] = make_float4(s1[r].x, s1[r].y, s2[r].x, s2[r].y);
+    }
   }
 }
 

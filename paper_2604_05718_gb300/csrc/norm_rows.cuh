@@ -2,6 +2,10 @@
 // spread over threads, its loads and stores, and sums over it.
 #pragma once
 
+#include <string.h>
+
+#include <type_traits>
+
 #include "block_launch.h"
 #include "common.cuh"
 
@@ -37,79 +41,113 @@ __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-__device__ __forceinline__ void widen(uint4 r, float (&v)[8]) {
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+// Eight values of a row as pairs: the kernels' arithmetic is on pairs, which
+// Blackwell issues as one instruction.
+struct F8 {
+  float2 p[4];
+};
+__device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 add(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ F8 all8(float v) { return {{pair(v), pair(v), pair(v), pair(v)}}; }
+
+__device__ __forceinline__ F8 widen(uint4 r) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  F8 v;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 f = __bfloat1622float2(h[k]);
-    v[2 * k] = f.x;
-    v[2 * k + 1] = f.y;
-  }
+  for (int k = 0; k < 4; ++k) v.p[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
+  return v;
+}
+__device__ __forceinline__ F8 join(float4 a, float4 b) {
+  return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
 }
 
 // Eight columns of a row of tokens; zeros outside the row.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int col, int dim, float (&v)[8]) {
+__device__ __forceinline__ F8 load8(const T* __restrict__ row, int col, int dim) {
   if constexpr (VEC) {
-    if (col >= dim) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    } else if constexpr (sizeof(T) == 2) {
-      widen(ld_stream(reinterpret_cast<const uint4*>(row + col)), v);
+    if (col >= dim) return all8(0.f);
+    if constexpr (sizeof(T) == 2) {
+      return widen(ld_stream(reinterpret_cast<const uint4*>(row + col)));
     } else {
-      const uint4 a = ld_stream(reinterpret_cast<const uint4*>(row + col));
-      const uint4 b = ld_stream(reinterpret_cast<const uint4*>(row + col) + 1);
-      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+      const float4* p = reinterpret_cast<const float4*>(row + col);
+      return join(__ldcs(p), __ldcs(p + 1));
     }
   } else {
+    float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = col + 32 * i < dim ? to_f32(row[col + 32 * i]) : 0.f;
+    return {{make_float2(v[0], v[1]), make_float2(v[2], v[3]), make_float2(v[4], v[5]), make_float2(v[6], v[7])}};
   }
 }
 
 // Eight columns of a parameter vector (kept in the caches); `otherwise` where it is absent.
 template <bool VEC>
-__device__ __forceinline__ void param8(const float* __restrict__ p, int col, int dim, float otherwise,
-                                       float (&v)[8]) {
-  if (p == nullptr) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = otherwise;
-  } else if constexpr (VEC) {
-    if (col < dim) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p + col));
-      const float4 b = __ldg(reinterpret_cast<const float4*>(p + col) + 1);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    }
+__device__ __forceinline__ F8 param8(const float* __restrict__ p, int col, int dim, float otherwise) {
+  if (p == nullptr) return all8(otherwise);
+  if constexpr (VEC) {
+    if (col >= dim) return all8(0.f);
+    const float4* q = reinterpret_cast<const float4*>(p + col);
+    return join(__ldg(q), __ldg(q + 1));
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = col + 32 * i < dim ? __ldg(p + col + 32 * i) : 0.f;
+    return load8<float, false>(p, col, dim);
   }
 }
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* __restrict__ row, int col, int dim, const float (&v)[8]) {
+__device__ __forceinline__ void store8(T* __restrict__ row, int col, int dim, const F8& v) {
   if constexpr (VEC) {
     if (col >= dim) return;
     if constexpr (sizeof(T) == 2) {
       uint4 r;
       __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+      for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(v.p[k].x, v.p[k].y);
       st_stream(reinterpret_cast<uint4*>(row + col), r);
     } else {
-      uint4* p = reinterpret_cast<uint4*>(row + col);
-      st_stream(p, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-      st_stream(p + 1, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+      float4* p = reinterpret_cast<float4*>(row + col);
+      __stcs(p, make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y));
+      __stcs(p + 1, make_float4(v.p[2].x, v.p[2].y, v.p[3].x, v.p[3].y));
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (col + 32 * i < dim) row[col + 32 * i] = from_f32<T>(v[i]);
+      if (col + 32 * i < dim) row[col + 32 * i] = from_f32<T>(i & 1 ? v.p[i / 2].y : v.p[i / 2].x);
+  }
+}
+
+// Eight columns of a vector in shared memory.
+template <bool VEC>
+__device__ __forceinline__ F8 load8_shared(const float* v, int col, int dim) {
+  if constexpr (VEC) {
+    if (col >= dim) return all8(0.f);
+    return join(*reinterpret_cast<const float4*>(v + col), *reinterpret_cast<const float4*>(v + col + 4));
+  } else {
+    return load8<float, false>(v, col, dim);
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8_shared(float* v, int col, int dim, const F8& f) {
+  if constexpr (VEC) {
+    if (col >= dim) return;
+    *reinterpret_cast<float4*>(v + col) = make_float4(f.p[0].x, f.p[0].y, f.p[1].x, f.p[1].y);
+    *reinterpret_cast<float4*>(v + col + 4) = make_float4(f.p[2].x, f.p[2].y, f.p[3].x, f.p[3].y);
+  } else {
+    store8<float, false>(v, col, dim, f);
+  }
+}
+
+// 1 for the columns inside the row, 0 for the others (a factor, so that pairs stay pairs).
+template <bool VEC>
+__device__ __forceinline__ F8 mask8(int col, int dim) {
+  if constexpr (VEC) {
+    return all8(col < dim ? 1.f : 0.f);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = col + 32 * i < dim ? 1.f : 0.f;
+    return {{make_float2(v[0], v[1]), make_float2(v[2], v[3]), make_float2(v[4], v[5]), make_float2(v[6], v[7])}};
   }
 }
 
@@ -142,6 +180,61 @@ struct RowSum {
       }
     }
     return v;
+  }
+};
+
+// N values (2 or 4) summed over a warp: afterwards lane l holds the sum of
+// value l / (32 / N).  Lanes first trade values, so that N values take
+// N - 1 + log2(32 / N) shuffles instead of 5 N.
+template <int N>
+__device__ __forceinline__ float warp_sums(const float (&v)[N]) {
+  static_assert(N == 2 || N == 4, "two or four values");
+  const int lane = threadIdx.x & 31;
+  float s;
+  if constexpr (N == 4) {
+    const bool hi = (lane & 16) != 0;
+    const float a = (hi ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[2], 16);
+    const float b = (hi ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[1] : v[3], 16);
+    const bool odd = (lane & 8) != 0;
+    s = (odd ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 8);
+  } else {
+    const bool hi = (lane & 16) != 0;
+    s = (hi ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 16);
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+  }
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  return s;
+}
+
+// The same over the W warps of a group, all N sums to every thread.  `sh`
+// holds 2 x W x N floats (16-byte aligned); its halves alternate as in RowSum.
+template <int N, bool MULTI>
+struct GroupSums {
+  float* sh;
+  int warps, warp, barrier, turn;
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
+    const float s = warp_sums<N>(v);
+    const int lane = threadIdx.x & 31;
+    if constexpr (MULTI) {
+      float* half = sh + (turn & 1) * warps * N;
+      ++turn;
+      if (lane % (32 / N) == 0) half[warp * N + lane / (32 / N)] = s;
+      asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(warps * 32) : "memory");
+      using Row = typename std::conditional<N == 4, float4, float2>::type;
+      const Row first = *reinterpret_cast<const Row*>(half);
+      memcpy(v, &first, sizeof(v));
+      for (int w = 1; w < warps; ++w) {
+        const Row more = *reinterpret_cast<const Row*>(half + w * N);
+        float m[N];
+        memcpy(m, &more, sizeof(m));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += m[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, s, i * (32 / N));
+    }
   }
 };
 
