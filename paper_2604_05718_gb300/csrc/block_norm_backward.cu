@@ -14,18 +14,19 @@
 // sums of the rows under one gate follow from two, S1 = sum G n1 and S0 = sum G:
 // d w_post += gate S1, d b_post += gate S0, d gate = w_post S1 + b_post S0.
 //
-// Bound: HBM (y, x, dx' and dh in, dy and dx out).  A group of warps keeps
-// eight columns a thread of a run of neighbouring rows, with A, B and the
-// column sums in registers; the sums leave them once, at the end of the run
-// (or of an image, for its gate).  Column sums are joined in fixed order, first
-// over the groups of a block in shared memory, then over blocks by a second
-// kernel: no atomics, the same bits every time.
+// Bound: HBM (y, x, dx' and dh in, dy and dx out).  A group of warps, one where
+// the row has up to 768 features, works on a run of neighbouring rows, with
+// four column sums in registers; they leave them once, at the end of the run
+// (or of an image, for its gate).  Column sums are joined in fixed order,
+// first over the groups of a block in shared memory, then over blocks by a
+// second kernel: no atomics, the same bits every time.
 //
-// The sums take many registers, so few warps are there to hide the loads.
+// The sums take most registers, so few warps are there to hide latencies.
 // Rows that are 16-byte aligned therefore come through a ring in shared
-// memory, filled by bulk copies some pairs of rows ahead; two rows are worked
-// on at once and share their two barriers.  54208 x 768 bf16, layer norm on
-// both sides: BWD0 us from loads in place, BWD1 through the ring.
+// memory that bulk copies fill rows ahead; and a thread has up to 24 columns
+// of a row, whose chains overlap, without barriers in between.  54208 x 768
+// bf16, layer norm on both sides: 192 us from loads in place, 164 with rows
+// spread over three warps (two barriers a row), BWD1 with a warp a row.
 #include <atomic>
 
 #include "block_launch.h"
@@ -39,25 +40,24 @@ using namespace norm;
 
 constexpr int kMaxBlocks = 160;  // blocks of the row kernel: one per SM
 constexpr int kSums = 5;         // column sums: w_pre, b_pre, w_post, b_post, gate per channel
-constexpr int kMaxRing = 4;      // stages of a group's ring
+constexpr int kMaxRing = 4;      // rows in a group's ring
 constexpr uint64_t kWaitNs = 2000000000ull;
 
-// Chunks of columns that a thread holds: one as long as 12 warps span the row
-// (168 registers a thread hold the sums and two rows), two as long as 12 warps
-// do then, else four in up to 16 warps.
-__host__ __device__ constexpr int chunks_per_thread(int dim) {
-  return dim <= 12 * kNormWarpCols ? 1 : (dim <= 24 * kNormWarpCols ? 2 : 4);
+// Chunks of 256 columns that a warp holds (8 C columns a thread): the whole row
+// if it can, else the count that leaves no warp of a group half empty.  Their
+// sums and row take about 30 + 56 C registers, which sets the block's warps.
+__host__ __device__ constexpr int chunks_per_warp(int dim) {
+  const int chunks = (dim + kNormWarpCols - 1) / kNormWarpCols;
+  return chunks == 1 ? 1 : chunks > 24 ? 4 : chunks % 3 == 0 ? 3 : 2;
 }
-__host__ __device__ constexpr int block_warps(int chunks) { return chunks == 4 ? 16 : 12; }
+__host__ __device__ constexpr int block_warps(int c) { return c == 3 ? 8 : c == 2 ? 12 : 16; }
 __host__ __device__ constexpr int warps_per_row(int dim) {
-  return (dim + kNormWarpCols * chunks_per_thread(dim) - 1) / (kNormWarpCols * chunks_per_thread(dim));
+  return (dim + kNormWarpCols * chunks_per_warp(dim) - 1) / (kNormWarpCols * chunks_per_warp(dim));
 }
-// Shared memory for the rings: what a block may have (227 KB), less the weight in it and 2 KB of barriers and sums.
-__host__ __device__ constexpr int ring_bytes(int chunks) {
-  return 225 * 1024 - chunks * 2 * block_warps(chunks) * 32 * 16;
-}
-// Rows that a group works on at once.
-__host__ __device__ constexpr int rows_at_once(int chunks) { return chunks == 1 ? 2 : 1; }
+// Most groups of a block (a ring of long rows may leave room for fewer).
+__host__ __device__ constexpr int max_groups(int dim) { return block_warps(chunks_per_warp(dim)) / warps_per_row(dim); }
+// Shared memory of a block for the groups: 227 KB less 2 KB of barriers and sums.
+constexpr int kSharedBytes = 225 * 1024;
 
 // The run of rows of group g out of `all`, sizes one apart at most.
 struct Run {
@@ -73,17 +73,20 @@ __device__ __forceinline__ int64_t group_of(int64_t row, int64_t all, int64_t to
   return row < long_rows ? row / (per + 1) : extra + (row - long_rows) / per;
 }
 
-// Workspace: column sums [kSums][blocks][dim], then the gate's parts of the
-// images that a run shares with an earlier one (head) or a later one (tail).
+// Workspace: column sums [kSums][blocks][dim], then for each group the gate's
+// parts of the images that its run shares with an earlier one (head) or a
+// later one (tail), and the sums for w_post and b_post over the gates closed so far.
 struct Parts {
   float* sums;
   float* head;
   float* tail;
+  float* w_post;
+  float* b_post;
 };
 __device__ __forceinline__ Parts parts_of(const NormBackward& a, int blocks, int64_t all) {
   float* sums = a.partial;
   float* head = sums + static_cast<int64_t>(kSums) * blocks * a.dim;
-  return {sums, head, head + all * a.dim};
+  return {sums, head, head + all * a.dim, head + 2 * all * a.dim, head + 3 * all * a.dim};
 }
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -93,32 +96,22 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-// One stage of a group's ring: R rows of y, x, dh and dx' one after another, and their statistics.
-template <typename TY, typename TX, int R>
-struct Stage {
-  static constexpr int kRowBytes = 2 * sizeof(TY) + 2 * sizeof(TX);
-  __host__ __device__ static constexpr int bytes(int dim) { return R * (dim * kRowBytes + 16); }
+// A row in a group's ring: y, dh, x and dx' one after another, and the statistics.
+template <typename TY, typename TX>
+struct Slot {
+  __host__ __device__ static constexpr int bytes(int dim) {
+    return dim * static_cast<int>(2 * sizeof(TY) + 2 * sizeof(TX)) + 16;
+  }
   uint8_t* base;
   int dim;
   __device__ __forceinline__ TY* y() const { return reinterpret_cast<TY*>(base); }
-  __device__ __forceinline__ TY* d_h() const { return y() + R * dim; }
-  __device__ __forceinline__ TX* x() const { return reinterpret_cast<TX*>(d_h() + R * dim); }
-  __device__ __forceinline__ TX* d_x() const { return x() + R * dim; }
-  __device__ __forceinline__ float4* stats() const { return reinterpret_cast<float4*>(d_x() + R * dim); }
+  __device__ __forceinline__ TY* d_h() const { return y() + dim; }
+  __device__ __forceinline__ TX* x() const { return reinterpret_cast<TX*>(d_h() + dim); }
+  __device__ __forceinline__ TX* d_x() const { return x() + dim; }
+  __device__ __forceinline__ float4* stats() const { return reinterpret_cast<float4*>(d_x() + dim); }
 };
 
-// n rows of a matrix into a stage: one copy if they lie next to one another.
-template <typename T>
-__device__ __forceinline__ void load_rows(T* dst, const void* src, int64_t stride, int64_t row, int n, int dim, uint64_t* bar) {
-  const T* from = static_cast<const T*>(src) + row * stride;
-  if (stride == dim) {
-    bulk_load(dst, from, static_cast<uint32_t>(n * dim * sizeof(T)), bar);
-  } else {
-    for (int i = 0; i < n; ++i) bulk_load(dst + i * dim, from + i * stride, static_cast<uint32_t>(dim * sizeof(T)), bar);
-  }
-}
-
-// Eight columns of a staged row.
+// Eight columns of a row in the ring.
 template <typename T>
 __device__ __forceinline__ F8 staged8(const T* row, int col, int dim) {
   if (col >= dim) return all8(0.f);
@@ -130,16 +123,30 @@ __device__ __forceinline__ F8 staged8(const T* row, int col, int dim) {
   }
 }
 
-// RING: 16-byte aligned rows through shared memory (VEC accesses); otherwise loads of single elements.
+// Vectors in shared memory, eight columns a thread, without bank conflicts:
+// chunk, half of the eight, thread of the row.
+struct SharedVector {
+  float4* v;
+  int threads, at;
+  __device__ __forceinline__ F8 get(int c) const { return join(v[2 * c * threads + at], v[(2 * c + 1) * threads + at]); }
+  __device__ __forceinline__ void set(int c, const F8& f) const {
+    v[2 * c * threads + at] = make_float4(f.p[0].x, f.p[0].y, f.p[1].x, f.p[1].y);
+    v[(2 * c + 1) * threads + at] = make_float4(f.p[2].x, f.p[2].y, f.p[3].x, f.p[3].y);
+  }
+};
+// Bytes of one such vector.
+__host__ __device__ constexpr int vector_bytes(int dim) {
+  return warps_per_row(dim) * chunks_per_warp(dim) * kNormWarpCols * static_cast<int>(sizeof(float));
+}
+
+// RING: 16-byte aligned rows through shared memory (vector accesses); otherwise loads of single elements.
 template <typename TY, typename TX, int C, bool RING, bool MULTI>
 __global__ void __launch_bounds__(block_warps(C) * 32, 1)
     block_norm_backward_kernel(NormBackward a, int row_warps, int ring) {
-  constexpr int R = rows_at_once(C), N = 2 * R;
-  using S = Stage<TY, TX, R>;
-  extern __shared__ __align__(16) uint8_t dynamic[];  // the groups' rings; afterwards float [dim] to join sums in
-  __shared__ __align__(16) float sh[2 * block_warps(C) * N];
-  // The weight that is used least, out of registers: chunk, half of its eight columns, thread of the row.
-  __shared__ float4 pre_weight[C][2][block_warps(C) * 32];
+  using Row = Slot<TY, TX>;
+  // w_pre; A and B of each group; the groups' rings.  Afterwards the groups' column sums.
+  extern __shared__ __align__(16) uint8_t dynamic[];
+  __shared__ __align__(16) float sh[4 * block_warps(C)];
   __shared__ uint64_t full[block_warps(C)][kMaxRing];
   __shared__ int dead;  // a wait ran out: no further one is taken
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -157,53 +164,48 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
   wait_for_previous_grid();
   allow_next_grid();
   check_offsets(a.offsets, a.batch, a.rows, a.status);
-  GroupSums<N, MULTI> sum{sh + group * 2 * w * N, w, in_group, group + 1, 0};
+  GroupSums<2, MULTI> sum{sh + group * 4 * w, w, in_group, group + 1, 0};
   const int64_t total = used_rows(a.offsets, a.batch, a.rows);
   const int64_t all = static_cast<int64_t>(gridDim.x) * groups, g = static_cast<int64_t>(blockIdx.x) * groups + group;
   const Run run = run_of(g, all, total);
   const Parts parts = parts_of(a, gridDim.x, all);
   const float inv_dim = 1.f / static_cast<float>(a.dim);
   const bool post = a.post_weight != nullptr, per_image = a.gate != nullptr && a.gate_per_image;
-
-  // Stage s of the run: rows run.begin + s R .., into slot s % ring.
-  auto slot = [&](int64_t s) {
-    return S{dynamic + (static_cast<int64_t>(group) * ring + s % ring) * S::bytes(a.dim), a.dim};
+  const int vector = vector_bytes(a.dim);
+  const auto shared_vector = [&](int k) {
+    return SharedVector{reinterpret_cast<float4*>(dynamic + k * vector), w * 32, in_group * 32 + lane};
   };
-  const int64_t stages = (run.end - run.begin + R - 1) / R;
-  auto fill = [&](int64_t s) {  // by one thread of the group
-    const int64_t row = run.begin + s * R;
-    const int n = run.end - row < R ? static_cast<int>(run.end - row) : R;
-    uint64_t* bar = &full[group][s % ring];
-    const S to = slot(s);
-    const uint32_t bytes = n * (a.dim * (sizeof(TY) + sizeof(TX) + (a.d_h != nullptr ? sizeof(TY) : 0) +
-                                         (a.d_residual_out != nullptr ? sizeof(TX) : 0)) + 16);
-    ptx::mbar_arrive_expect_tx(bar, bytes);
-    load_rows<TY>(to.y(), a.y, a.y_stride, row, n, a.dim, bar);
-    load_rows<TX>(to.x(), a.residual, a.residual_stride, row, n, a.dim, bar);
-    if (a.d_h != nullptr) load_rows<TY>(to.d_h(), a.d_h, a.d_h_stride, row, n, a.dim, bar);
+  const SharedVector pre_weight = shared_vector(0), scale = shared_vector(1 + 2 * group), shift = shared_vector(2 + 2 * group);
+
+  uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * ring * Row::bytes(a.dim);
+  auto fill = [&](int64_t row, int k) {  // by one thread of the group
+    const Row to{ring_base + k * Row::bytes(a.dim), a.dim};
+    uint64_t* bar = &full[group][k];
+    const uint32_t bytes_y = a.dim * static_cast<uint32_t>(sizeof(TY)), bytes_x = a.dim * static_cast<uint32_t>(sizeof(TX));
+    ptx::mbar_arrive_expect_tx(bar, bytes_y + bytes_x + (a.d_h != nullptr ? bytes_y : 0) +
+                                        (a.d_residual_out != nullptr ? bytes_x : 0) + 16);
+    bulk_load(to.y(), static_cast<const TY*>(a.y) + row * a.y_stride, bytes_y, bar);
+    bulk_load(to.x(), static_cast<const TX*>(a.residual) + row * a.residual_stride, bytes_x, bar);
+    if (a.d_h != nullptr) bulk_load(to.d_h(), static_cast<const TY*>(a.d_h) + row * a.d_h_stride, bytes_y, bar);
     if (a.d_residual_out != nullptr)
-      load_rows<TX>(to.d_x(), a.d_residual_out, a.d_residual_out_stride, row, n, a.dim, bar);
-    bulk_load(to.stats(), a.stats + row, n * 16, bar);
+      bulk_load(to.d_x(), static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, bytes_x, bar);
+    bulk_load(to.stats(), a.stats + row, 16, bar);
   };
   const bool filler = in_group == 0 && lane == 0;
   if constexpr (RING) {
-    if (filler)
-      for (int64_t s = 0; s < ring && s < stages; ++s) fill(s);
+    if (filler) {
+#pragma unroll 1
+      for (int k = 0; k < ring && run.begin + k < run.end; ++k) fill(run.begin + k, k);
+    }
   }
 
   int col[C];
-  F8 scale[C], shift[C];                      // A and B
-  F8 s_wpre[C], s_bpre[C], s_one[C], s_n1[C]; // sums of dh n2, dh, G and G n1
-  F8 s_wpost[C], s_bpost[C], s_gate[C];       // of the gates closed so far; the last gate's
+  F8 s_wpre[C], s_bpre[C], s_one[C], s_n1[C];  // sums of dh n2, dh, G and G n1
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     col[c] = first_column<RING>(c * w + in_group, lane);
-    if (group == 0) {
-      const F8 v = param8<RING>(a.pre_weight, col[c], a.dim, 0.f);  // absent: h has no part in the gradients
-      pre_weight[c][0][in_group * 32 + lane] = make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y);
-      pre_weight[c][1][in_group * 32 + lane] = make_float4(v.p[2].x, v.p[2].y, v.p[3].x, v.p[3].y);
-    }
-    s_wpre[c] = s_bpre[c] = s_one[c] = s_n1[c] = s_wpost[c] = s_bpost[c] = s_gate[c] = all8(0.f);
+    if (group == 0) pre_weight.set(c, param8<RING>(a.pre_weight, col[c], a.dim, 0.f));  // absent: no part in the gradients
+    s_wpre[c] = s_bpre[c] = s_one[c] = s_n1[c] = all8(0.f);
   }
   __syncthreads();
 
@@ -212,30 +214,33 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const F8 g8 = param8<RING>(gate, col[c], a.dim, 1.f);
-      const F8 w8 = param8<RING>(a.post_weight, col[c], a.dim, 1.f), b8 = param8<RING>(a.post_bias, col[c], a.dim, 0.f);
+      F8 w8 = param8<RING>(a.post_weight, col[c], a.dim, 1.f), b8 = param8<RING>(a.post_bias, col[c], a.dim, 0.f);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        scale[c].p[k] = mul(g8.p[k], w8.p[k]);
-        shift[c].p[k] = mul(g8.p[k], b8.p[k]);
+        w8.p[k] = mul(g8.p[k], w8.p[k]);
+        b8.p[k] = mul(g8.p[k], b8.p[k]);
       }
+      scale.set(c, w8);  // each thread reads back its own columns only
+      shift.set(c, b8);
     }
   };
-  auto close_gate = [&](const float* gate) {
+  // What the sums under a gate give: the gradients of w_post and b_post (times gate), and of the gate.
+  auto gated = [&](const F8& gate, const F8& s) {
+    F8 r;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const F8 g8 = param8<RING>(gate, col[c], a.dim, 1.f);
-      const F8 w8 = param8<RING>(a.post_weight, col[c], a.dim, 1.f), b8 = param8<RING>(a.post_bias, col[c], a.dim, 0.f);
+    for (int k = 0; k < 4; ++k) r.p[k] = mul(gate.p[k], s.p[k]);
+    return r;
+  };
+  auto gate_gradient = [&](int c) {
+    const F8 w8 = param8<RING>(a.post_weight, col[c], a.dim, 1.f), b8 = param8<RING>(a.post_bias, col[c], a.dim, 0.f);
+    F8 r;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        s_wpost[c].p[k] = fma(g8.p[k], s_n1[c].p[k], s_wpost[c].p[k]);
-        s_bpost[c].p[k] = fma(g8.p[k], s_one[c].p[k], s_bpost[c].p[k]);
-        s_gate[c].p[k] = fma(w8.p[k], s_n1[c].p[k], mul(b8.p[k], s_one[c].p[k]));
-      }
-      s_n1[c] = s_one[c] = all8(0.f);
-    }
+    for (int k = 0; k < 4; ++k) r.p[k] = fma(w8.p[k], s_n1[c].p[k], mul(b8.p[k], s_one[c].p[k]));
+    return r;
   };
   int image = 0;
   int64_t image_begin = 0, image_end = INT64_MAX;
+  bool closed = false;
   auto gate_of = [&](int b) { return a.gate + static_cast<int64_t>(b) * a.dim; };
   auto open_image = [&](int b) {
     image = b;
@@ -243,197 +248,192 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
     image_end = __ldg(a.offsets + b + 1);
     open_gate(gate_of(b));
   };
-  // The gate's gradient over this run's rows of the image: all of its rows, or a part.
+  // The gate's gradient over this run's rows of the image: all of its rows, or
+  // a part.  The sums of w_post and b_post wait in the workspace, out of registers.
   auto close_image = [&]() {
-    close_gate(gate_of(image));
     float* to = image_begin < run.begin ? parts.head + g * a.dim
                 : image_end <= run.end  ? (a.d_gate == nullptr ? nullptr : a.d_gate + static_cast<int64_t>(image) * a.dim)
                                         : parts.tail + g * a.dim;
-    if (to == nullptr) return;
 #pragma unroll
-    for (int c = 0; c < C; ++c) store8<float, RING>(to, col[c], a.dim, s_gate[c]);
+    for (int c = 0; c < C; ++c) {
+      if (to != nullptr) store8<float, RING>(to, col[c], a.dim, gate_gradient(c));
+      const F8 g8 = param8<RING>(gate_of(image), col[c], a.dim, 0.f);
+      F8 w8 = gated(g8, s_n1[c]), b8 = gated(g8, s_one[c]);
+      if (closed) {
+        const F8 w0 = load8<float, RING>(parts.w_post + g * a.dim, col[c], a.dim);
+        const F8 b0 = load8<float, RING>(parts.b_post + g * a.dim, col[c], a.dim);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          w8.p[k] = add(w8.p[k], w0.p[k]);
+          b8.p[k] = add(b8.p[k], b0.p[k]);
+        }
+      }
+      store8<float, RING>(parts.w_post + g * a.dim, col[c], a.dim, w8);
+      store8<float, RING>(parts.b_post + g * a.dim, col[c], a.dim, b8);
+      s_n1[c] = s_one[c] = all8(0.f);
+    }
+    closed = true;
   };
   if (!per_image) open_gate(a.gate);
   else if (run.begin < run.end) open_image(find_image(a.offsets, a.batch, run.begin));
 
-  // Rows lo .. hi - 1 out of the R of stage s, all of them (ALL) or some; `last`: no others of the stage follow.
-  auto work = [&](auto all_rows, int64_t s, int64_t lo, int64_t hi, bool last) {
-    constexpr bool ALL = decltype(all_rows)::value;
-    const int64_t row0 = run.begin + s * R;
-    const S in = slot(s);
-    auto live = [&](int r) { return ALL || (row0 + r >= lo && row0 + r < hi); };
-    F8 y[R][C], x[R][C], dh[R][C];
-    float4 st[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if constexpr (!ALL) {  // rows of zeros add nothing to any sum
-        st[r] = make_float4(0.f, 1.f, 0.f, 1.f);
-#pragma unroll
-        for (int c = 0; c < C; ++c) y[r][c] = x[r][c] = all8(0.f);
+  int k_slot = 0;
+  uint32_t phase = 0;
+#pragma unroll 1
+  for (int64_t row = run.begin; row < run.end; ++row) {
+    if (row >= image_end && image < a.batch - 1) {
+      close_image();
+      int b = image + 1;
+      while (b < a.batch - 1 && row >= __ldg(a.offsets + b + 1)) ++b;
+      open_image(b);
+    }
+    const Row in{ring_base + k_slot * Row::bytes(a.dim), a.dim};
+    F8 y[C], x[C], dh[C];
+    float4 st;
+    if constexpr (RING) {
+      // After a wait that ran out the rows are worked on as they are: the call
+      // has failed, and leaving would strand the group's other warps.
+      if (!ptx::mbar_wait(&full[group][k_slot], phase, &dead, kWaitNs)) {
+        dead = 1;
+        report(a.status, MPM_ERR_DEVICE_TIMEOUT, 31);
       }
+      st = *in.stats();
+    } else {
+      st = __ldg(a.stats + row);
+    }
 #pragma unroll
-      for (int c = 0; c < C; ++c) dh[r][c] = all8(0.f);
-      if (!live(r)) continue;
-      const int64_t row = row0 + r;
+    for (int c = 0; c < C; ++c) {
       if constexpr (RING) {
-        st[r] = in.stats()[r];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          y[r][c] = staged8(in.y() + r * a.dim, col[c], a.dim);
-          x[r][c] = staged8(in.x() + r * a.dim, col[c], a.dim);
-          if (a.d_h != nullptr) dh[r][c] = staged8(in.d_h() + r * a.dim, col[c], a.dim);
-        }
+        y[c] = staged8(in.y(), col[c], a.dim);
+        x[c] = staged8(in.x(), col[c], a.dim);
+        dh[c] = a.d_h != nullptr ? staged8(in.d_h(), col[c], a.dim) : all8(0.f);
       } else {
-        st[r] = __ldg(a.stats + row);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          y[r][c] = load8<TY, false>(static_cast<const TY*>(a.y) + row * a.y_stride, col[c], a.dim);
-          x[r][c] = load8<TX, false>(static_cast<const TX*>(a.residual) + row * a.residual_stride, col[c], a.dim);
-          if (a.d_h != nullptr)
-            dh[r][c] = load8<TY, false>(static_cast<const TY*>(a.d_h) + row * a.d_h_stride, col[c], a.dim);
-        }
+        y[c] = load8<TY, false>(static_cast<const TY*>(a.y) + row * a.y_stride, col[c], a.dim);
+        x[c] = load8<TX, false>(static_cast<const TX*>(a.residual) + row * a.residual_stride, col[c], a.dim);
+        dh[c] = a.d_h != nullptr ? load8<TY, false>(static_cast<const TY*>(a.d_h) + row * a.d_h_stride, col[c], a.dim)
+                                 : all8(0.f);
       }
     }
-    float v[N];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
+    float v[2];
+    {
       float2 sa = pair(0.f), san = pair(0.f);
+      const float2 minus_m1 = pair(-st.x), r1 = pair(st.y), minus_m2 = pair(-st.z), r2 = pair(st.w), alpha = pair(a.alpha);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const F8 w_pre = join(pre_weight[c][0][in_group * 32 + lane], pre_weight[c][1][in_group * 32 + lane]);
+        const F8 w_pre = pre_weight.get(c), A = scale.get(c), B = shift.get(c);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float2 n1 = mul(add(y[r][c].p[k], pair(-st[r].x)), pair(st[r].y));
-          const float2 xo = fma(n1, scale[c].p[k], fma(pair(a.alpha), x[r][c].p[k], shift[c].p[k]));
-          const float2 n2 = mul(add(xo, pair(-st[r].z)), pair(st[r].w));
-          const float2 d = dh[r][c].p[k], aw = mul(d, w_pre.p[k]);  // zero outside the row: dh is
+          const float2 n1 = mul(add(y[c].p[k], minus_m1), r1);
+          const float2 xo = fma(n1, A.p[k], fma(alpha, x[c].p[k], B.p[k]));
+          const float2 n2 = mul(add(xo, minus_m2), r2);
+          const float2 d = dh[c].p[k], aw = mul(d, w_pre.p[k]);  // zero outside the row: dh is
           s_bpre[c].p[k] = add(s_bpre[c].p[k], d);
           s_wpre[c].p[k] = fma(d, n2, s_wpre[c].p[k]);
           sa = add(sa, aw);
           san = fma(aw, n2, san);
-          y[r][c].p[k] = n1;
-          x[r][c].p[k] = n2;
-          dh[r][c].p[k] = aw;
+          y[c].p[k] = n1;
+          x[c].p[k] = n2;
+          dh[c].p[k] = aw;
         }
       }
-      v[2 * r] = sa.x + sa.y;
-      v[2 * r + 1] = san.x + san.y;
+      v[0] = sa.x + sa.y;
+      v[1] = san.x + san.y;
     }
     sum(v);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float2 minus_a = pair(a.layer ? -v[2 * r] * inv_dim : 0.f), minus_an = pair(-v[2 * r + 1] * inv_dim);
-      const int64_t row = row0 + r;
+    {
+      const float2 minus_a = pair(a.layer ? -v[0] * inv_dim : 0.f), minus_an = pair(-v[1] * inv_dim);
+      const float2 r2 = pair(st.w), alpha = pair(a.alpha);
       float2 sc = pair(0.f), scn = pair(0.f);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         // Taken as late as this: its registers are needed until here.
         F8 dx = all8(0.f), out;
-        if (live(r) && a.d_residual_out != nullptr) {
+        if (a.d_residual_out != nullptr) {
           if constexpr (RING)
-            dx = staged8(in.d_x() + r * a.dim, col[c], a.dim);
+            dx = staged8(in.d_x(), col[c], a.dim);
           else
             dx = load8<TX, false>(static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, col[c], a.dim);
         }
+        const F8 A = scale.get(c);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float2 n1 = y[r][c].p[k];
-          const float2 t = fma(x[r][c].p[k], minus_an, add(dh[r][c].p[k], minus_a));
-          const float2 grad = fma(pair(st[r].w), t, dx.p[k]);
+          const float2 n1 = y[c].p[k];
+          const float2 t = fma(x[c].p[k], minus_an, add(dh[c].p[k], minus_a));
+          const float2 grad = fma(r2, t, dx.p[k]);
           s_one[c].p[k] = add(s_one[c].p[k], grad);
           s_n1[c].p[k] = fma(grad, n1, s_n1[c].p[k]);
-          const float2 cw = mul(grad, scale[c].p[k]);
+          const float2 cw = mul(grad, A.p[k]);
           sc = add(sc, cw);  // used with a norm after the block only: its weight is zero outside the row
           scn = fma(cw, n1, scn);
-          out.p[k] = mul(pair(a.alpha), grad);
-          dh[r][c].p[k] = cw;
+          out.p[k] = mul(alpha, grad);
+          dh[c].p[k] = cw;
         }
-        if (live(r)) store8<TX, RING>(static_cast<TX*>(a.d_residual) + row * a.dim, col[c], a.dim, out);
+        store8<TX, RING>(static_cast<TX*>(a.d_residual) + row * a.dim, col[c], a.dim, out);
       }
-      v[2 * r] = sc.x + sc.y;
-      v[2 * r + 1] = scn.x + scn.y;
+      v[0] = sc.x + sc.y;
+      v[1] = scn.x + scn.y;
     }
-    // Past this barrier every warp of the group has taken the stage's rows.
+    // Past this every warp of the group has taken the slot's row.
     if (post)
       sum(v);
     else if constexpr (RING && MULTI)
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(w * 32) : "memory");
     if constexpr (RING) {
-      if (last) {
-        if constexpr (!MULTI) __syncwarp();
-        if (filler && s + ring < stages) fill(s + ring);
+      if constexpr (!MULTI) __syncwarp();
+      if (filler && row + ring < run.end) fill(row + ring, k_slot);
+      if (++k_slot == ring) {
+        k_slot = 0;
+        phase ^= 1u;
       }
     }
     if (post) {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float2 minus_c = pair(a.layer ? -v[2 * r] * inv_dim : 0.f), minus_cn = pair(-v[2 * r + 1] * inv_dim);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            dh[r][c].p[k] = mul(pair(st[r].y), fma(y[r][c].p[k], minus_cn, add(dh[r][c].p[k], minus_c)));
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
+      const float2 minus_c = pair(a.layer ? -v[0] * inv_dim : 0.f), minus_cn = pair(-v[1] * inv_dim), r1 = pair(st.y);
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (live(r)) store8<TY, RING>(static_cast<TY*>(a.d_y) + (row0 + r) * a.dim, col[c], a.dim, dh[r][c]);
-  };
-
-  for (int64_t s = 0; s < stages; ++s) {
-    const int64_t row0 = run.begin + s * R;
-    const int64_t stop = run.end < row0 + R ? run.end : row0 + R;
-    if constexpr (RING) {
-      // After a wait that ran out the rows are worked on as they are: the call
-      // has failed, and leaving would strand the group's other warps.
-      if (!ptx::mbar_wait(&full[group][s % ring], static_cast<uint32_t>(s / ring) & 1u, &dead, kWaitNs)) {
-        dead = 1;
-        report(a.status, MPM_ERR_DEVICE_TIMEOUT, 31);
-      }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          dh[c].p[k] = mul(r1, fma(y[c].p[k], minus_cn, add(dh[c].p[k], minus_c)));
     }
-    for (int64_t lo = row0; lo < stop;) {  // rows under one gate at a time
-      if (lo >= image_end && image < a.batch - 1) {
-        close_image();
-        int b = image + 1;
-        while (b < a.batch - 1 && lo >= __ldg(a.offsets + b + 1)) ++b;
-        open_image(b);
-      }
-      const int64_t hi = image_end < stop && image < a.batch - 1 ? image_end : stop;
-      if (hi - lo == R) work(std::true_type{}, s, lo, hi, true);
-      else work(std::false_type{}, s, lo, hi, hi == stop);
-      lo = hi;
-    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) store8<TY, RING>(static_cast<TY*>(a.d_y) + row * a.dim, col[c], a.dim, dh[c]);
   }
-  if (!per_image) close_gate(a.gate);
-  else if (run.begin < run.end) close_image();
+  if (per_image && run.begin < run.end) close_image();
 
-  // Column sums of the block's groups, joined in the groups' order.
-  float* joined = reinterpret_cast<float*>(dynamic);
-  auto leave = [&](F8(&sums)[C], int which) {
+  // Column sums of the block's groups, side by side in shared memory (where A
+  // and B and the rings were), then added in the groups' order.
+  const int quads = vector / 16;
+  float4* const side = reinterpret_cast<float4*>(dynamic);
+  auto leave = [&](int which, auto value) {
     float* out = parts.sums + (static_cast<int64_t>(which) * gridDim.x + blockIdx.x) * a.dim;
-    for (int k = 0; k < groups; ++k) {
-      if (groups > 1) __syncthreads();
-      if (group != k) continue;
+    const SharedVector mine{side + group * quads, w * 32, in_group * 32 + lane};
+    __syncthreads();
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        // Each column belongs to the same lane and warp of every group.
-        if (k > 0) {
-          const F8 before = load8_shared<RING>(joined, col[c], a.dim);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sums[c].p[i] = add(sums[c].p[i], before.p[i]);
-        }
-        if (k == groups - 1) store8<float, RING>(out, col[c], a.dim, sums[c]);
-        else store8_shared<RING>(joined, col[c], a.dim, sums[c]);
+    for (int c = 0; c < C; ++c) mine.set(c, value(c));
+    __syncthreads();
+    for (int q = threadIdx.x; q < quads; q += blockDim.x) {
+      float4 s = side[q];
+      for (int k = 1; k < groups; ++k) {
+        const float4 t = side[k * quads + q];
+        s = make_float4(s.x + t.x, s.y + t.y, s.z + t.z, s.w + t.w);
       }
+      const int at = q % (w * 32), c = q / (w * 32) / 2, half = q / (w * 32) % 2;
+      const int first = first_column<RING>(c * w + at / 32, at % 32);
+      const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (column<RING>(first, 4 * half + i) < a.dim) out[column<RING>(first, 4 * half + i)] = v[i];
     }
   };
-  if (a.d_pre_weight != nullptr) leave(s_wpre, 0);
-  if (a.d_pre_bias != nullptr) leave(s_bpre, 1);
-  if (a.d_post_weight != nullptr) leave(s_wpost, 2);
-  if (a.d_post_bias != nullptr) leave(s_bpost, 3);
-  if (a.d_gate != nullptr && !per_image) leave(s_gate, 4);
+  // Over the gates of a run: what its images left in the workspace, or the one gate's sums.
+  auto over_gates = [&](const float* kept, const F8(&s)[C], int c) {
+    if (!per_image) return gated(param8<RING>(a.gate, col[c], a.dim, 1.f), s[c]);
+    return closed ? load8<float, RING>(kept + g * a.dim, col[c], a.dim) : all8(0.f);
+  };
+  if (a.d_pre_weight != nullptr) leave(0, [&](int c) { return s_wpre[c]; });
+  if (a.d_pre_bias != nullptr) leave(1, [&](int c) { return s_bpre[c]; });
+  if (a.d_post_weight != nullptr) leave(2, [&](int c) { return over_gates(parts.w_post, s_n1, c); });
+  if (a.d_post_bias != nullptr) leave(3, [&](int c) { return over_gates(parts.b_post, s_one, c); });
+  if (a.d_gate != nullptr && !per_image) leave(4, [&](int c) { return gate_gradient(c); });
 }
 
 constexpr int kJoinCols = 32, kJoinRows = 16;
@@ -485,30 +485,48 @@ __global__ void __launch_bounds__(kJoinCols * kJoinRows) block_norm_join_kernel(
   *out = s;
 }
 
-int groups_of(int dim) { return block_warps(chunks_per_thread(dim)) / warps_per_row(dim); }
+// Groups of a block and rows of each one's ring: as many groups as warps allow
+// two rows each, and up to kMaxRing rows.  No groups: the rows are too long for it.
+struct RingPlan {
+  int groups, rows;
+};
+RingPlan plan_ring(int dim, int row_bytes) {
+  const int vector = vector_bytes(dim);
+  for (int depth = 2; depth > 0; --depth) {
+    int groups = (kSharedBytes - vector) / (depth * row_bytes + 2 * vector);
+    if (groups > max_groups(dim)) groups = max_groups(dim);
+    if (groups > 0) {
+      const int rows = ((kSharedBytes - vector) / groups - 2 * vector) / row_bytes;
+      return {groups, rows < kMaxRing ? rows : kMaxRing};
+    }
+  }
+  return {0, 0};
+}
 
 template <typename TY, typename TX, int C, bool RING, bool MULTI>
-cudaError_t launch_instance(const NormBackward& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
   const auto kernel = block_norm_backward_kernel<TY, TX, C, RING, MULTI>;
-  const int w = warps_per_row(a.dim), groups = groups_of(a.dim);
-  const int stage = Stage<TY, TX, rows_at_once(C)>::bytes(a.dim);
-  int ring = RING ? ring_bytes(C) / (groups * stage) : 0;
-  if (ring > kMaxRing) ring = kMaxRing;
-  const size_t rings = static_cast<size_t>(groups) * ring * stage, joined = groups > 1 ? sizeof(float) * a.dim : 0;
+  const int w = warps_per_row(a.dim), vector = vector_bytes(a.dim);
+  int groups = ring.groups;
+  if (!RING) {
+    groups = (kSharedBytes - vector) / (2 * vector);
+    if (groups > max_groups(a.dim)) groups = max_groups(a.dim);
+  }
+  const size_t smem = vector + groups * (2 * static_cast<size_t>(vector) + (RING ? ring.rows * Slot<TY, TX>::bytes(a.dim) : 0));
   static std::atomic<uint64_t> attr_done{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(attr_done.load() & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(C));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
     attr_done.fetch_or(bit);
   }
   const int64_t want = a.rows > 0 ? (a.rows + groups - 1) / groups : 1;  // without rows the sums are still written
   const int most = num_sms < kMaxBlocks ? num_sms : kMaxBlocks;
   const int grid = static_cast<int>(want < most ? want : most);
-  e = launch_dependent(kernel, dim3(grid), dim3(groups * w * 32), rings > joined ? rings : joined, stream, a, w, ring);
+  e = launch_dependent(kernel, dim3(grid), dim3(groups * w * 32), smem, stream, a, w, ring.rows);
   if (e != cudaSuccess) return e;
   const bool per_image = a.gate != nullptr && a.gate_per_image && a.d_gate != nullptr;
   if (a.d_gate == nullptr && a.d_pre_weight == nullptr && a.d_pre_bias == nullptr && a.d_post_weight == nullptr &&
@@ -522,28 +540,29 @@ cudaError_t launch_instance(const NormBackward& a, int num_sms, cudaStream_t str
 }
 
 template <typename TY, typename TX, bool RING>
-cudaError_t launch_types(const NormBackward& a, int num_sms, cudaStream_t stream) {
-  if (warps_per_row(a.dim) == 1) return launch_instance<TY, TX, 1, RING, false>(a, num_sms, stream);
-  switch (chunks_per_thread(a.dim)) {
-    case 1: return launch_instance<TY, TX, 1, RING, true>(a, num_sms, stream);
-    case 2: return launch_instance<TY, TX, 2, RING, true>(a, num_sms, stream);
-    default: return launch_instance<TY, TX, 4, RING, true>(a, num_sms, stream);
+cudaError_t launch_types(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
+  const bool multi = warps_per_row(a.dim) > 1;
+  switch (chunks_per_warp(a.dim)) {
+    case 1: return launch_instance<TY, TX, 1, RING, false>(a, ring, num_sms, stream);
+    case 2: return multi ? launch_instance<TY, TX, 2, RING, true>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, 2, RING, false>(a, ring, num_sms, stream);
+    case 3: return multi ? launch_instance<TY, TX, 3, RING, true>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, 3, RING, false>(a, ring, num_sms, stream);
+    default: return launch_instance<TY, TX, 4, RING, true>(a, ring, num_sms, stream);
   }
 }
 
 template <typename TY, typename TX>
 cudaError_t launch_vec(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream) {
-  // Rows too long for a stage of the ring (fp32 from about 13,000 features) are loaded in place.
-  const int rows = rows_at_once(chunks_per_thread(a.dim));
-  const int stage = rows == 2 ? Stage<TY, TX, 2>::bytes(a.dim) : Stage<TY, TX, 1>::bytes(a.dim);
-  const bool ring = vec && groups_of(a.dim) * stage <= ring_bytes(chunks_per_thread(a.dim));
-  return ring ? launch_types<TY, TX, true>(a, num_sms, stream) : launch_types<TY, TX, false>(a, num_sms, stream);
+  const RingPlan ring = vec ? plan_ring(a.dim, Slot<TY, TX>::bytes(a.dim)) : RingPlan{0, 0};
+  return ring.groups > 0 ? launch_types<TY, TX, true>(a, ring, num_sms, stream)
+                         : launch_types<TY, TX, false>(a, ring, num_sms, stream);
 }
 
 }  // namespace
 
 size_t block_norm_workspace_floats(int dim) {
-  return static_cast<size_t>(dim) * kMaxBlocks * (kSums + 2 * static_cast<size_t>(groups_of(dim)));
+  return static_cast<size_t>(dim) * kMaxBlocks * (kSums + 4 * static_cast<size_t>(max_groups(dim)));
 }
 
 cudaError_t launch_block_norm_backward(const NormBackward& a, NormTypes types, bool vec, int num_sms,

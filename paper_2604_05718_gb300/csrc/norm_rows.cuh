@@ -26,12 +26,6 @@ template <bool VEC>
 __device__ __forceinline__ int column(int col, int i) {
   return VEC ? col + i : col + 32 * i;
 }
-// In a vector chunk all eight columns lie inside the row or none does (dim is a multiple of 8).
-template <bool VEC>
-__device__ __forceinline__ bool inside(int col, int i, int dim) {
-  return column<VEC>(col, VEC ? 0 : i) < dim;
-}
-
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 template <typename T>
@@ -114,27 +108,6 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int col, int dim, co
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (col + 32 * i < dim) row[col + 32 * i] = from_f32<T>(i & 1 ? v.p[i / 2].y : v.p[i / 2].x);
-  }
-}
-
-// Eight columns of a vector in shared memory.
-template <bool VEC>
-__device__ __forceinline__ F8 load8_shared(const float* v, int col, int dim) {
-  if constexpr (VEC) {
-    if (col >= dim) return all8(0.f);
-    return join(*reinterpret_cast<const float4*>(v + col), *reinterpret_cast<const float4*>(v + col + 4));
-  } else {
-    return load8<float, false>(v, col, dim);
-  }
-}
-template <bool VEC>
-__device__ __forceinline__ void store8_shared(float* v, int col, int dim, const F8& f) {
-  if constexpr (VEC) {
-    if (col >= dim) return;
-    *reinterpret_cast<float4*>(v + col) = make_float4(f.p[0].x, f.p[0].y, f.p[1].x, f.p[1].y);
-    *reinterpret_cast<float4*>(v + col + 4) = make_float4(f.p[2].x, f.p[2].y, f.p[3].x, f.p[3].y);
-  } else {
-    store8<float, false>(v, col, dim, f);
   }
 }
 
