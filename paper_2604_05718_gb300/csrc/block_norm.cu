@@ -22,6 +22,7 @@
 // norm on both sides: 85 us; now FWD1).
 #include "block_launch.h"
 #include "norm_rows.cuh"
+#include "ptx.cuh"
 
 namespace mpm {
 namespace {
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, MULTI ? 1 : (VEC ? C <
     }
     __syncthreads();
   }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
   const int groups = (blockDim.x >> 5) / w, group = warp / w, in_group = warp % w;
   RowSum<MULTI> sum{sh + group * 2 * w, w, in_group, group + 1, 0};

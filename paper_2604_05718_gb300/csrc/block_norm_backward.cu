@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
   __shared__ __align__(16) float sh[4 * block_warps(C)];
   __shared__ uint64_t full[block_warps(C)][kMaxRing];
   __shared__ int dead;  // a wait ran out: no further one is taken
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
   const int groups = (blockDim.x >> 5) / w, group = warp / w, in_group = warp % w;
   if (threadIdx.x == 0) {
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
   const SharedVector pre_weight = shared_vector(0), scale = shared_vector(1 + 2 * group), shift = shared_vector(2 + 2 * group);
 
   uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * ring * Row::bytes(a.dim);
-  auto fill = [&](int64_t row, int k) {  // by one thread of the group
+  auto fill = [&](int64_t row, int k) {  // by an elected lane of the group's first warp
     const Row to{ring_base + k * Row::bytes(a.dim), a.dim};
     uint64_t* bar = &full[group][k];
     const uint32_t bytes_y = a.dim * static_cast<uint32_t>(sizeof(TY)), bytes_x = a.dim * static_cast<uint32_t>(sizeof(TX));
@@ -191,9 +191,8 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
       bulk_load(to.d_x(), static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, bytes_x, bar);
     bulk_load(to.stats(), a.stats + row, 16, bar);
   };
-  const bool filler = in_group == 0 && lane == 0;
   if constexpr (RING) {
-    if (filler) {
+    if (in_group == 0 && ptx::elect_one()) {
 #pragma unroll 1
       for (int k = 0; k < ring && run.begin + k < run.end; ++k) fill(run.begin + k, k);
     }
@@ -380,7 +379,8 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(w * 32) : "memory");
     if constexpr (RING) {
       if constexpr (!MULTI) __syncwarp();
-      if (filler && row + ring < run.end) fill(row + ring, k_slot);
+      if (in_group == 0 && row + ring < run.end && ptx::elect_one()) fill(row + ring, k_slot);
+      __syncwarp();
       if (++k_slot == ring) {
         k_slot = 0;
         phase ^= 1u;

@@ -147,44 +147,32 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(QuantizeArgs a, bool
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_unit(T* p, int left, bool vec, const __nv_bfloat162 (&v)[4]) {
-  if constexpr (sizeof(T) == 2) {
-    if (vec && left >= kUnit) {
-      st_stream(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(v));
-    } else {
+// Eight values of a row where all of them lie inside it and 16-byte aligned.
+__device__ __forceinline__ void store_unit(__nv_bfloat16* p, const __nv_bfloat162 (&v)[4]) {
+  st_stream(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(v));
+}
+__device__ __forceinline__ void store_unit(float* p, const __nv_bfloat162 (&v)[4]) {
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i)
-        if (i < left) p[i] = i & 1 ? __high2bfloat16(v[i / 2]) : __low2bfloat16(v[i / 2]);
-    }
-  } else {
-    float f[kUnit];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 w = __bfloat1622float2(v[i]);
-      f[2 * i] = w.x;
-      f[2 * i + 1] = w.y;
-    }
-    if (vec && left >= kUnit) {
-      __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
-      __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < kUnit; ++i)
-        if (i < left) p[i] = f[i];
-    }
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = __bfloat1622float2(v[2 * i]), b = __bfloat1622float2(v[2 * i + 1]);
+    __stcs(reinterpret_cast<float4*>(p) + i, make_float4(a.x, a.y, b.x, b.y));
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, bool vec, int64_t scale_tiles) {
+// VEC: rows of 16-byte aligned values.  Otherwise a row's values (bf16 holds
+// them all) cross over in shared memory, so that a half warp stores 16
+// neighbours at a time: 50000 x 769 bf16 in DQ1 us, 122 with a lane's eight
+// values stored one by one.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, int64_t scale_tiles) {
   wait_for_previous_grid();
   allow_next_grid();
+  __shared__ __align__(16) __nv_bfloat16 rows[VEC ? 1 : kRowsAtOnce][VEC ? 8 : kTileCols + 8];
   const int tiles_k = mx::scale_tiles(a.dim), pitch = mx::code_pitch(a.dim);
   const int lane = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
   for (int64_t tile = blockIdx.x; tile < scale_tiles; tile += gridDim.x) {
     const int64_t row_tile = tile / tiles_k;
-    const int col = static_cast<int>(tile - row_tile * tiles_k) * kTileCols + lane * kUnit;
+    const int col0 = static_cast<int>(tile - row_tile * tiles_k) * kTileCols, col = col0 + lane * kUnit;
     const int64_t row0 = row_tile * mx::kTileRows + first;
     const uint8_t* codes = a.codes + row0 * pitch + col / 2;
     const uint8_t* scales = a.scales + tile * mx::kTileBytes + lane / 4;
@@ -202,28 +190,56 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, 
     for (int i = 0; i < kRows; ++i) {
       __nv_bfloat162 v[4];
       decode8(code[i], scale[i], v);
-      if (row0 + i * kRowsAtOnce < a.rows) store_unit(out + i * kRowsAtOnce * a.stride, a.dim - col, vec, v);
+      T* to = out + i * kRowsAtOnce * a.stride;
+      if constexpr (VEC) {
+        if (row0 + i * kRowsAtOnce < a.rows && col + kUnit <= a.dim) {
+          store_unit(to, v);
+          continue;
+        }
+        if (row0 + i * kRowsAtOnce < a.rows) {
+#pragma unroll
+          for (int j = 0; j < kUnit; ++j)
+            if (col + j < a.dim) to[j] = j & 1 ? T(__high2float(v[j / 2])) : T(__low2float(v[j / 2]));
+        }
+      } else {
+        __nv_bfloat16* mine = rows[first];
+        __syncwarp();  // the row before has been read
+        *reinterpret_cast<uint4*>(mine + lane * kUnit) = *reinterpret_cast<const uint4*>(v);
+        __syncwarp();
+        if (row0 + i * kRowsAtOnce < a.rows) {
+          T* row = to - lane * kUnit;
+#pragma unroll
+          for (int j = 0; j < kUnit; ++j) {
+            const int c = j * kLanes + lane;
+            if (col0 + c < a.dim) row[c] = T(__bfloat162float(mine[c]));
+          }
+        }
+      }
     }
   }
 }
 
-template <typename Kernel, typename Args>
-cudaError_t launch_tiles(Kernel kernel, int per_sm, const Args& a, bool vec, int num_sms, cudaStream_t stream) {
-  const int64_t tiles = mx::row_tiles(a.rows) * mx::scale_tiles(a.dim), most = static_cast<int64_t>(num_sms) * per_sm;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(tiles < most ? tiles : most)), dim3(kThreads), 0, stream, a,
-                          vec, tiles);
+template <typename Args>
+int tile_grid(const Args& a, int per_sm, int num_sms, int64_t* tiles) {
+  *tiles = mx::row_tiles(a.rows) * mx::scale_tiles(a.dim);
+  const int64_t most = static_cast<int64_t>(num_sms) * per_sm;
+  return static_cast<int>(*tiles < most ? *tiles : most);
 }
 
 template <typename T>
 cudaError_t quantize(const QuantizeArgs& a, bool vec, int num_sms, cudaStream_t stream) {
   static const int per_sm = resident_per_sm(quantize_kernel<T>, kThreads, 8);
-  return launch_tiles(quantize_kernel<T>, per_sm, a, vec, num_sms, stream);
+  int64_t tiles;
+  const int grid = tile_grid(a, per_sm, num_sms, &tiles);
+  return launch_dependent(quantize_kernel<T>, dim3(grid), dim3(kThreads), 0, stream, a, vec, tiles);
 }
 
-template <typename T>
-cudaError_t dequantize(const DequantizeArgs& a, bool vec, int num_sms, cudaStream_t stream) {
-  static const int per_sm = resident_per_sm(dequantize_kernel<T>, kThreads, 8);
-  return launch_tiles(dequantize_kernel<T>, per_sm, a, vec, num_sms, stream);
+template <typename T, bool VEC>
+cudaError_t dequantize(const DequantizeArgs& a, int num_sms, cudaStream_t stream) {
+  static const int per_sm = resident_per_sm(dequantize_kernel<T, VEC>, kThreads, 8);
+  int64_t tiles;
+  const int grid = tile_grid(a, per_sm, num_sms, &tiles);
+  return launch_dependent(dequantize_kernel<T, VEC>, dim3(grid), dim3(kThreads), 0, stream, a, tiles);
 }
 
 }  // namespace
@@ -233,7 +249,9 @@ cudaError_t launch_mxfp4_quantize(const QuantizeArgs& a, bool bf16, bool vec, in
 }
 
 cudaError_t launch_mxfp4_dequantize(const DequantizeArgs& a, bool bf16, bool vec, int num_sms, cudaStream_t stream) {
-  return bf16 ? dequantize<__nv_bfloat16>(a, vec, num_sms, stream) : dequantize<float>(a, vec, num_sms, stream);
+  if (bf16)
+    return vec ? dequantize<__nv_bfloat16, true>(a, num_sms, stream) : dequantize<__nv_bfloat16, false>(a, num_sms, stream);
+  return vec ? dequantize<float, true>(a, num_sms, stream) : dequantize<float, false>(a, num_sms, stream);
 }
 
 }  // namespace mpm

@@ -133,12 +133,6 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, 
 }
 __device__ __forceinline__ void wait_box_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void wait_box_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// True in one lane of a converged warp, always the same one.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t e;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-  return e != 0;
-}
 // Bounded wait of a whole warp: one answer for all of its lanes, which go on converged.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
@@ -224,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t at = smem0 + stage * kStageBytes, full = full0 + stage * 8;
           // A scale tile past the last one along K belongs to other rows, or reads as zeros: no product uses it.
           const int32_t kt = kb * kScaleTiles, nt = n0 / mx::kTileRows;
-          if (elect_one()) {
+          if (ptx::elect_one()) {
             if (leader) ptx::mbar_arrive_expect_tx(&ctl->full[stage], 2 * kStageBytes);
             load_pair(at, &map_a, full, kb * 128, m0);
             load_pair(at + kBytesA, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
@@ -276,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t scales = smem0 + stage * kStageBytes + kBytesA + kBytesB;
           const uint32_t sa = tmem0 + kScaleCols + stage * kStageCols, sb = sa + kScaleTiles * kColsSA;
           const int products = min(kStageK / 64, (a.k - kb * kStageK + 63) / 64);
-          if (elect_one()) {
+          if (ptx::elect_one()) {
 #pragma unroll
             for (int j = 0; j < kScaleTiles; ++j) {
               if (2 * j < products) {
@@ -300,14 +294,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (!ok) break;
-        if (elect_one()) commit_both(&ctl->acc_full[acc]);
+        if (ptx::elect_one()) commit_both(&ctl->acc_full[acc]);
         __syncwarp();
         if (++acc == 2) {
           acc = 0;
           acc_phase ^= 1u;
         }
       }
-      if (elect_one()) commit_local(&ctl->drain);
+      if (ptx::elect_one()) commit_local(&ctl->drain);
       __syncwarp();
       ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
     }

@@ -211,6 +211,17 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&v)[16]) {
                : "memory");
 }
 
+// True in one lane of a converged warp, always the same one.  What such a lane
+// issues takes its operands from uniform registers as they are; in a branch of
+// one lane each operand is moved there first (about 70 cycles an instruction).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+// The warp's index, in a form that the compiler knows to be uniform.
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0); }
+
 __device__ __forceinline__ void named_barrier_sync(uint32_t id, uint32_t threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
