@@ -2,20 +2,28 @@
 // accumulated in fp32 on the tensor cores: tcgen05.mma kind::mxf4 with a
 // power-of-two scale per 32 elements.
 //
-// A cluster of two CTAs (an SM pair) computes 256 x 192 tiles with
-// cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows of
-// B, the scales of its A rows and those of all of the tile's B rows.  A stage
-// holds 256 elements of every row, one 128-byte swizzle row of packed codes,
-// and takes four K = 64 products.  Scales go from shared memory to tensor
-// memory by tcgen05.cp, into columns that belong to the stage: the products
-// that read them have completed before the stage is filled again.
+// A cluster of two CTAs (an SM pair) computes 256 x 192 tiles with cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows
+// of B, the scales of its A rows and those of all of the tile's B rows.  A step
+// takes 256 elements of every row, one 128-byte swizzle row of packed codes,
+// and four K = 64 products.  Scales go from shared memory to tensor memory by
+// tcgen05.cp, into columns that belong to the slot they came in: the products
+// that read them have completed before the slot is filled again.
 //
 // Bound: with few features the output's bytes (2 M N of them against
-// (M + N) K / 2: 256 x 192 tiles of K = 768 take the tensor cores a quarter of
+// (M + N) K / 2: 256 x 192 tiles of K = 768 take the tensor cores a third of
 // the time that their output takes HBM), with many the tensor cores.  Hence
-// two accumulators (2 x 192 of the 512 tensor-memory columns, which leaves
-// 128 for the scales of five stages): a tile's output is written while the
-// next tile is computed.
+//  - two accumulators: a tile's output is written while the next one is
+//    computed;
+//  - A and B in rings of their own: where a row of A fits (K <= 1280), the A
+//    panel of a run of tiles stays in shared memory, and with it its scales in
+//    tensor memory.  Loading it again for every tile took as long as half of
+//    the output's writes (54208 x 768 x 2304 to bf16: 61 us, resident 57).
+// With many features the bound is shared memory: a step's operands are written
+// there once (32 KB) and read once (28 KB a CTA), 467 cycles at 128 bytes a
+// cycle against 384 of the products.  Tiles of 256 columns would halve that
+// gap but leave no tensor memory for a second accumulator or the scales; tiles
+// of 128 took as long as 192 for two thirds of the work, and a narrower last
+// tile (N = 1024 is 5.3 tiles) with runs of equal cost gained nothing.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -30,45 +38,75 @@ namespace {
 
 constexpr int kHalf = 128;             // rows of A per CTA
 constexpr int kTileM = 2 * kHalf;
-constexpr int kTileN = 192;
-constexpr int kStageK = 256;           // elements of a row per stage: 128 bytes
-constexpr int kBytesA = kHalf * 128;
-constexpr int kBytesB = kTileN / 2 * 128;
-constexpr int kScaleTiles = kStageK / (mx::kBlock * mx::kTileBlocks);      // scale tiles along K per stage
-constexpr int kBytesSA = kScaleTiles * mx::kTileBytes;
-constexpr int kBytesSB = 2 * kBytesSA;  // a tile's 192 rows of B lie in at most two row tiles
-constexpr int kStageBytes = kBytesA + kBytesB + kBytesSA + kBytesSB;
-constexpr int kStages = 5;
+constexpr int kStepK = 256;            // elements of a row per step: 128 bytes
+constexpr int kScaleTiles = kStepK / (mx::kBlock * mx::kTileBlocks);  // scale tiles along K per step
+constexpr int kSlotsA = 6;
+constexpr int kBytesA = kHalf * 128, kBytesSA = kScaleTiles * mx::kTileBytes, kSlotA = kBytesA + kBytesSA;
+constexpr int kMaxResident = kSlotsA - 1;  // steps of a panel that stays: one slot is left to begin the next one
+constexpr int kWarpCols = 64;              // columns of the tile that an epilogue warp writes
+constexpr int kBoxBytes = 32 * 128;        // staged output: 32 rows of 128 bytes, swizzled
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kScaleCols = 2 * kTileN;                 // first column of the scales
-constexpr uint32_t kColsSA = 4, kColsSB = 8;                // columns of one scale tile of A, of two of B
-constexpr uint32_t kStageCols = kScaleTiles * (kColsSA + kColsSB);
-constexpr int kWarpCols = 64;                               // columns of the tile that an epilogue warp writes
+constexpr uint32_t kColsSA = 4;            // tensor-memory columns of a scale tile
+constexpr uint64_t kWaitNs = 2000000000ull;
+
+constexpr int kTileN = 192;
+constexpr int kRowTiles = 2;               // scale tiles along N that a tile's 192 rows of B lie in, at most
+constexpr int kBytesB = kTileN / 2 * 128, kBytesSB = kRowTiles * kBytesSA, kSlotB = kBytesB + kBytesSB;
+constexpr int kSlotsB = 5;
+constexpr uint32_t kColsSB = kRowTiles * kColsSA;
+// Tensor memory: two accumulators, the scales of A's slots, those of B's.
+constexpr uint32_t kScalesA = 2 * kTileN, kScalesB = kScalesA + kSlotsA * kScaleTiles * kColsSA;
 constexpr int kEpilogueWarps = 4 * (kTileN / kWarpCols);
 constexpr int kThreads = (2 + kEpilogueWarps) * 32;
-constexpr int kBoxBytes = 32 * 128;                         // staged output: 32 rows of 128 bytes, swizzled
-constexpr uint64_t kWaitNs = 2000000000ull;
-static_assert(kScaleCols + kStages * kStageCols <= kTmemCols, "accumulators and scales share tensor memory");
-static_assert(kStageBytes % 1024 == 0 && kBytesA % 1024 == 0 && kBytesB % 1024 == 0, "swizzled tiles on 1024 bytes");
+constexpr int kRings = kSlotsA * kSlotA + kSlotsB * kSlotB;
+static_assert(kScalesB + kSlotsB * kScaleTiles * kColsSB <= kTmemCols, "accumulators and scales share tensor memory");
+static_assert(kSlotA % 1024 == 0 && kSlotB % 1024 == 0 && kBytesB % 1024 == 0, "swizzled tiles on 1024 bytes");
 
 // Instruction descriptor of kind::mxf4: E2M1 operands (1) in K-major order,
 // scales of type UE8M0 (bit 23), N / 8 and M / 16 in their fields.
-constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kTileN >> 3) << 17) | (1u << 23) |
-                            (static_cast<uint32_t>(kTileM >> 4) << 24);
+constexpr uint32_t kInstruction = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kTileN >> 3) << 17) | (1u << 23) |
+                                  (static_cast<uint32_t>(kTileM >> 4) << 24);
 // Which half of a 32-bit column's four scales a K = 64 product takes: fields of B and of A.
 __device__ __forceinline__ constexpr uint32_t scale_half(uint32_t which) { return (which << 4) | (which << 29); }
 
 struct Control {
-  uint64_t full[kStages];   // leader: both CTAs' operands of the stage landed
-  uint64_t empty[kStages];  // both: products reading the stage completed
-  uint64_t acc_full[2];     // both: accumulator complete
-  uint64_t acc_empty[2];    // leader: both CTAs read the accumulator
+  uint64_t full_a[kSlotsA], full_b[kSlotsB];    // leader: both CTAs' operands of the slot landed
+  uint64_t empty_a[kSlotsA], empty_b[kSlotsB];  // both: products reading the slot completed
+  uint64_t acc_full[2];                           // both: accumulator complete
+  uint64_t acc_empty[2];                          // leader: both CTAs read the accumulator
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
 };
 
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + kEpilogueWarps * kBoxBytes + sizeof(Control);
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kRings) + kEpilogueWarps * kBoxBytes + sizeof(Control);
+static_assert(kSmemBytes <= 227 * 1024, "a block's shared memory");
+
+// Place in a ring.
+template <int SLOTS>
+struct Ring {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == SLOTS) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// A cluster's run of tiles, numbered with n fastest.
+struct Tiles {
+  int64_t begin, end;
+  int n;  // tiles along n
+  __device__ __forceinline__ int64_t m_of(int64_t t) const { return t / n; }
+};
+__device__ __forceinline__ Tiles tiles_of(const MxMatmulArgs& a) {
+  const int n = (a.n + kTileN - 1) / kTileN;
+  const int64_t all = (a.m + kTileM - 1) / kTileM * n, clusters = gridDim.x / 2, c = blockIdx.x / 2;
+  const int64_t per = all / clusters, extra = all % clusters, begin = c * per + (c < extra ? c : extra);
+  return {begin, begin + per + (c < extra ? 1 : 0), n};
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -149,15 +187,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const __grid_constant__ CUtensorMap map_out, MxMatmulArgs a, bool tma_out, bool bias_vec) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
-  Control* ctl = reinterpret_cast<Control*>(smem + kStages * kStageBytes + kEpilogueWarps * kBoxBytes);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  Control* ctl = reinterpret_cast<Control*>(smem + kRings + kEpilogueWarps * kBoxBytes);
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      ptx::mbar_init(&ctl->full[s], 1);
-      ptx::mbar_init(&ctl->empty[s], 1);
+    for (int s = 0; s < kSlotsA; ++s) {
+      ptx::mbar_init(&ctl->full_a[s], 1);
+      ptx::mbar_init(&ctl->empty_a[s], 1);
+    }
+    for (int s = 0; s < kSlotsB; ++s) {
+      ptx::mbar_init(&ctl->full_b[s], 1);
+      ptx::mbar_init(&ctl->empty_b[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&ctl->acc_full[i], 1);
@@ -187,11 +229,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   wait_for_previous_grid();
   allow_next_grid();
 
-  const int tiles_n = (a.n + kTileN - 1) / kTileN;
-  const int64_t tiles = (a.m + kTileM - 1) / kTileM * tiles_n;
-  const int64_t clusters = gridDim.x / 2, cluster = blockIdx.x / 2;
-  const int stages_k = (a.k + kStageK - 1) / kStageK;
+  const Tiles run = tiles_of(a);
+  const int steps = (a.k + kStepK - 1) / kStepK;
   const int tiles_k = mx::scale_tiles(a.k);
+  // A panel (the 256 rows of A of a tile) stays for the run's next tiles of the same rows.
+  const bool resident = steps <= kMaxResident;
+  auto panel_begins = [&](int64_t t) { return !resident || t == run.begin || run.m_of(t) != run.m_of(t - 1); };
+  auto panel_ends = [&](int64_t t) { return !resident || t + 1 == run.end || run.m_of(t + 1) != run.m_of(t); };
   volatile int* abort_flag = &ctl->abort_flag;
 
   if (warp == 0) {
@@ -200,100 +244,125 @@ __global__ void __launch_bounds__(kThreads, 1)
     // In a branch of one lane every operand of a copy or product first moves to
     // a uniform register, about 70 cycles an instruction, which bound the
     // kernel: 8192 x 8192 x 8192 took 316 us instead of 176.
-    {
-      int stage = 0, issued = 0;
-      uint32_t phase = 0, issued_phase = 0;
-      bool ok = true;
-      const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
-      const uint32_t full0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full[0]), 0), 0);
-      for (int64_t t = cluster; ok && t < tiles; t += clusters) {
-        const int32_t m0 = static_cast<int32_t>(t / tiles_n) * kTileM + kHalf * static_cast<int32_t>(rank);
-        const int32_t n0 = static_cast<int32_t>(t % tiles_n) * kTileN;
-        for (int kb = 0; kb < stages_k; ++kb) {
-          if (!warp_wait(&ctl->empty[stage], phase ^ 1u, abort_flag)) {
+    Ring<kSlotsA> ra;
+    Ring<kSlotsB> rb;
+    int issued_a = 0, issued_b = 0;
+    uint32_t phase_a = 0, phase_b = 0;  // of the slots' last loads
+    bool ok = true;
+    const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
+    const uint32_t full_a0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full_a[0]), 0), 0);
+    const uint32_t full_b0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full_b[0]), 0), 0);
+    for (int64_t t = run.begin; ok && t < run.end; ++t) {
+      const int32_t m0 = static_cast<int32_t>(run.m_of(t)) * kTileM + kHalf * static_cast<int32_t>(rank);
+      const int32_t n0 = static_cast<int32_t>(t - run.m_of(t) * run.n) * kTileN, nt = n0 / mx::kTileRows;
+      const bool begins = panel_begins(t);
+      for (int kb = 0; kb < steps; ++kb) {
+        // A scale tile past the last one along K belongs to other rows, or reads as zeros: no product uses it.
+        const int32_t kt = kb * kScaleTiles;
+        if (begins) {
+          if (!warp_wait(&ctl->empty_a[ra.slot], ra.phase ^ 1u, abort_flag)) {
             fail(ctl, a.status, 21);
             ok = false;
             break;
           }
-          const uint32_t at = smem0 + stage * kStageBytes, full = full0 + stage * 8;
-          // A scale tile past the last one along K belongs to other rows, or reads as zeros: no product uses it.
-          const int32_t kt = kb * kScaleTiles, nt = n0 / mx::kTileRows;
+          const uint32_t at = smem0 + ra.slot * kSlotA, full = full_a0 + ra.slot * 8;
           if (ptx::elect_one()) {
-            if (leader) ptx::mbar_arrive_expect_tx(&ctl->full[stage], 2 * kStageBytes);
+            if (leader) ptx::mbar_arrive_expect_tx(&ctl->full_a[ra.slot], 2 * kSlotA);
             load_pair(at, &map_a, full, kb * 128, m0);
-            load_pair(at + kBytesA, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
-            load_pair(at + kBytesA + kBytesB, &map_sa, full, 0, m0 / mx::kTileRows * tiles_k + kt);
-            load_pair(at + kBytesA + kBytesB + kBytesSA, &map_sb, full, 0, nt * tiles_k + kt);
-            load_pair(at + kBytesA + kBytesB + 2 * kBytesSA, &map_sb, full, 0, (nt + 1) * tiles_k + kt);
+            load_pair(at + kBytesA, &map_sa, full, 0, m0 / mx::kTileRows * tiles_k + kt);
           }
           __syncwarp();
-          issued |= 1 << stage;
-          issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1u;
-          }
+          issued_a |= 1 << ra.slot;
+          phase_a = (phase_a & ~(1u << ra.slot)) | (ra.phase << ra.slot);
+          ra.next();
         }
+        if (!warp_wait(&ctl->empty_b[rb.slot], rb.phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 22);
+          ok = false;
+          break;
+        }
+        const uint32_t at = smem0 + kSlotsA * kSlotA + rb.slot * kSlotB, full = full_b0 + rb.slot * 8;
+        if (ptx::elect_one()) {
+          if (leader) ptx::mbar_arrive_expect_tx(&ctl->full_b[rb.slot], 2 * kSlotB);
+          load_pair(at, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
+#pragma unroll
+          for (int j = 0; j < kRowTiles; ++j)
+            load_pair(at + kBytesB + j * kBytesSA, &map_sb, full, 0, (nt + j) * tiles_k + kt);
+        }
+        __syncwarp();
+        issued_b |= 1 << rb.slot;
+        phase_b = (phase_b & ~(1u << rb.slot)) | (rb.phase << rb.slot);
+        rb.next();
       }
-      if (!ok && leader) {
-        for (int s = 0; s < kStages; ++s)
-          if (issued & (1 << s)) ptx::mbar_wait(&ctl->full[s], (issued_phase >> s) & 1u, nullptr, kWaitNs);
-      }
+    }
+    if (!ok && leader) {  // no copy may land after the block is gone
+      for (int s = 0; s < kSlotsA; ++s)
+        if (issued_a & (1 << s)) ptx::mbar_wait(&ctl->full_a[s], (phase_a >> s) & 1u, nullptr, kWaitNs);
+      for (int s = 0; s < kSlotsB; ++s)
+        if (issued_b & (1 << s)) ptx::mbar_wait(&ctl->full_b[s], (phase_b >> s) & 1u, nullptr, kWaitNs);
     }
     __syncwarp();
   } else if (warp == 1) {
     // ---------------- MMA issuer (leader) ----------------
     if (leader) {
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
+      Ring<kSlotsA> ra;
+      Ring<kSlotsB> rb;
+      int acc = 0;
+      uint32_t acc_phase = 0;
       bool ok = true;
       const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
       const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
       const uint64_t desc0 = ptx::sdesc_k_sw128(smem0);
-      for (int64_t t = cluster; ok && t < tiles; t += clusters) {
+      for (int64_t t = run.begin; ok && t < run.end; ++t) {
         if (!warp_wait(&ctl->acc_empty[acc], acc_phase ^ 1u, abort_flag)) {
-          fail(ctl, a.status, 22);
+          fail(ctl, a.status, 23);
           break;
         }
         ptx::tc_fence_after_sync();
         const uint32_t d = tmem0 + static_cast<uint32_t>(acc * kTileN);
         // The tile's first row of B within its scale tile: a column of scales holds 32 rows.
-        const uint32_t sb_shift = static_cast<uint32_t>(t % tiles_n) * kTileN % mx::kTileRows / 32;
-        for (int kb = 0; kb < stages_k; ++kb) {
-          if (!warp_wait(&ctl->full[stage], phase, abort_flag)) {
-            fail(ctl, a.status, 23);
+        const uint32_t sb_shift = static_cast<uint32_t>(t - run.m_of(t) * run.n) * kTileN % mx::kTileRows / 32;
+        const bool begins = panel_begins(t), ends = panel_ends(t);
+        Ring<kSlotsA> at = ra;  // the panel's slots
+        for (int kb = 0; kb < steps; ++kb) {
+          if ((begins && !warp_wait(&ctl->full_a[at.slot], at.phase, abort_flag)) ||
+              !warp_wait(&ctl->full_b[rb.slot], rb.phase, abort_flag)) {
+            fail(ctl, a.status, 24);
             ok = false;
             break;
           }
           ptx::tc_fence_after_sync();
-          const uint64_t da = desc0 + static_cast<uint64_t>((stage * kStageBytes) >> 4), db = da + (kBytesA >> 4);
-          const uint32_t scales = smem0 + stage * kStageBytes + kBytesA + kBytesB;
-          const uint32_t sa = tmem0 + kScaleCols + stage * kStageCols, sb = sa + kScaleTiles * kColsSA;
-          const int products = min(kStageK / 64, (a.k - kb * kStageK + 63) / 64);
+          const uint32_t slot_a = at.slot * kSlotA, slot_b = kSlotsA * kSlotA + rb.slot * kSlotB;
+          const uint64_t da = desc0 + static_cast<uint64_t>(slot_a >> 4), db = desc0 + static_cast<uint64_t>(slot_b >> 4);
+          const uint32_t sa = tmem0 + kScalesA + at.slot * (kScaleTiles * kColsSA);
+          const uint32_t sb = tmem0 + kScalesB + rb.slot * (kScaleTiles * kColsSB);
+          const int products = min(kStepK / 64, (a.k - kb * kStepK + 63) / 64);
           if (ptx::elect_one()) {
 #pragma unroll
             for (int j = 0; j < kScaleTiles; ++j) {
               if (2 * j < products) {
-                copy_scales(sa + j * kColsSA, scale_desc(scales + j * mx::kTileBytes));
-                copy_scales(sb + j * kColsSB, scale_desc(scales + kBytesSA + j * mx::kTileBytes));
-                copy_scales(sb + j * kColsSB + 4, scale_desc(scales + 2 * kBytesSA + j * mx::kTileBytes));
+                if (begins) copy_scales(sa + j * kColsSA, scale_desc(smem0 + slot_a + kBytesA + j * mx::kTileBytes));
+#pragma unroll
+                for (int i = 0; i < kRowTiles; ++i)
+                  copy_scales(sb + j * kColsSB + 4 * i,
+                              scale_desc(smem0 + slot_b + kBytesB + i * kBytesSA + j * mx::kTileBytes));
               }
             }
 #pragma unroll
-            for (int p = 0; p < kStageK / 64; ++p) {
+            for (int p = 0; p < kStepK / 64; ++p) {
               if (p < products)
-                mma_mx(d, da + 2 * p, db + 2 * p, kIdesc | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
+                mma_mx(d, da + 2 * p, db + 2 * p, kInstruction | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
                        sb + (p / 2) * kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
             }
-            commit_both(&ctl->empty[stage]);
+            commit_both(&ctl->empty_b[rb.slot]);
+            if (ends) commit_both(&ctl->empty_a[at.slot]);
           }
           __syncwarp();
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1u;
-          }
+          at.next();
+          rb.next();
         }
         if (!ok) break;
+        if (ends) ra = at;
         if (ptx::elect_one()) commit_both(&ctl->acc_full[acc]);
         __syncwarp();
         if (++acc == 2) {
@@ -318,16 +387,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t empty0 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[0]), 0);
     const uint32_t empty1 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[1]), 0);
-    uint8_t* box = smem + kStages * kStageBytes + (warp - 2) * kBoxBytes;
+    uint8_t* box = smem + kRings + (warp - 2) * kBoxBytes;
     constexpr int kBoxCols = 128 / static_cast<int>(sizeof(T));
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (int64_t t = cluster; t < tiles; t += clusters) {
-      const int64_t row0 = t / tiles_n * kTileM + kHalf * rank + q * 32;
-      const int n0 = static_cast<int>(t % tiles_n) * kTileN + part * kWarpCols;
+    for (int64_t t = run.begin; t < run.end; ++t) {
+      const int64_t row0 = run.m_of(t) * kTileM + kHalf * rank + q * 32;
+      const int n0 = static_cast<int>(t - run.m_of(t) * run.n) * kTileN + part * kWarpCols;
       const bool live = row0 < a.m && n0 < a.n;
       if (!warp_wait(&ctl->acc_full[acc], acc_phase, abort_flag)) {
-        fail(ctl, a.status, 24);
+        fail(ctl, a.status, 25);
         break;
       }
       ptx::tc_fence_after_sync();
@@ -462,6 +531,7 @@ bool map_output(CUtensorMap* map, const MxMatmulArgs& a) {
 template <typename T>
 cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t stream) {
   if (encoder() == nullptr) return cudaErrorNotSupported;
+  const auto kernel = mxfp4_matmul_kernel<T>;
   CUtensorMap map_a, map_b, map_sa, map_sb;
   if (!map_codes(&map_a, a.a_codes, a.m, a.k, kHalf) || !map_codes(&map_b, a.b_codes, a.n, a.k, kTileN / 2) ||
       !map_scales(&map_sa, a.a_scales, a.m, a.k) || !map_scales(&map_sb, a.b_scales, a.n, a.k))
@@ -472,8 +542,7 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(attr_done.load() & bit)) {
-    e = cudaFuncSetAttribute(mxfp4_matmul_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(kSmemBytes));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
     if (e != cudaSuccess) return e;
     attr_done.fetch_or(bit);
   }
@@ -498,8 +567,7 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, mxfp4_matmul_kernel<T>, map_a, map_b, map_sa, map_sb, map_out, a, tma_out,
-                            bias_vec);
+  return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_sa, map_sb, map_out, a, tma_out, bias_vec);
 }
 
 }  // namespace
