@@ -2,7 +2,9 @@
 
 Each .cu file under csrc/ is compiled in parallel to an object file in
 _build/, then linked into paper_2604_05718_gb300/libmpm.so with the CUDA
-runtime linked statically and only the mpm_* symbols exported.
+runtime linked statically and only the mpm_* symbols exported.  Beside it,
+csrc/blocks_binding.cpp becomes the extension module _blocks, the Python
+binding of the encoder-block entry points.
 """
 
 from __future__ import annotations
@@ -12,6 +14,7 @@ import glob
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -25,6 +28,10 @@ LIB_TRACE = os.path.join(PKG, "libmpm_trace.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-fvisibility=hidden",
                      "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+
+
+BINDING_SRC = os.path.join(CSRC, "blocks_binding.cpp")
+BINDING = os.path.join(PKG, "_blocks" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def nvcc() -> str:
@@ -52,9 +59,24 @@ def _run(cmd: list) -> None:
         raise RuntimeError(f"command failed ({res.returncode}): {' '.join(cmd)}\n{res.stdout}\n{res.stderr}")
 
 
+def _binding_command(out: str) -> list:
+    """g++ over the binding, against the torch that runs this."""
+    import torch
+
+    root = os.path.join(os.path.dirname(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
+    lib = os.path.join(root, "lib")
+    return [os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-O2", "-std=c++17", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", BINDING_SRC, "-o", out] + \
+        [f"-I{d}" for d in include] + [f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
+                                       f"-Wl,-rpath,{lib}"]
+
+
 def build(force: bool = False, extra_flags: list | None = None, trace: bool = False) -> str:
-    """Compiles and links libmpm.so (libmpm_trace.so with trace=True) if any
-    source changed; returns its path."""
+    """Compiles and links libmpm.so (libmpm_trace.so with trace=True) and the
+    binding module if any source changed; returns the library's path."""
     build_dir, lib_path = (BUILD_TRACE, LIB_TRACE) if trace else (BUILD, LIB)
     os.makedirs(build_dir, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
@@ -67,10 +89,17 @@ def build(force: bool = False, extra_flags: list | None = None, trace: bool = Fa
         objs.append(obj)
         if force or _stale(obj, [src] + headers):
             jobs.append([nvcc(), "-c", src, "-o", obj] + flags)
+    binding = BINDING + ".tmp"
+    bind = not trace and (force or _stale(BINDING, [BINDING_SRC, os.path.join(ROOT, "include", "mpm.h")]))
+    compiled = bool(jobs)
+    if bind:
+        jobs.insert(0, _binding_command(binding))
     if jobs:
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
             list(ex.map(_run, jobs))
-    if force or jobs or _stale(lib_path, objs):
+    if bind:
+        os.replace(binding, BINDING)
+    if force or compiled or _stale(lib_path, objs):
         tmp = lib_path + ".tmp"
         _run([nvcc(), "-shared", "-o", tmp] + objs + ARCH +
              ["-cudart", "static", "-Xlinker", "--version-script=" + os.path.join(CSRC, "exports.map")])
