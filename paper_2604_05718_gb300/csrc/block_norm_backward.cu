@@ -25,8 +25,11 @@
 // Rows that are 16-byte aligned therefore come through a ring in shared
 // memory that bulk copies fill rows ahead; and a thread has up to 24 columns
 // of a row, whose chains overlap, without barriers in between.  54208 x 768
-// bf16, layer norm on both sides: 192 us from loads in place, 164 with rows
-// spread over three warps (two barriers a row), BWD1 with a warp a row.
+// bf16, layer norm on both sides and a gate per image (500 MB): 192 us from
+// loads in place, 164 with rows spread over three warps (two barriers a row),
+// 111 with a warp a row, 9 of them the join: 4.5 TB/s.  Two warps a scheduler
+// issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
+// fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
 #include <atomic>
 
 #include "block_launch.h"
@@ -63,14 +66,18 @@ constexpr int kSharedBytes = 225 * 1024;
 struct Run {
   int64_t begin, end;
 };
+// (32-bit quotients: rows are at most 2^31 - 1, and 64-bit ones are long subroutines.)
 __device__ __forceinline__ Run run_of(int64_t g, int64_t all, int64_t total) {
-  const int64_t per = total / all, extra = total % all;
+  const uint32_t per = static_cast<uint32_t>(total) / static_cast<uint32_t>(all);
+  const int64_t extra = total - static_cast<int64_t>(per) * all;
   const int64_t begin = g * per + (g < extra ? g : extra);
   return {begin, begin + per + (g < extra ? 1 : 0)};
 }
 __device__ __forceinline__ int64_t group_of(int64_t row, int64_t all, int64_t total) {
-  const int64_t per = total / all, extra = total % all, long_rows = extra * (per + 1);
-  return row < long_rows ? row / (per + 1) : extra + (row - long_rows) / per;
+  const uint32_t per = static_cast<uint32_t>(total) / static_cast<uint32_t>(all);
+  const int64_t extra = total - static_cast<int64_t>(per) * all, long_rows = extra * (per + 1);
+  return row < long_rows ? static_cast<uint32_t>(row) / (per + 1)
+                         : extra + static_cast<uint32_t>(row - long_rows) / per;
 }
 
 // Workspace: column sums [kSums][blocks][dim], then for each group the gate's
@@ -96,25 +103,29 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-// A row in a group's ring: y, dh, x and dx' one after another, and the statistics.
+// A row in a group's ring: y, dh, x and dx' one after another, each as wide as
+// the warps' chunks, and the statistics.  What no copy fills (columns past the
+// row, a gradient that is absent) is zero from the start, so that it can be
+// read like the rest.
 template <typename TY, typename TX>
 struct Slot {
-  __host__ __device__ static constexpr int bytes(int dim) {
-    return dim * static_cast<int>(2 * sizeof(TY) + 2 * sizeof(TX)) + 16;
+  static constexpr int kValueBytes = 2 * sizeof(TY) + 2 * sizeof(TX);
+  __host__ __device__ static constexpr int bytes(int dim) { return width(dim) * kValueBytes + 16; }
+  __host__ __device__ static constexpr int width(int dim) {
+    return warps_per_row(dim) * chunks_per_warp(dim) * kNormWarpCols;
   }
   uint8_t* base;
-  int dim;
+  int wide;
   __device__ __forceinline__ TY* y() const { return reinterpret_cast<TY*>(base); }
-  __device__ __forceinline__ TY* d_h() const { return y() + dim; }
-  __device__ __forceinline__ TX* x() const { return reinterpret_cast<TX*>(d_h() + dim); }
-  __device__ __forceinline__ TX* d_x() const { return x() + dim; }
-  __device__ __forceinline__ float4* stats() const { return reinterpret_cast<float4*>(d_x() + dim); }
+  __device__ __forceinline__ TY* d_h() const { return y() + wide; }
+  __device__ __forceinline__ TX* x() const { return reinterpret_cast<TX*>(d_h() + wide); }
+  __device__ __forceinline__ TX* d_x() const { return x() + wide; }
+  __device__ __forceinline__ float4* stats() const { return reinterpret_cast<float4*>(d_x() + wide); }
 };
 
 // Eight columns of a row in the ring.
 template <typename T>
-__device__ __forceinline__ F8 staged8(const T* row, int col, int dim) {
-  if (col >= dim) return all8(0.f);
+__device__ __forceinline__ F8 staged8(const T* row, int col) {
   if constexpr (sizeof(T) == 2) {
     return widen(*reinterpret_cast<const uint4*>(row + col));
   } else {
@@ -177,9 +188,19 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
   };
   const SharedVector pre_weight = shared_vector(0), scale = shared_vector(1 + 2 * group), shift = shared_vector(2 + 2 * group);
 
-  uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * ring * Row::bytes(a.dim);
+  const int wide = w * C * kNormWarpCols, slot_bytes = wide * Row::kValueBytes + 16;
+  uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * ring * slot_bytes;
+  if constexpr (RING) {
+    if (wide != a.dim || a.d_h == nullptr || a.d_residual_out == nullptr) {
+      uint4* const rings = reinterpret_cast<uint4*>(dynamic + (1 + 2 * groups) * vector);
+      for (int i = threadIdx.x; i < groups * ring * slot_bytes / 16; i += blockDim.x) rings[i] = make_uint4(0, 0, 0, 0);
+      // Before the copies into the same slots.
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncthreads();
+    }
+  }
   auto fill = [&](int64_t row, int k) {  // by an elected lane of the group's first warp
-    const Row to{ring_base + k * Row::bytes(a.dim), a.dim};
+    const Row to{ring_base + k * slot_bytes, wide};
     uint64_t* bar = &full[group][k];
     const uint32_t bytes_y = a.dim * static_cast<uint32_t>(sizeof(TY)), bytes_x = a.dim * static_cast<uint32_t>(sizeof(TX));
     ptx::mbar_arrive_expect_tx(bar, bytes_y + bytes_x + (a.d_h != nullptr ? bytes_y : 0) +
@@ -286,7 +307,7 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
       while (b < a.batch - 1 && row >= __ldg(a.offsets + b + 1)) ++b;
       open_image(b);
     }
-    const Row in{ring_base + k_slot * Row::bytes(a.dim), a.dim};
+    const Row in{ring_base + k_slot * slot_bytes, wide};
     F8 y[C], x[C], dh[C];
     float4 st;
     if constexpr (RING) {
@@ -303,9 +324,9 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if constexpr (RING) {
-        y[c] = staged8(in.y(), col[c], a.dim);
-        x[c] = staged8(in.x(), col[c], a.dim);
-        dh[c] = a.d_h != nullptr ? staged8(in.d_h(), col[c], a.dim) : all8(0.f);
+        y[c] = staged8(in.y(), col[c]);
+        x[c] = staged8(in.x(), col[c]);
+        dh[c] = staged8(in.d_h(), col[c]);
       } else {
         y[c] = load8<TY, false>(static_cast<const TY*>(a.y) + row * a.y_stride, col[c], a.dim);
         x[c] = load8<TX, false>(static_cast<const TX*>(a.residual) + row * a.residual_stride, col[c], a.dim);
@@ -346,13 +367,13 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         // Taken as late as this: its registers are needed until here.
-        F8 dx = all8(0.f), out;
-        if (a.d_residual_out != nullptr) {
-          if constexpr (RING)
-            dx = staged8(in.d_x(), col[c], a.dim);
-          else
-            dx = load8<TX, false>(static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, col[c], a.dim);
-        }
+        F8 dx, out;
+        if constexpr (RING)
+          dx = staged8(in.d_x(), col[c]);
+        else
+          dx = a.d_residual_out == nullptr
+                   ? all8(0.f)
+                   : load8<TX, false>(static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, col[c], a.dim);
         const F8 A = scale.get(c);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -436,53 +457,67 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
   if (a.d_gate != nullptr && !per_image) leave(4, [&](int c) { return gate_gradient(c); });
 }
 
-constexpr int kJoinCols = 32, kJoinRows = 16;
+// Blocks of the join: columns x parts that are added at once.  Many parts per
+// column (one a block) for the parameters, a few (runs per image) for a gate.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinCols = 32;
+constexpr int kGateCols = 128;
+
+// Adds parts first, first + 1, .. last (their column's addresses by `at`) and
+// writes the sum: rows of threads take every ROWS-th, and are added in order.
+template <int COLS, typename At>
+__device__ __forceinline__ void join_parts(float* part, int64_t first, int64_t last, bool in, float* out, At at) {
+  constexpr int ROWS = kJoinThreads / COLS;
+  const int x = threadIdx.x % COLS, r = threadIdx.x / COLS;
+  float s = 0.f;
+  if (in)
+    for (int64_t g = first + r; g <= last; g += ROWS) s += *at(g);
+  part[r * COLS + x] = s;
+  __syncthreads();
+  if (r == 0 && in) {
+    for (int i = 1; i < ROWS; ++i) s += part[i * COLS + x];
+    *out = s;
+  }
+}
 
 // Column sums over blocks, and the gates of images that several runs share.
-__global__ void __launch_bounds__(kJoinCols * kJoinRows) block_norm_join_kernel(NormBackward a, int blocks, int groups) {
+__global__ void __launch_bounds__(kJoinThreads) block_norm_join_kernel(NormBackward a, int blocks, int groups) {
   wait_for_previous_grid();
   allow_next_grid();
-  __shared__ float part[kJoinRows][kJoinCols];
+  __shared__ float part[kJoinThreads];
+  __shared__ int64_t ends[2];  // first and last group of the image's rows
   const int64_t all = static_cast<int64_t>(blocks) * groups;
   const Parts parts = parts_of(a, blocks, all);
   const bool per_image = a.gate != nullptr && a.gate_per_image;
   float* const outs[kSums] = {a.d_pre_weight, a.d_pre_bias, a.d_post_weight, a.d_post_bias,
                               per_image ? nullptr : a.d_gate};
   const int col_blocks = (a.dim + kJoinCols - 1) / kJoinCols;
-  const int x = threadIdx.x % kJoinCols, r = threadIdx.x / kJoinCols;
   const int which = blockIdx.x / col_blocks;
   if (which < kSums) {
     if (outs[which] == nullptr) return;
-    const int col = blockIdx.x % col_blocks * kJoinCols + x;
-    const float* in = parts.sums + static_cast<int64_t>(which) * blocks * a.dim;
-    float s = 0.f;
-    if (col < a.dim)
-      for (int b = r; b < blocks; b += kJoinRows) s += in[static_cast<int64_t>(b) * a.dim + col];
-    part[r][x] = s;
-    __syncthreads();
-    if (r == 0 && col < a.dim) {
-      for (int k = 1; k < kJoinRows; ++k) s += part[k][x];
-      outs[which][col] = s;
-    }
+    const int col = blockIdx.x % col_blocks * kJoinCols + threadIdx.x % kJoinCols;
+    const float* in = parts.sums + static_cast<int64_t>(which) * blocks * a.dim + col;
+    join_parts<kJoinCols>(part, 0, blocks - 1, col < a.dim, outs[which] + col,
+                          [&](int64_t b) { return in + b * a.dim; });
     return;
   }
-  const int wide = (a.dim + blockDim.x - 1) / blockDim.x, k = blockIdx.x - kSums * col_blocks;
-  const int image = k / wide, col = k % wide * blockDim.x + threadIdx.x;
-  if (image >= a.batch || col >= a.dim || a.d_gate == nullptr) return;
-  const int64_t total = used_rows(a.offsets, a.batch, a.rows);
-  int64_t lo = __ldg(a.offsets + image), hi = __ldg(a.offsets + image + 1);
-  lo = lo < 0 ? 0 : lo;
-  hi = hi < total ? hi : total;
-  float* out = a.d_gate + static_cast<int64_t>(image) * a.dim + col;
-  if (hi <= lo) {
-    *out = 0.f;
-    return;
+  const int gate_blocks = (a.dim + kGateCols - 1) / kGateCols, k = blockIdx.x - kSums * col_blocks;
+  const int image = k / gate_blocks, col = k % gate_blocks * kGateCols + threadIdx.x % kGateCols;
+  if (image >= a.batch || a.d_gate == nullptr) return;
+  if (threadIdx.x == 0) {
+    const int64_t total = used_rows(a.offsets, a.batch, a.rows);
+    int64_t lo = __ldg(a.offsets + image), hi = __ldg(a.offsets + image + 1);
+    lo = lo < 0 ? 0 : lo;
+    hi = hi < total ? hi : total;
+    ends[0] = hi > lo ? group_of(lo, all, total) : 0;
+    ends[1] = hi > lo ? group_of(hi - 1, all, total) : -1;
   }
-  const int64_t first = group_of(lo, all, total), last = group_of(hi - 1, all, total);
-  if (first == last) return;  // written by its run
-  float s = parts.tail[first * a.dim + col];
-  for (int64_t g = first + 1; g <= last; ++g) s += parts.head[g * a.dim + col];
-  *out = s;
+  __syncthreads();
+  const int64_t first = ends[0], last = ends[1];
+  if (last >= 0 && first == last) return;  // written by its run
+  // Without rows (last < first) the sum is zero.
+  join_parts<kGateCols>(part, first, last, col < a.dim, a.d_gate + static_cast<int64_t>(image) * a.dim + col,
+                        [&](int64_t g) { return (g == first ? parts.tail : parts.head) + g * a.dim + col; });
 }
 
 // Groups of a block and rows of each one's ring: as many groups as warps allow
@@ -532,10 +567,9 @@ cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, c
   if (a.d_gate == nullptr && a.d_pre_weight == nullptr && a.d_pre_bias == nullptr && a.d_post_weight == nullptr &&
       a.d_post_bias == nullptr)
     return cudaSuccess;
-  const int threads = kJoinCols * kJoinRows;
   const int64_t joins = static_cast<int64_t>(kSums) * ((a.dim + kJoinCols - 1) / kJoinCols) +
-                        (per_image ? static_cast<int64_t>(a.batch) * ((a.dim + threads - 1) / threads) : 0);
-  return launch_dependent(block_norm_join_kernel, dim3(static_cast<unsigned>(joins)), dim3(threads), 0, stream, a, grid,
+                        (per_image ? static_cast<int64_t>(a.batch) * ((a.dim + kGateCols - 1) / kGateCols) : 0);
+  return launch_dependent(block_norm_join_kernel, dim3(static_cast<unsigned>(joins)), dim3(kJoinThreads), 0, stream, a, grid,
                           groups);
 }
 

@@ -161,7 +161,7 @@ __device__ __forceinline__ void store_unit(float* p, const __nv_bfloat162 (&v)[4
 
 // VEC: rows of 16-byte aligned values.  Otherwise a row's values (bf16 holds
 // them all) cross over in shared memory, so that a half warp stores 16
-// neighbours at a time: 50000 x 769 bf16 in DQ1 us, 122 with a lane's eight
+// neighbours at a time: 50000 x 769 bf16 in 30 us, 122 with a lane's eight
 // values stored one by one.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(DequantizeArgs a, int64_t scale_tiles) {

@@ -61,12 +61,19 @@ __device__ __forceinline__ F8 join(float4 a, float4 b) {
 template <typename T, bool VEC>
 __device__ __forceinline__ F8 load8(const T* __restrict__ row, int col, int dim) {
   if constexpr (VEC) {
-    if (col >= dim) return all8(0.f);
+    // Zeros as they lie in memory: selecting among widened values would take twice the instructions.
     if constexpr (sizeof(T) == 2) {
-      return widen(ld_stream(reinterpret_cast<const uint4*>(row + col)));
+      uint4 r = make_uint4(0, 0, 0, 0);
+      if (col < dim) r = ld_stream(reinterpret_cast<const uint4*>(row + col));
+      return widen(r);
     } else {
-      const float4* p = reinterpret_cast<const float4*>(row + col);
-      return join(__ldcs(p), __ldcs(p + 1));
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+      if (col < dim) {
+        const float4* p = reinterpret_cast<const float4*>(row + col);
+        a = __ldcs(p);
+        b = __ldcs(p + 1);
+      }
+      return join(a, b);
     }
   } else {
     float v[8];
