@@ -17,8 +17,7 @@
 //
 // A warp's parameters are as many bytes as several rows.  They lie in shared
 // memory in the order in which lanes take them (16 bytes a lane, no bank
-// conflicts), and a warp takes two rows of one image for each of their loads;
-// read through L1 for every row, they bound the kernel (54208 x 768 bf16, layer
+// conflicts); read through L1 they bound the kernel (54208 x 768 bf16, layer
 // norm on both sides, 333 MB: 85 us; now 64).
 #include "block_launch.h"
 #include "norm_rows.cuh"
@@ -49,13 +48,17 @@ struct SharedParams {
   }
 };
 
-// Rows that a warp takes at once.
+// Blocks that an SM has to hold: the registers a thread may take (80 for 3 blocks, 64 for 4).
+__host__ __device__ constexpr int min_blocks(int chunks, bool vec, bool multi) {
+  return multi ? 1 : vec ? (chunks == 1 ? 4 : chunks < 4 ? 3 : 2) : chunks < 3 ? 3 : 2;
+}
+// Rows that a warp takes at once: two where they are short (registers for more warps do more for longer ones).
 __host__ __device__ constexpr int rows_at_once(int chunks, bool multi) { return multi || chunks > 1 ? 1 : 2; }
 
 template <typename TY, typename TX, int C, bool VEC, bool MULTI>
-__global__ void __launch_bounds__(MULTI ? 512 : kThreads, MULTI ? 1 : (VEC ? C < 4 : C < 3) ? 3 : 2) block_norm_kernel(NormForward a, int row_warps) {
+__global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MULTI)) block_norm_kernel(NormForward a, int row_warps) {
   constexpr int R = rows_at_once(C, MULTI);
-  __shared__ float2 sh[MULTI ? 32 : 1];
+  __shared__ float sh[MULTI ? 32 : 1];
   __shared__ SharedParams<MULTI ? 1 : C, VEC> shared;
   wait_for_previous_grid();
   allow_next_grid();
@@ -141,7 +144,7 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, MULTI ? 1 : (VEC ? C <
           s[r].x = t.x + t.y;
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r].x = sum(s[r].x, 0.f).x * inv_dim;
+        for (int r = 0; r < R; ++r) s[r].x = sum(s[r].x) * inv_dim;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const F8 in = mask8<VEC>(col[c], a.dim);
@@ -161,7 +164,7 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, MULTI ? 1 : (VEC ? C <
         s[r].y = t.x + t.y;
       }
 #pragma unroll
-      for (int r = 0; r < R; ++r) s[r].y = 1.f / sqrtf(fmaf(sum(s[r].y, 0.f).x, inv_dim, a.eps));
+      for (int r = 0; r < R; ++r) s[r].y = 1.f / sqrtf(fmaf(sum(s[r].y), inv_dim, a.eps));
     };
 
     float2 s1[R], s2[R];

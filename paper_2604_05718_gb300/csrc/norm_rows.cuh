@@ -137,27 +137,24 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums over a row held by the W warps of a group, the same in every thread.
-// MULTI = false: one warp, no shared memory.  `sh` holds 2 x W float2 of the
+// The sum over a row held by the W warps of a group, the same in every thread.
+// MULTI = false: one warp, no shared memory.  `sh` holds 2 x W floats of the
 // group; the two halves alternate, so that one barrier a sum is enough: a
 // warp writes a half again only after the next sum's barrier, which every
 // warp reaches after it has read this one.
 template <bool MULTI>
 struct RowSum {
-  float2* sh;
+  float* sh;
   int warps, warp, barrier, turn;
-  __device__ __forceinline__ float2 operator()(float a, float b) {
-    float2 v = make_float2(warp_sum(a), warp_sum(b));
+  __device__ __forceinline__ float operator()(float a) {
+    float v = warp_sum(a);
     if constexpr (MULTI) {
-      float2* half = sh + (turn & 1) * warps;
+      float* half = sh + (turn & 1) * warps;
       ++turn;
       if ((threadIdx.x & 31) == 0) half[warp] = v;
       asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(warps * 32) : "memory");
       v = half[0];
-      for (int w = 1; w < warps; ++w) {
-        v.x += half[w].x;
-        v.y += half[w].y;
-      }
+      for (int w = 1; w < warps; ++w) v += half[w];
     }
     return v;
   }
