@@ -17,8 +17,13 @@
 //
 // A warp's parameters are as many bytes as several rows.  They lie in shared
 // memory in the order in which lanes take them (16 bytes a lane, no bank
-// conflicts); read through L1 they bound the kernel (54208 x 768 bf16, layer
-// norm on both sides, 333 MB: 85 us; now 64).
+// conflicts), the norm after the block and the gate folded into two vectors,
+// A = gate w_post and B = gate b_post: x' = alpha x + n1 A + B.  What bounds the
+// kernel beside HBM is the accesses to them (54208 x 768 bf16, layer norm on both
+// sides and a gate per image, 333 MB: 85 us with all five vectors read through
+// L1, 64 with the gate alone, 62 folded; 30000 x 1024: 49 to 45).
+#include <atomic>
+
 #include "block_launch.h"
 #include "norm_rows.cuh"
 #include "ptx.cuh"
@@ -29,24 +34,8 @@ namespace {
 using namespace norm;
 
 constexpr int kThreads = 256;
-
-// The parameters of one row in shared memory: vector v, chunk c, element i of
-// a lane.  Absent vectors stand there too (as ones or zeros).
-enum Vector : int { kPostWeight, kPostBias, kPreWeight, kPreBias, kVectors };
-template <int C, bool VEC>
-struct SharedParams {
-  float v[kVectors][C][2][32][4];
-  __device__ __forceinline__ void fill(Vector which, const float* p, float otherwise, int dim) {
-    for (int e = threadIdx.x; e < C * kNormWarpCols; e += blockDim.x) {
-      const int c = e / kNormWarpCols, k = e % kNormWarpCols;
-      const int lane = VEC ? k / 8 : k % 32, i = VEC ? k % 8 : k / 32;
-      v[which][c][i / 4][lane][i % 4] = p == nullptr ? otherwise : e < dim ? __ldg(p + e) : 0.f;
-    }
-  }
-  __device__ __forceinline__ F8 get(Vector which, int c, int lane) const {
-    return join(*reinterpret_cast<const float4*>(v[which][c][0][lane]), *reinterpret_cast<const float4*>(v[which][c][1][lane]));
-  }
-};
+constexpr int kSmShared = 228 * 1024;     // shared memory of an SM
+constexpr int kBlockShared = 225 * 1024;  // the most that a block's vectors take
 
 // Blocks that an SM has to hold: the registers a thread may take (80 for 3 blocks, 64 for 4).
 __host__ __device__ constexpr int min_blocks(int chunks, bool vec, bool multi) {
@@ -56,25 +45,19 @@ __host__ __device__ constexpr int min_blocks(int chunks, bool vec, bool multi) {
 __host__ __device__ constexpr int rows_at_once(int chunks, bool multi) { return multi || chunks > 1 ? 1 : 2; }
 
 template <typename TY, typename TX, int C, bool VEC, bool MULTI>
-__global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MULTI)) block_norm_kernel(NormForward a, int row_warps) {
+__global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MULTI))
+    block_norm_kernel(NormForward a, int row_warps, int staged_vectors) {
   constexpr int R = rows_at_once(C, MULTI);
+  // Rows so long that the vectors have no room in shared memory read them through L1.
+  const bool staged = !MULTI || staged_vectors != 0;
   __shared__ float sh[MULTI ? 32 : 1];
-  __shared__ SharedParams<MULTI ? 1 : C, VEC> shared;
+  // w_pre and b_pre, then A and B: of the block, or (a gate per image) of each group.
+  extern __shared__ __align__(16) float4 vectors[];
   wait_for_previous_grid();
   allow_next_grid();
   check_offsets(a.offsets, a.batch, a.rows, a.status);
   const bool post = a.post_weight != nullptr, pre = a.pre_weight != nullptr;
-  if constexpr (!MULTI) {
-    if (post) {
-      shared.fill(kPostWeight, a.post_weight, 1.f, a.dim);
-      shared.fill(kPostBias, a.post_bias, 0.f, a.dim);
-    }
-    if (pre) {
-      shared.fill(kPreWeight, a.pre_weight, 1.f, a.dim);
-      shared.fill(kPreBias, a.pre_bias, 0.f, a.dim);
-    }
-    __syncthreads();
-  }
+  const bool per_image = a.gate != nullptr && a.gate_per_image;
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
   const int groups = (blockDim.x >> 5) / w, group = warp / w, in_group = warp % w;
@@ -82,30 +65,63 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MUL
   const int64_t total = used_rows(a.offsets, a.batch, a.rows);
   const int64_t all = static_cast<int64_t>(gridDim.x) * groups, g = static_cast<int64_t>(blockIdx.x) * groups + group;
   // Neighbouring rows to one group: its image changes only now and then.
-  const int64_t per = total / all, extra = total % all;
+  const int64_t per = static_cast<uint32_t>(total) / static_cast<uint32_t>(all), extra = total - per * all;
   const int64_t begin = g * per + (g < extra ? g : extra), end = begin + per + (g < extra ? 1 : 0);
   const float inv_dim = 1.f / static_cast<float>(a.dim);
-  const float* gate = a.gate;
-  int image = 0;
-  int64_t image_end = INT64_MAX;
-  if (gate != nullptr && a.gate_per_image && begin < end) {
-    image = find_image(a.offsets, a.batch, begin);
-    image_end = __ldg(a.offsets + image + 1);
-    gate = a.gate + static_cast<int64_t>(image) * a.dim;
-  }
   int col[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) col[c] = first_column<VEC>(c * w + in_group, lane);
-  auto param = [&](Vector which, const float* p, int c, float otherwise) {
-    if constexpr (MULTI) return param8<VEC>(p, col[c], a.dim, otherwise);
-    else return shared.get(which, c, lane);
+
+  const int quads = w * C * kNormWarpCols / 4;  // of one vector
+  const auto shared_vector = [&](int k) { return SharedVector{vectors + k * quads, w * 32, in_group * 32 + lane}; };
+  const SharedVector w_pre = shared_vector(0), b_pre = shared_vector(1);
+  const SharedVector scale = shared_vector(2 + (per_image ? 2 * group : 0)), shift = shared_vector(3 + (per_image ? 2 * group : 0));
+  auto fold = [&](const float* gate, int c, F8& A, F8& B) {
+    const F8 g8 = param8<VEC>(gate, col[c], a.dim, 1.f);
+    A = param8<VEC>(a.post_weight, col[c], a.dim, 1.f);
+    B = param8<VEC>(a.post_bias, col[c], a.dim, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      A.p[k] = mul(g8.p[k], A.p[k]);
+      B.p[k] = mul(g8.p[k], B.p[k]);
+    }
   };
+  auto open_gate = [&](const float* gate) {  // each thread reads back its own columns only
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      F8 A, B;
+      fold(gate, c, A, B);
+      scale.set(c, A);
+      shift.set(c, B);
+    }
+  };
+  const float* gate = a.gate;
+  int image = 0;
+  int64_t image_end = INT64_MAX;
+  auto open_image = [&](int b) {
+    image = b;
+    image_end = __ldg(a.offsets + b + 1);
+    gate = a.gate + static_cast<int64_t>(b) * a.dim;
+    if (staged) open_gate(gate);
+  };
+  if (staged) {
+    if (group == 0) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        w_pre.set(c, param8<VEC>(a.pre_weight, col[c], a.dim, 1.f));
+        b_pre.set(c, param8<VEC>(a.pre_bias, col[c], a.dim, 0.f));
+      }
+      if (!per_image) open_gate(gate);
+    }
+    __syncthreads();
+  }
+  if (per_image && begin < end) open_image(find_image(a.offsets, a.batch, begin));
 
   for (int64_t row = begin; row < end;) {
-    while (row >= image_end && image < a.batch - 1) {
-      ++image;
-      image_end = __ldg(a.offsets + image + 1);
-      gate = a.gate + static_cast<int64_t>(image) * a.dim;
+    if (row >= image_end && image < a.batch - 1) {
+      int b = image + 1;
+      while (b < a.batch - 1 && row >= __ldg(a.offsets + b + 1)) ++b;
+      open_image(b);
     }
     // The last row stands in for one past the run's or the image's end, and is written once.
     int64_t at[R];
@@ -173,19 +189,19 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MUL
     if (post) standardise(u, s1);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (post) {
-        const F8 wv = param(kPostWeight, a.post_weight, c, 1.f), bv = param(kPostBias, a.post_bias, c, 0.f);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) u[r][c].p[k] = fma(mul(u[r][c].p[k], pair(s1[r].y)), wv.p[k], bv.p[k]);
+      F8 A, B;
+      if (staged) {
+        A = scale.get(c);
+        B = shift.get(c);
+      } else {
+        fold(gate, c, A, B);
       }
-      // Outside the row u and x are zeros, and so is x'.
-      const F8 gv = param8<VEC>(gate, col[c], a.dim, 1.f);
+      // Outside the row u, x and B are zeros, and so is x'.
 #pragma unroll
       for (int r = 0; r < R; ++r) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[r][c].p[k] = fma(gv.p[k], u[r][c].p[k], mul(pair(a.alpha), x[r][c].p[k]));
+        for (int k = 0; k < 4; ++k)
+          x[r][c].p[k] = fma(mul(u[r][c].p[k], pair(s1[r].y)), A.p[k], fma(pair(a.alpha), x[r][c].p[k], B.p[k]));
         if (r < count) store8<TX, VEC>(static_cast<TX*>(a.residual_out) + at[r] * a.dim, col[c], a.dim, x[r][c]);
       }
     }
@@ -193,7 +209,8 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MUL
       standardise(x, s2);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const F8 wv = param(kPreWeight, a.pre_weight, c, 1.f), bv = param(kPreBias, a.pre_bias, c, 0.f);
+        const F8 wv = staged ? w_pre.get(c) : param8<VEC>(a.pre_weight, col[c], a.dim, 1.f);
+        const F8 bv = staged ? b_pre.get(c) : param8<VEC>(a.pre_bias, col[c], a.dim, 0.f);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -212,13 +229,29 @@ __global__ void __launch_bounds__(MULTI ? 512 : kThreads, min_blocks(C, VEC, MUL
 
 template <typename TY, typename TX, int C, bool VEC, bool MULTI>
 cudaError_t launch_instance(const NormForward& a, int row_warps, int num_sms, cudaStream_t stream) {
+  const auto kernel = block_norm_kernel<TY, TX, C, VEC, MULTI>;
   const int warps = MULTI ? 16 / row_warps * row_warps : kThreads / 32;
   const int groups = warps / row_warps;
-  static const int per_sm = resident_per_sm(block_norm_kernel<TY, TX, C, VEC, MULTI>, MULTI ? 512 : kThreads, 8);
+  static const int by_registers = resident_per_sm(kernel, MULTI ? 512 : kThreads, 8);
+  const int owners = a.gate != nullptr && a.gate_per_image ? groups : 1;
+  int smem = (2 + 2 * owners) * row_warps * C * kNormWarpCols * static_cast<int>(sizeof(float));
+  const int staged = smem <= kBlockShared;
+  if (!staged) smem = 0;
+  static std::atomic<uint64_t> attr_done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(attr_done.load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlockShared);
+    if (e != cudaSuccess) return e;
+    attr_done.fetch_or(bit);
+  }
+  const int fit = kSmShared / (smem + 2048);
+  const int per_sm = fit < by_registers ? fit : by_registers;
   const int64_t want = (a.rows + groups - 1) / groups, most = static_cast<int64_t>(num_sms) * per_sm;
   const int grid = static_cast<int>(want < most ? want : most);
-  return launch_dependent(block_norm_kernel<TY, TX, C, VEC, MULTI>, dim3(grid), dim3(warps * 32), 0, stream, a,
-                          row_warps);
+  return launch_dependent(kernel, dim3(grid), dim3(warps * 32), static_cast<size_t>(smem), stream, a, row_warps, staged);
 }
 
 template <typename TY, typename TX, bool VEC>

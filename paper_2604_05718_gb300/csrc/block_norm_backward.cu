@@ -134,18 +134,7 @@ __device__ __forceinline__ F8 staged8(const T* row, int col) {
   }
 }
 
-// Vectors in shared memory, eight columns a thread, without bank conflicts:
-// chunk, half of the eight, thread of the row.
-struct SharedVector {
-  float4* v;
-  int threads, at;
-  __device__ __forceinline__ F8 get(int c) const { return join(v[2 * c * threads + at], v[(2 * c + 1) * threads + at]); }
-  __device__ __forceinline__ void set(int c, const F8& f) const {
-    v[2 * c * threads + at] = make_float4(f.p[0].x, f.p[0].y, f.p[1].x, f.p[1].y);
-    v[(2 * c + 1) * threads + at] = make_float4(f.p[2].x, f.p[2].y, f.p[3].x, f.p[3].y);
-  }
-};
-// Bytes of one such vector.
+// Bytes of a SharedVector.
 __host__ __device__ constexpr int vector_bytes(int dim) {
   return warps_per_row(dim) * chunks_per_warp(dim) * kNormWarpCols * static_cast<int>(sizeof(float));
 }
@@ -399,7 +388,7 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
     else if constexpr (RING && MULTI)
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(w * 32) : "memory");
     if constexpr (RING) {
-      if constexpr (!MULTI) __syncwarp();
+      __syncwarp();
       if (in_group == 0 && row + ring < run.end && ptx::elect_one()) fill(row + ring, k_slot);
       __syncwarp();
       if (++k_slot == ring) {

@@ -131,6 +131,17 @@ __device__ __forceinline__ F8 mask8(int col, int dim) {
   }
 }
 
+// Vectors in shared memory, eight columns a thread, without bank conflicts:
+// chunk, half of the eight, thread of the row.
+struct SharedVector {
+  float4* v;
+  int threads, at;
+  __device__ __forceinline__ F8 get(int c) const { return join(v[2 * c * threads + at], v[(2 * c + 1) * threads + at]); }
+  __device__ __forceinline__ void set(int c, const F8& f) const {
+    v[2 * c * threads + at] = make_float4(f.p[0].x, f.p[0].y, f.p[1].x, f.p[1].y);
+    v[(2 * c + 1) * threads + at] = make_float4(f.p[2].x, f.p[2].y, f.p[3].x, f.p[3].y);
+  }
+};
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
