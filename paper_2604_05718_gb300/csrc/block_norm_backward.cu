@@ -27,7 +27,7 @@
 // of a row, whose chains overlap, without barriers in between.  54208 x 768
 // bf16, layer norm on both sides and a gate per image (500 MB): 192 us from
 // loads in place, 164 with rows spread over three warps (two barriers a row),
-// 111 with a warp a row, 9 of them the join: 4.5 TB/s.  Two warps a scheduler
+// 107 with a warp a row, 9 of them the join: 4.7 TB/s.  Two warps a scheduler
 // issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
 // fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
 #include <atomic>
@@ -142,7 +142,7 @@ __host__ __device__ constexpr int vector_bytes(int dim) {
 // RING: 16-byte aligned rows through shared memory (vector accesses); otherwise loads of single elements.
 template <typename TY, typename TX, int C, bool RING, bool MULTI>
 __global__ void __launch_bounds__(block_warps(C) * 32, 1)
-    block_norm_backward_kernel(NormBackward a, int row_warps, int ring) {
+    block_norm_backward_kernel(NormBackward a, int row_warps, int ring, int room) {
   using Row = Slot<TY, TX>;
   // w_pre; A and B of each group; the groups' rings.  Afterwards the groups' column sums.
   extern __shared__ __align__(16) uint8_t dynamic[];
@@ -258,8 +258,9 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
     open_gate(gate_of(b));
   };
   // The gate's gradient over this run's rows of the image: all of its rows, or
-  // a part.  The sums of w_post and b_post wait in the workspace, out of registers.
-  auto close_image = [&]() {
+  // a part.  The sums of w_post and b_post wait in the workspace, out of
+  // registers; the run's last image leaves them in s_n1 and s_one.
+  auto close_image = [&](bool at_end) {
     float* to = image_begin < run.begin ? parts.head + g * a.dim
                 : image_end <= run.end  ? (a.d_gate == nullptr ? nullptr : a.d_gate + static_cast<int64_t>(image) * a.dim)
                                         : parts.tail + g * a.dim;
@@ -277,6 +278,11 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
           b8.p[k] = add(b8.p[k], b0.p[k]);
         }
       }
+      if (at_end) {
+        s_n1[c] = w8;
+        s_one[c] = b8;
+        continue;
+      }
       store8<float, RING>(parts.w_post + g * a.dim, col[c], a.dim, w8);
       store8<float, RING>(parts.b_post + g * a.dim, col[c], a.dim, b8);
       s_n1[c] = s_one[c] = all8(0.f);
@@ -291,7 +297,7 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll 1
   for (int64_t row = run.begin; row < run.end; ++row) {
     if (row >= image_end && image < a.batch - 1) {
-      close_image();
+      close_image(false);
       int b = image + 1;
       while (b < a.batch - 1 && row >= __ldg(a.offsets + b + 1)) ++b;
       open_image(b);
@@ -407,50 +413,63 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll
     for (int c = 0; c < C; ++c) store8<TY, RING>(static_cast<TY*>(a.d_y) + row * a.dim, col[c], a.dim, dh[c]);
   }
-  if (per_image && run.begin < run.end) close_image();
+  if (per_image && run.begin < run.end) close_image(true);
 
   // Column sums of the block's groups, side by side in shared memory (where A
-  // and B and the rings were), then added in the groups' order.
+  // and B and the rings were), as many at a time as have room there, then added
+  // in the groups' order.
   const int quads = vector / 16;
   float4* const side = reinterpret_cast<float4*>(dynamic);
-  auto leave = [&](int which, auto value) {
-    float* out = parts.sums + (static_cast<int64_t>(which) * gridDim.x + blockIdx.x) * a.dim;
-    const SharedVector mine{side + group * quads, w * 32, in_group * 32 + lane};
+  int kept = 0;
+  uint32_t which_kept = 0;  // four bits each
+  auto join_kept = [&]() {
     __syncthreads();
-#pragma unroll
-    for (int c = 0; c < C; ++c) mine.set(c, value(c));
-    __syncthreads();
-    for (int q = threadIdx.x; q < quads; q += blockDim.x) {
-      float4 s = side[q];
+    for (int i = threadIdx.x; i < kept * quads; i += blockDim.x) {
+      const int n = i / quads, q = i - n * quads;
+      const float4* from = side + n * groups * quads + q;
+      float4 s = from[0];
       for (int k = 1; k < groups; ++k) {
-        const float4 t = side[k * quads + q];
+        const float4 t = from[k * quads];
         s = make_float4(s.x + t.x, s.y + t.y, s.z + t.z, s.w + t.w);
       }
+      float* out = parts.sums + (static_cast<int64_t>((which_kept >> (4 * n)) & 15u) * gridDim.x + blockIdx.x) * a.dim;
       const int at = q % (w * 32), c = q / (w * 32) / 2, half = q / (w * 32) % 2;
       const int first = first_column<RING>(c * w + at / 32, at % 32);
       const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (column<RING>(first, 4 * half + i) < a.dim) out[column<RING>(first, 4 * half + i)] = v[i];
+      for (int j = 0; j < 4; ++j)
+        if (column<RING>(first, 4 * half + j) < a.dim) out[column<RING>(first, 4 * half + j)] = v[j];
     }
+    __syncthreads();
+    kept = 0;
+    which_kept = 0;
   };
-  // Over the gates of a run: what its images left in the workspace, or the one gate's sums.
-  auto over_gates = [&](const float* kept, const F8(&s)[C], int c) {
-    if (!per_image) return gated(param8<RING>(a.gate, col[c], a.dim, 1.f), s[c]);
-    return closed ? load8<float, RING>(kept + g * a.dim, col[c], a.dim) : all8(0.f);
+  auto leave = [&](int which, auto value) {
+    const SharedVector mine{side + (kept * groups + group) * quads, w * 32, in_group * 32 + lane};
+#pragma unroll
+    for (int c = 0; c < C; ++c) mine.set(c, value(c));
+    which_kept |= static_cast<uint32_t>(which) << (4 * kept);
+    if (++kept == room) join_kept();
   };
+  // Over the gates of a run: what its last image left, or the one gate's sums.
+  auto over_gates = [&](const F8(&s)[C], int c) {
+    return per_image ? s[c] : gated(param8<RING>(a.gate, col[c], a.dim, 1.f), s[c]);
+  };
+  __syncthreads();
   if (a.d_pre_weight != nullptr) leave(0, [&](int c) { return s_wpre[c]; });
   if (a.d_pre_bias != nullptr) leave(1, [&](int c) { return s_bpre[c]; });
-  if (a.d_post_weight != nullptr) leave(2, [&](int c) { return over_gates(parts.w_post, s_n1, c); });
-  if (a.d_post_bias != nullptr) leave(3, [&](int c) { return over_gates(parts.b_post, s_one, c); });
   if (a.d_gate != nullptr && !per_image) leave(4, [&](int c) { return gate_gradient(c); });
+  if (a.d_post_weight != nullptr) leave(2, [&](int c) { return over_gates(s_n1, c); });
+  if (a.d_post_bias != nullptr) leave(3, [&](int c) { return over_gates(s_one, c); });
+  if (kept > 0) join_kept();
 }
 
-// Blocks of the join: columns x parts that are added at once.  Many parts per
-// column (one a block) for the parameters, a few (runs per image) for a gate.
+// Blocks of the join: columns x parts that are added at once, 32 x 16 for the
+// parameters (a part a block) and for gates whose images are shared by many
+// runs, 128 x 4 where they are shared by few.
 constexpr int kJoinThreads = 512;
-constexpr int kJoinCols = 32;
-constexpr int kGateCols = 128;
+constexpr int kJoinCols = 32, kGateCols = 128;
+constexpr int kManyRuns = 32;
 
 // Adds parts first, first + 1, .. last (their column's addresses by `at`) and
 // writes the sum: rows of threads take every ROWS-th, and are added in order.
@@ -459,8 +478,10 @@ __device__ __forceinline__ void join_parts(float* part, int64_t first, int64_t l
   constexpr int ROWS = kJoinThreads / COLS;
   const int x = threadIdx.x % COLS, r = threadIdx.x / COLS;
   float s = 0.f;
-  if (in)
+  if (in) {
+#pragma unroll 4
     for (int64_t g = first + r; g <= last; g += ROWS) s += *at(g);
+  }
   part[r * COLS + x] = s;
   __syncthreads();
   if (r == 0 && in) {
@@ -470,7 +491,7 @@ __device__ __forceinline__ void join_parts(float* part, int64_t first, int64_t l
 }
 
 // Column sums over blocks, and the gates of images that several runs share.
-__global__ void __launch_bounds__(kJoinThreads) block_norm_join_kernel(NormBackward a, int blocks, int groups) {
+__global__ void __launch_bounds__(kJoinThreads) block_norm_join_kernel(NormBackward a, int blocks, int groups, int gate_cols) {
   wait_for_previous_grid();
   allow_next_grid();
   __shared__ float part[kJoinThreads];
@@ -490,8 +511,8 @@ __global__ void __launch_bounds__(kJoinThreads) block_norm_join_kernel(NormBackw
                           [&](int64_t b) { return in + b * a.dim; });
     return;
   }
-  const int gate_blocks = (a.dim + kGateCols - 1) / kGateCols, k = blockIdx.x - kSums * col_blocks;
-  const int image = k / gate_blocks, col = k % gate_blocks * kGateCols + threadIdx.x % kGateCols;
+  const int gate_blocks = (a.dim + gate_cols - 1) / gate_cols, k = blockIdx.x - kSums * col_blocks;
+  const int image = k / gate_blocks, col = k % gate_blocks * gate_cols + threadIdx.x % gate_cols;
   if (image >= a.batch || a.d_gate == nullptr) return;
   if (threadIdx.x == 0) {
     const int64_t total = used_rows(a.offsets, a.batch, a.rows);
@@ -505,8 +526,10 @@ __global__ void __launch_bounds__(kJoinThreads) block_norm_join_kernel(NormBackw
   const int64_t first = ends[0], last = ends[1];
   if (last >= 0 && first == last) return;  // written by its run
   // Without rows (last < first) the sum is zero.
-  join_parts<kGateCols>(part, first, last, col < a.dim, a.d_gate + static_cast<int64_t>(image) * a.dim + col,
-                        [&](int64_t g) { return (g == first ? parts.tail : parts.head) + g * a.dim + col; });
+  float* out = a.d_gate + static_cast<int64_t>(image) * a.dim + col;
+  auto at = [&](int64_t g) { return (g == first ? parts.tail : parts.head) + g * a.dim + col; };
+  if (gate_cols == kGateCols) join_parts<kGateCols>(part, first, last, col < a.dim, out, at);
+  else join_parts<kJoinCols>(part, first, last, col < a.dim, out, at);
 }
 
 // Groups of a block and rows of each one's ring: as many groups as warps allow
@@ -550,16 +573,19 @@ cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, c
   const int64_t want = a.rows > 0 ? (a.rows + groups - 1) / groups : 1;  // without rows the sums are still written
   const int most = num_sms < kMaxBlocks ? num_sms : kMaxBlocks;
   const int grid = static_cast<int>(want < most ? want : most);
-  e = launch_dependent(kernel, dim3(grid), dim3(groups * w * 32), smem, stream, a, w, ring.rows);
+  const int room = static_cast<int>(smem / (static_cast<size_t>(groups) * vector));  // sums side by side at the end: two at least
+  e = launch_dependent(kernel, dim3(grid), dim3(groups * w * 32), smem, stream, a, w, ring.rows,
+                       room < kSums ? room : kSums);
   if (e != cudaSuccess) return e;
   const bool per_image = a.gate != nullptr && a.gate_per_image && a.d_gate != nullptr;
   if (a.d_gate == nullptr && a.d_pre_weight == nullptr && a.d_pre_bias == nullptr && a.d_post_weight == nullptr &&
       a.d_post_bias == nullptr)
     return cudaSuccess;
+  const int gate_cols = static_cast<int64_t>(grid) * groups > static_cast<int64_t>(kManyRuns) * a.batch ? kJoinCols : kGateCols;
   const int64_t joins = static_cast<int64_t>(kSums) * ((a.dim + kJoinCols - 1) / kJoinCols) +
-                        (per_image ? static_cast<int64_t>(a.batch) * ((a.dim + kGateCols - 1) / kGateCols) : 0);
+                        (per_image ? static_cast<int64_t>(a.batch) * ((a.dim + gate_cols - 1) / gate_cols) : 0);
   return launch_dependent(block_norm_join_kernel, dim3(static_cast<unsigned>(joins)), dim3(kJoinThreads), 0, stream, a, grid,
-                          groups);
+                          groups, gate_cols);
 }
 
 template <typename TY, typename TX, bool RING>
