@@ -2,7 +2,8 @@
 // accumulated in fp32 on the tensor cores: tcgen05.mma kind::mxf4 with a
 // power-of-two scale per 32 elements.
 //
-// A cluster of two CTAs (an SM pair) computes 256 x 192 tiles with cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows
+// A cluster of two CTAs (an SM pair) computes 256 x N tiles (N = 192 or 256)
+// with cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows
 // of B, the scales of its A rows and those of all of the tile's B rows.  A step
 // takes 256 elements of every row, one 128-byte swizzle row of packed codes,
 // and four K = 64 products.  Scales go from shared memory to tensor memory by
@@ -11,19 +12,20 @@
 //
 // Bound: with few features the output's bytes (2 M N of them against
 // (M + N) K / 2: 256 x 192 tiles of K = 768 take the tensor cores a third of
-// the time that their output takes HBM), with many the tensor cores.  Hence
-//  - two accumulators: a tile's output is written while the next one is
-//    computed;
+// the time that their output takes HBM), with many shared memory.  Hence
+//  - tiles of 192 columns with two accumulators: a tile's output is written
+//    while the next one is computed;
 //  - A and B in rings of their own: where a row of A fits (K <= 1280), the A
 //    panel of a run of tiles stays in shared memory, and with it its scales in
 //    tensor memory.  Loading it again for every tile took as long as half of
-//    the output's writes (54208 x 768 x 2304 to bf16: 61 us, resident 57).
-// With many features the bound is shared memory: a step's operands are written
-// there once (32 KB) and read once (28 KB a CTA), 467 cycles at 128 bytes a
-// cycle against 384 of the products.  Tiles of 256 columns would halve that
-// gap but leave no tensor memory for a second accumulator or the scales; tiles
-// of 128 took as long as 192 for two thirds of the work, and a narrower last
-// tile (N = 1024 is 5.3 tiles) with runs of equal cost gained nothing.
+//    the output's writes (54208 x 768 x 2304 to bf16: 61 us, resident 57, which
+//    is 4.4 TB/s of writes; filling as much memory with zeros reaches 3.9);
+//  - tiles of 256 columns for many features.  A step's operands are written to
+//    shared memory once and read once: 60 KB a CTA for 192 columns, 467 cycles
+//    at 128 bytes a cycle against 384 of the products; 68 KB and 530 cycles
+//    against 512 for 256 columns.  Tensor memory has room for one accumulator
+//    then, and a tile waits until the last one's has been read (16384 x 4096 x
+//    1024: 34 us with 192 columns, 30 with 256; 8192 x 8192 x 8192: 180 and 172).  Tiles of 128 took as long as 192 for two thirds of the work.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -40,38 +42,44 @@ constexpr int kHalf = 128;             // rows of A per CTA
 constexpr int kTileM = 2 * kHalf;
 constexpr int kStepK = 256;            // elements of a row per step: 128 bytes
 constexpr int kScaleTiles = kStepK / (mx::kBlock * mx::kTileBlocks);  // scale tiles along K per step
-constexpr int kSlotsA = 6;
 constexpr int kBytesA = kHalf * 128, kBytesSA = kScaleTiles * mx::kTileBytes, kSlotA = kBytesA + kBytesSA;
-constexpr int kMaxResident = kSlotsA - 1;  // steps of a panel that stays: one slot is left to begin the next one
+constexpr int kRowTiles = 2;               // scale tiles along N that a tile's rows of B lie in, at most
 constexpr int kWarpCols = 64;              // columns of the tile that an epilogue warp writes
 constexpr int kBoxBytes = 32 * 128;        // staged output: 32 rows of 128 bytes, swizzled
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColsSA = 4;            // tensor-memory columns of a scale tile
+constexpr uint32_t kColsSA = 4, kColsSB = kRowTiles * kColsSA;  // tensor-memory columns of a scale tile of A, of those of B
 constexpr uint64_t kWaitNs = 2000000000ull;
 
-constexpr int kTileN = 192;
-constexpr int kRowTiles = 2;               // scale tiles along N that a tile's 192 rows of B lie in, at most
-constexpr int kBytesB = kTileN / 2 * 128, kBytesSB = kRowTiles * kBytesSA, kSlotB = kBytesB + kBytesSB;
-constexpr int kSlotsB = 5;
-constexpr uint32_t kColsSB = kRowTiles * kColsSA;
-// Tensor memory: two accumulators, the scales of A's slots, those of B's.
-constexpr uint32_t kScalesA = 2 * kTileN, kScalesB = kScalesA + kSlotsA * kScaleTiles * kColsSA;
-constexpr int kEpilogueWarps = 4 * (kTileN / kWarpCols);
-constexpr int kThreads = (2 + kEpilogueWarps) * 32;
-constexpr int kRings = kSlotsA * kSlotA + kSlotsB * kSlotB;
-static_assert(kScalesB + kSlotsB * kScaleTiles * kColsSB <= kTmemCols, "accumulators and scales share tensor memory");
-static_assert(kSlotA % 1024 == 0 && kSlotB % 1024 == 0 && kBytesB % 1024 == 0, "swizzled tiles on 1024 bytes");
+// What depends on a tile's columns.
+template <int N>
+struct Tile {
+  static constexpr int kAccumulators = N == 192 ? 2 : 1;
+  static constexpr int kSlotsA = N == 192 ? 6 : 5, kSlotsB = N == 192 ? 5 : 4;
+  static constexpr int kMaxResident = kSlotsA - 1;  // steps of a panel that stays: one slot is left to begin the next one
+  static constexpr int kBytesB = N / 2 * 128, kBytesSB = kRowTiles * kBytesSA, kSlotB = kBytesB + kBytesSB;
+  // Tensor memory: the accumulators, the scales of A's slots, those of B's.
+  static constexpr uint32_t kScalesA = kAccumulators * N, kScalesB = kScalesA + kSlotsA * kScaleTiles * kColsSA;
+  static constexpr int kEpilogueWarps = 4 * (N / kWarpCols);
+  static constexpr int kThreads = (2 + kEpilogueWarps) * 32;
+  static constexpr int kRings = kSlotsA * kSlotA + kSlotsB * kSlotB;
+  static_assert(kScalesB + kSlotsB * kScaleTiles * kColsSB <= kTmemCols, "accumulators and scales share tensor memory");
+  static_assert(kSlotA % 1024 == 0 && kSlotB % 1024 == 0 && kBytesB % 1024 == 0, "swizzled tiles on 1024 bytes");
+};
+constexpr int kWideK = 2048;  // features from which tiles take 256 columns, if there is a round of them
 
 // Instruction descriptor of kind::mxf4: E2M1 operands (1) in K-major order,
 // scales of type UE8M0 (bit 23), N / 8 and M / 16 in their fields.
-constexpr uint32_t kInstruction = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kTileN >> 3) << 17) | (1u << 23) |
-                                  (static_cast<uint32_t>(kTileM >> 4) << 24);
+__host__ __device__ constexpr uint32_t instruction(int n) {
+  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) |
+         (static_cast<uint32_t>(kTileM >> 4) << 24);
+}
 // Which half of a 32-bit column's four scales a K = 64 product takes: fields of B and of A.
 __device__ __forceinline__ constexpr uint32_t scale_half(uint32_t which) { return (which << 4) | (which << 29); }
 
+constexpr int kMaxSlots = 6;
 struct Control {
-  uint64_t full_a[kSlotsA], full_b[kSlotsB];    // leader: both CTAs' operands of the slot landed
-  uint64_t empty_a[kSlotsA], empty_b[kSlotsB];  // both: products reading the slot completed
+  uint64_t full_a[kMaxSlots], full_b[kMaxSlots];    // leader: both CTAs' operands of the slot landed
+  uint64_t empty_a[kMaxSlots], empty_b[kMaxSlots];  // both: products reading the slot completed
   uint64_t acc_full[2];                           // both: accumulator complete
   uint64_t acc_empty[2];                          // leader: both CTAs read the accumulator
   uint64_t drain;
@@ -79,8 +87,11 @@ struct Control {
   int abort_flag;
 };
 
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kRings) + kEpilogueWarps * kBoxBytes + sizeof(Control);
-static_assert(kSmemBytes <= 227 * 1024, "a block's shared memory");
+template <int N>
+constexpr size_t smem_bytes() {
+  return 1024 + static_cast<size_t>(Tile<N>::kRings) + Tile<N>::kEpilogueWarps * kBoxBytes + sizeof(Control);
+}
+static_assert(smem_bytes<192>() <= 227 * 1024 && smem_bytes<256>() <= 227 * 1024, "a block's shared memory");
 
 // Place in a ring.
 template <int SLOTS>
@@ -101,8 +112,8 @@ struct Tiles {
   int n;  // tiles along n
   __device__ __forceinline__ int64_t m_of(int64_t t) const { return t / n; }
 };
-__device__ __forceinline__ Tiles tiles_of(const MxMatmulArgs& a) {
-  const int n = (a.n + kTileN - 1) / kTileN;
+__device__ __forceinline__ Tiles tiles_of(const MxMatmulArgs& a, int tile_n) {
+  const int n = (a.n + tile_n - 1) / tile_n;
   const int64_t all = (a.m + kTileM - 1) / kTileM * n, clusters = gridDim.x / 2, c = blockIdx.x / 2;
   const int64_t per = all / clusters, extra = all % clusters, begin = c * per + (c < extra ? c : extra);
   return {begin, begin + per + (c < extra ? 1 : 0), n};
@@ -180,30 +191,31 @@ __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+template <typename T, int N>
+__global__ void __launch_bounds__(Tile<N>::kThreads, 1)
     mxfp4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                         const __grid_constant__ CUtensorMap map_out, MxMatmulArgs a, bool tma_out, bool bias_vec) {
+  using W = Tile<N>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
-  Control* ctl = reinterpret_cast<Control*>(smem + kRings + kEpilogueWarps * kBoxBytes);
+  Control* ctl = reinterpret_cast<Control*>(smem + W::kRings + W::kEpilogueWarps * kBoxBytes);
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kSlotsA; ++s) {
+    for (int s = 0; s < W::kSlotsA; ++s) {
       ptx::mbar_init(&ctl->full_a[s], 1);
       ptx::mbar_init(&ctl->empty_a[s], 1);
     }
-    for (int s = 0; s < kSlotsB; ++s) {
+    for (int s = 0; s < W::kSlotsB; ++s) {
       ptx::mbar_init(&ctl->full_b[s], 1);
       ptx::mbar_init(&ctl->empty_b[s], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < W::kAccumulators; ++i) {
       ptx::mbar_init(&ctl->acc_full[i], 1);
-      ptx::mbar_init(&ctl->acc_empty[i], 2 * kEpilogueWarps);
+      ptx::mbar_init(&ctl->acc_empty[i], 2 * W::kEpilogueWarps);
     }
     ptx::mbar_init(&ctl->drain, 1);
     ctl->abort_flag = 0;
@@ -229,11 +241,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   wait_for_previous_grid();
   allow_next_grid();
 
-  const Tiles run = tiles_of(a);
+  const Tiles run = tiles_of(a, N);
   const int steps = (a.k + kStepK - 1) / kStepK;
   const int tiles_k = mx::scale_tiles(a.k);
   // A panel (the 256 rows of A of a tile) stays for the run's next tiles of the same rows.
-  const bool resident = steps <= kMaxResident;
+  const bool resident = steps <= W::kMaxResident;
   auto panel_begins = [&](int64_t t) { return !resident || t == run.begin || run.m_of(t) != run.m_of(t - 1); };
   auto panel_ends = [&](int64_t t) { return !resident || t + 1 == run.end || run.m_of(t + 1) != run.m_of(t); };
   volatile int* abort_flag = &ctl->abort_flag;
@@ -244,8 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // In a branch of one lane every operand of a copy or product first moves to
     // a uniform register, about 70 cycles an instruction, which bound the
     // kernel: 8192 x 8192 x 8192 took 316 us instead of 176.
-    Ring<kSlotsA> ra;
-    Ring<kSlotsB> rb;
+    Ring<W::kSlotsA> ra;
+    Ring<W::kSlotsB> rb;
     int issued_a = 0, issued_b = 0;
     uint32_t phase_a = 0, phase_b = 0;  // of the slots' last loads
     bool ok = true;
@@ -254,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t full_b0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full_b[0]), 0), 0);
     for (int64_t t = run.begin; ok && t < run.end; ++t) {
       const int32_t m0 = static_cast<int32_t>(run.m_of(t)) * kTileM + kHalf * static_cast<int32_t>(rank);
-      const int32_t n0 = static_cast<int32_t>(t - run.m_of(t) * run.n) * kTileN, nt = n0 / mx::kTileRows;
+      const int32_t n0 = static_cast<int32_t>(t - run.m_of(t) * run.n) * N, nt = n0 / mx::kTileRows;
       const bool begins = panel_begins(t);
       for (int kb = 0; kb < steps; ++kb) {
         // A scale tile past the last one along K belongs to other rows, or reads as zeros: no product uses it.
@@ -281,13 +293,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = false;
           break;
         }
-        const uint32_t at = smem0 + kSlotsA * kSlotA + rb.slot * kSlotB, full = full_b0 + rb.slot * 8;
+        const uint32_t at = smem0 + W::kSlotsA * kSlotA + rb.slot * W::kSlotB, full = full_b0 + rb.slot * 8;
         if (ptx::elect_one()) {
-          if (leader) ptx::mbar_arrive_expect_tx(&ctl->full_b[rb.slot], 2 * kSlotB);
-          load_pair(at, &map_b, full, kb * 128, n0 + kTileN / 2 * static_cast<int32_t>(rank));
+          if (leader) ptx::mbar_arrive_expect_tx(&ctl->full_b[rb.slot], 2 * W::kSlotB);
+          load_pair(at, &map_b, full, kb * 128, n0 + N / 2 * static_cast<int32_t>(rank));
 #pragma unroll
           for (int j = 0; j < kRowTiles; ++j)
-            load_pair(at + kBytesB + j * kBytesSA, &map_sb, full, 0, (nt + j) * tiles_k + kt);
+            load_pair(at + W::kBytesB + j * kBytesSA, &map_sb, full, 0, (nt + j) * tiles_k + kt);
         }
         __syncwarp();
         issued_b |= 1 << rb.slot;
@@ -296,17 +308,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     if (!ok && leader) {  // no copy may land after the block is gone
-      for (int s = 0; s < kSlotsA; ++s)
+      for (int s = 0; s < W::kSlotsA; ++s)
         if (issued_a & (1 << s)) ptx::mbar_wait(&ctl->full_a[s], (phase_a >> s) & 1u, nullptr, kWaitNs);
-      for (int s = 0; s < kSlotsB; ++s)
+      for (int s = 0; s < W::kSlotsB; ++s)
         if (issued_b & (1 << s)) ptx::mbar_wait(&ctl->full_b[s], (phase_b >> s) & 1u, nullptr, kWaitNs);
     }
     __syncwarp();
   } else if (warp == 1) {
     // ---------------- MMA issuer (leader) ----------------
     if (leader) {
-      Ring<kSlotsA> ra;
-      Ring<kSlotsB> rb;
+      Ring<W::kSlotsA> ra;
+      Ring<W::kSlotsB> rb;
       int acc = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
@@ -319,11 +331,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         ptx::tc_fence_after_sync();
-        const uint32_t d = tmem0 + static_cast<uint32_t>(acc * kTileN);
+        const uint32_t d = tmem0 + static_cast<uint32_t>(acc * N);
         // The tile's first row of B within its scale tile: a column of scales holds 32 rows.
-        const uint32_t sb_shift = static_cast<uint32_t>(t - run.m_of(t) * run.n) * kTileN % mx::kTileRows / 32;
+        const uint32_t sb_shift = static_cast<uint32_t>(t - run.m_of(t) * run.n) * N % mx::kTileRows / 32;
         const bool begins = panel_begins(t), ends = panel_ends(t);
-        Ring<kSlotsA> at = ra;  // the panel's slots
+        Ring<W::kSlotsA> at = ra;  // the panel's slots
         for (int kb = 0; kb < steps; ++kb) {
           if ((begins && !warp_wait(&ctl->full_a[at.slot], at.phase, abort_flag)) ||
               !warp_wait(&ctl->full_b[rb.slot], rb.phase, abort_flag)) {
@@ -332,10 +344,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           ptx::tc_fence_after_sync();
-          const uint32_t slot_a = at.slot * kSlotA, slot_b = kSlotsA * kSlotA + rb.slot * kSlotB;
+          const uint32_t slot_a = at.slot * kSlotA, slot_b = W::kSlotsA * kSlotA + rb.slot * W::kSlotB;
           const uint64_t da = desc0 + static_cast<uint64_t>(slot_a >> 4), db = desc0 + static_cast<uint64_t>(slot_b >> 4);
-          const uint32_t sa = tmem0 + kScalesA + at.slot * (kScaleTiles * kColsSA);
-          const uint32_t sb = tmem0 + kScalesB + rb.slot * (kScaleTiles * kColsSB);
+          const uint32_t sa = tmem0 + W::kScalesA + at.slot * (kScaleTiles * kColsSA);
+          const uint32_t sb = tmem0 + W::kScalesB + rb.slot * (kScaleTiles * kColsSB);
           const int products = min(kStepK / 64, (a.k - kb * kStepK + 63) / 64);
           if (ptx::elect_one()) {
 #pragma unroll
@@ -345,13 +357,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int i = 0; i < kRowTiles; ++i)
                   copy_scales(sb + j * kColsSB + 4 * i,
-                              scale_desc(smem0 + slot_b + kBytesB + i * kBytesSA + j * mx::kTileBytes));
+                              scale_desc(smem0 + slot_b + W::kBytesB + i * kBytesSA + j * mx::kTileBytes));
               }
             }
 #pragma unroll
             for (int p = 0; p < kStepK / 64; ++p) {
               if (p < products)
-                mma_mx(d, da + 2 * p, db + 2 * p, kInstruction | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
+                mma_mx(d, da + 2 * p, db + 2 * p, instruction(N) | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
                        sb + (p / 2) * kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
             }
             commit_both(&ctl->empty_b[rb.slot]);
@@ -365,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ends) ra = at;
         if (ptx::elect_one()) commit_both(&ctl->acc_full[acc]);
         __syncwarp();
-        if (++acc == 2) {
+        if (++acc == W::kAccumulators) {
           acc = 0;
           acc_phase ^= 1u;
         }
@@ -387,20 +399,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t empty0 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[0]), 0);
     const uint32_t empty1 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[1]), 0);
-    uint8_t* box = smem + kRings + (warp - 2) * kBoxBytes;
+    uint8_t* box = smem + W::kRings + (warp - 2) * kBoxBytes;
     constexpr int kBoxCols = 128 / static_cast<int>(sizeof(T));
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int64_t t = run.begin; t < run.end; ++t) {
       const int64_t row0 = run.m_of(t) * kTileM + kHalf * rank + q * 32;
-      const int n0 = static_cast<int>(t - run.m_of(t) * run.n) * kTileN + part * kWarpCols;
+      const int n0 = static_cast<int>(t - run.m_of(t) * run.n) * N + part * kWarpCols;
       const bool live = row0 < a.m && n0 < a.n;
       if (!warp_wait(&ctl->acc_full[acc], acc_phase, abort_flag)) {
         fail(ctl, a.status, 25);
         break;
       }
       ptx::tc_fence_after_sync();
-      const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * kTileN + part * kWarpCols);
+      const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * N + part * kWarpCols);
 #pragma unroll
       for (int c = 0; c < kWarpCols; c += 32) {
         uint32_t r[32];
@@ -468,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
       }
-      if (++acc == 2) {
+      if (++acc == W::kAccumulators) {
         acc = 0;
         acc_phase ^= 1u;
       }
@@ -528,12 +540,12 @@ bool map_output(CUtensorMap* map, const MxMatmulArgs& a) {
                    CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T>
+template <typename T, int N>
 cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t stream) {
   if (encoder() == nullptr) return cudaErrorNotSupported;
-  const auto kernel = mxfp4_matmul_kernel<T>;
+  const auto kernel = mxfp4_matmul_kernel<T, N>;
   CUtensorMap map_a, map_b, map_sa, map_sb;
-  if (!map_codes(&map_a, a.a_codes, a.m, a.k, kHalf) || !map_codes(&map_b, a.b_codes, a.n, a.k, kTileN / 2) ||
+  if (!map_codes(&map_a, a.a_codes, a.m, a.k, kHalf) || !map_codes(&map_b, a.b_codes, a.n, a.k, N / 2) ||
       !map_scales(&map_sa, a.a_scales, a.m, a.k) || !map_scales(&map_sb, a.b_scales, a.n, a.k))
     return cudaErrorInvalidValue;
   static std::atomic<uint64_t> attr_done{0};
@@ -542,11 +554,11 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(attr_done.load() & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<N>()));
     if (e != cudaSuccess) return e;
     attr_done.fetch_or(bit);
   }
-  const int64_t tiles = (a.m + kTileM - 1) / kTileM * ((a.n + kTileN - 1) / kTileN);
+  const int64_t tiles = (a.m + kTileM - 1) / kTileM * ((a.n + N - 1) / N);
   const int64_t pairs = num_sms > 1 ? num_sms / 2 : 1;
   CUtensorMap map_out = map_a;
   const bool tma_out = (a.m == 1 || a.stride * static_cast<int64_t>(sizeof(T)) % 16 == 0) &&
@@ -555,8 +567,8 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   const bool bias_vec = reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs)));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.blockDim = dim3(Tile<N>::kThreads);
+  cfg.dynamicSmemBytes = smem_bytes<N>();
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -570,10 +582,19 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_sa, map_sb, map_out, a, tma_out, bias_vec);
 }
 
+template <typename T>
+cudaError_t launch_widths(const MxMatmulArgs& a, int num_sms, cudaStream_t stream) {
+  // Both at 20000 x 2048 x 2048: 39 us with 256 columns, 40 with 192; at 16384 x
+  // 1280 x 4096 42 and 39; with tiles for less than a round, 3000 x 2048 x 1024, 7.8 and 7.1.
+  const int64_t wide = (a.m + kTileM - 1) / kTileM * ((static_cast<int64_t>(a.n) + 255) / 256);
+  return a.k >= kWideK && wide >= num_sms / 2 ? launch_instance<T, 256>(a, num_sms, stream)
+                                              : launch_instance<T, 192>(a, num_sms, stream);
+}
+
 }  // namespace
 
 cudaError_t launch_mxfp4_matmul(const MxMatmulArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
-  return bf16 ? launch_instance<__nv_bfloat16>(a, num_sms, stream) : launch_instance<float>(a, num_sms, stream);
+  return bf16 ? launch_widths<__nv_bfloat16>(a, num_sms, stream) : launch_widths<float>(a, num_sms, stream);
 }
 
 }  // namespace mpm
