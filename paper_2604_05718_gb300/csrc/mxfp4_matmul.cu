@@ -25,7 +25,8 @@
 //    at 128 bytes a cycle against 384 of the products; 68 KB and 530 cycles
 //    against 512 for 256 columns.  Tensor memory has room for one accumulator
 //    then, and a tile waits until the last one's has been read (16384 x 4096 x
-//    1024: 34 us with 192 columns, 30 with 256; 8192 x 8192 x 8192: 180 and 172).  Tiles of 128 took as long as 192 for two thirds of the work.
+//    1024: 34 us with 192 columns, 30 with 256; 8192 x 8192 x 8192: 180 and
+//    172).  Tiles of 128 took as long as 192 for two thirds of the work.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -270,3 +270,9 @@ def test_refusals(mpm):
     with pytest.raises(mpm.MPMError) as e:
         mpm.quantize_mxfp4(torch.empty(0, (1 << 20) + 1, device=DEV))
     assert e.value.code == 2
+
+
+@pytest.mark.parametrize("m,n,k", [(5000, 4096, 2048), (19500, 257, 2049), (4900, 1027, 4100), (2560, 2048, 5120)])
+def test_wide_tiles_of_many_features(mpm, m, n, k):
+    check_product(mpm, m, n, k, seed=m)
+    check_product(mpm, m, n, k, torch.float32, bias=False, seed=m)
