@@ -183,6 +183,7 @@ struct NormArgs {
     device = y->get_device();
     rows = y->size(0);
     dim = y->size(1);
+    if (dim > INT32_MAX) value_error("y", "has too many features");
     dtype = dtype_of(*y, "y");
     stream_dtype = dtype_of(*residual, "residual");
     if (!PyUnicode_Check(p[2])) type_error("norm", "must be a string");
@@ -263,7 +264,7 @@ PyObject* block_norm_backward(PyObject* const* p) {
   void* pws;
   int64_t ws_bytes;
   if (p[14] == Py_None) {
-    ws_bytes = static_cast<int64_t>(entry.block_norm_workspace_size(static_cast<int32_t>(a.dim > INT32_MAX ? 0 : a.dim)));
+    ws_bytes = static_cast<int64_t>(entry.block_norm_workspace_size(static_cast<int32_t>(a.dim)));
     workspace = new_like(*a.y, {ws_bytes}, at::kByte);
     pws = workspace.data_ptr();
   } else {
