@@ -2,8 +2,8 @@
 // accumulated in fp32 on the tensor cores: tcgen05.mma kind::mxf4 with a
 // power-of-two scale per 32 elements.
 //
-// A cluster of two CTAs (an SM pair) computes 256 x N tiles (N = 192 or 256)
-// with cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows
+// A cluster of two CTAs (an SM pair) computes 256 x N tiles (N = 192, or 64, 128
+// or 256) with cta_group::2: each CTA stages its 128 rows of A, half of the tile's rows
 // of B, the scales of its A rows and those of all of the tile's B rows.  A step
 // takes 256 elements of every row, one 128-byte swizzle row of packed codes,
 // and four K = 64 products.  Scales go from shared memory to tensor memory by
@@ -44,18 +44,19 @@ constexpr int kTileM = 2 * kHalf;
 constexpr int kStepK = 256;            // elements of a row per step: 128 bytes
 constexpr int kScaleTiles = kStepK / (mx::kBlock * mx::kTileBlocks);  // scale tiles along K per step
 constexpr int kBytesA = kHalf * 128, kBytesSA = kScaleTiles * mx::kTileBytes, kSlotA = kBytesA + kBytesSA;
-constexpr int kRowTiles = 2;               // scale tiles along N that a tile's rows of B lie in, at most
 constexpr int kWarpCols = 64;              // columns of the tile that an epilogue warp writes
 constexpr int kBoxBytes = 32 * 128;        // staged output: 32 rows of 128 bytes, swizzled
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColsSA = 4, kColsSB = kRowTiles * kColsSA;  // tensor-memory columns of a scale tile of A, of those of B
+constexpr uint32_t kColsSA = 4;            // tensor-memory columns of a scale tile
 constexpr uint64_t kWaitNs = 2000000000ull;
 
 // What depends on a tile's columns.
 template <int N>
 struct Tile {
-  static constexpr int kAccumulators = N == 192 ? 2 : 1;
-  static constexpr int kSlotsA = N == 192 ? 6 : 5, kSlotsB = N == 192 ? 5 : 4;
+  static constexpr int kAccumulators = N == 256 ? 1 : 2;
+  static constexpr int kSlotsA = N == 256 ? 5 : 6, kSlotsB = N == 256 ? 4 : N == 192 ? 5 : 6;
+  static constexpr int kRowTiles = N > mx::kTileRows ? 2 : 1;  // scale tiles along N that a tile's rows of B lie in
+  static constexpr uint32_t kColsSB = kRowTiles * kColsSA;
   static constexpr int kMaxResident = kSlotsA - 1;  // steps of a panel that stays: one slot is left to begin the next one
   static constexpr int kBytesB = N / 2 * 128, kBytesSB = kRowTiles * kBytesSA, kSlotB = kBytesB + kBytesSB;
   // Tensor memory: the accumulators, the scales of A's slots, those of B's.
@@ -92,7 +93,9 @@ template <int N>
 constexpr size_t smem_bytes() {
   return 1024 + static_cast<size_t>(Tile<N>::kRings) + Tile<N>::kEpilogueWarps * kBoxBytes + sizeof(Control);
 }
-static_assert(smem_bytes<192>() <= 227 * 1024 && smem_bytes<256>() <= 227 * 1024, "a block's shared memory");
+static_assert(smem_bytes<64>() <= 227 * 1024 && smem_bytes<128>() <= 227 * 1024 && smem_bytes<192>() <= 227 * 1024 &&
+                  smem_bytes<256>() <= 227 * 1024,
+              "a block's shared memory");
 
 // Place in a ring.
 template <int SLOTS>
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
           if (leader) ptx::mbar_arrive_expect_tx(&ctl->full_b[rb.slot], 2 * W::kSlotB);
           load_pair(at, &map_b, full, kb * 128, n0 + N / 2 * static_cast<int32_t>(rank));
 #pragma unroll
-          for (int j = 0; j < kRowTiles; ++j)
+          for (int j = 0; j < W::kRowTiles; ++j)
             load_pair(at + W::kBytesB + j * kBytesSA, &map_sb, full, 0, (nt + j) * tiles_k + kt);
         }
         __syncwarp();
@@ -348,7 +351,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
           const uint32_t slot_a = at.slot * kSlotA, slot_b = W::kSlotsA * kSlotA + rb.slot * W::kSlotB;
           const uint64_t da = desc0 + static_cast<uint64_t>(slot_a >> 4), db = desc0 + static_cast<uint64_t>(slot_b >> 4);
           const uint32_t sa = tmem0 + W::kScalesA + at.slot * (kScaleTiles * kColsSA);
-          const uint32_t sb = tmem0 + W::kScalesB + rb.slot * (kScaleTiles * kColsSB);
+          const uint32_t sb = tmem0 + W::kScalesB + rb.slot * (kScaleTiles * W::kColsSB);
           const int products = min(kStepK / 64, (a.k - kb * kStepK + 63) / 64);
           if (ptx::elect_one()) {
 #pragma unroll
@@ -356,8 +359,8 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
               if (2 * j < products) {
                 if (begins) copy_scales(sa + j * kColsSA, scale_desc(smem0 + slot_a + kBytesA + j * mx::kTileBytes));
 #pragma unroll
-                for (int i = 0; i < kRowTiles; ++i)
-                  copy_scales(sb + j * kColsSB + 4 * i,
+                for (int i = 0; i < W::kRowTiles; ++i)
+                  copy_scales(sb + j * W::kColsSB + 4 * i,
                               scale_desc(smem0 + slot_b + W::kBytesB + i * kBytesSA + j * mx::kTileBytes));
               }
             }
@@ -365,7 +368,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
             for (int p = 0; p < kStepK / 64; ++p) {
               if (p < products)
                 mma_mx(d, da + 2 * p, db + 2 * p, instruction(N) | scale_half((p & 1) * 2), sa + (p / 2) * kColsSA,
-                       sb + (p / 2) * kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
+                       sb + (p / 2) * W::kColsSB + sb_shift, (kb | p) != 0 ? 1u : 0u);
             }
             commit_both(&ctl->empty_b[rb.slot]);
             if (ends) commit_both(&ctl->empty_a[at.slot]);
@@ -583,13 +586,22 @@ cudaError_t launch_instance(const MxMatmulArgs& a, int num_sms, cudaStream_t str
   return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_sa, map_sb, map_out, a, tma_out, bias_vec);
 }
 
+// The width of the tiles.  Where they are fewer than the SM pairs, narrow ones:
+// more pairs share the work (graph of launches, N = 64 / 128 / 192: 128 x 768 x
+// 768 3.5 / 4.0 / 4.5 us, 1000 x 1024 x 1024 4.3 / 4.3 / 4.7, 1 x 1024 x 4096 4.6
+// / 3.9 / 4.0: 64 columns for at most two thirds of the pairs).  256 columns
+// where those make one round and 192 would make two (1 x 4096 x 16384: 15.3 us
+// with 192, 13.7), and for many features and at least a round of them
+// (20000 x 2048 x 2048: 40 us with 192, 39; at 16384 x 1280 x 4096 39 and 42).
 template <typename T>
 cudaError_t launch_widths(const MxMatmulArgs& a, int num_sms, cudaStream_t stream) {
-  // Both at 20000 x 2048 x 2048: 39 us with 256 columns, 40 with 192; at 16384 x
-  // 1280 x 4096 42 and 39; with tiles for less than a round, 3000 x 2048 x 1024, 7.8 and 7.1.
-  const int64_t wide = (a.m + kTileM - 1) / kTileM * ((static_cast<int64_t>(a.n) + 255) / 256);
-  return a.k >= kWideK && wide >= num_sms / 2 ? launch_instance<T, 256>(a, num_sms, stream)
-                                              : launch_instance<T, 192>(a, num_sms, stream);
+  const int64_t pairs = num_sms > 1 ? num_sms / 2 : 1;
+  auto tiles = [&](int width) { return (a.m + kTileM - 1) / kTileM * ((static_cast<int64_t>(a.n) + width - 1) / width); };
+  if (3 * tiles(64) <= 2 * pairs) return launch_instance<T, 64>(a, num_sms, stream);
+  if (tiles(128) <= pairs) return launch_instance<T, 128>(a, num_sms, stream);
+  const bool one_round = a.m <= kTileM && tiles(256) <= pairs && tiles(192) > pairs;
+  if (one_round || (a.k >= kWideK && tiles(256) >= pairs)) return launch_instance<T, 256>(a, num_sms, stream);
+  return launch_instance<T, 192>(a, num_sms, stream);
 }
 
 }  // namespace
