@@ -276,3 +276,13 @@ def test_refusals(mpm):
 def test_wide_tiles_of_many_features(mpm, m, n, k):
     check_product(mpm, m, n, k, seed=m)
     check_product(mpm, m, n, k, torch.float32, bias=False, seed=m)
+
+
+@pytest.mark.parametrize("m,n", [(6000, 129), (6000, 200), (5900, 257), (6144, 383), (6000, 384),      # 128 columns
+                                 (19500, 1), (19500, 65), (19456, 191), (19500, 193), (19500, 385),    # 192 columns
+                                 (100, 16000), (250, 18001)])                                          # 256 columns
+@pytest.mark.parametrize("k", [31, 256, 300, 1280, 1400])
+def test_every_tile_width(mpm, m, n, k):
+    check_product(mpm, m, n, k, seed=n)
+    if k == 300:
+        check_product(mpm, m, n, k, torch.float32, seed=n, in_dtype=torch.float32)
