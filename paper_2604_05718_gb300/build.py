@@ -63,15 +63,15 @@ def _binding_command(out: str) -> list:
     """g++ over the binding, against the torch that runs this."""
     import torch
 
-    root = os.path.join(os.path.dirname(torch.__file__))
+    root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
     lib = os.path.join(root, "lib")
     return [os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-O2", "-std=c++17", "-fvisibility=hidden",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", BINDING_SRC, "-o", out] + \
-        [f"-I{d}" for d in include] + [f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
-                                       f"-Wl,-rpath,{lib}"]
+        [f"-I{d}" for d in include] + [f"-L{lib}", "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10",
+                                       "-lc10_cuda", f"-Wl,-rpath,{lib}"]
 
 
 def build(force: bool = False, extra_flags: list | None = None, trace: bool = False) -> str:
