@@ -4,7 +4,7 @@
 // for the merge through ctypes; every step of the computation is the C ABI's,
 // whose addresses blocks.py hands over at start.  Small calls are bound by the
 // host, and these take up to thirty arguments: one row through block_norm took
-// 19 us a call through ctypes (14 with every check in one expression), 5 here.
+// 19 us a call through ctypes (14 with every check in one expression), 4.4 here.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
