@@ -449,7 +449,9 @@ __global__ void __launch_bounds__(block_warps(C) * 32, 1)
 #pragma unroll
     for (int c = 0; c < C; ++c) mine.set(c, value(c));
     which_kept |= static_cast<uint32_t>(which) << (4 * kept);
-    if (++kept == room) join_kept();
+    // One at a time for groups of several warps: with more, the compiler's code
+    // for the rows is slower (30000 x 1024 bf16: 76 us, 95 with two or five).
+    if (++kept == (MULTI ? 1 : room)) join_kept();
   };
   // Over the gates of a run: what its last image left, or the one gate's sums.
   auto over_gates = [&](const F8(&s)[C], int c) {
