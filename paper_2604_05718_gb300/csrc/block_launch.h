@@ -67,6 +67,10 @@ constexpr int kNormWarpCols = 256;
 cudaError_t launch_block_norm(const NormForward& a, NormTypes types, bool vec, int num_sms, cudaStream_t stream);
 cudaError_t launch_block_norm_backward(const NormBackward& a, NormTypes types, bool vec, int num_sms,
                                        cudaStream_t stream);
+// Its parts, a file each.
+cudaError_t launch_block_norm_backward_f32(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
+cudaError_t launch_block_norm_backward_bf16(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
+cudaError_t launch_block_norm_backward_mixed(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
 // Floats of workspace that the backward pass's partial sums take.
 size_t block_norm_workspace_floats(int dim);
 

@@ -30,6 +30,11 @@
 // 107 with a warp a row, 9 of them the join: 4.7 TB/s.  Two warps a scheduler
 // issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
 // fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
+//
+// A file per pair of token types includes this one: the kernels of all three
+// take over a minute to compile.
+#pragma once
+
 #include <atomic>
 
 #include "block_launch.h"
@@ -48,17 +53,22 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 
 // Chunks of 256 columns that a warp holds (8 C columns a thread): the whole row
 // if it can, else the count that leaves no warp of a group half empty.  Their
-// sums and row take about 30 + 56 C registers, which sets the block's warps.
+// sums and row take about 30 + 56 C registers, which sets the block's warps: 8
+// of 255 registers, 12 of 168, 16 of 128 (rows of more than 8192 features need
+// 16 and spill).
 __host__ __device__ constexpr int chunks_per_warp(int dim) {
   const int chunks = (dim + kNormWarpCols - 1) / kNormWarpCols;
   return chunks == 1 ? 1 : chunks > 24 ? 4 : chunks % 3 == 0 ? 3 : 2;
 }
-__host__ __device__ constexpr int block_warps(int c) { return c == 3 ? 8 : c == 2 ? 12 : 16; }
+__host__ __device__ constexpr int block_warps(int dim) {
+  const int c = chunks_per_warp(dim);
+  return c == 3 ? 8 : c == 2 ? 12 : c == 1 || dim > 32 * kNormWarpCols ? 16 : 8;
+}
 __host__ __device__ constexpr int warps_per_row(int dim) {
   return (dim + kNormWarpCols * chunks_per_warp(dim) - 1) / (kNormWarpCols * chunks_per_warp(dim));
 }
 // Most groups of a block (a ring of long rows may leave room for fewer).
-__host__ __device__ constexpr int max_groups(int dim) { return block_warps(chunks_per_warp(dim)) / warps_per_row(dim); }
+__host__ __device__ constexpr int max_groups(int dim) { return block_warps(dim) / warps_per_row(dim); }
 // Shared memory of a block for the groups: 227 KB less 2 KB of barriers and sums.
 constexpr int kSharedBytes = 225 * 1024;
 
@@ -140,14 +150,14 @@ __host__ __device__ constexpr int vector_bytes(int dim) {
 }
 
 // RING: 16-byte aligned rows through shared memory (vector accesses); otherwise loads of single elements.
-template <typename TY, typename TX, int C, bool RING, bool MULTI>
-__global__ void __launch_bounds__(block_warps(C) * 32, 1)
+template <typename TY, typename TX, int C, bool RING, bool MULTI, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1)
     block_norm_backward_kernel(NormBackward a, int row_warps, int ring, int room) {
   using Row = Slot<TY, TX>;
   // w_pre; A and B of each group; the groups' rings.  Afterwards the groups' column sums.
   extern __shared__ __align__(16) uint8_t dynamic[];
-  __shared__ __align__(16) float sh[4 * block_warps(C)];
-  __shared__ uint64_t full[block_warps(C)][kMaxRing];
+  __shared__ __align__(16) float sh[4 * WARPS];
+  __shared__ uint64_t full[WARPS][kMaxRing];
   __shared__ int dead;  // a wait ran out: no further one is taken
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
@@ -552,9 +562,9 @@ RingPlan plan_ring(int dim, int row_bytes) {
   return {0, 0};
 }
 
-template <typename TY, typename TX, int C, bool RING, bool MULTI>
+template <typename TY, typename TX, int C, bool RING, bool MULTI, int WARPS>
 cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
-  const auto kernel = block_norm_backward_kernel<TY, TX, C, RING, MULTI>;
+  const auto kernel = block_norm_backward_kernel<TY, TX, C, RING, MULTI, WARPS>;
   const int w = warps_per_row(a.dim), vector = vector_bytes(a.dim);
   int groups = ring.groups;
   if (!RING) {
@@ -594,12 +604,13 @@ template <typename TY, typename TX, bool RING>
 cudaError_t launch_types(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
   const bool multi = warps_per_row(a.dim) > 1;
   switch (chunks_per_warp(a.dim)) {
-    case 1: return launch_instance<TY, TX, 1, RING, false>(a, ring, num_sms, stream);
-    case 2: return multi ? launch_instance<TY, TX, 2, RING, true>(a, ring, num_sms, stream)
-                         : launch_instance<TY, TX, 2, RING, false>(a, ring, num_sms, stream);
-    case 3: return multi ? launch_instance<TY, TX, 3, RING, true>(a, ring, num_sms, stream)
-                         : launch_instance<TY, TX, 3, RING, false>(a, ring, num_sms, stream);
-    default: return launch_instance<TY, TX, 4, RING, true>(a, ring, num_sms, stream);
+    case 1: return launch_instance<TY, TX, 1, RING, false, 16>(a, ring, num_sms, stream);
+    case 2: return multi ? launch_instance<TY, TX, 2, RING, true, 12>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, 2, RING, false, 12>(a, ring, num_sms, stream);
+    case 3: return multi ? launch_instance<TY, TX, 3, RING, true, 8>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, 3, RING, false, 8>(a, ring, num_sms, stream);
+    default: return block_warps(a.dim) == 8 ? launch_instance<TY, TX, 4, RING, true, 8>(a, ring, num_sms, stream)
+                                            : launch_instance<TY, TX, 4, RING, true, 16>(a, ring, num_sms, stream);
   }
 }
 
@@ -611,19 +622,4 @@ cudaError_t launch_vec(const NormBackward& a, bool vec, int num_sms, cudaStream_
 }
 
 }  // namespace
-
-size_t block_norm_workspace_floats(int dim) {
-  return static_cast<size_t>(dim) * kMaxBlocks * (kSums + 4 * static_cast<size_t>(max_groups(dim)));
-}
-
-cudaError_t launch_block_norm_backward(const NormBackward& a, NormTypes types, bool vec, int num_sms,
-                                       cudaStream_t stream) {
-  switch (types) {
-    case NormTypes::kF32: return launch_vec<float, float>(a, vec, num_sms, stream);
-    case NormTypes::kBf16: return launch_vec<__nv_bfloat16, __nv_bfloat16>(a, vec, num_sms, stream);
-    case NormTypes::kBf16StreamF32: return launch_vec<__nv_bfloat16, float>(a, vec, num_sms, stream);
-  }
-  return cudaErrorInvalidValue;
-}
-
 }  // namespace mpm
