@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   using Row = Slot<TY, TX>;
   // w_pre; A and B of each group; the groups' rings.  Afterwards the groups' column sums.
   extern __shared__ __align__(16) uint8_t dynamic[];
-  __shared__ __align__(16) float sh[4 * WARPS];
+  __shared__ float2 sh[2 * WARPS];
   __shared__ uint64_t full[WARPS][kMaxRing];
   __shared__ int dead;  // a wait ran out: no further one is taken
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   wait_for_previous_grid();
   allow_next_grid();
   check_offsets(a.offsets, a.batch, a.rows, a.status);
-  GroupSums<2, MULTI> sum{sh + group * 4 * w, w, in_group, group + 1, 0};
+  PairSum<MULTI> sum{sh + group * 2 * w, w, in_group, group + 1, 0};
   const int64_t total = used_rows(a.offsets, a.batch, a.rows);
   const int64_t all = static_cast<int64_t>(gridDim.x) * groups, g = static_cast<int64_t>(blockIdx.x) * groups + group;
   const Run run = run_of(g, all, total);

@@ -22,15 +22,8 @@ constexpr int kTileBytes = 512;
 constexpr int kNanScale = 255;
 
 __host__ __device__ constexpr int code_pitch(int dim) { return (dim + 63) / 64 * 32; }
-__host__ __device__ constexpr int blocks_of(int dim) { return (dim + kBlock - 1) / kBlock; }
 __host__ __device__ constexpr int scale_tiles(int dim) { return (dim + kBlock * kTileBlocks - 1) / (kBlock * kTileBlocks); }
 __host__ __device__ constexpr int64_t row_tiles(int64_t rows) { return (rows + kTileRows - 1) / kTileRows; }
-
-__device__ __forceinline__ int64_t scale_byte(int64_t row, int block, int tiles) {
-  const int r = static_cast<int>(row % kTileRows);
-  return ((row / kTileRows) * tiles + block / kTileBlocks) * kTileBytes + (r % 32) * 16 + (r / 32) * 4 +
-         block % kTileBlocks;
-}
 
 }  // namespace mx
 

@@ -2,10 +2,6 @@
 // spread over threads, its loads and stores, and sums over it.
 #pragma once
 
-#include <string.h>
-
-#include <type_traits>
-
 #include "block_launch.h"
 #include "common.cuh"
 
@@ -171,57 +167,41 @@ struct RowSum {
   }
 };
 
-// N values (2 or 4) summed over a warp: afterwards lane l holds the sum of
-// value l / (32 / N).  Lanes first trade values, so that N values take
-// N - 1 + log2(32 / N) shuffles instead of 5 N.
-template <int N>
-__device__ __forceinline__ float warp_sums(const float (&v)[N]) {
-  static_assert(N == 2 || N == 4, "two or four values");
-  const int lane = threadIdx.x & 31;
-  float s;
-  if constexpr (N == 4) {
-    const bool hi = (lane & 16) != 0;
-    const float a = (hi ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[2], 16);
-    const float b = (hi ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[1] : v[3], 16);
-    const bool odd = (lane & 8) != 0;
-    s = (odd ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 8);
-  } else {
-    const bool hi = (lane & 16) != 0;
-    s = (hi ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 16);
-    s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
-  }
+// Two values summed over a warp: lanes 0 to 15 get the sum of the first, the
+// others of the second.  They trade values first, so that both take six
+// shuffles instead of ten.
+__device__ __forceinline__ float warp_sums(const float (&v)[2]) {
+  const bool hi = (threadIdx.x & 16) != 0;
+  float s = (hi ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 16);
 #pragma unroll
-  for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
   return s;
 }
 
-// The same over the W warps of a group, all N sums to every thread.  `sh`
-// holds 2 x W x N floats (16-byte aligned); its halves alternate as in RowSum.
-template <int N, bool MULTI>
-struct GroupSums {
-  float* sh;
+// The same over the W warps of a group, both sums to every thread.  `sh` holds
+// 2 x W pairs; its halves alternate as in RowSum.
+template <bool MULTI>
+struct PairSum {
+  float2* sh;
   int warps, warp, barrier, turn;
-  __device__ __forceinline__ void operator()(float (&v)[N]) {
-    const float s = warp_sums<N>(v);
-    const int lane = threadIdx.x & 31;
+  __device__ __forceinline__ void operator()(float (&v)[2]) {
+    const float s = warp_sums(v);
     if constexpr (MULTI) {
-      float* half = sh + (turn & 1) * warps * N;
+      const int lane = threadIdx.x & 31;
+      float2* half = sh + (turn & 1) * warps;
       ++turn;
-      if (lane % (32 / N) == 0) half[warp * N + lane / (32 / N)] = s;
+      if (lane % 16 == 0) (lane == 0 ? half[warp].x : half[warp].y) = s;
       asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(warps * 32) : "memory");
-      using Row = typename std::conditional<N == 4, float4, float2>::type;
-      const Row first = *reinterpret_cast<const Row*>(half);
-      memcpy(v, &first, sizeof(v));
+      float2 t = half[0];
       for (int w = 1; w < warps; ++w) {
-        const Row more = *reinterpret_cast<const Row*>(half + w * N);
-        float m[N];
-        memcpy(m, &more, sizeof(m));
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += m[i];
+        t.x += half[w].x;
+        t.y += half[w].y;
       }
+      v[0] = t.x;
+      v[1] = t.y;
     } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, s, i * (32 / N));
+      v[0] = __shfl_sync(0xFFFFFFFFu, s, 0);
+      v[1] = __shfl_sync(0xFFFFFFFFu, s, 16);
     }
   }
 };
