@@ -27,7 +27,7 @@
 // of a row, whose chains overlap, without barriers in between.  54208 x 768
 // bf16, layer norm on both sides and a gate per image (500 MB): 192 us from
 // loads in place, 164 with rows spread over three warps (two barriers a row),
-// 107 with a warp a row, 9 of them the join: 4.7 TB/s.  Two warps a scheduler
+// 111 with a warp a row, 9 of them the join: 4.5 TB/s.  Two warps a scheduler
 // issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
 // fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
 //

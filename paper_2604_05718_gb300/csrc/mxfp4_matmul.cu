@@ -259,7 +259,8 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
     // The whole warp runs this loop and the next one; an elected lane issues.
     // In a branch of one lane every operand of a copy or product first moves to
     // a uniform register, about 70 cycles an instruction, which bound the
-    // kernel: 8192 x 8192 x 8192 took 316 us instead of 176.
+    // kernel: 8192 x 8192 x 8192 took 316 us instead of 176 (192
+    // columns; 172 with 256).
     Ring<W::kSlotsA> ra;
     Ring<W::kSlotsB> rb;
     int issued_a = 0, issued_b = 0;
@@ -398,8 +399,8 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
     // fp32): a lane writes its own row, 16-byte piece p at p ^ (row & 7), which
     // is the 128-byte swizzle and free of bank conflicts; a TMA store takes the
     // box to global memory in whole 128-byte runs.  Stores from registers,
-    // 16 bytes a row and instruction, took 144 us instead of the 75 that this
-    // takes for 54208 x 768 x 2304 to bf16.
+    // 16 bytes a row and instruction, took 144 us instead of 75 for 54208 x
+    // 768 x 2304 to bf16, before the A panel stayed (54 to 57 now).
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t empty0 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[0]), 0);
     const uint32_t empty1 = map_to_rank(ptx::smem_addr(&ctl->acc_empty[1]), 0);
