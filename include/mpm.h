@@ -463,6 +463,8 @@ MPM_API size_t mpm_block_norm_workspace_size(int32_t dim);
  *                        (zeros for an empty image, or without rows).
  *   workspace            mpm_block_norm_workspace_size(dim) bytes
  * Sums are taken in fp32 in a fixed order: the same call gives the same bits.
+ * An output, the workspace or the status word over an input or over one
+ * another: MPM_ERR_ALIASING.
  */
 MPM_API mpm_status mpm_block_norm_backward(
     const void* d_residual_out, int64_t d_residual_out_stride, const void* d_h, int64_t d_h_stride, const void* y,

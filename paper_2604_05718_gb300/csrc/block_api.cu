@@ -23,6 +23,7 @@ struct Range {
 };
 
 constexpr int64_t kMaxMatmulRows = int64_t{1} << 30;  // tile coordinates are 32-bit
+constexpr size_t kStatusBytes = 2 * sizeof(int32_t);
 
 int elem(mpm_dtype t) { return t == MPM_BF16 ? 2 : 4; }
 bool valid_dtype(mpm_dtype t) { return t == MPM_F32 || t == MPM_BF16; }
@@ -74,6 +75,11 @@ struct NormShape {
   const float *post_weight, *post_bias, *gate, *pre_weight;
   int32_t gate_per_image;
 };
+size_t gate_bytes(const NormShape& s) {
+  return sizeof(float) * static_cast<size_t>(s.dim) * (s.gate_per_image ? static_cast<size_t>(s.batch) : 1);
+}
+Extent gate_extent(const NormShape& s) { return extent(s.gate, gate_bytes(s)); }
+Extent offsets_extent(const NormShape& s) { return extent(s.offsets, sizeof(int64_t) * (static_cast<size_t>(s.batch) + 1)); }
 
 mpm_status check_norm(const NormShape& s, mpm::NormTypes* types) {
   if (!valid_dtype(s.dtype) || !valid_dtype(s.stream_dtype) || s.dim < 1 || s.batch < 1 || s.rows < 0 ||
@@ -130,8 +136,12 @@ mpm_status mpm_block_norm(const void* y, int64_t y_stride, const void* residual,
   const Extent out_s = extent(stats, static_cast<size_t>(rows) * 16);
   // In place on the stream: each thread reads its own columns of a row before it writes them.
   const bool in_place = residual_out == residual && (residual_stride == dim || rows == 1);
-  if (any_overlap({out_x, out_h, out_s}, {in_y}) || any_overlap({out_h, out_s}, {in_x}) ||
-      (!in_place && overlap(out_x, in_x)))
+  const Extent out_status = extent(device_status, kStatusBytes);
+  const size_t vector = sizeof(float) * static_cast<size_t>(dim);
+  if (any_overlap({out_x, out_h, out_s, out_status},
+                  {in_y, extent(post_weight, vector), extent(post_bias, vector), gate_extent(shape),
+                   extent(pre_weight, vector), extent(pre_bias, vector), offsets_extent(shape)}) ||
+      any_overlap({out_h, out_s, out_status}, {in_x}) || (!in_place && overlap(out_x, in_x)))
     return MPM_ERR_ALIASING;
   const bool vec = dim % 8 == 0 && vector_rows(y, y_stride, e) && vector_rows(residual, residual_stride, es) &&
                    aligned(residual_out, 16) && aligned(h, 16) && aligned(post_weight, 16) && aligned(post_bias, 16) &&
@@ -206,14 +216,14 @@ mpm_status mpm_block_norm_backward(const void* d_residual_out, int64_t d_residua
   const size_t need = mpm_block_norm_workspace_size(dim);
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need) return MPM_ERR_WORKSPACE;
   const size_t vector = sizeof(float) * static_cast<size_t>(dim);
-  const size_t gate_bytes = gate_per_image ? vector * batch : vector;
   if (any_overlap({extent(d_y, rows, dim, dim, e), extent(d_residual, rows, dim, dim, es), extent(d_post_weight, vector),
-                   extent(d_post_bias, vector), extent(d_gate, gate_bytes), extent(d_pre_weight, vector),
-                   extent(d_pre_bias, vector), extent(workspace, need)},
+                   extent(d_post_bias, vector), extent(d_gate, gate_bytes(shape)), extent(d_pre_weight, vector),
+                   extent(d_pre_bias, vector), extent(workspace, need), extent(device_status, kStatusBytes)},
                   {extent(y, rows, dim, y_stride, e), extent(residual, rows, dim, residual_stride, es),
                    extent(d_h, rows, dim, d_h_stride, e),
                    extent(d_residual_out, rows, dim, d_residual_out_stride, es),
-                   extent(stats, static_cast<size_t>(rows) * 16)}))
+                   extent(stats, static_cast<size_t>(rows) * 16), extent(post_weight, vector), extent(post_bias, vector),
+                   gate_extent(shape), extent(pre_weight, vector), offsets_extent(shape)}))
     return MPM_ERR_ALIASING;
   const bool vec = dim % 8 == 0 && vector_rows(y, y_stride, e) && vector_rows(residual, residual_stride, es) &&
                    (d_h == nullptr || vector_rows(d_h, d_h_stride, e)) &&
@@ -317,7 +327,7 @@ mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int
   for (const uint8_t* p : {a_codes, a_scales, b_codes, b_scales})
     if (!aligned(p, 16)) return MPM_ERR_ALIGNMENT;
   if (!aligned(out, e) || !aligned(bias, 4)) return MPM_ERR_ALIGNMENT;
-  if (any_overlap({extent(out, m, n, out_stride, e)},
+  if (any_overlap({extent(out, m, n, out_stride, e), extent(device_status, kStatusBytes)},
                   {extent(a_codes, mx_code_bytes(m, k)), extent(a_scales, mx_scale_bytes(m, k)),
                    extent(b_codes, mx_code_bytes(n, k)), extent(b_scales, mx_scale_bytes(n, k)),
                    extent(bias, sizeof(float) * static_cast<size_t>(n))}))
