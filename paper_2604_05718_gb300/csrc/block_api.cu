@@ -129,7 +129,7 @@ mpm_status mpm_block_norm(const void* y, int64_t y_stride, const void* residual,
   if (!stride_ok(y_stride, rows, dim) || !stride_ok(residual_stride, rows, dim)) return MPM_ERR_INVALID_ARG;
   const int e = elem(dtype), es = elem(stream_dtype);
   if (!aligned(y, e) || !aligned(h, e) || !aligned(residual, es) || !aligned(residual_out, es) || !aligned(stats, 16) ||
-      !aligned(pre_bias, 4))
+      !aligned(pre_bias, 4) || !aligned(device_status, 4))
     return MPM_ERR_ALIGNMENT;
   const Extent in_y = extent(y, rows, dim, y_stride, e), in_x = extent(residual, rows, dim, residual_stride, es);
   const Extent out_x = extent(residual_out, rows, dim, dim, es), out_h = extent(h, rows, dim, dim, e);
@@ -205,7 +205,7 @@ mpm_status mpm_block_norm_backward(const void* d_residual_out, int64_t d_residua
     return MPM_ERR_INVALID_ARG;
   const int e = elem(dtype), es = elem(stream_dtype);
   if (!aligned(y, e) || !aligned(d_h, e) || !aligned(d_y, e) || !aligned(residual, es) || !aligned(d_residual_out, es) ||
-      !aligned(d_residual, es) || !aligned(stats, 16))
+      !aligned(d_residual, es) || !aligned(stats, 16) || !aligned(device_status, 4))
     return MPM_ERR_ALIGNMENT;
   const float* const grads[] = {d_post_weight, d_post_bias, d_gate, d_pre_weight, d_pre_bias};
   bool grads16 = true;
@@ -326,7 +326,7 @@ mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int
   const int e = elem(dtype);
   for (const uint8_t* p : {a_codes, a_scales, b_codes, b_scales})
     if (!aligned(p, 16)) return MPM_ERR_ALIGNMENT;
-  if (!aligned(out, e) || !aligned(bias, 4)) return MPM_ERR_ALIGNMENT;
+  if (!aligned(out, e) || !aligned(bias, 4) || !aligned(device_status, 4)) return MPM_ERR_ALIGNMENT;
   if (any_overlap({extent(out, m, n, out_stride, e), extent(device_status, kStatusBytes)},
                   {extent(a_codes, mx_code_bytes(m, k)), extent(a_scales, mx_scale_bytes(m, k)),
                    extent(b_codes, mx_code_bytes(n, k)), extent(b_scales, mx_scale_bytes(n, k)),

@@ -111,3 +111,11 @@ def test_mxfp4(lib):
     assert matmul(ac=at(0) + 8) == 3 and matmul(out=at(5) + 1) == 3 and matmul(bias=at(4) + 2) == 3
     assert matmul(out=at(0)) == 8 and matmul(out=at(4) + 16) == 8
     assert matmul(m=0) == 0
+
+
+def test_misaligned_status_word(lib):
+    """The kernels report by an atomic on the word: off 4 bytes it would be a misaligned address on the device."""
+    for off in (1, 2, 3):
+        assert forward(lib, status=at(12) + off) == 3
+        assert backward(lib, status=at(20) + off) == 3
+        assert lib.mpm_mxfp4_matmul(at(0), at(1), 10, at(2), at(3), 20, 64, at(4), 1, at(5), 20, at(6) + off, None) == 3
