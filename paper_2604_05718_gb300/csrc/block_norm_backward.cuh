@@ -40,6 +40,7 @@
 #include "block_launch.h"
 #include "norm_rows.cuh"
 #include "ptx.cuh"
+#include "row_ring.cuh"
 
 namespace mpm {
 namespace {
@@ -152,21 +153,24 @@ __host__ __device__ constexpr int vector_bytes(int dim) {
 // RING: 16-byte aligned rows through shared memory (vector accesses); otherwise loads of single elements.
 template <typename TY, typename TX, int C, bool RING, bool MULTI, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 1)
-    block_norm_backward_kernel(NormBackward a, int row_warps, int ring, int room) {
+    block_norm_backward_kernel(NormBackward a, int row_warps, int slots, int room) {
   using Row = Slot<TY, TX>;
   // w_pre; A and B of each group; the groups' rings.  Afterwards the groups' column sums.
   extern __shared__ __align__(16) uint8_t dynamic[];
   __shared__ float2 sh[2 * WARPS];
   __shared__ uint64_t full[WARPS][kMaxRing];
-  __shared__ int dead;  // a wait ran out: no further one is taken
+  __shared__ int dead;          // a wait ran out: no further one is taken
+  __shared__ int asked[WARPS];  // rows that the group asked for
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const int w = MULTI ? row_warps : 1;
   const int groups = (blockDim.x >> 5) / w, group = warp / w, in_group = warp % w;
   if (threadIdx.x == 0) {
     dead = 0;
     if constexpr (RING) {
-      for (int k = 0; k < groups; ++k)
-        for (int s = 0; s < ring; ++s) ptx::mbar_init(&full[k][s], 1);
+      for (int k = 0; k < groups; ++k) {
+        asked[k] = 0;
+        for (int s = 0; s < slots; ++s) ptx::mbar_init(&full[k][s], 1);
+      }
       ptx::fence_barrier_init();
     }
   }
@@ -188,11 +192,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   const SharedVector pre_weight = shared_vector(0), scale = shared_vector(1 + 2 * group), shift = shared_vector(2 + 2 * group);
 
   const int wide = w * C * kNormWarpCols, slot_bytes = wide * Row::kValueBytes + 16;
-  uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * ring * slot_bytes;
+  uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * slots * slot_bytes;
   if constexpr (RING) {
     if (wide != a.dim || a.d_h == nullptr || a.d_residual_out == nullptr) {
       uint4* const rings = reinterpret_cast<uint4*>(dynamic + (1 + 2 * groups) * vector);
-      for (int i = threadIdx.x; i < groups * ring * slot_bytes / 16; i += blockDim.x) rings[i] = make_uint4(0, 0, 0, 0);
+      for (int i = threadIdx.x; i < groups * slots * slot_bytes / 16; i += blockDim.x) rings[i] = make_uint4(0, 0, 0, 0);
       // Before the copies into the same slots.
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncthreads();
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   if constexpr (RING) {
     if (in_group == 0 && ptx::elect_one()) {
 #pragma unroll 1
-      for (int k = 0; k < ring && run.begin + k < run.end; ++k) fill(run.begin + k, k);
+      for (int k = 0; k < slots && run.begin + k < run.end; ++k) ring::refill(&dead, &asked[group], [&] { fill(run.begin + k, k); });
     }
   }
 
@@ -317,7 +321,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     float4 st;
     if constexpr (RING) {
       // After a wait that ran out the rows are worked on as they are: the call
-      // has failed, and leaving would strand the group's other warps.
+      // has failed, and leaving would strand the group's other warps.  No more
+      // rows are asked for, and what is under way is waited for at the end.
       if (!ptx::mbar_wait(&full[group][k_slot], phase, &dead, kWaitNs)) {
         dead = 1;
         report(a.status, MPM_ERR_DEVICE_TIMEOUT, 31);
@@ -405,9 +410,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(w * 32) : "memory");
     if constexpr (RING) {
       __syncwarp();
-      if (in_group == 0 && row + ring < run.end && ptx::elect_one()) fill(row + ring, k_slot);
+      if (in_group == 0 && row + slots < run.end && ptx::elect_one())
+        ring::refill(&dead, &asked[group], [&] { fill(row + slots, k_slot); });
       __syncwarp();
-      if (++k_slot == ring) {
+      if (++k_slot == slots) {
         k_slot = 0;
         phase ^= 1u;
       }
@@ -468,6 +474,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     return per_image ? s[c] : gated(param8<RING>(a.gate, col[c], a.dim, 1.f), s[c]);
   };
   __syncthreads();
+  if constexpr (RING) {
+    if (dead != 0) {
+      if (in_group == 0 && lane == 0) ring::drain(full[group], slots, asked[group], kWaitNs);
+      __syncthreads();
+    }
+  }
   if (a.d_pre_weight != nullptr) leave(0, [&](int c) { return s_wpre[c]; });
   if (a.d_pre_bias != nullptr) leave(1, [&](int c) { return s_bpre[c]; });
   if (a.d_gate != nullptr && !per_image) leave(4, [&](int c) { return gate_gradient(c); });
