@@ -71,6 +71,10 @@ cudaError_t launch_block_norm_backward(const NormBackward& a, NormTypes types, b
 cudaError_t launch_block_norm_backward_f32(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
 cudaError_t launch_block_norm_backward_bf16(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
 cudaError_t launch_block_norm_backward_mixed(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
+// And without pre_weight.
+cudaError_t launch_block_norm_backward_f32_no_pre(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
+cudaError_t launch_block_norm_backward_bf16_no_pre(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
+cudaError_t launch_block_norm_backward_mixed_no_pre(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream);
 // Floats of workspace that the backward pass's partial sums take.
 size_t block_norm_workspace_floats(int dim);
 

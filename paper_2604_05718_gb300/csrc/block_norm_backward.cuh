@@ -31,8 +31,8 @@
 // issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
 // fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
 //
-// A file per pair of token types includes this one: the kernels of all three
-// take over a minute to compile.
+// Two files per pair of token types include this one, with and without a norm
+// before the next block: the kernels of all take minutes to compile.
 #pragma once
 
 #include <atomic>
@@ -151,7 +151,9 @@ __host__ __device__ constexpr int vector_bytes(int dim) {
 }
 
 // RING: 16-byte aligned rows through shared memory (vector accesses); otherwise loads of single elements.
-template <typename TY, typename TX, int C, bool RING, bool MULTI, int WARPS>
+// PRE: with a norm before the next block.  Without it G = dx': neither x nor x' has a
+// part in the gradients, and where they are not finite the gradients are all the same.
+template <typename TY, typename TX, bool PRE, int C, bool RING, bool MULTI, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 1)
     block_norm_backward_kernel(NormBackward a, int row_warps, int slots, int room) {
   using Row = Slot<TY, TX>;
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   const int wide = w * C * kNormWarpCols, slot_bytes = wide * Row::kValueBytes + 16;
   uint8_t* const ring_base = dynamic + (1 + 2 * groups) * vector + group * slots * slot_bytes;
   if constexpr (RING) {
-    if (wide != a.dim || a.d_h == nullptr || a.d_residual_out == nullptr) {
+    if (wide != a.dim || (PRE && a.d_h == nullptr) || a.d_residual_out == nullptr) {
       uint4* const rings = reinterpret_cast<uint4*>(dynamic + (1 + 2 * groups) * vector);
       for (int i = threadIdx.x; i < groups * slots * slot_bytes / 16; i += blockDim.x) rings[i] = make_uint4(0, 0, 0, 0);
       // Before the copies into the same slots.
@@ -206,11 +208,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     const Row to{ring_base + k * slot_bytes, wide};
     uint64_t* bar = &full[group][k];
     const uint32_t bytes_y = a.dim * static_cast<uint32_t>(sizeof(TY)), bytes_x = a.dim * static_cast<uint32_t>(sizeof(TX));
-    ptx::mbar_arrive_expect_tx(bar, bytes_y + bytes_x + (a.d_h != nullptr ? bytes_y : 0) +
+    ptx::mbar_arrive_expect_tx(bar, bytes_y + (PRE ? bytes_x : 0) + (PRE && a.d_h != nullptr ? bytes_y : 0) +
                                         (a.d_residual_out != nullptr ? bytes_x : 0) + 16);
     bulk_load(to.y(), static_cast<const TY*>(a.y) + row * a.y_stride, bytes_y, bar);
-    bulk_load(to.x(), static_cast<const TX*>(a.residual) + row * a.residual_stride, bytes_x, bar);
-    if (a.d_h != nullptr) bulk_load(to.d_h(), static_cast<const TY*>(a.d_h) + row * a.d_h_stride, bytes_y, bar);
+    if constexpr (PRE) bulk_load(to.x(), static_cast<const TX*>(a.residual) + row * a.residual_stride, bytes_x, bar);
+    if (PRE && a.d_h != nullptr) bulk_load(to.d_h(), static_cast<const TY*>(a.d_h) + row * a.d_h_stride, bytes_y, bar);
     if (a.d_residual_out != nullptr)
       bulk_load(to.d_x(), static_cast<const TX*>(a.d_residual_out) + row * a.d_residual_out_stride, bytes_x, bar);
     bulk_load(to.stats(), a.stats + row, 16, bar);
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     col[c] = first_column<RING>(c * w + in_group, lane);
-    if (group == 0) pre_weight.set(c, param8<RING>(a.pre_weight, col[c], a.dim, 0.f));  // absent: no part in the gradients
+    if (PRE && group == 0) pre_weight.set(c, param8<RING>(a.pre_weight, col[c], a.dim, 0.f));
     s_wpre[c] = s_bpre[c] = s_one[c] = s_n1[c] = all8(0.f);
   }
   __syncthreads();
@@ -335,17 +337,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     for (int c = 0; c < C; ++c) {
       if constexpr (RING) {
         y[c] = staged8(in.y(), col[c]);
-        x[c] = staged8(in.x(), col[c]);
-        dh[c] = staged8(in.d_h(), col[c]);
+        if constexpr (PRE) {
+          x[c] = staged8(in.x(), col[c]);
+          dh[c] = staged8(in.d_h(), col[c]);
+        }
       } else {
         y[c] = load8<TY, false>(static_cast<const TY*>(a.y) + row * a.y_stride, col[c], a.dim);
+        if constexpr (!PRE) continue;
         x[c] = load8<TX, false>(static_cast<const TX*>(a.residual) + row * a.residual_stride, col[c], a.dim);
         dh[c] = a.d_h != nullptr ? load8<TY, false>(static_cast<const TY*>(a.d_h) + row * a.d_h_stride, col[c], a.dim)
                                  : all8(0.f);
       }
     }
     float v[2];
-    {
+    if constexpr (!PRE) {
+      const float2 minus_m1 = pair(-st.x), r1 = pair(st.y);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[c].p[k] = mul(add(y[c].p[k], minus_m1), r1);
+    } else {
       float2 sa = pair(0.f), san = pair(0.f);
       const float2 minus_m1 = pair(-st.x), r1 = pair(st.y), minus_m2 = pair(-st.z), r2 = pair(st.w), alpha = pair(a.alpha);
 #pragma unroll
@@ -368,10 +379,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       }
       v[0] = sa.x + sa.y;
       v[1] = san.x + san.y;
+      sum(v);
     }
-    sum(v);
     {
-      const float2 minus_a = pair(a.layer ? -v[0] * inv_dim : 0.f), minus_an = pair(-v[1] * inv_dim);
+      const float2 minus_a = pair(PRE && a.layer ? -v[0] * inv_dim : 0.f), minus_an = pair(PRE ? -v[1] * inv_dim : 0.f);
       const float2 r2 = pair(st.w), alpha = pair(a.alpha);
       float2 sc = pair(0.f), scn = pair(0.f);
 #pragma unroll
@@ -388,8 +399,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float2 n1 = y[c].p[k];
-          const float2 t = fma(x[c].p[k], minus_an, add(dh[c].p[k], minus_a));
-          const float2 grad = fma(r2, t, dx.p[k]);
+          float2 grad = dx.p[k];
+          if constexpr (PRE) grad = fma(r2, fma(x[c].p[k], minus_an, add(dh[c].p[k], minus_a)), grad);
           s_one[c].p[k] = add(s_one[c].p[k], grad);
           s_n1[c].p[k] = fma(grad, n1, s_n1[c].p[k]);
           const float2 cw = mul(grad, A.p[k]);
@@ -480,8 +491,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       __syncthreads();
     }
   }
-  if (a.d_pre_weight != nullptr) leave(0, [&](int c) { return s_wpre[c]; });
-  if (a.d_pre_bias != nullptr) leave(1, [&](int c) { return s_bpre[c]; });
+  if (PRE && a.d_pre_weight != nullptr) leave(0, [&](int c) { return s_wpre[c]; });
+  if (PRE && a.d_pre_bias != nullptr) leave(1, [&](int c) { return s_bpre[c]; });
   if (a.d_gate != nullptr && !per_image) leave(4, [&](int c) { return gate_gradient(c); });
   if (a.d_post_weight != nullptr) leave(2, [&](int c) { return over_gates(s_n1, c); });
   if (a.d_post_bias != nullptr) leave(3, [&](int c) { return over_gates(s_one, c); });
@@ -574,9 +585,9 @@ RingPlan plan_ring(int dim, int row_bytes) {
   return {0, 0};
 }
 
-template <typename TY, typename TX, int C, bool RING, bool MULTI, int WARPS>
+template <typename TY, typename TX, bool PRE, int C, bool RING, bool MULTI, int WARPS>
 cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
-  const auto kernel = block_norm_backward_kernel<TY, TX, C, RING, MULTI, WARPS>;
+  const auto kernel = block_norm_backward_kernel<TY, TX, PRE, C, RING, MULTI, WARPS>;
   const int w = warps_per_row(a.dim), vector = vector_bytes(a.dim);
   int groups = ring.groups;
   if (!RING) {
@@ -612,25 +623,25 @@ cudaError_t launch_instance(const NormBackward& a, RingPlan ring, int num_sms, c
                           groups, gate_cols);
 }
 
-template <typename TY, typename TX, bool RING>
+template <typename TY, typename TX, bool PRE, bool RING>
 cudaError_t launch_types(const NormBackward& a, RingPlan ring, int num_sms, cudaStream_t stream) {
   const bool multi = warps_per_row(a.dim) > 1;
   switch (chunks_per_warp(a.dim)) {
-    case 1: return launch_instance<TY, TX, 1, RING, false, 16>(a, ring, num_sms, stream);
-    case 2: return multi ? launch_instance<TY, TX, 2, RING, true, 12>(a, ring, num_sms, stream)
-                         : launch_instance<TY, TX, 2, RING, false, 12>(a, ring, num_sms, stream);
-    case 3: return multi ? launch_instance<TY, TX, 3, RING, true, 8>(a, ring, num_sms, stream)
-                         : launch_instance<TY, TX, 3, RING, false, 8>(a, ring, num_sms, stream);
-    default: return block_warps(a.dim) == 8 ? launch_instance<TY, TX, 4, RING, true, 8>(a, ring, num_sms, stream)
-                                            : launch_instance<TY, TX, 4, RING, true, 16>(a, ring, num_sms, stream);
+    case 1: return launch_instance<TY, TX, PRE, 1, RING, false, 16>(a, ring, num_sms, stream);
+    case 2: return multi ? launch_instance<TY, TX, PRE, 2, RING, true, 12>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, PRE, 2, RING, false, 12>(a, ring, num_sms, stream);
+    case 3: return multi ? launch_instance<TY, TX, PRE, 3, RING, true, 8>(a, ring, num_sms, stream)
+                         : launch_instance<TY, TX, PRE, 3, RING, false, 8>(a, ring, num_sms, stream);
+    default: return block_warps(a.dim) == 8 ? launch_instance<TY, TX, PRE, 4, RING, true, 8>(a, ring, num_sms, stream)
+                                            : launch_instance<TY, TX, PRE, 4, RING, true, 16>(a, ring, num_sms, stream);
   }
 }
 
-template <typename TY, typename TX>
+template <typename TY, typename TX, bool PRE>
 cudaError_t launch_vec(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream) {
   const RingPlan ring = vec ? plan_ring(a.dim, Slot<TY, TX>::bytes(a.dim)) : RingPlan{0, 0};
-  return ring.groups > 0 ? launch_types<TY, TX, true>(a, ring, num_sms, stream)
-                         : launch_types<TY, TX, false>(a, ring, num_sms, stream);
+  return ring.groups > 0 ? launch_types<TY, TX, PRE, true>(a, ring, num_sms, stream)
+                         : launch_types<TY, TX, PRE, false>(a, ring, num_sms, stream);
 }
 
 }  // namespace

@@ -4,7 +4,7 @@
 namespace mpm {
 
 cudaError_t launch_block_norm_backward_bf16(const NormBackward& a, bool vec, int num_sms, cudaStream_t stream) {
-  return launch_vec<__nv_bfloat16, __nv_bfloat16>(a, vec, num_sms, stream);
+  return launch_vec<__nv_bfloat16, __nv_bfloat16, true>(a, vec, num_sms, stream);
 }
 
 size_t block_norm_workspace_floats(int dim) {
@@ -13,10 +13,17 @@ size_t block_norm_workspace_floats(int dim) {
 
 cudaError_t launch_block_norm_backward(const NormBackward& a, NormTypes types, bool vec, int num_sms,
                                        cudaStream_t stream) {
+  const bool pre = a.pre_weight != nullptr;
   switch (types) {
-    case NormTypes::kF32: return launch_block_norm_backward_f32(a, vec, num_sms, stream);
-    case NormTypes::kBf16: return launch_block_norm_backward_bf16(a, vec, num_sms, stream);
-    case NormTypes::kBf16StreamF32: return launch_block_norm_backward_mixed(a, vec, num_sms, stream);
+    case NormTypes::kF32:
+      return pre ? launch_block_norm_backward_f32(a, vec, num_sms, stream)
+                 : launch_block_norm_backward_f32_no_pre(a, vec, num_sms, stream);
+    case NormTypes::kBf16:
+      return pre ? launch_block_norm_backward_bf16(a, vec, num_sms, stream)
+                 : launch_block_norm_backward_bf16_no_pre(a, vec, num_sms, stream);
+    case NormTypes::kBf16StreamF32:
+      return pre ? launch_block_norm_backward_mixed(a, vec, num_sms, stream)
+                 : launch_block_norm_backward_mixed_no_pre(a, vec, num_sms, stream);
   }
   return cudaErrorInvalidValue;
 }
