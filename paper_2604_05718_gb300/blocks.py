@@ -7,6 +7,10 @@ gradients.  ``quantize_mxfp4`` and ``matmul_mxfp4`` are a linear layer on
 4-bit operands.  As in ``mpm``, arguments are checked and marshalled only, and
 every step runs in the library's kernels on the current torch stream; the
 marshalling is the extension module ``_blocks`` (csrc/blocks_binding.cpp).
+
+Nothing is recorded for autograd: ``block_norm_backward`` is called by hand (or
+from a ``torch.autograd.Function``), and a tensor that requires grad is refused
+while grad mode is on.
 """
 
 from __future__ import annotations

@@ -10,6 +10,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -61,6 +62,9 @@ const at::Tensor* tensor(PyObject* o, const char* name, bool optional = false) {
   if (!THPVariable_Check(o)) value_error(name, "must be a CUDA tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) value_error(name, "must be a CUDA tensor");
+  // Outputs belong to no graph: a gradient would be lost without a word.
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    value_error(name, "must not require grad outside torch.no_grad(): the block operators record nothing for autograd");
   return &t;
 }
 
