@@ -118,6 +118,13 @@ at::Tensor new_like(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType t
   return at::Tensor(at::detail::empty_cuda(shape, type, t.device(), at::MemoryFormat::Contiguous));
 }
 
+// A tensor of the caller's has been written: autograd's check of saved tensors goes by the version.
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();  // (those have none)
+}
+
 double number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Raised{};
@@ -250,6 +257,8 @@ PyObject* block_norm(PyObject* const* p) {
                          a.eps, a.scale, a.post_weight, a.post_bias, a.gate, a.per_image, a.pre_weight, a.pre_bias, pout, ph,
                          stats.defined() ? static_cast<float*>(stats.data_ptr()) : nullptr, status_word(p[14], a.device),
                          on.stream));
+  written(p[11]);
+  written(p[12]);
   return tuple_of({out.defined() ? wrapped(out) : again(p[11]), h.defined() ? wrapped(h) : pre ? again(p[12]) : nullptr,
                    wrapped(stats)});
 }
@@ -338,6 +347,8 @@ PyObject* quantize(PyObject* const* p) {
   check("mpm_mxfp4_quantize", entry.mxfp4_quantize(x->data_ptr(), x->stride(0), rows,
                                                    static_cast<int32_t>(dim > INT32_MAX ? INT32_MAX : dim),
                                                    dtype_of(*x, "tokens"), pc, ps, on.stream));
+  written(p[1]);
+  written(p[2]);
   return tuple_of({codes.defined() ? wrapped(codes) : again(p[1]), scales.defined() ? wrapped(scales) : again(p[2])});
 }
 
@@ -357,6 +368,7 @@ PyObject* dequantize(PyObject* const* p) {
   const at::Tensor out = output(p[4], p[3], *x.codes, x.rows, x.dim);
   check("mpm_mxfp4_dequantize", entry.mxfp4_dequantize(x.pcodes, x.pscales, x.rows, static_cast<int32_t>(x.dim),
                                                        dtype_of(out, "out"), out.data_ptr(), out.stride(0), on.stream));
+  written(p[4]);
   return p[4] == Py_None ? THPVariable_Wrap(out) : again(p[4]);
 }
 
@@ -373,6 +385,7 @@ PyObject* matmul(PyObject* const* p) {
         entry.mxfp4_matmul(a.pcodes, a.pscales, a.rows, b.pcodes, b.pscales,
                            static_cast<int32_t>(b.rows > INT32_MAX ? INT32_MAX : b.rows), static_cast<int32_t>(a.dim), bias,
                            dtype_of(out, "out"), out.data_ptr(), out.stride(0), status_word(p[9], a.device), on.stream));
+  written(p[8]);
   return p[8] == Py_None ? THPVariable_Wrap(out) : again(p[8]);
 }
 

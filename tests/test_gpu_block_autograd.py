@@ -100,3 +100,45 @@ def test_within_a_function_of_autograd(mpm):
     _, _, stats = mpm.block_norm(with_stats=True, **t, **rest)
     want = mpm.block_norm_backward(torch.ones_like(xo), torch.ones_like(h), stats=stats, **t, **rest)
     assert torch.equal(got[0], want.d_y) and torch.equal(got[1], want.d_residual)
+
+
+def test_writes_in_place_are_new_versions(mpm):
+    t, rest = norm_args()
+    xo, h = torch.zeros(6, 32, device=DEV), torch.zeros(6, 32, device=DEV)
+    mpm.block_norm(**t, **rest, residual_out=xo, h=h)
+    assert (xo._version, h._version) == (1, 1)
+    assert all(v._version == 0 for v in t.values())
+    x = t["residual"].clone()
+    before = x._version
+    mpm.block_norm(**{**t, "residual": x}, **rest, residual_out=x)
+    assert x._version == before + 1
+    q = mpm.quantize_mxfp4(t["y"])
+    into = mpm.MXFP4(torch.zeros_like(q.codes), torch.zeros_like(q.scales), q.dim)
+    mpm.quantize_mxfp4(t["y"], out=into)
+    assert (into.codes._version, into.scales._version) == (1, 1)
+    wide = torch.zeros(6, 64, device=DEV)
+    mpm.dequantize_mxfp4(q, out=wide[:, 8:40])
+    mpm.matmul_mxfp4(q, q, out=wide[:, 8:14])
+    assert wide._version == 2                     # a view and its base share one
+    with pytest.raises(mpm.MPMError):             # nothing is written by a call that fails
+        mpm.block_norm(**t, **rest, h=h, eps=float("nan"))
+    assert h._version == 1
+
+
+def test_a_saved_tensor_that_is_written_is_noticed(mpm):
+    t, rest = norm_args()
+    h = torch.ones(6, 32, device=DEV)
+    leaf = torch.ones(6, 32, device=DEV, requires_grad=True)
+    product = leaf * h                            # keeps h for the gradient
+    mpm.block_norm(**t, **rest, h=h)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.sum().backward()
+
+
+def test_outputs_of_inference_mode(mpm):
+    t, rest = norm_args()
+    with torch.inference_mode():
+        h = torch.zeros(6, 32, device=DEV)
+        mpm.block_norm(**t, **rest, h=h)
+        mpm.block_norm(**t, **rest, h=h)
+    assert torch.equal(h, mpm.block_norm(**t, **rest)[1])
