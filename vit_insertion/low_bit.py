@@ -31,6 +31,7 @@ import torch.nn.functional as F  # noqa: E402
 from vit_insertion.model import VIT_CONFIGS, ViT, synthetic_images, varlen_attention  # noqa: E402
 
 LINEARS = ("qkv", "proj", "fc1", "fc2")
+EPS = 1e-5  # torch's layer norm, which the full model calls without one
 
 
 class LowBitViT(ViT):
@@ -56,7 +57,7 @@ class LowBitViT(ViT):
 
     def norm(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> torch.Tensor:
         """Layer norm of a stream that no branch is added to: at the start and behind a merge."""
-        return F.layer_norm(x, (self.cfg.dim,), weight.to(x.dtype), bias.to(x.dtype), eps=1e-6)
+        return F.layer_norm(x, (self.cfg.dim,), weight.to(x.dtype), bias.to(x.dtype), eps=EPS)
 
     def branches(self, x: torch.Tensor, h: torch.Tensor, p: dict, cu: torch.Tensor, max_len: int):
         """One block from the stream x and its norm h: (stream after attention, output of the MLP branch)."""
@@ -65,7 +66,7 @@ class LowBitViT(ViT):
         qkv = self.linear(h, p, "qkv").view(s, 3, cfg.heads, cfg.dim // cfg.heads)
         a = varlen_attention(*(qkv[:, i].contiguous() for i in range(3)), cu, max_len).reshape(s, cfg.dim)
         x, h, _ = self.ops.block_norm(self.linear(a, p, "proj"), x, norm="layer", gate=p["gate1"], pre_weight=p["ln2_w"],
-                                      pre_bias=p["ln2_b"])
+                                      pre_bias=p["ln2_b"], eps=EPS)
         return x, self.linear(F.gelu(self.linear(h, p, "fc1")), p, "fc2")
 
     def run_blocks(self, images: torch.Tensor, mpm=None, workspace=None, insert_at=None):
@@ -98,7 +99,7 @@ class LowBitViT(ViT):
             after = None if i + 1 in points else self.blocks[i + 1]
             x, h, _ = self.ops.block_norm(y, x, norm="layer", gate=p["gate2"],
                                           pre_weight=None if after is None else after["ln1_w"],
-                                          pre_bias=None if after is None else after["ln1_b"])
+                                          pre_bias=None if after is None else after["ln1_b"], eps=EPS)
         raise ValueError("a model needs blocks")
 
     def to_grid(self, rows: torch.Tensor, off: torch.Tensor, maps: list, mpm) -> torch.Tensor:
@@ -119,7 +120,7 @@ class LowBitViT(ViT):
             raise ValueError("LowBitViT keeps no trace of its insertions")
         x, y, maps, off = self.run_blocks(images, mpm, workspace, insert_at)
         _, h, _ = self.ops.block_norm(y, x, norm="layer", gate=self.blocks[-1]["gate2"], pre_weight=self.head_ln_w,
-                                      pre_bias=self.head_ln_b)
+                                      pre_bias=self.head_ln_b, eps=EPS)
         return F.linear(self.to_grid(h, off, maps, mpm), self.head_w, self.head_b)
 
     def tune_last_gate(self, images: torch.Tensor, target: torch.Tensor, mpm=None, steps: int = 20, rate: float = 0.5,
@@ -133,7 +134,7 @@ class LowBitViT(ViT):
         """
         x, y, _, _ = self.run_blocks(images, mpm, insert_at=insert_at)
         gate = self.blocks[-1]["gate2"]
-        args = dict(norm="layer", gate=gate, pre_weight=self.head_ln_w, pre_bias=self.head_ln_b)
+        args = dict(norm="layer", gate=gate, pre_weight=self.head_ln_w, pre_bias=self.head_ln_b, eps=EPS)
         workspace = self.ops.block_norm_workspace(self.cfg.dim, self.device)
         losses = []
         for _ in range(steps):
