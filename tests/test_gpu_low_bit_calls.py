@@ -55,3 +55,21 @@ def test_norms_have_the_full_models_eps(mpm):  # noqa: F811
         _, h, _ = mpm.block_norm(torch.zeros_like(x), x, norm="layer", pre_weight=w, pre_bias=b, eps=kw["eps"])
         # One bf16 rounding apart at most: at 1e-3 an eps ten times smaller makes h three times as large.
         torch.testing.assert_close(h, want, rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+def test_device_errors_reach_the_caller(mpm):  # noqa: F811
+    full, low, calls = run_all(mpm)
+    reporting = [(name, kw) for name, kw in calls if name in ("block_norm", "block_norm_backward", "matmul_mxfp4")]
+    assert {name for name, _ in reporting} == {"block_norm", "block_norm_backward", "matmul_mxfp4"}
+    for name, kw in reporting:
+        assert kw.get("device_status") is low.status, name
+    low.check_status()
+    low.status[0], low.status[1] = 7, 31          # what a kernel writes when a wait ran out
+    with pytest.raises(mpm.MPMError) as e:
+        low.check_status()
+    assert e.value.code == 7
+    low.check_status()                            # once told, cleared
+    low.status[0] = 7
+    _, _, _, images = models()
+    with torch.inference_mode(), pytest.raises(mpm.MPMError):
+        low.tune_last_gate(images, torch.zeros(3 * (full.cfg.tokens + full.cfg.special), full.cfg.dim, device=DEV), steps=1)

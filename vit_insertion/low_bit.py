@@ -51,9 +51,19 @@ class LowBitViT(ViT):
             p["gate1"] = torch.ones(cfg.dim, device=self.device)
             p["gate2"] = torch.ones(cfg.dim, device=self.device)
         self.head_ln_w, self.head_ln_b = self.head_ln_w.float(), self.head_ln_b.float()
+        # Where the kernels report errors of their own; check_status() reads it.
+        self.status = torch.zeros(2, dtype=torch.int32, device=self.device)
+
+    def check_status(self) -> None:
+        """Waits for the device, and raises what a kernel has reported since the last check."""
+        code = int(self.status[0])
+        if code != 0:
+            self.status.zero_()
+            raise self.ops.MPMError("a kernel of the 4-bit encoder", code)
 
     def linear(self, x: torch.Tensor, p: dict, name: str) -> torch.Tensor:
-        return self.ops.matmul_mxfp4(self.ops.quantize_mxfp4(x), p[name], bias=p[name + "_b"], out_dtype=x.dtype)
+        return self.ops.matmul_mxfp4(self.ops.quantize_mxfp4(x), p[name], bias=p[name + "_b"], out_dtype=x.dtype,
+                                     device_status=self.status)
 
     def norm(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> torch.Tensor:
         """Layer norm of a stream that no branch is added to: at the start and behind a merge."""
@@ -66,7 +76,7 @@ class LowBitViT(ViT):
         qkv = self.linear(h, p, "qkv").view(s, 3, cfg.heads, cfg.dim // cfg.heads)
         a = varlen_attention(*(qkv[:, i].contiguous() for i in range(3)), cu, max_len).reshape(s, cfg.dim)
         x, h, _ = self.ops.block_norm(self.linear(a, p, "proj"), x, norm="layer", gate=p["gate1"], pre_weight=p["ln2_w"],
-                                      pre_bias=p["ln2_b"], eps=EPS)
+                                      pre_bias=p["ln2_b"], eps=EPS, device_status=self.status)
         return x, self.linear(F.gelu(self.linear(h, p, "fc1")), p, "fc2")
 
     def run_blocks(self, images: torch.Tensor, mpm=None, workspace=None, insert_at=None):
@@ -99,7 +109,8 @@ class LowBitViT(ViT):
             after = None if i + 1 in points else self.blocks[i + 1]
             x, h, _ = self.ops.block_norm(y, x, norm="layer", gate=p["gate2"],
                                           pre_weight=None if after is None else after["ln1_w"],
-                                          pre_bias=None if after is None else after["ln1_b"], eps=EPS)
+                                          pre_bias=None if after is None else after["ln1_b"], eps=EPS,
+                                          device_status=self.status)
         raise ValueError("a model needs blocks")
 
     def to_grid(self, rows: torch.Tensor, off: torch.Tensor, maps: list, mpm) -> torch.Tensor:
@@ -115,12 +126,12 @@ class LowBitViT(ViT):
         return mpm.compose_gather(patches, off, first, off0, maps[-1][0], maps[-1][1])
 
     def forward(self, images: torch.Tensor, mpm=None, workspace=None, insert_at=None, trace=None):
-        """Dense logits [B*N, classes] on the patch grid."""
+        """Dense logits [B*N, classes] on the patch grid.  check_status() says whether a kernel failed on the way."""
         if trace is not None:
             raise ValueError("LowBitViT keeps no trace of its insertions")
         x, y, maps, off = self.run_blocks(images, mpm, workspace, insert_at)
         _, h, _ = self.ops.block_norm(y, x, norm="layer", gate=self.blocks[-1]["gate2"], pre_weight=self.head_ln_w,
-                                      pre_bias=self.head_ln_b, eps=EPS)
+                                      pre_bias=self.head_ln_b, eps=EPS, device_status=self.status)
         return F.linear(self.to_grid(h, off, maps, mpm), self.head_w, self.head_b)
 
     def tune_last_gate(self, images: torch.Tensor, target: torch.Tensor, mpm=None, steps: int = 20, rate: float = 0.5,
@@ -134,7 +145,8 @@ class LowBitViT(ViT):
         """
         x, y, _, _ = self.run_blocks(images, mpm, insert_at=insert_at)
         gate = self.blocks[-1]["gate2"]
-        args = dict(norm="layer", gate=gate, pre_weight=self.head_ln_w, pre_bias=self.head_ln_b, eps=EPS)
+        args = dict(norm="layer", gate=gate, pre_weight=self.head_ln_w, pre_bias=self.head_ln_b, eps=EPS,
+                    device_status=self.status)
         workspace = self.ops.block_norm_workspace(self.cfg.dim, self.device)
         losses = []
         for _ in range(steps):
@@ -145,6 +157,7 @@ class LowBitViT(ViT):
             grads = self.ops.block_norm_backward(None, (2.0 / h.shape[0] * off).to(h.dtype), y, x, stats,
                                                  workspace=workspace, **args)
             gate -= rate * grads.d_gate
+        self.check_status()
         return [float(v) for v in losses]
 
 
@@ -175,6 +188,7 @@ def main() -> int:
               "low_bit": timed(lambda: low.forward(images), args.steps, args.warmup),
               "low_bit_merged": timed(lambda: low.forward(images, mpm=mpm, workspace=ws), args.steps, args.warmup)}
         got = low.forward(images, mpm=mpm, workspace=ws)
+        low.check_status()
         likeness = F.cosine_similarity(got.float(), want.float(), dim=1).mean().item()
     print(json.dumps({"metric": "ViT encoder + dense head, 4-bit linear layers and fused norms", "model": cfg.name,
                       "batch": args.batch, "ms": ms, "fps": {k: args.batch / v * 1e3 for k, v in ms.items()},
