@@ -28,8 +28,8 @@ _ENTRIES = ("mpm_block_norm", "mpm_block_norm_workspace_size", "mpm_block_norm_b
 _module = None
 
 
-def _ext():
-    """The extension module, bound to the loaded library's entry points."""
+def load_binding():
+    """The extension module, bound to the loaded library's entry points; raises where it has not been built."""
     global _module
     if _module is None:
         lib = library()
@@ -93,8 +93,8 @@ def block_norm(y: torch.Tensor, residual: torch.Tensor, *, norm: str = "layer", 
     Returns (residual_out, h, stats): h is None without pre_weight, stats
     (float32 [rows, 4], for ``block_norm_backward``) None unless with_stats.
     """
-    return (_module or _ext()).block_norm(y, residual, norm, pre_weight, pre_bias, post_weight, post_bias, gate, offsets,
-                                          residual_scale, eps, residual_out, h, with_stats, device_status)
+    return (_module or load_binding()).block_norm(y, residual, norm, pre_weight, pre_bias, post_weight, post_bias, gate,
+                                                  offsets, residual_scale, eps, residual_out, h, with_stats, device_status)
 
 
 def block_norm_workspace(dim: int, device) -> torch.Tensor:
@@ -118,7 +118,7 @@ def block_norm_backward(d_residual_out: torch.Tensor | None, d_h: torch.Tensor |
     Token gradients have the tokens' types, parameter gradients are fp32 and
     summed in a fixed order.  Rows from offsets[B] on are left alone.
     """
-    return BlockNormGrads(*(_module or _ext()).block_norm_backward(
+    return BlockNormGrads(*(_module or load_binding()).block_norm_backward(
         y, residual, norm, pre_weight, pre_bias, post_weight, post_bias, gate, offsets, residual_scale, eps, d_residual_out,
         d_h, stats, workspace, device_status))
 
@@ -129,18 +129,18 @@ def quantize_mxfp4(tokens: torch.Tensor, out: MXFP4 | None = None) -> MXFP4:
     A block with a NaN or an infinity becomes NaN as a whole.
     """
     if out is None:
-        codes, scales = (_module or _ext()).quantize(tokens, None, None)
+        codes, scales = (_module or load_binding()).quantize(tokens, None, None)
         return MXFP4(codes, scales, tokens.shape[1])
     if out.dim != tokens.shape[-1]:
         raise ValueError("out must have the tokens' shape")
-    (_module or _ext()).quantize(tokens, out.codes, out.scales)
+    (_module or load_binding()).quantize(tokens, out.codes, out.scales)
     return out
 
 
 def dequantize_mxfp4(x: MXFP4, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that x stands for, [rows, D] in bf16 or fp32."""
     codes, scales, dim = x
-    return (_module or _ext()).dequantize(codes, scales, dim, dtype, out)
+    return (_module or load_binding()).dequantize(codes, scales, dim, dtype, out)
 
 
 def matmul_mxfp4(a: MXFP4, b: MXFP4, bias: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
@@ -151,4 +151,4 @@ def matmul_mxfp4(a: MXFP4, b: MXFP4, bias: torch.Tensor | None = None, out_dtype
     """
     ac, asc, k = a
     bc, bs, kb = b
-    return (_module or _ext()).matmul(ac, asc, k, bc, bs, kb, bias, out_dtype, out, device_status)
+    return (_module or load_binding()).matmul(ac, asc, k, bc, bs, kb, bias, out_dtype, out, device_status)
