@@ -77,10 +77,29 @@ def _binding_command(out: str) -> list:
                                        "-lc10_cuda", f"-Wl,-rpath,{lib}"]
 
 
+def _binding_key() -> str:
+    """What the binding is built for, next to its sources: this torch, whose ABI it has, and the command."""
+    import torch
+
+    return " ".join([torch.__version__, str(torch.version.git_version)] + _binding_command(""))
+
+
+def _binding_stale() -> bool:
+    if _stale(BINDING, [BINDING_SRC, os.path.join(ROOT, "include", "mpm.h")]):
+        return True
+    try:
+        with open(os.path.join(BUILD, "blocks_binding.txt")) as f:
+            return f.read() != _binding_key()
+    except Exception:  # never noted, or no torch here
+        return True
+
+
 def _build_binding() -> None:
     tmp = BINDING + ".tmp"
     try:
         _run(_binding_command(tmp))
+        with open(os.path.join(BUILD, "blocks_binding.txt"), "w") as f:
+            f.write(_binding_key())
     except Exception as e:  # no torch, no compiler, or one that fails: the merge needs none of them
         if os.path.exists(BINDING):
             os.remove(BINDING)
@@ -105,7 +124,7 @@ def build(force: bool = False, extra_flags: list | None = None, trace: bool = Fa
         if force or _stale(obj, [src] + headers):
             jobs.append([nvcc(), "-c", src, "-o", obj] + flags)
     compiled = bool(jobs)
-    bind = not trace and (force or _stale(BINDING, [BINDING_SRC, os.path.join(ROOT, "include", "mpm.h")]))
+    bind = not trace and (force or _binding_stale())
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
         binding = ex.submit(_build_binding) if bind else None
         list(ex.map(_run, jobs))

@@ -70,3 +70,34 @@ def test_block_operators_say_that_the_binding_is_missing(monkeypatch):
     monkeypatch.setattr(blocks.importlib, "import_module", missing)
     with pytest.raises(RuntimeError, match="binding of the block operators"):
         blocks.matmul_mxfp4(blocks.MXFP4(None, None, 1), blocks.MXFP4(None, None, 1))
+
+
+def test_the_binding_follows_the_torch_it_is_built_for(tree, monkeypatch):
+    """Its ABI is that torch's: another one, or another command, builds it again; the same does not."""
+    made = []
+
+    def command(out):
+        made.append(out)
+        return ["sh", "-c", f"echo {len(made)} > '{out}'"]
+
+    monkeypatch.setattr(build, "_binding_command", command)
+    version = ["2.0"]
+    monkeypatch.setattr(build, "_binding_key", lambda: f"torch {version[0]}", raising=False)
+    binding = tree / "_blocks.so"
+    build.build()
+    assert binding.read_text() == "1\n"
+    build.build()
+    assert binding.read_text() == "1\n"
+    version[0] = "2.1"
+    build.build()
+    assert binding.read_text() == "2\n"
+    build.build()
+    assert binding.read_text() == "2\n"
+
+
+def test_the_binding_key_names_torch(monkeypatch):
+    import torch
+
+    key = build._binding_key()
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    assert build._binding_key() != key
