@@ -93,3 +93,16 @@ def test_gradients_against_differences_in_64_bits(mpm, norm, dim, types):
         noise = 2.0 ** -50 * ((dxo.double() * exact["residual"]).abs().sum() + dh.double().abs().sum() * 4).item() * 2 ** 10
         assert abs((got["d_" + name].double() * way).sum().item() - best) <= \
             (bound * way.abs()).sum().item() + abs(best - once[1]) + noise, name
+
+
+@pytest.mark.parametrize("biases", [(), ("post_bias",), ("pre_bias",), ("post_bias", "pre_bias")])
+@pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("dim", [100, 768, 1024])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_every_set_of_biases(mpm, norm, dim, types, biases):
+    """Either norm with either bias: layer norm has them as a rule, root mean square has not."""
+    counts, alpha = [9, 0, 31], 0.5
+    t, off, rows_of, (dxo, dh) = inputs(counts, dim, types, seed=dim, device=DEV)
+    t = {k: v for k, v in t.items() if not k.endswith("bias") or k in biases}
+    want = norm_bounds.reference(t, rows_of, norm, EPS, alpha, dxo, dh, len(counts))
+    norm_bounds.check(run(mpm, t, off, norm, alpha, dxo, dh), want)
