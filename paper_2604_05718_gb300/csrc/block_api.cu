@@ -56,7 +56,7 @@ bool any_overlap(std::initializer_list<Extent> outs, std::initializer_list<Exten
 bool stride_ok(int64_t stride, int64_t rows, int64_t dim) { return rows <= 1 || stride >= dim; }
 bool vector_rows(const void* p, int64_t stride, int size) { return aligned(p, 16) && stride * size % 16 == 0; }
 
-// The current device's SMs, or an error: the kernels are built for compute capability 10.3 alone.
+// The current device's SMs.  (The kernels are built for compute capability 10.3: elsewhere launches fail.)
 mpm_status device_sms(int* sms) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MPM_ERR_CUDA;

@@ -23,13 +23,17 @@
 //
 // The sums take most registers, so few warps are there to hide latencies.
 // Rows that are 16-byte aligned therefore come through a ring in shared
-// memory that bulk copies fill rows ahead; and a thread has up to 24 columns
-// of a row, whose chains overlap, without barriers in between.  54208 x 768
-// bf16, layer norm on both sides and a gate per image (500 MB): 192 us from
-// loads in place, 164 with rows spread over three warps (two barriers a row),
-// 111 with a warp a row, 9 of them the join: 4.5 TB/s.  Two warps a scheduler
-// issue too little for bf16 (0.36 instructions a cycle each scheduler); with an
-// fp32 stream, twice the bytes for the same work, it is at 5.4 TB/s.
+// memory that bulk copies fill rows ahead; and a thread has 8 to 24 columns of
+// a row (32 of one with more than 6144 features), whose chains overlap, without
+// barriers in between.  54208 x 768 bf16, layer norm on both sides and a gate
+// per image (500 MB): 192 us from loads in place, 164 with rows spread over
+// three warps (two barriers a row), 107 with a warp a row, 8 of them the join.
+// Opening and closing the images' gates is 9 of them: a gate per channel takes
+// 98, none 97.  A copy of as many bytes takes 77, and with half of the reads
+// from L2 (dx' and dh the tensors of x and y) it is 83: what is left is neither
+// memory's alone nor the instructions', of which two warps a scheduler issue
+// 0.35 a cycle.  With an fp32 stream, 1.5 times the bytes for the same work, the
+// pass runs at 5.3 TB/s.
 //
 // Two files per pair of token types include this one, with and without a norm
 // before the next block: the kernels of all take minutes to compile.
@@ -52,11 +56,12 @@ constexpr int kSums = 5;         // column sums: w_pre, b_pre, w_post, b_post, g
 constexpr int kMaxRing = 4;      // rows in a group's ring
 constexpr uint64_t kWaitNs = 2000000000ull;
 
-// Chunks of 256 columns that a warp holds (8 C columns a thread): the whole row
-// if it can, else the count that leaves no warp of a group half empty.  Their
-// sums and row take about 30 + 56 C registers, which sets the block's warps: 8
-// of 255 registers, 12 of 168, 16 of 128 (rows of more than 8192 features need
-// 16 and spill).
+// Chunks of 256 columns that a warp holds (8 C columns a thread): a row's only
+// one; three where they divide its chunks, or else two, the last warp of a row of
+// an odd number half empty; four in rows of more than 24, which have to fit
+// the block's warps.  Their sums and row take about 30 + 56 C registers, which
+// sets the warps: 8 of 255 registers for three and four, 12 of 168, 16 of 128
+// (rows of more than 8192 features need 16 for four chunks each, and spill).
 __host__ __device__ constexpr int chunks_per_warp(int dim) {
   const int chunks = (dim + kNormWarpCols - 1) / kNormWarpCols;
   return chunks == 1 ? 1 : chunks > 24 ? 4 : chunks % 3 == 0 ? 3 : 2;
@@ -477,7 +482,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     for (int c = 0; c < C; ++c) mine.set(c, value(c));
     which_kept |= static_cast<uint32_t>(which) << (4 * kept);
     // One at a time for groups of several warps: with more, the compiler's code
-    // for the rows is slower (30000 x 1024 bf16: 76 us, 95 with two or five).
+    // for the rows is slower (30000 x 1024 bf16, dx' and dh the tensors of x and y:
+    // 76 us, 95 with two or five; 81 with four tensors).
     if (++kept == (MULTI ? 1 : room)) join_kept();
   };
   // Over the gates of a run: what its last image left, or the one gate's sums.

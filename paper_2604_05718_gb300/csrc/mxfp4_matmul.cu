@@ -15,18 +15,20 @@
 // the time that their output takes HBM), with many shared memory.  Hence
 //  - tiles of 192 columns with two accumulators: a tile's output is written
 //    while the next one is computed;
-//  - A and B in rings of their own: where a row of A fits (K <= 1280), the A
-//    panel of a run of tiles stays in shared memory, and with it its scales in
-//    tensor memory.  Loading it again for every tile took as long as half of
-//    the output's writes (54208 x 768 x 2304 to bf16: 61 us, resident 57, which
-//    is 4.4 TB/s of writes; filling as much memory with zeros reaches 3.9);
+//  - A and B in rings of their own: where a row of A fits (K <= 1280; 1024 with
+//    tiles of 256 columns), the A panel of a run of tiles stays in shared memory,
+//    and with it its scales in tensor memory.  Loading it again for every tile
+//    took as long as half of the output's writes (54208 x 768 x 2304 to bf16: 61
+//    us, resident 57, which is 4.4 TB/s of writes; filling as much memory with
+//    zeros reaches 3.9);
 //  - tiles of 256 columns for many features.  A step's operands are written to
 //    shared memory once and read once: 60 KB a CTA for 192 columns, 467 cycles
 //    at 128 bytes a cycle against 384 of the products; 68 KB and 530 cycles
 //    against 512 for 256 columns.  Tensor memory has room for one accumulator
-//    then, and a tile waits until the last one's has been read (16384 x 4096 x
-//    1024: 34 us with 192 columns, 30 with 256; 8192 x 8192 x 8192: 180 and
-//    172).  Tiles of 128 took as long as 192 for two thirds of the work.
+//    then, and a tile waits until the last one's has been read: 16384 x 4096 x
+//    1024 takes 34 us with 192 columns and 30 with 256, where that traffic and
+//    the rounds of tiles alone would allow 22; 8192 x 8192 x 8192 180 and 172.
+//    Tiles of 128 took as long as 192 for two thirds of the work.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
