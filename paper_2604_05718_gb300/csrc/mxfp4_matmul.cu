@@ -36,10 +36,15 @@
 
 #include "common.cuh"
 #include "mxfp4.cuh"
+#include "pair_ring.cuh"
 #include "ptx.cuh"
 
 namespace mpm {
 namespace {
+
+using pair::cluster_sync;
+using pair::load_pair;
+using pair::map_to_rank;
 
 constexpr int kHalf = 128;             // rows of A per CTA
 constexpr int kTileM = 2 * kHalf;
@@ -88,7 +93,7 @@ struct Control {
   uint64_t acc_empty[2];                          // leader: both CTAs read the accumulator
   uint64_t drain;
   uint32_t tmem_base;
-  int abort_flag;
+  pair::State pair;  // its rings: A, B
 };
 
 template <int N>
@@ -125,29 +130,8 @@ __device__ __forceinline__ Tiles tiles_of(const MxMatmulArgs& a, int tile_n) {
   return {begin, begin + per + (c < extra ? 1 : 0), n};
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t map_to_rank(uint32_t saddr, uint32_t rank) {
-  uint32_t out;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(out) : "r"(saddr), "r"(rank));
-  return out;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void remote_arrive(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-// Load into this CTA, counted on a barrier of either CTA of the pair.
-__device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
-      "[%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
-      : "memory");
 }
 // Scales are stored as 8-row x 16-byte matrices 128 bytes apart, unswizzled.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
@@ -193,7 +177,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
 }
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
-  ctl->abort_flag = 1;
+  pair::give_up(&ctl->pair);
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
 }
 
@@ -207,7 +191,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
   Control* ctl = reinterpret_cast<Control*>(smem + W::kRings + W::kEpilogueWarps * kBoxBytes);
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank();
+  const uint32_t rank = pair::cluster_rank();
   const bool leader = rank == 0;
 
   if (threadIdx.x == 0) {
@@ -224,7 +208,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
       ptx::mbar_init(&ctl->acc_empty[i], 2 * W::kEpilogueWarps);
     }
     ptx::mbar_init(&ctl->drain, 1);
-    ctl->abort_flag = 0;
+    ctl->pair.failed = ctl->pair.peer_failed = 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tensor_map(&map_a);
     ptx::prefetch_tensor_map(&map_b);
@@ -254,7 +238,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
   const bool resident = steps <= W::kMaxResident;
   auto panel_begins = [&](int64_t t) { return !resident || t == run.begin || run.m_of(t) != run.m_of(t - 1); };
   auto panel_ends = [&](int64_t t) { return !resident || t + 1 == run.end || run.m_of(t + 1) != run.m_of(t); };
-  volatile int* abort_flag = &ctl->abort_flag;
+  volatile int* abort_flag = &ctl->pair.failed;
 
   if (warp == 0) {
     // ---------------- TMA producer (both CTAs) ----------------
@@ -265,8 +249,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
     // columns; 172 with 256).
     Ring<W::kSlotsA> ra;
     Ring<W::kSlotsB> rb;
-    int issued_a = 0, issued_b = 0;
-    uint32_t phase_a = 0, phase_b = 0;  // of the slots' last loads
+    int loads_a = 0, loads_b = 0;
     bool ok = true;
     const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
     const uint32_t full_a0 = __shfl_sync(0xFFFFFFFFu, map_to_rank(ptx::smem_addr(&ctl->full_a[0]), 0), 0);
@@ -291,8 +274,7 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
             load_pair(at + kBytesA, &map_sa, full, 0, m0 / mx::kTileRows * tiles_k + kt);
           }
           __syncwarp();
-          issued_a |= 1 << ra.slot;
-          phase_a = (phase_a & ~(1u << ra.slot)) | (ra.phase << ra.slot);
+          ++loads_a;
           ra.next();
         }
         if (!warp_wait(&ctl->empty_b[rb.slot], rb.phase ^ 1u, abort_flag)) {
@@ -309,16 +291,13 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
             load_pair(at + W::kBytesB + j * kBytesSA, &map_sb, full, 0, (nt + j) * tiles_k + kt);
         }
         __syncwarp();
-        issued_b |= 1 << rb.slot;
-        phase_b = (phase_b & ~(1u << rb.slot)) | (rb.phase << rb.slot);
+        ++loads_b;
         rb.next();
       }
     }
-    if (!ok && leader) {  // no copy may land after the block is gone
-      for (int s = 0; s < W::kSlotsA; ++s)
-        if (issued_a & (1 << s)) ptx::mbar_wait(&ctl->full_a[s], (phase_a >> s) & 1u, nullptr, kWaitNs);
-      for (int s = 0; s < W::kSlotsB; ++s)
-        if (issued_b & (1 << s)) ptx::mbar_wait(&ctl->full_b[s], (phase_b >> s) & 1u, nullptr, kWaitNs);
+    if (lane == 0) {
+      ctl->pair.loads[0] = loads_a;
+      ctl->pair.loads[1] = loads_b;
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -498,7 +477,11 @@ __global__ void __launch_bounds__(Tile<N>::kThreads, 1)
 
   ptx::tc_fence_before_sync();
   __syncthreads();
-  cluster_sync();  // no CTA leaves while its peer may still signal it
+  // No CTA leaves while its peer may still signal it, or a copy of a pair that gave up may still land.
+  pair::leave(&ctl->pair, [&] {
+    pair::drain(ctl->full_a, W::kSlotsA, kSlotA, ctl->pair.loads[0], ctl->pair.peer_loads[0], kWaitNs);
+    pair::drain(ctl->full_b, W::kSlotsB, W::kSlotB, ctl->pair.loads[1], ctl->pair.peer_loads[1], kWaitNs);
+  });
   if (warp == 1) {
     ptx::tc_fence_after_sync();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
