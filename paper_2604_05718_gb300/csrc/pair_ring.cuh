@@ -43,7 +43,7 @@ __device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* map, 
 // By one thread of the leader, once neither CTA issues any more: waits, each
 // time up to limit_ns, for the last loads of a ring, of which the leader issued
 // `mine` and its peer `theirs`; `bytes` is one CTA's half.  False if one did not land.
-__device__ __noinline__ bool drain(uint64_t* full, int slots, uint32_t bytes, int mine, int theirs, uint64_t limit_ns) {
+static __device__ __noinline__ bool drain(uint64_t* full, int slots, uint32_t bytes, int mine, int theirs, uint64_t limit_ns) {
   const int last = mine > theirs ? mine : theirs;
   bool landed = true;
   for (int n = last > slots ? last - slots : 0; n < last; ++n) {

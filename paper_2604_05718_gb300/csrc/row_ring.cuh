@@ -25,7 +25,7 @@ __device__ __forceinline__ void refill(const volatile int* dead, int* asked, Fil
 
 // Waits, each time up to limit_ns, for the copies of the last of the `asked`
 // rows; false if one did not land.
-__device__ __forceinline__ bool drain(uint64_t* full, int slots, int asked, uint64_t limit_ns) {
+static __device__ __noinline__ bool drain(uint64_t* full, int slots, int asked, uint64_t limit_ns) {
   bool landed = true;
   for (int n = asked > slots ? asked - slots : 0; n < asked; ++n)
     landed = ptx::mbar_wait(&full[n % slots], static_cast<uint32_t>(n / slots) & 1u, nullptr, limit_ns) && landed;
