@@ -513,6 +513,110 @@ MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_sca
                                     const uint8_t* b_scales, int32_t n, int32_t k, const float* bias, mpm_dtype dtype,
                                     void* out, int64_t out_stride, int32_t* device_status, void* stream);
 
+/*
+ * Attention between packed sequences (the paper has no counterpart: it leaves
+ * attention to the model).  The queries of sequence b are rows
+ * [q_offsets[b], q_offsets[b + 1]) of q, its keys rows [k_offsets[b],
+ * k_offsets[b + 1]) of k and v: another length, an encoder's states, or the
+ * same tokens.  For query i and head h, over the keys j of its sequence that
+ * key_mask leaves, with kv head g = h / (q_heads / kv_heads):
+ *   s_j = scale * q_i,h . k_j,g;  lse = log sum_j exp(s_j);  out = sum_j exp(s_j - lse) v_j,g
+ * A query without a key gets out = 0 and lse = -infinity.
+ *
+ *   q             [q_rows, q_heads, head_dim] (dtype); row r, head h begins
+ *                 r * q_row_stride + h * q_head_stride elements on
+ *   k, v          [k_rows, kv_heads, head_dim] (dtype), strides likewise
+ *   q_offsets, k_offsets  int64 [batch + 1] device offsets, or both NULL with
+ *                 batch == 1: one sequence of all rows.  Rows from
+ *                 offsets[batch] on are neither read nor written.
+ *   key_mask      uint8 [k_rows], 0: the key is left out, whatever its row and
+ *                 its value hold; or NULL
+ *   out           [q_rows, q_heads, head_dim] (dtype), contiguous
+ *   lse           optional float [q_rows, q_heads], for the backward pass
+ *   workspace     mpm_cross_attention_workspace_size(..) bytes, 256-byte aligned
+ *                 (NULL where that is 0)
+ *   device_status optional int32 [2] device word: offsets that are not
+ *                 0 = off[0] <= ... <= off[batch] <= rows are reported as
+ *                 MPM_ERR_DEVICE_CHECK (detail = index), a wait in a kernel that
+ *                 ran out as MPM_ERR_DEVICE_TIMEOUT; no access leaves the
+ *                 buffers either way.
+ * Rows and heads of a tensor must not overlap: with several of them, either
+ * stride is at least head_dim, and one at least what the other dimension spans.
+ * Buffers need only the alignment of their elements; 16-byte aligned rows and
+ * heads of bf16 run on the tensor cores (products of bf16 values, probabilities
+ * rounded to bf16), all else, fp32 among it, in fp32 on the CUDA cores.
+ * Statistics and sums are fp32, taken in a fixed order: the same call gives the
+ * same bits.  1 <= head_dim <= MPM_ATTENTION_MAX_HEAD_DIM, kv_heads divides
+ * q_heads, scale > 0.  out or lse over an input or over one another:
+ * MPM_ERR_ALIASING.
+ */
+#define MPM_ATTENTION_MAX_HEAD_DIM 128
+#define MPM_ATTENTION_MAX_HEADS 4096
+MPM_API mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, const void* k,
+                                       int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
+                                       int64_t v_head_stride, const int64_t* q_offsets, const int64_t* k_offsets,
+                                       int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads,
+                                       int32_t head_dim, mpm_dtype dtype, float scale, const uint8_t* key_mask, void* out,
+                                       float* lse, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                                       void* stream);
+/* Bytes of device workspace; 0 for invalid sizes, or where none is needed. */
+MPM_API size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads,
+                                                  int32_t kv_heads, int32_t head_dim, mpm_dtype dtype);
+
+/*
+ * Gradients of mpm_cross_attention from that of its output, its inputs, its
+ * output and the lse that it kept:
+ *   delta = d_out . out;  p_j = exp(s_j - lse);  ds_j = p_j (d_out . v_j - delta)
+ *   d_q = scale sum_j ds_j k_j;  d_k = scale sum ds q;  d_v = sum p d_out
+ * d_k and d_v sum over the sequence's queries and over the query heads that
+ * share the kv head.
+ *   d_out         [q_rows, q_heads, head_dim] (dtype), strides as q's
+ *   out, lse      as mpm_cross_attention wrote them
+ *   d_q           [q_rows, q_heads, head_dim], d_k and d_v [k_rows, kv_heads,
+ *                 head_dim] (dtype), contiguous, written for the rows of
+ *                 sequences (zeros where no sum has a term)
+ * Everything else as above.
+ */
+MPM_API mpm_status mpm_cross_attention_backward(
+    const void* d_out, int64_t d_out_row_stride, int64_t d_out_head_stride, const void* q, int64_t q_row_stride,
+    int64_t q_head_stride, const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
+    int64_t v_head_stride, const void* out, const float* lse, const int64_t* q_offsets, const int64_t* k_offsets,
+    int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim, mpm_dtype dtype,
+    float scale, const uint8_t* key_mask, void* d_q, void* d_k, void* d_v, void* workspace, size_t workspace_bytes,
+    int32_t* device_status, void* stream);
+MPM_API size_t mpm_cross_attention_backward_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads,
+                                                           int32_t kv_heads, int32_t head_dim, mpm_dtype dtype);
+
+/*
+ * Rotary positions of several axes (time, height, width; fractions, as merged
+ * tokens have them).  The first `pairs` pairs of every head's features belong to
+ * the axes in turn, sections[a] of them to axis a.  Pair p of axis a turns by
+ * positions[row, a] * frequencies[p] radians, and the other way where inverse
+ * != 0, which is the backward pass:
+ *   (u, v) -> (u cos - v sin, u sin + v cos)
+ *   x, out        [rows, heads, head_dim] (dtype), strides as above; out may be x
+ *                 with its strides, otherwise they must not overlap
+ *   positions     float [rows, axes], contiguous
+ *   frequencies   double [pairs] in DEVICE memory, pairs = sum of sections
+ *   sections      int32 [axes] in HOST memory, each >= 1;
+ *                 1 <= axes <= MPM_ROTARY_MAX_AXES, 2 * pairs <= head_dim <= MPM_ROTARY_MAX_HEAD_DIM
+ *   layout        pairs features (p, p + pairs) or (2 p, 2 p + 1); features from
+ *                 2 * pairs on are copied
+ *   offsets       optional int64 [batch + 1]: rows from offsets[batch] on are left alone
+ * Angles are exact to about 2^-24 turns at any position below 2^24 turns.
+ */
+#define MPM_ROTARY_MAX_AXES 8
+#define MPM_ROTARY_MAX_HEAD_DIM 1024
+typedef enum mpm_rotary_layout {
+  MPM_ROTARY_HALVES = 0,      /* features p and p + pairs */
+  MPM_ROTARY_INTERLEAVED = 1  /* features 2 p and 2 p + 1 */
+} mpm_rotary_layout;
+MPM_API mpm_status mpm_rotary(const void* x, int64_t x_row_stride, int64_t x_head_stride, const float* positions,
+                              const double* frequencies, const int32_t* sections, int32_t axes, mpm_rotary_layout layout,
+                              int32_t inverse, const int64_t* offsets, int32_t batch, int64_t rows, int32_t heads,
+                              int32_t head_dim, mpm_dtype dtype, void* out, int64_t out_row_stride,
+                              int64_t out_head_stride, int32_t* device_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

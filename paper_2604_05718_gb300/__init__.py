@@ -2,11 +2,21 @@
 
 The compute path lives in ``libmpm.so`` (CUDA kernels for sm_103a, built by
 ``paper_2604_05718_gb300.build.build()``); ``paper_2604_05718_gb300.mpm``
-(the merge) and ``paper_2604_05718_gb300.blocks`` (the encoder blocks around
-it: fused norms, 4-bit linear layers) marshal torch tensors into its C entry
-points.
+(the merge), ``paper_2604_05718_gb300.blocks`` (the encoder blocks around it:
+fused norms, 4-bit linear layers) and ``paper_2604_05718_gb300.attention``
+(attention between packed sequences, rotary positions) marshal torch tensors
+into its C entry points.
 """
 
+from .attention import (  # noqa: F401
+    AttentionGrads,
+    cross_attention,
+    cross_attention_backward,
+    cross_attention_workspace,
+    rotary,
+    rotary_backward,
+    rotary_frequencies,
+)
 from .blocks import (  # noqa: F401
     MXFP4,
     BlockNormGrads,

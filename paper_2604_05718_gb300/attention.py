@@ -1,0 +1,103 @@
+"""Python binding of attention between packed sequences and of rotary positions.
+
+``cross_attention`` lets the queries of every sequence attend to keys of another
+length: an encoder's states, a batch's merged tokens, or the queries' own tokens.
+``rotary`` turns queries and keys by positions of several axes before that.  As in
+``blocks``, arguments are checked and marshalled only, and every step runs in
+the library's kernels on the current torch stream.
+
+Nothing is recorded for autograd: ``cross_attention_backward`` and
+``rotary_backward`` are called by hand (or from a ``torch.autograd.Function``), and
+a tensor that requires grad is refused while grad mode is on.
+"""
+
+from __future__ import annotations
+
+from typing import NamedTuple, Sequence
+
+import torch
+
+from . import blocks
+from .mpm import _dtype_code, library
+
+
+class AttentionGrads(NamedTuple):
+    """Gradients of cross_attention's inputs."""
+
+    d_q: torch.Tensor
+    d_k: torch.Tensor
+    d_v: torch.Tensor
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_offsets: torch.Tensor | None = None,
+                    k_offsets: torch.Tensor | None = None, key_mask: torch.Tensor | None = None,
+                    scale: float | None = None, out: torch.Tensor | None = None, with_lse: bool = False,
+                    workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None):
+    """Softmax attention of each sequence's queries to its keys, which may be of another length.
+
+        out = softmax(scale * q k^T) v        (0 for a query without keys)
+
+    q [Tq, H, D] bf16 or fp32, k and v [Tk, Hkv, D] of the same type, H a multiple
+    of Hkv, D <= 128; rows and heads may be any distance apart (views of a joint
+    projection go in as they are).  q_offsets and k_offsets (int64 [B+1]) are
+    where the sequences begin; without them all rows are one.  Rows from
+    offsets[B] on are left alone.  key_mask (bool or uint8 [Tk]) leaves out keys
+    that are 0: for a padded batch, offsets of equal lengths and ``pad_batch``'s
+    mask.  scale: 1 / sqrt(D) unless given.
+
+    Returns (out, lse): lse (float32 [Tq, H], for ``cross_attention_backward``) is
+    None unless with_lse.
+    """
+    return (blocks._module or blocks.load_binding()).cross_attention(q, k, v, q_offsets, k_offsets, key_mask, scale, out,
+                                                                     with_lse, workspace, device_status)
+
+
+def cross_attention_workspace(q: torch.Tensor, k: torch.Tensor, batch: int = 1, backward: bool = False) -> torch.Tensor:
+    """Device scratch of cross_attention, or of cross_attention_backward, for tensors of these shapes (uint8)."""
+    size = library().mpm_cross_attention_backward_workspace_size if backward else library().mpm_cross_attention_workspace_size
+    n = size(int(batch), q.shape[0], k.shape[0], q.shape[1], k.shape[1], q.shape[2], _dtype_code(q))
+    return torch.empty(int(n), dtype=torch.uint8, device=q.device)
+
+
+def cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                             lse: torch.Tensor, *, q_offsets: torch.Tensor | None = None,
+                             k_offsets: torch.Tensor | None = None, key_mask: torch.Tensor | None = None,
+                             scale: float | None = None, workspace: torch.Tensor | None = None,
+                             device_status: torch.Tensor | None = None) -> AttentionGrads:
+    """Gradients of cross_attention from that of its output.
+
+    The other arguments are cross_attention's own, ``out`` and ``lse`` what it
+    returned.  Gradients have the tokens' type and are summed in a fixed order;
+    rows from offsets[B] on are left alone.
+    """
+    return AttentionGrads(*(blocks._module or blocks.load_binding()).cross_attention_backward(
+        q, k, v, q_offsets, k_offsets, key_mask, scale, d_out, out, lse, workspace, device_status))
+
+
+def rotary_frequencies(sections: Sequence[int], base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The usual frequencies, float64 [sum(sections)]: pair i of an axis of n pairs turns by base^(-i / n) a position."""
+    return torch.tensor([float(base) ** (-i / n) for n in sections for i in range(n)], dtype=torch.float64, device=device)
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, sections: Sequence[int], *,
+           layout: str = "halves", offsets: torch.Tensor | None = None, out: torch.Tensor | None = None,
+           device_status: torch.Tensor | None = None) -> torch.Tensor:
+    """Turns pairs of every head's features by the row's positions on several axes.
+
+    x [T, H, D] bf16 or fp32, rows and heads any distance apart; positions
+    float32 [T, axes] (time, height, width, ..; fractions too); sections: how many
+    pairs each axis turns, in order; frequencies float64 [sum(sections)], radians
+    per unit of position (``rotary_frequencies``).  layout: "halves" pairs feature p
+    with p + sum(sections), "interleaved" 2 p with 2 p + 1; features after the pairs
+    are copied.  With offsets, rows from offsets[B] on are left alone.  out may be x.
+    """
+    return (blocks._module or blocks.load_binding()).rotary(x, positions, frequencies, sections, layout, False, offsets,
+                                                            out, device_status)
+
+
+def rotary_backward(d_out: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, sections: Sequence[int], *,
+                    layout: str = "halves", offsets: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                    device_status: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of rotary's x from that of its output: the pairs turned back.  Arguments are rotary's."""
+    return (blocks._module or blocks.load_binding()).rotary(d_out, positions, frequencies, sections, layout, True, offsets,
+                                                            out, device_status)

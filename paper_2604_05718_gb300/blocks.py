@@ -24,7 +24,8 @@ import torch
 from .mpm import _check, library
 
 _ENTRIES = ("mpm_block_norm", "mpm_block_norm_workspace_size", "mpm_block_norm_backward", "mpm_mxfp4_quantize",
-            "mpm_mxfp4_dequantize", "mpm_mxfp4_matmul")
+            "mpm_mxfp4_dequantize", "mpm_mxfp4_matmul", "mpm_cross_attention", "mpm_cross_attention_workspace_size",
+            "mpm_cross_attention_backward", "mpm_cross_attention_backward_workspace_size", "mpm_rotary")
 _module = None
 
 

@@ -1,0 +1,571 @@
+// Attention between packed sequences on the CUDA cores, in fp32 throughout: for
+// fp32 tokens, and for bf16 tokens whose rows the tensor-core kernels cannot load
+// (strides or addresses that are not 16-byte multiples).
+//
+//   s = scale q.k;  p = exp(s - lse);  o = sum p v
+//   ds = p (do.v - delta), delta = do.o;  dq = scale sum ds k;  dk = scale sum ds q;  dv = sum p do
+//
+// One scheme serves the three passes.  A block of 256 threads keeps a tile of 64
+// rows (queries, or keys for dk and dv) in shared memory and streams tiles of 64
+// columns past it.  Thread (y, x) of 16 x 16 computes rows 4 y .. + 3 and columns
+// x, x + 16, .. of the scores, so that neighbours read rows whose 16-byte pieces
+// lie in different banks; a row's statistics are joined by shuffles within a
+// half-warp.  The probabilities go to shared memory and multiply a streamed tile,
+// 4 rows by 4 (dim <= 64) or 8 features a thread.  The running maximum and sum
+// make it one pass over the keys.
+//
+// Bound: fp32 FMAs.  Eight 16-byte shared loads feed 64 FMAs.
+//
+// Nothing outside a sequence enters a sum: rows past its end and masked keys are
+// loaded as zeros (a NaN there would survive a product with 0) and their scores
+// count as minus infinity.
+#include "attention_common.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+
+constexpr int kTile = 64;
+constexpr int kThreads = 256;
+
+template <int DP>
+struct Shape {
+  static constexpr int kPitch = DP + 4;        // floats of a row in shared memory
+  static constexpr int kCols = DP / 16;        // features that a thread sums
+  static constexpr int kMatrix = kTile * kPitch;
+};
+constexpr int kScorePitch = kTile + 4;
+constexpr int kScores = kTile * kScorePitch;
+
+// Rows first .. first + 63 of one head into shared memory, four features at a
+// time; zeros past the sequence, past the head's width (up to d4) and for masked rows.
+template <typename T, int DP>
+__device__ __forceinline__ void load_tile(float* sm, const Heads& x, int head, const Span& s, int first, int dim, int d4,
+                                          bool vec, const uint8_t* __restrict__ mask) {
+  const T* base = static_cast<const T*>(x.p) + x.head * head;
+  for (int i = threadIdx.x; i < kTile * (d4 / 4); i += kThreads) {
+    const int r = i / (d4 / 4), c = i % (d4 / 4) * 4, row = first + r;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row < s.n && (mask == nullptr || __ldg(mask + s.lo + row) != 0)) {
+      const T* p = base + x.row * (s.lo + row) + c;
+      if (vec) {
+        if constexpr (sizeof(T) == 4) {
+          v = __ldg(reinterpret_cast<const float4*>(p));
+        } else {
+          const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+          v = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                          __uint_as_float(u.y & 0xFFFF0000u));
+        }
+      } else {
+        if (c < dim) v.x = to_f32(p[0]);
+        if (c + 1 < dim) v.y = to_f32(p[1]);
+        if (c + 2 < dim) v.z = to_f32(p[2]);
+        if (c + 3 < dim) v.w = to_f32(p[3]);
+      }
+    }
+    *reinterpret_cast<float4*>(sm + r * Shape<DP>::kPitch + c) = v;
+  }
+}
+// Zeros in the columns of a tile that loads never write and sums read.
+template <int DP>
+__device__ __forceinline__ void clear_tail(float* sm, int d4) {
+  for (int i = threadIdx.x; i < kTile * (DP - d4); i += kThreads)
+    sm[i / (DP - d4) * Shape<DP>::kPitch + d4 + i % (DP - d4)] = 0.f;
+}
+
+// acc[i][j] = rows[4 y + i] . cols[x + 16 j]
+template <int DP>
+__device__ __forceinline__ void dot_tile(const float* rows, const float* cols, int d4, float (&acc)[4][4]) {
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 2
+  for (int d = 0; d < d4; d += 4) {
+    float4 r[4], c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = *reinterpret_cast<const float4*>(rows + (4 * y + i) * Shape<DP>::kPitch + d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = *reinterpret_cast<const float4*>(cols + (x + 16 * j) * Shape<DP>::kPitch + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = fmaf(r[i].x, c[j].x, acc[i][j]);
+        acc[i][j] = fmaf(r[i].y, c[j].y, acc[i][j]);
+        acc[i][j] = fmaf(r[i].z, c[j].z, acc[i][j]);
+        acc[i][j] = fmaf(r[i].w, c[j].w, acc[i][j]);
+      }
+  }
+}
+
+// acc[i][4 g + e] += sum over columns c of scores[4 y + i][c] * tile[c][4 x + 64 g + e]
+template <int DP>
+__device__ __forceinline__ void sum_tile(const float* scores, const float* tile, float (&acc)[4][Shape<DP>::kCols]) {
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+#pragma unroll 1
+  for (int c = 0; c < kTile; c += 4) {
+    float4 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const float4*>(scores + (4 * y + i) * kScorePitch + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int g = 0; g < DP / 64; ++g) {
+        const float4 t = *reinterpret_cast<const float4*>(tile + (c + k) * Shape<DP>::kPitch + 4 * x + 64 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = k == 0 ? s[i].x : k == 1 ? s[i].y : k == 2 ? s[i].z : s[i].w;
+          acc[i][4 * g] = fmaf(w, t.x, acc[i][4 * g]);
+          acc[i][4 * g + 1] = fmaf(w, t.y, acc[i][4 * g + 1]);
+          acc[i][4 * g + 2] = fmaf(w, t.z, acc[i][4 * g + 2]);
+          acc[i][4 * g + 3] = fmaf(w, t.w, acc[i][4 * g + 3]);
+        }
+      }
+    }
+  }
+}
+
+// The thread's scores to shared memory.
+__device__ __forceinline__ void put_scores(float* scores, const float (&v)[4][4]) {
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) scores[(4 * y + i) * kScorePitch + x + 16 * j] = v[i][j];
+}
+
+// The thread's sums, times a factor a row, to rows of `dim` contiguous values.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(T* out, int64_t row0, int rows, int heads, int head, int dim,
+                                           const float (&acc)[4][Shape<DP>::kCols], const float (&factor)[4]) {
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (4 * y + i >= rows) continue;
+    T* p = out + ((row0 + 4 * y + i) * heads + head) * dim;
+#pragma unroll
+    for (int e = 0; e < Shape<DP>::kCols; ++e) {
+      const int c = 4 * x + 64 * (e / 4) + e % 4;
+      if (c < dim) p[c] = from_f32<T>(acc[i][e] * factor[i]);
+    }
+  }
+}
+
+__device__ __forceinline__ float half_warp_max(float v) {
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+  return v;
+}
+__device__ __forceinline__ float half_warp_sum(float v) {
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+struct Item {
+  Tile tile;
+  int head, split;
+};
+// Items are numbered with the tile fastest: neighbours read the same head's rows.
+template <int T>
+__device__ __forceinline__ Item item_of(int64_t item, const int64_t* off, int batch, int64_t rows, int heads) {
+  const int64_t slots = tile_slots<T>(off, batch, rows), rest = item / slots;
+  return {tile_of<T>(off, batch, rows, item % slots), static_cast<int>(rest % heads), static_cast<int>(rest / heads)};
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  float* sq = sm;
+  float* sk = sq + Shape<DP>::kMatrix;
+  float* sv = sk + Shape<DP>::kMatrix;
+  float* sp = sv + Shape<DP>::kMatrix;
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {
+    check_offsets(a.q_offsets, a.batch, a.q_rows, a.status);
+    check_offsets(a.k_offsets, a.batch, a.k_rows, a.status);
+  }
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int d4 = (a.dim + 3) / 4 * 4;
+  const float c = a.scale * kLog2e;
+  if (d4 < DP) clear_tail<DP>(sv, d4);
+  const int64_t items = tile_slots<kTile>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kTile>(it, a.q_offsets, a.batch, a.q_rows, a.q_heads);
+    if (w.tile.image < 0) continue;
+    const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
+    const int kv = w.head / (a.q_heads / a.kv_heads);
+    const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    float acc[4][Shape<DP>::kCols] = {};
+    float top[4], sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      top[i] = -INFINITY;
+      sum[i] = 0.f;
+    }
+    __syncthreads();
+    load_tile<T, DP>(sq, a.q, w.head, w.tile.rows, w.tile.first, a.dim, d4, a.vec, nullptr);
+    for (int t = part.begin; t < part.end; ++t) {
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP>(sk, a.k, kv, ks, t * kTile, a.dim, d4, a.vec, a.mask);
+      load_tile<T, DP>(sv, a.v, kv, ks, t * kTile, a.dim, d4, a.vec, a.mask);
+      __syncthreads();
+      float s[4][4];
+      dot_tile<DP>(sq, sk, d4, s);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = t * kTile + x + 16 * j;
+        const bool there = key < ks.n && (a.mask == nullptr || __ldg(a.mask + ks.lo + key) != 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!there) s[i][j] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // In units of log2: c is positive, so the largest score is the largest product.
+        const float m = fmaxf(top[i], half_warp_max(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]))) * c);
+        const float base = m == -INFINITY ? 0.f : m;
+        const float shrink = exp2f(top[i] - base);
+        top[i] = m;
+        float part_sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = exp2f(fmaf(s[i][j], c, -base));
+          part_sum += s[i][j];
+        }
+        sum[i] = fmaf(sum[i], shrink, half_warp_sum(part_sum));
+#pragma unroll
+        for (int e = 0; e < Shape<DP>::kCols; ++e) acc[i][e] *= shrink;
+      }
+      put_scores(sp, s);
+      __syncwarp();  // a row's scores are read by the warp that wrote them
+      sum_tile<DP>(sp, sv, acc);
+    }
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    float factor[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) factor[i] = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+    const int64_t part0 = a.splits == 1 ? 0 : static_cast<int64_t>(w.split) * a.q_rows * a.q_heads;
+    if (a.splits == 1)
+      store_rows<T, DP>(static_cast<T*>(a.out), row0, rows, a.q_heads, w.head, a.dim, acc, factor);
+    else
+      store_rows<float, DP>(a.partial + part0 * a.dim, row0, rows, a.q_heads, w.head, a.dim, acc, factor);
+    float* lse = a.splits == 1 ? a.lse : a.partial_lse + part0;
+    if (lse != nullptr && x == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * y + i < rows)
+          lse[(row0 + 4 * y + i) * a.q_heads + w.head] = (top[i] + log2f(sum[i])) * (a.splits == 1 ? kLn2 : 1.f);
+    }
+  }
+}
+
+// p and ds of the thread's 4 x 4 scores; `there` holds for the column.
+__device__ __forceinline__ void back_scores(float s, float dp, float c, float lse2, float delta, bool there, float& p, float& ds) {
+  p = there ? exp2f(fmaf(s, c, -lse2)) : 0.f;
+  ds = there ? p * (dp - delta) : 0.f;
+}
+// The row's statistic in log2 units; a row without keys has no probabilities.
+__device__ __forceinline__ float log2_stat(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  float* sq = sm;
+  float* sg = sq + Shape<DP>::kMatrix;
+  float* sk = sg + Shape<DP>::kMatrix;
+  float* sv = sk + Shape<DP>::kMatrix;
+  float* sp = sv + Shape<DP>::kMatrix;
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int d4 = (a.dim + 3) / 4 * 4;
+  const float c = a.scale * kLog2e;
+  if (d4 < DP) clear_tail<DP>(sk, d4);
+  const int64_t items = tile_slots<kTile>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kTile>(it, a.q_offsets, a.batch, a.q_rows, a.q_heads);
+    if (w.tile.image < 0) continue;
+    const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
+    const int kv = w.head / (a.q_heads / a.kv_heads);
+    const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    float acc[4][Shape<DP>::kCols] = {};
+    float lse2[4], delta[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool live = 4 * y + i < rows;
+      lse2[i] = live ? log2_stat(__ldg(a.stats + (row0 + 4 * y + i) * a.q_heads + w.head)) : INFINITY;
+      delta[i] = live ? a.delta[(row0 + 4 * y + i) * a.q_heads + w.head] : 0.f;
+    }
+    __syncthreads();
+    load_tile<T, DP>(sq, a.q, w.head, w.tile.rows, w.tile.first, a.dim, d4, a.vec, nullptr);
+    load_tile<T, DP>(sg, a.d_out, w.head, w.tile.rows, w.tile.first, a.dim, d4, a.vec, nullptr);
+    for (int t = part.begin; t < part.end; ++t) {
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP>(sk, a.k, kv, ks, t * kTile, a.dim, d4, a.vec, a.mask);
+      load_tile<T, DP>(sv, a.v, kv, ks, t * kTile, a.dim, d4, a.vec, a.mask);
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      dot_tile<DP>(sq, sk, d4, s);
+      dot_tile<DP>(sg, sv, d4, dp);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = t * kTile + x + 16 * j;
+        const bool there = key < ks.n && (a.mask == nullptr || __ldg(a.mask + ks.lo + key) != 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float p;
+          back_scores(s[i][j], dp[i][j], c, lse2[i], delta[i], there && lse2[i] != INFINITY, p, s[i][j]);
+        }
+      }
+      put_scores(sp, s);
+      __syncwarp();
+      sum_tile<DP>(sp, sk, acc);
+    }
+    const float f = a.scale;
+    const float factor[4] = {f, f, f, f};
+    if (a.splits == 1)
+      store_rows<T, DP>(static_cast<T*>(a.d_q), row0, rows, a.q_heads, w.head, a.dim, acc, factor);
+    else
+      store_rows<float, DP>(a.partial + static_cast<int64_t>(w.split) * a.q_rows * a.q_heads * a.dim, row0, rows, a.q_heads,
+                            w.head, a.dim, acc, factor);
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  float* sk = sm;
+  float* sv = sk + Shape<DP>::kMatrix;
+  float* sq = sv + Shape<DP>::kMatrix;
+  float* sg = sq + Shape<DP>::kMatrix;
+  float* sp = sg + Shape<DP>::kMatrix;
+  __shared__ float stat[kTile], dot[kTile];
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int d4 = (a.dim + 3) / 4 * 4;
+  const float c = a.scale * kLog2e;
+  const int group = a.q_heads / a.kv_heads;
+  if (d4 < DP) {
+    clear_tail<DP>(sq, d4);
+    clear_tail<DP>(sg, d4);
+  }
+  const int64_t items = tile_slots<kTile>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kTile>(it, a.k_offsets, a.batch, a.k_rows, a.kv_heads);
+    if (w.tile.image < 0) continue;
+    const Span qs = span_of(a.q_offsets, w.tile.image, a.q_rows);
+    const int tiles = (qs.n + kTile - 1) / kTile;
+    const Part part = part_of(tiles * group, w.split, a.key_splits);
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    float dk[4][Shape<DP>::kCols] = {}, dv[4][Shape<DP>::kCols] = {};
+    bool there[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      there[i] = 4 * y + i < rows && (a.mask == nullptr || __ldg(a.mask + row0 + 4 * y + i) != 0);
+    __syncthreads();
+    load_tile<T, DP>(sk, a.k, w.head, w.tile.rows, w.tile.first, a.dim, d4, a.vec, a.mask);
+    load_tile<T, DP>(sv, a.v, w.head, w.tile.rows, w.tile.first, a.dim, d4, a.vec, a.mask);
+    for (int t = part.begin; t < part.end; ++t) {
+      const int head = w.head * group + t / tiles, first = t % tiles * kTile;
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP>(sq, a.q, head, qs, first, a.dim, d4, a.vec, nullptr);
+      load_tile<T, DP>(sg, a.d_out, head, qs, first, a.dim, d4, a.vec, nullptr);
+      if (threadIdx.x < kTile) {
+        const int r = first + threadIdx.x;
+        const int64_t at = (qs.lo + r) * a.q_heads + head;
+        stat[threadIdx.x] = r < qs.n ? log2_stat(__ldg(a.stats + at)) : INFINITY;
+        dot[threadIdx.x] = r < qs.n ? a.delta[at] : 0.f;
+      }
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      dot_tile<DP>(sk, sq, d4, s);
+      dot_tile<DP>(sv, sg, d4, dp);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float l = stat[x + 16 * j], e = dot[x + 16 * j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          back_scores(s[i][j], dp[i][j], c, l, e, there[i] && l != INFINITY, s[i][j], dp[i][j]);
+      }
+      put_scores(sp, s);
+      __syncwarp();
+      sum_tile<DP>(sp, sg, dv);
+      __syncwarp();
+      put_scores(sp, dp);
+      __syncwarp();
+      sum_tile<DP>(sp, sq, dk);
+    }
+    const float scales[4] = {a.scale, a.scale, a.scale, a.scale}, ones[4] = {1.f, 1.f, 1.f, 1.f};
+    if (a.key_splits == 1) {
+      store_rows<T, DP>(static_cast<T*>(a.d_k), row0, rows, a.kv_heads, w.head, a.dim, dk, scales);
+      store_rows<T, DP>(static_cast<T*>(a.d_v), row0, rows, a.kv_heads, w.head, a.dim, dv, ones);
+    } else {
+      const int64_t each = a.k_rows * a.kv_heads * a.dim;
+      float* p = a.partial + w.split * each;
+      store_rows<float, DP>(p, row0, rows, a.kv_heads, w.head, a.dim, dk, scales);
+      store_rows<float, DP>(p + a.key_splits * each, row0, rows, a.kv_heads, w.head, a.dim, dv, ones);
+    }
+  }
+}
+
+// out = sum over parts of 2^(l_s - l) o_s, l = log2 sum 2^l_s: a warp a row and head.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attention_join_kernel(const AttentionArgs a) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int lane = threadIdx.x & 31;
+  const int64_t all = a.q_rows * a.q_heads, live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
+  for (int64_t r = blockIdx.x * int64_t{kThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kThreads / 32}) {
+    // Two parts a lane.
+    float l[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) l[i] = lane + 32 * i < a.splits ? a.partial_lse[(lane + 32 * i) * all + r] : -INFINITY;
+    float top = fmaxf(l[0], l[1]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const float base = top == -INFINITY ? 0.f : top;
+    float w[2] = {exp2f(l[0] - base), exp2f(l[1] - base)};
+    float sum = w[0] + w[1];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    w[0] *= inv;
+    w[1] *= inv;
+    float v[kAttentionMaxDim / 32] = {};
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = __shfl_sync(0xFFFFFFFFu, s < 32 ? w[0] : w[1], s & 31);
+      const float* p = a.partial + (s * all + r) * a.dim;
+#pragma unroll
+      for (int i = 0; i < kAttentionMaxDim / 32; ++i)
+        if (lane + 32 * i < a.dim) v[i] = fmaf(f, p[lane + 32 * i], v[i]);
+    }
+    T* out = static_cast<T*>(a.out) + r * a.dim;
+#pragma unroll
+    for (int i = 0; i < kAttentionMaxDim / 32; ++i)
+      if (lane + 32 * i < a.dim) out[lane + 32 * i] = from_f32<T>(v[i]);
+    if (a.lse != nullptr && lane == 0) a.lse[r] = (top + log2f(sum)) * kLn2;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attention_delta_kernel(const AttentionArgs a) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {
+    check_offsets(a.q_offsets, a.batch, a.q_rows, a.status);
+    check_offsets(a.k_offsets, a.batch, a.k_rows, a.status);
+  }
+  const int lane = threadIdx.x & 31;
+  const int64_t live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
+  for (int64_t r = blockIdx.x * int64_t{kThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kThreads / 32}) {
+    const T* o = static_cast<const T*>(a.out) + r * a.dim;
+    const T* g = static_cast<const T*>(a.d_out.p) + a.d_out.row * (r / a.q_heads) + a.d_out.head * (r % a.q_heads);
+    float s = 0.f;
+    for (int d = lane; d < a.dim; d += 32) s = fmaf(to_f32(o[d]), to_f32(g[d]), s);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if (lane == 0) a.delta[r] = s;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attention_sum_kernel(const float* __restrict__ parts, int splits, int64_t rows,
+                                                                 const int64_t* __restrict__ offsets, int batch, int width,
+                                                                 T* __restrict__ out) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int64_t each = rows * width, live = live_rows(offsets, batch, rows) * width;
+  for (int64_t i = blockIdx.x * int64_t{kThreads} + threadIdx.x; i < live; i += gridDim.x * int64_t{kThreads}) {
+    float s = 0.f;
+    for (int p = 0; p < splits; ++p) s += parts[p * each + i];
+    out[i] = from_f32<T>(s);
+  }
+}
+
+int blocks_for(int64_t work, int64_t most) { return static_cast<int>(work < 1 ? 1 : work < most ? work : most); }
+
+// Launches with dynamic shared memory on as many blocks as are resident at once.
+template <typename K>
+cudaError_t launch_tiles(K kernel, size_t smem, int64_t items, const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  int each = 0;
+  e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3(blocks_for(items, int64_t{num_sms} * (each < 1 ? 1 : each))), dim3(kThreads), smem, stream, a);
+}
+
+template <typename T, int DP>
+cudaError_t forward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  const int64_t items = tile_slots<kTile>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  return launch_tiles(attention_simt_kernel<T, DP>, sizeof(float) * (3 * Shape<DP>::kMatrix + kScores), items, a, num_sms, stream);
+}
+template <typename T, int DP>
+cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  constexpr size_t smem = sizeof(float) * (4 * Shape<DP>::kMatrix + kScores);
+  const int64_t q_items = tile_slots<kTile>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  const int64_t k_items = tile_slots<kTile>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
+  cudaError_t e = cudaSuccess;
+  constexpr bool bf16 = sizeof(T) == 2;
+  if (a.q_rows > 0) {
+    e = launch_tiles(attention_simt_dq_kernel<T, DP>, smem, q_items, a, num_sms, stream);
+    if (e == cudaSuccess && a.splits > 1)
+      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, bf16, num_sms, stream);
+  }
+  if (e == cudaSuccess && a.k_rows > 0) {
+    e = launch_tiles(attention_simt_dkv_kernel<T, DP>, smem, k_items, a, num_sms, stream);
+    const int64_t each = a.k_rows * a.kv_heads * a.dim;
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, bf16, num_sms, stream);
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim,
+                               a.d_v, bf16, num_sms, stream);
+  }
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  if (bf16) return a.dim <= 64 ? forward<__nv_bfloat16, 64>(a, num_sms, stream) : forward<__nv_bfloat16, 128>(a, num_sms, stream);
+  return a.dim <= 64 ? forward<float, 64>(a, num_sms, stream) : forward<float, 128>(a, num_sms, stream);
+}
+
+cudaError_t launch_attention_backward_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  if (bf16) return a.dim <= 64 ? backward<__nv_bfloat16, 64>(a, num_sms, stream) : backward<__nv_bfloat16, 128>(a, num_sms, stream);
+  return a.dim <= 64 ? backward<float, 64>(a, num_sms, stream) : backward<float, 128>(a, num_sms, stream);
+}
+
+cudaError_t launch_attention_join(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  const int blocks = blocks_for((a.q_rows * a.q_heads + 7) / 8, int64_t{num_sms} * 8);
+  return bf16 ? launch_dependent(attention_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(kThreads), 0, stream, a)
+              : launch_dependent(attention_join_kernel<float>, dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+
+cudaError_t launch_attention_delta(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  const int blocks = blocks_for((a.q_rows * a.q_heads + 7) / 8, int64_t{num_sms} * 8);
+  return bf16 ? launch_dependent(attention_delta_kernel<__nv_bfloat16>, dim3(blocks), dim3(kThreads), 0, stream, a)
+              : launch_dependent(attention_delta_kernel<float>, dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+
+cudaError_t launch_attention_sum(const float* parts, int splits, int64_t rows, const int64_t* offsets, int batch, int heads,
+                                 int dim, void* out, bool bf16, int num_sms, cudaStream_t stream) {
+  const int width = heads * dim;
+  const int blocks = blocks_for((rows * width + kThreads - 1) / kThreads, int64_t{num_sms} * 8);
+  return bf16 ? launch_dependent(attention_sum_kernel<__nv_bfloat16>, dim3(blocks), dim3(kThreads), 0, stream, parts, splits, rows,
+                                 offsets, batch, width, static_cast<__nv_bfloat16*>(out))
+              : launch_dependent(attention_sum_kernel<float>, dim3(blocks), dim3(kThreads), 0, stream, parts, splits, rows, offsets,
+                                 batch, width, static_cast<float*>(out));
+}
+
+}  // namespace mpm

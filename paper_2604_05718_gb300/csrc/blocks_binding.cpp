@@ -1,4 +1,4 @@
-// Python binding of the encoder-block entry points, as a CPython extension.
+// Python binding of the encoder-block, attention and rotary entry points, as a CPython extension.
 //
 // It checks and marshals torch tensors and allocates outputs, as mpm.py does
 // for the merge through ctypes; every step of the computation is the C ABI's,
@@ -32,6 +32,11 @@ struct EntryPoints {
   decltype(&mpm_mxfp4_quantize) mxfp4_quantize;
   decltype(&mpm_mxfp4_dequantize) mxfp4_dequantize;
   decltype(&mpm_mxfp4_matmul) mxfp4_matmul;
+  decltype(&mpm_cross_attention) cross_attention;
+  decltype(&mpm_cross_attention_workspace_size) cross_attention_workspace_size;
+  decltype(&mpm_cross_attention_backward) cross_attention_backward;
+  decltype(&mpm_cross_attention_backward_workspace_size) cross_attention_backward_workspace_size;
+  decltype(&mpm_rotary) rotary;
 };
 EntryPoints entry = {};
 PyObject* raise_status = nullptr;  // Python callable (name, code) that raises the library's error
@@ -389,6 +394,197 @@ PyObject* matmul(PyObject* const* p) {
   return p[8] == Py_None ? THPVariable_Wrap(out) : again(p[8]);
 }
 
+// [rows, heads, head_dim] bf16 or fp32 values with contiguous heads, any distance apart.
+const at::Tensor* heads_of(PyObject* o, const char* name) {
+  const at::Tensor* t = tensor(o, name);
+  if (t->dim() != 3) value_error(name, "must be [rows, heads, head_dim]");
+  dtype_of(*t, name);
+  if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX || t->size(2) > INT32_MAX) value_error(name, "is too large");
+  if (t->size(1) < 1 || t->size(2) < 1) value_error(name, "must have heads and features");
+  if (t->size(2) > 1 && t->stride(2) != 1) value_error(name, "must have contiguous heads");
+  const int64_t rows = t->size(0), heads = t->size(1), dim = t->size(2), row = t->stride(0), head = t->stride(1);
+  if ((rows > 1 && row < dim) || (heads > 1 && head < dim) ||
+      (rows > 1 && heads > 1 && row < (heads - 1) * head + dim && head < (rows - 1) * row + dim))
+    value_error(name, "must have rows and heads that do not overlap");
+  return t;
+}
+void same_kind(const at::Tensor& t, const char* name, const at::Tensor& like) {
+  if (t.get_device() != like.get_device()) value_error(name, "must be on the other tensors' device");
+  if (t.scalar_type() != like.scalar_type()) type_error(name, "must have the other tensors' type");
+}
+// int64 offsets of sequences, and how many those are (null and 1 for None).
+const int64_t* offsets_of(PyObject* o, const char* name, int64_t device, int64_t* batch) {
+  *batch = 1;
+  const at::Tensor* t = tensor(o, name, true);
+  if (t == nullptr) return nullptr;
+  if (t->scalar_type() != at::kLong) type_error(name, "must be int64");
+  if (t->dim() != 1 || t->numel() < 2 || t->get_device() != device || !t->is_contiguous())
+    value_error(name, "must be a contiguous [B+1] tensor on the other tensors' device");
+  *batch = t->numel() - 1;
+  if (*batch > INT32_MAX) value_error(name, "has too many sequences");
+  return static_cast<const int64_t*>(t->data_ptr());
+}
+
+// The arguments that both directions of cross_attention share.
+struct AttentionInputs {
+  const at::Tensor *q, *k, *v;
+  int64_t device, batch;
+  const int64_t *q_offsets, *k_offsets;
+  const uint8_t* mask = nullptr;
+  int32_t q_heads, kv_heads, dim;
+  mpm_dtype dtype;
+  float scale;
+
+  // q, k, v, q_offsets, k_offsets, key_mask, scale
+  explicit AttentionInputs(PyObject* const* p) {
+    q = heads_of(p[0], "q");
+    k = heads_of(p[1], "k");
+    v = heads_of(p[2], "v");
+    device = q->get_device();
+    dtype = dtype_of(*q, "q");
+    same_kind(*k, "k", *q);
+    same_kind(*v, "v", *q);
+    if (k->sizes() != v->sizes()) value_error("v", "must have k's shape");
+    if (k->size(2) != q->size(2)) value_error("k", "must have heads as wide as q's");
+    if (q->size(1) % k->size(1) != 0) value_error("q", "must have a multiple of k's heads");
+    q_heads = static_cast<int32_t>(q->size(1));
+    kv_heads = static_cast<int32_t>(k->size(1));
+    dim = static_cast<int32_t>(q->size(2));
+    int64_t k_batch;
+    q_offsets = offsets_of(p[3], "q_offsets", device, &batch);
+    k_offsets = offsets_of(p[4], "k_offsets", device, &k_batch);
+    if (batch != k_batch || (q_offsets == nullptr) != (k_offsets == nullptr))
+      value_error("q_offsets and k_offsets", "must be of as many sequences");
+    if (const at::Tensor* m = tensor(p[5], "key_mask", true)) {
+      if (m->scalar_type() != at::kByte && m->scalar_type() != at::kBool) type_error("key_mask", "must be bool or uint8");
+      if (m->get_device() != device || !m->is_contiguous() || m->numel() != k->size(0))
+        value_error("key_mask", "must be contiguous, a value per row of k, on the other tensors' device");
+      mask = static_cast<const uint8_t*>(m->data_ptr());
+    }
+    scale = p[6] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(dim))) : static_cast<float>(number(p[6]));
+  }
+};
+// Scratch of `need` bytes: the caller's, or new.
+struct Scratch {
+  at::Tensor made;
+  void* p = nullptr;
+  size_t bytes = 0;
+  Scratch(PyObject* given, size_t need, const at::Tensor& like) {
+    if (given != Py_None) {
+      p = buffer(given, "workspace", at::kByte, like.get_device(), at::IntArrayRef());
+      bytes = static_cast<size_t>(THPVariable_Unpack(given).numel());
+    } else if (need > 0) {
+      made = new_like(like, {static_cast<int64_t>(need)}, at::kByte);
+      p = made.data_ptr();
+      bytes = need;
+    }
+  }
+};
+
+// cross_attention(<AttentionInputs>, out, with_lse, workspace, device_status)
+PyObject* cross_attention(PyObject* const* p) {
+  const AttentionInputs a(p);
+  const OnDevice on(a.device);
+  at::Tensor out, lse;
+  void* pout;
+  if (p[7] == Py_None) {
+    out = new_like(*a.q, a.q->sizes(), a.q->scalar_type());
+    pout = out.data_ptr();
+  } else {
+    pout = buffer(p[7], "out", a.q->scalar_type(), a.device, a.q->sizes());
+  }
+  if (truth(p[8])) lse = new_like(*a.q, {a.q->size(0), a.q->size(1)}, at::kFloat);
+  const Scratch scratch(p[9],
+                        entry.cross_attention_workspace_size(static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0),
+                                                             a.q_heads, a.kv_heads, a.dim, a.dtype),
+                        *a.q);
+  check("mpm_cross_attention",
+        entry.cross_attention(a.q->data_ptr(), a.q->stride(0), a.q->stride(1), a.k->data_ptr(), a.k->stride(0),
+                              a.k->stride(1), a.v->data_ptr(), a.v->stride(0), a.v->stride(1), a.q_offsets, a.k_offsets,
+                              static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0), a.q_heads, a.kv_heads, a.dim,
+                              a.dtype, a.scale, a.mask, pout, lse.defined() ? static_cast<float*>(lse.data_ptr()) : nullptr,
+                              scratch.p, scratch.bytes, status_word(p[10], a.device), on.stream));
+  written(p[7]);
+  return tuple_of({out.defined() ? wrapped(out) : again(p[7]), wrapped(lse)});
+}
+
+// cross_attention_backward(<AttentionInputs>, d_out, out, lse, workspace, device_status)
+PyObject* cross_attention_backward(PyObject* const* p) {
+  const AttentionInputs a(p);
+  const OnDevice on(a.device);
+  const at::Tensor* g = heads_of(p[7], "d_out");
+  same_kind(*g, "d_out", *a.q);
+  if (g->sizes() != a.q->sizes()) value_error("d_out", "must have q's shape");
+  const void* out = buffer(p[8], "out", a.q->scalar_type(), a.device, a.q->sizes(), false);
+  const int64_t rows_heads[2] = {a.q->size(0), a.q->size(1)};
+  const float* lse = static_cast<float*>(buffer(p[9], "lse", at::kFloat, a.device, rows_heads, false));
+  at::Tensor d_q = new_like(*a.q, a.q->sizes(), a.q->scalar_type());
+  at::Tensor d_k = new_like(*a.k, a.k->sizes(), a.k->scalar_type()), d_v = new_like(*a.k, a.k->sizes(), a.k->scalar_type());
+  const Scratch scratch(p[10],
+                        entry.cross_attention_backward_workspace_size(static_cast<int32_t>(a.batch), a.q->size(0),
+                                                                      a.k->size(0), a.q_heads, a.kv_heads, a.dim, a.dtype),
+                        *a.q);
+  check("mpm_cross_attention_backward",
+        entry.cross_attention_backward(
+            g->data_ptr(), g->stride(0), g->stride(1), a.q->data_ptr(), a.q->stride(0), a.q->stride(1), a.k->data_ptr(),
+            a.k->stride(0), a.k->stride(1), a.v->data_ptr(), a.v->stride(0), a.v->stride(1), out, lse, a.q_offsets,
+            a.k_offsets, static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0), a.q_heads, a.kv_heads, a.dim, a.dtype,
+            a.scale, a.mask, d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), scratch.p, scratch.bytes,
+            status_word(p[11], a.device), on.stream));
+  return tuple_of({wrapped(d_q), wrapped(d_k), wrapped(d_v)});
+}
+
+// rotary(x, positions, frequencies, sections, layout, inverse, offsets, out, device_status)
+PyObject* rotary(PyObject* const* p) {
+  const at::Tensor* x = heads_of(p[0], "x");
+  const int64_t device = x->get_device(), rows = x->size(0);
+  if (!PyTuple_Check(p[3]) && !PyList_Check(p[3])) type_error("sections", "must be a tuple or a list");
+  int32_t sections[MPM_ROTARY_MAX_AXES];
+  const Py_ssize_t axes = PySequence_Size(p[3]);
+  if (axes < 1 || axes > MPM_ROTARY_MAX_AXES) value_error("sections", "must be of 1 to 8 axes");
+  int64_t pairs = 0;
+  for (Py_ssize_t i = 0; i < axes; ++i) {
+    PyObject* item = PySequence_GetItem(p[3], i);
+    const long long n = item == nullptr ? -1 : PyLong_AsLongLong(item);
+    Py_XDECREF(item);
+    if (n == -1 && PyErr_Occurred()) throw Raised{};
+    if (n < 1 || n > x->size(2)) value_error("sections", "must be positive, and no more than a head's pairs in all");
+    sections[i] = static_cast<int32_t>(n);
+    pairs += n;
+  }
+  if (2 * pairs > x->size(2)) value_error("sections", "must be positive, and no more than a head's pairs in all");
+  const at::Tensor* at = tensor(p[1], "positions");
+  if (at->scalar_type() != at::kFloat) type_error("positions", "must be float32");
+  if (at->get_device() != device || !at->is_contiguous() || at->numel() != rows * axes || at->dim() < 1 || at->size(0) != rows)
+    value_error("positions", "must be a contiguous [rows, axes] tensor on x's device");
+  const int64_t vector[1] = {pairs};
+  const double* frequencies = static_cast<double*>(buffer(p[2], "frequencies", at::kDouble, device, vector, false));
+  if (!PyUnicode_Check(p[4])) type_error("layout", "must be a string");
+  mpm_rotary_layout layout;
+  if (PyUnicode_CompareWithASCIIString(p[4], "halves") == 0) layout = MPM_ROTARY_HALVES;
+  else if (PyUnicode_CompareWithASCIIString(p[4], "interleaved") == 0) layout = MPM_ROTARY_INTERLEAVED;
+  else value_error("layout", "must be 'halves' or 'interleaved'");
+  int64_t batch;
+  const int64_t* offsets = offsets_of(p[6], "offsets", device, &batch);
+  const OnDevice on(device);
+  at::Tensor out;
+  if (p[7] == Py_None) {
+    out = new_like(*x, x->sizes(), x->scalar_type());
+  } else {
+    const at::Tensor* t = heads_of(p[7], "out");
+    same_kind(*t, "out", *x);
+    if (t->sizes() != x->sizes()) value_error("out", "must have x's shape");
+    out = *t;
+  }
+  check("mpm_rotary",
+        entry.rotary(x->data_ptr(), x->stride(0), x->stride(1), static_cast<const float*>(at->data_ptr()), frequencies,
+                     sections, static_cast<int32_t>(axes), layout, truth(p[5]), offsets, static_cast<int32_t>(batch), rows,
+                     static_cast<int32_t>(x->size(1)), static_cast<int32_t>(x->size(2)), dtype_of(*x, "x"), out.data_ptr(),
+                     out.stride(0), out.stride(1), status_word(p[8], device), on.stream));
+  written(p[7]);
+  return p[7] == Py_None ? THPVariable_Wrap(out) : again(p[7]);
+}
+
 // Calls F with its arguments, of which there are N; no C++ exception leaves.
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -439,8 +635,11 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"quantize", fast<quantize, 3>(), METH_FASTCALL, nullptr},
                          {"dequantize", fast<dequantize, 5>(), METH_FASTCALL, nullptr},
                          {"matmul", fast<matmul, 10>(), METH_FASTCALL, nullptr},
+                         {"cross_attention", fast<cross_attention, 11>(), METH_FASTCALL, nullptr},
+                         {"cross_attention_backward", fast<cross_attention_backward, 12>(), METH_FASTCALL, nullptr},
+                         {"rotary", fast<rotary, 9>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blocks", "Binding of the encoder-block entry points of libmpm.so.", -1,
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blocks", "Binding of the encoder-block, attention and rotary entry points of libmpm.so.", -1,
                       methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

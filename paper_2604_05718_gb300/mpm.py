@@ -34,7 +34,9 @@ EXPORTS = ("mpm_abi_version", "mpm_status_string", "mpm_merge_workspace_size", "
            "mpm_merge_no_alloc", "mpm_no_alloc_get_device_status", "mpm_compose_gather", "mpm_pad_batch",
            "mpm_unpad_batch", "mpm_merge_chunked", "mpm_nearest_neighbors_chunked", "mpm_block_norm",
            "mpm_block_norm_workspace_size", "mpm_block_norm_backward", "mpm_mxfp4_code_bytes", "mpm_mxfp4_scale_bytes",
-           "mpm_mxfp4_quantize", "mpm_mxfp4_dequantize", "mpm_mxfp4_matmul")
+           "mpm_mxfp4_quantize", "mpm_mxfp4_dequantize", "mpm_mxfp4_matmul", "mpm_cross_attention",
+           "mpm_cross_attention_workspace_size", "mpm_cross_attention_backward",
+           "mpm_cross_attention_backward_workspace_size", "mpm_rotary")
 
 _lib = None
 
@@ -80,6 +82,15 @@ def _declare(lib: ctypes.CDLL) -> None:
         "mpm_mxfp4_quantize": (ctypes.c_int, [P, I64, I64, I32, ctypes.c_int, P, P, P]),
         "mpm_mxfp4_dequantize": (ctypes.c_int, [P, P, I64, I32, ctypes.c_int, P, I64, P]),
         "mpm_mxfp4_matmul": (ctypes.c_int, [P, P, I64, P, P, I32, I32, P, ctypes.c_int, P, I64, P, P]),
+        "mpm_cross_attention": (ctypes.c_int, [P, I64, I64, P, I64, I64, P, I64, I64, P, P, I32, I64, I64, I32, I32, I32,
+                                               ctypes.c_int, F32, P, P, P, P, SZ, P, P]),
+        "mpm_cross_attention_workspace_size": (SZ, [I32, I64, I64, I32, I32, I32, ctypes.c_int]),
+        "mpm_cross_attention_backward": (ctypes.c_int, [P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, I32,
+                                                        I64, I64, I32, I32, I32, ctypes.c_int, F32, P, P, P, P, P, SZ, P,
+                                                        P]),
+        "mpm_cross_attention_backward_workspace_size": (SZ, [I32, I64, I64, I32, I32, I32, ctypes.c_int]),
+        "mpm_rotary": (ctypes.c_int, [P, I64, I64, P, P, P, I32, ctypes.c_int, I32, P, I32, I64, I32, I32, ctypes.c_int, P,
+                                      I64, I64, P, P]),
         "mpm_selftest_wait_timeout": (ctypes.c_int, [P, ctypes.c_uint32, P]),
         "mpm_trace_read": (ctypes.c_int, [P]),
         "mpm_trace_reset": (ctypes.c_int, []),
