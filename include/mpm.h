@@ -532,6 +532,10 @@ MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_sca
  *   key_mask      uint8 [k_rows], 0: the key is left out, whatever its row and
  *                 its value hold; or NULL
  *   out           [q_rows, q_heads, head_dim] (dtype), contiguous
+ *   out_rest      optional, bf16 only: what the rounding of out left, rounded to
+ *                 bf16 (as out), for the backward pass: delta below is a small
+ *                 difference of large sums, and without the rest its error grows
+ *                 against d_q as sequences get longer
  *   lse           optional float [q_rows, q_heads], for the backward pass
  *   workspace     mpm_cross_attention_workspace_size(..) bytes, 256-byte aligned
  *                 (NULL where that is 0)
@@ -547,8 +551,8 @@ MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_sca
  * rounded to bf16), all else, fp32 among it, in fp32 on the CUDA cores.
  * Statistics and sums are fp32, taken in a fixed order: the same call gives the
  * same bits.  1 <= head_dim <= MPM_ATTENTION_MAX_HEAD_DIM, kv_heads divides
- * q_heads, scale > 0.  out or lse over an input or over one another:
- * MPM_ERR_ALIASING.
+ * q_heads, scale > 0.  An output, the workspace or the status word over an input
+ * or over one another: MPM_ERR_ALIASING.
  */
 #define MPM_ATTENTION_MAX_HEAD_DIM 128
 #define MPM_ATTENTION_MAX_HEADS 4096
@@ -557,8 +561,8 @@ MPM_API mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int6
                                        int64_t v_head_stride, const int64_t* q_offsets, const int64_t* k_offsets,
                                        int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads,
                                        int32_t head_dim, mpm_dtype dtype, float scale, const uint8_t* key_mask, void* out,
-                                       float* lse, void* workspace, size_t workspace_bytes, int32_t* device_status,
-                                       void* stream);
+                                       void* out_rest, float* lse, void* workspace, size_t workspace_bytes,
+                                       int32_t* device_status, void* stream);
 /* Bytes of device workspace; 0 for invalid sizes, or where none is needed. */
 MPM_API size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads,
                                                   int32_t kv_heads, int32_t head_dim, mpm_dtype dtype);
@@ -566,12 +570,12 @@ MPM_API size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows,
 /*
  * Gradients of mpm_cross_attention from that of its output, its inputs, its
  * output and the lse that it kept:
- *   delta = d_out . out;  p_j = exp(s_j - lse);  ds_j = p_j (d_out . v_j - delta)
+ *   delta = d_out . (out + out_rest);  p_j = exp(s_j - lse);  ds_j = p_j (d_out . v_j - delta)
  *   d_q = scale sum_j ds_j k_j;  d_k = scale sum ds q;  d_v = sum p d_out
  * d_k and d_v sum over the sequence's queries and over the query heads that
  * share the kv head.
  *   d_out         [q_rows, q_heads, head_dim] (dtype), strides as q's
- *   out, lse      as mpm_cross_attention wrote them
+ *   out, out_rest, lse  as mpm_cross_attention wrote them (out_rest may be NULL)
  *   d_q           [q_rows, q_heads, head_dim], d_k and d_v [k_rows, kv_heads,
  *                 head_dim] (dtype), contiguous, written for the rows of
  *                 sequences (zeros where no sum has a term)
@@ -580,7 +584,7 @@ MPM_API size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows,
 MPM_API mpm_status mpm_cross_attention_backward(
     const void* d_out, int64_t d_out_row_stride, int64_t d_out_head_stride, const void* q, int64_t q_row_stride,
     int64_t q_head_stride, const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
-    int64_t v_head_stride, const void* out, const float* lse, const int64_t* q_offsets, const int64_t* k_offsets,
+    int64_t v_head_stride, const void* out, const void* out_rest, const float* lse, const int64_t* q_offsets, const int64_t* k_offsets,
     int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim, mpm_dtype dtype,
     float scale, const uint8_t* key_mask, void* d_q, void* d_k, void* d_v, void* workspace, size_t workspace_bytes,
     int32_t* device_status, void* stream);

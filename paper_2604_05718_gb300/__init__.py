@@ -10,6 +10,7 @@ into its C entry points.
 
 from .attention import (  # noqa: F401
     AttentionGrads,
+    AttentionStats,
     cross_attention,
     cross_attention_backward,
     cross_attention_workspace,

@@ -21,6 +21,13 @@ from . import blocks
 from .mpm import _dtype_code, library
 
 
+class AttentionStats(NamedTuple):
+    """What cross_attention keeps for its backward pass."""
+
+    lse: torch.Tensor           # float32 [Tq, H]: log of a query's sum of exponentials, -inf without keys
+    rest: torch.Tensor | None   # bf16 tokens: [Tq, H, D], what the rounding of the output left
+
+
 class AttentionGrads(NamedTuple):
     """Gradients of cross_attention's inputs."""
 
@@ -45,11 +52,12 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_offs
     that are 0: for a padded batch, offsets of equal lengths and ``pad_batch``'s
     mask.  scale: 1 / sqrt(D) unless given.
 
-    Returns (out, lse): lse (float32 [Tq, H], for ``cross_attention_backward``) is
+    Returns (out, stats): the AttentionStats that ``cross_attention_backward`` takes,
     None unless with_lse.
     """
-    return (blocks._module or blocks.load_binding()).cross_attention(q, k, v, q_offsets, k_offsets, key_mask, scale, out,
-                                                                     with_lse, workspace, device_status)
+    out, lse, rest = (blocks._module or blocks.load_binding()).cross_attention(
+        q, k, v, q_offsets, k_offsets, key_mask, scale, out, with_lse, workspace, device_status)
+    return out, None if lse is None else AttentionStats(lse, rest)
 
 
 def cross_attention_workspace(q: torch.Tensor, k: torch.Tensor, batch: int = 1, backward: bool = False) -> torch.Tensor:
@@ -60,18 +68,19 @@ def cross_attention_workspace(q: torch.Tensor, k: torch.Tensor, batch: int = 1, 
 
 
 def cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
-                             lse: torch.Tensor, *, q_offsets: torch.Tensor | None = None,
+                             stats: AttentionStats, *, q_offsets: torch.Tensor | None = None,
                              k_offsets: torch.Tensor | None = None, key_mask: torch.Tensor | None = None,
                              scale: float | None = None, workspace: torch.Tensor | None = None,
                              device_status: torch.Tensor | None = None) -> AttentionGrads:
     """Gradients of cross_attention from that of its output.
 
-    The other arguments are cross_attention's own, ``out`` and ``lse`` what it
-    returned.  Gradients have the tokens' type and are summed in a fixed order;
+    The other arguments are cross_attention's own, ``out`` and ``stats`` what
+    it returned.  Gradients have the tokens' type and are summed in a fixed order;
     rows from offsets[B] on are left alone.
     """
+    lse, rest = stats
     return AttentionGrads(*(blocks._module or blocks.load_binding()).cross_attention_backward(
-        q, k, v, q_offsets, k_offsets, key_mask, scale, d_out, out, lse, workspace, device_status))
+        q, k, v, q_offsets, k_offsets, key_mask, scale, d_out, out, lse, rest, workspace, device_status))
 
 
 def rotary_frequencies(sections: Sequence[int], base: float = 10000.0, device="cuda") -> torch.Tensor:

@@ -26,6 +26,7 @@ struct AttentionArgs {
   float scale;
   const uint8_t* mask;       // [k_rows], 0: key left out; or null
   void* out;                 // [q_rows, q_heads, dim]
+  void* rest;                // bf16 [q_rows, q_heads, dim], what the rounding of out left; or null
   float* lse;                // [q_rows, q_heads], or null (forward)
   // Backward.
   Heads d_out;
@@ -46,6 +47,8 @@ struct AttentionArgs {
 
 cudaError_t launch_attention_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 cudaError_t launch_attention_backward_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
+// bf16 whose rows and heads are 16-byte aligned, on the tensor cores.
+cudaError_t launch_attention_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream);
 // out (and lse) from the parts.
 cudaError_t launch_attention_join(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 // delta from out and d_out.

@@ -62,9 +62,9 @@ bool any_overlap(std::initializer_list<Extent> outs, std::initializer_list<Exten
 }
 
 // Strides of [rows, heads, dim] whose rows and heads do not overlap; strides that
-// nothing goes by are set to what a contiguous tensor has.
+// nothing goes by are set to ones that suit every kernel.
 bool strides_ok(Heads* x, int64_t rows, int64_t heads, int64_t dim) {
-  if (heads <= 1) x->head = dim;
+  if (heads <= 1) x->head = (dim + 7) / 8 * 8;
   if (rows <= 1) x->row = heads * x->head;
   if (x->row < dim || x->head < dim) return false;
   return x->row >= (heads - 1) * x->head + dim || x->head >= (rows - 1) * x->row + dim;
@@ -106,6 +106,14 @@ Plan plan_simt(const Shape& s) {
   return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 2),
           splits_for(s.k_rows, 64, s.kv_heads, s.q_rows * group, 64, s.batch, 2)};
 }
+
+// The tensor-core kernels' tiles.
+Plan plan_tc(const Shape& s) {
+  const Plan simt = plan_simt(s);
+  return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 1), simt.key_splits};
+}
+// Whether the tensor-core kernels can load a tensor: TMA's addresses and strides are multiples of 16 bytes.
+bool tc_heads(const Heads& x) { return vector_heads(x, 2, 8); }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t part_bytes(int splits, int64_t rows, int heads, int dim) {
@@ -168,7 +176,7 @@ extern "C" {
 size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads,
                                           int32_t head_dim, mpm_dtype dtype) {
   const Shape s{batch, q_rows, k_rows, q_heads, kv_heads, head_dim, dtype};
-  return check_shape(s) != MPM_OK ? 0 : forward_bytes(s, plan_simt(s));
+  return check_shape(s) != MPM_OK ? 0 : std::max(forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s)));
 }
 
 size_t mpm_cross_attention_backward_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads,
@@ -181,8 +189,9 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
                                int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
                                int64_t v_head_stride, const int64_t* q_offsets, const int64_t* k_offsets, int32_t batch,
                                int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                               mpm_dtype dtype, float scale, const uint8_t* key_mask, void* out, float* lse,
-                               void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream) {
+                               mpm_dtype dtype, float scale, const uint8_t* key_mask, void* out,
+                               void* out_rest, float* lse, void* workspace, size_t workspace_bytes,
+                               int32_t* device_status, void* stream) {
   const Range range("mpm_cross_attention");
   const Shape s{batch, q_rows, k_rows, q_heads, kv_heads, head_dim, dtype};
   mpm_status st = check_shape(s);
@@ -193,12 +202,15 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   if (q_rows == 0) return MPM_OK;
   if (out == nullptr) return MPM_ERR_INVALID_ARG;
   const int e = elem(dtype);
-  if (!aligned(out, e) || !aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
-  const Plan plan = plan_simt(s);
+  if (dtype == MPM_F32 && out_rest != nullptr) return MPM_ERR_UNSUPPORTED;
+  if (!aligned(out, e) || !aligned(out_rest, e) || !aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
+  const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv);
+  const Plan plan = tc ? plan_tc(s) : plan_simt(s);
   const size_t need = forward_bytes(s, plan);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads;
-  if (any_overlap({extent(out, q_values * head_dim * e), extent(lse, q_values * 4), extent(workspace, need),
+  if (any_overlap({extent(out, q_values * head_dim * e), extent(out_rest, q_values * head_dim * e), extent(lse, q_values * 4),
+                   extent(workspace, need),
                    extent(device_status, kStatusBytes)},
                   {extent(hq, q_rows, q_heads, head_dim, e), extent(hk, k_rows, kv_heads, head_dim, e),
                    extent(hv, k_rows, kv_heads, head_dim, e), offsets_extent(q_offsets, batch),
@@ -209,13 +221,14 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   if (st != MPM_OK) return st;
   mpm::AttentionArgs a = common_args(s, hq, hk, hv, q_offsets, k_offsets, scale, key_mask, device_status);
   a.out = out;
+  a.rest = out_rest;
   a.lse = lse;
   a.splits = plan.splits;
   a.partial = static_cast<float*>(workspace);
   a.partial_lse = a.partial + part_bytes(plan.splits, q_rows, q_heads, head_dim) / sizeof(float);
   a.vec = head_dim % 4 == 0 && vector_heads(hq, e, 4) && vector_heads(hk, e, 4) && vector_heads(hv, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
-  cudaError_t err = mpm::launch_attention_simt(a, dtype == MPM_BF16, sms, on);
+  cudaError_t err = tc ? mpm::launch_attention_tc(a, sms, on) : mpm::launch_attention_simt(a, dtype == MPM_BF16, sms, on);
   if (err == cudaSuccess && a.splits > 1) err = mpm::launch_attention_join(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }
@@ -223,7 +236,8 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
 mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_stride, int64_t d_out_head_stride,
                                         const void* q, int64_t q_row_stride, int64_t q_head_stride, const void* k,
                                         int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
-                                        int64_t v_head_stride, const void* out, const float* lse, const int64_t* q_offsets,
+                                        int64_t v_head_stride, const void* out, const void* out_rest,
+                                        const float* lse, const int64_t* q_offsets,
                                         const int64_t* k_offsets, int32_t batch, int64_t q_rows, int64_t k_rows,
                                         int32_t q_heads, int32_t kv_heads, int32_t head_dim, mpm_dtype dtype, float scale,
                                         const uint8_t* key_mask, void* d_q, void* d_k, void* d_v, void* workspace,
@@ -241,7 +255,8 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
       (k_rows > 0 && (d_k == nullptr || d_v == nullptr)))
     return MPM_ERR_INVALID_ARG;
   const int e = elem(dtype);
-  for (const void* p : {out, static_cast<const void*>(d_q), static_cast<const void*>(d_k), static_cast<const void*>(d_v)})
+  if (dtype == MPM_F32 && out_rest != nullptr) return MPM_ERR_UNSUPPORTED;
+  for (const void* p : {out, out_rest, static_cast<const void*>(d_q), static_cast<const void*>(d_k), static_cast<const void*>(d_v)})
     if (!aligned(p, e)) return MPM_ERR_ALIGNMENT;
   if (!aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
   const Plan plan = plan_simt(s);
@@ -252,7 +267,8 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
                    extent(device_status, kStatusBytes)},
                   {extent(hq, q_rows, q_heads, head_dim, e), extent(hg, q_rows, q_heads, head_dim, e),
                    extent(hk, k_rows, kv_heads, head_dim, e), extent(hv, k_rows, kv_heads, head_dim, e),
-                   extent(out, q_values * head_dim * e), extent(lse, q_values * 4), offsets_extent(q_offsets, batch),
+                   extent(out, q_values * head_dim * e), extent(out_rest, q_values * head_dim * e), extent(lse, q_values * 4),
+                   offsets_extent(q_offsets, batch),
                    offsets_extent(k_offsets, batch), extent(key_mask, static_cast<size_t>(k_rows))}))
     return MPM_ERR_ALIASING;
   int sms = 0;
@@ -261,6 +277,7 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
   mpm::AttentionArgs a = common_args(s, hq, hk, hv, q_offsets, k_offsets, scale, key_mask, device_status);
   a.d_out = hg;
   a.out = const_cast<void*>(out);
+  a.rest = const_cast<void*>(out_rest);
   a.stats = lse;
   a.d_q = d_q;
   a.d_k = d_k;

@@ -20,6 +20,13 @@ using norm::to_f32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// What the rounding of a value to T leaves, rounded to T (0 where it overflowed).
+template <typename T>
+__device__ __forceinline__ T rest_of(float v) {
+  const float r = v - to_f32(from_f32<T>(v));
+  return from_f32<T>(isfinite(r) ? r : 0.f);
+}
+
 struct Span {
   int64_t lo;
   int n;

@@ -137,19 +137,23 @@ __device__ __forceinline__ void put_scores(float* scores, const float (&v)[4][4]
     for (int j = 0; j < 4; ++j) scores[(4 * y + i) * kScorePitch + x + 16 * j] = v[i][j];
 }
 
-// The thread's sums, times a factor a row, to rows of `dim` contiguous values.
+// The thread's sums, times a factor a row, to rows of `dim` contiguous values, and
+// what their rounding left to rows of `rest`, if that is wanted.
 template <typename T, int DP>
 __device__ __forceinline__ void store_rows(T* out, int64_t row0, int rows, int heads, int head, int dim,
-                                           const float (&acc)[4][Shape<DP>::kCols], const float (&factor)[4]) {
+                                           const float (&acc)[4][Shape<DP>::kCols], const float (&factor)[4], T* rest = nullptr) {
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (4 * y + i >= rows) continue;
-    T* p = out + ((row0 + 4 * y + i) * heads + head) * dim;
+    const int64_t at = ((row0 + 4 * y + i) * heads + head) * dim;
 #pragma unroll
     for (int e = 0; e < Shape<DP>::kCols; ++e) {
       const int c = 4 * x + 64 * (e / 4) + e % 4;
-      if (c < dim) p[c] = from_f32<T>(acc[i][e] * factor[i]);
+      if (c >= dim) continue;
+      const float v = acc[i][e] * factor[i];
+      out[at + c] = from_f32<T>(v);
+      if (rest != nullptr) rest[at + c] = rest_of<T>(v);
     }
   }
 }
@@ -252,7 +256,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(const Attentio
     for (int i = 0; i < 4; ++i) factor[i] = sum[i] == 0.f ? 0.f : 1.f / sum[i];
     const int64_t part0 = a.splits == 1 ? 0 : static_cast<int64_t>(w.split) * a.q_rows * a.q_heads;
     if (a.splits == 1)
-      store_rows<T, DP>(static_cast<T*>(a.out), row0, rows, a.q_heads, w.head, a.dim, acc, factor);
+      store_rows<T, DP>(static_cast<T*>(a.out), row0, rows, a.q_heads, w.head, a.dim, acc, factor, static_cast<T*>(a.rest));
     else
       store_rows<float, DP>(a.partial + part0 * a.dim, row0, rows, a.q_heads, w.head, a.dim, acc, factor);
     float* lse = a.splits == 1 ? a.lse : a.partial_lse + part0;
@@ -452,7 +456,10 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(const Attentio
     T* out = static_cast<T*>(a.out) + r * a.dim;
 #pragma unroll
     for (int i = 0; i < kAttentionMaxDim / 32; ++i)
-      if (lane + 32 * i < a.dim) out[lane + 32 * i] = from_f32<T>(v[i]);
+      if (lane + 32 * i < a.dim) {
+        out[lane + 32 * i] = from_f32<T>(v[i]);
+        if (a.rest != nullptr) static_cast<T*>(a.rest)[r * a.dim + lane + 32 * i] = rest_of<T>(v[i]);
+      }
     if (a.lse != nullptr && lane == 0) a.lse[r] = (top + log2f(sum)) * kLn2;
   }
 }
@@ -469,9 +476,10 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(const Attenti
   const int64_t live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
   for (int64_t r = blockIdx.x * int64_t{kThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kThreads / 32}) {
     const T* o = static_cast<const T*>(a.out) + r * a.dim;
+    const T* rest = a.rest == nullptr ? nullptr : static_cast<const T*>(a.rest) + r * a.dim;
     const T* g = static_cast<const T*>(a.d_out.p) + a.d_out.row * (r / a.q_heads) + a.d_out.head * (r % a.q_heads);
     float s = 0.f;
-    for (int d = lane; d < a.dim; d += 32) s = fmaf(to_f32(o[d]), to_f32(g[d]), s);
+    for (int d = lane; d < a.dim; d += 32) s = fmaf(to_f32(o[d]) + (rest == nullptr ? 0.f : to_f32(rest[d])), to_f32(g[d]), s);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     if (lane == 0) a.delta[r] = s;

@@ -1,0 +1,226 @@
+// What the tensor-core attention kernels share: tiles of 128 rows by TMA, products
+// whose left operand lies in tensor memory, and the tables and waits of their roles.
+//
+// A tile is 128 rows of one head: per 64 features a block of 128 x 128 bytes in
+// the 128-byte swizzle.  The same bytes serve as an operand with the features
+// along K (scores: rows x rows) and, with the rows along K, as the right operand
+// of a product over rows (p v, ds k, ..): then the features are the contiguous
+// dimension, in blocks of 64 that lie a block apart, and eight rows of 128 bytes
+// are a group along K.  Features past the head's width read as zeros.
+#pragma once
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <atomic>
+
+#include "attention_common.cuh"
+#include "ptx.cuh"
+
+namespace mpm {
+namespace attn {
+
+constexpr int kRows = 128;                  // rows of a tile
+constexpr int kBlockBytes = kRows * 128;    // 64 features of a tile
+constexpr uint64_t kWaitNs = 2000000000ull;
+
+// Tokens as (feature, head, row); boxes of 64 features of one head of 128 rows.
+inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return static_cast<PFN_cuTensorMapEncodeTiled_v12000>(nullptr);
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+  }();
+  return fn;
+}
+inline bool map_heads(CUtensorMap* map, const Heads& x, int64_t rows, int heads, int dim) {
+  if (tensor_map_encoder() == nullptr) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
+  // A stride that nothing goes by still has to be a multiple of 16 bytes.
+  const int64_t head = heads > 1 ? x.head : (dim + 7) / 8 * 8, row = rows > 1 ? x.row : heads * head;
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(head) * 2, static_cast<cuuint64_t>(row) * 2};
+  const cuuint32_t box[3] = {64, 1, kRows}, each[3] = {1, 1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.p), dims, strides, box, each,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+__device__ __forceinline__ void load_block(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int32_t x, int32_t head,
+                                           int32_t row) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(ptx::smem_addr(bar)), "r"(x), "r"(head), "r"(row)
+      : "memory");
+}
+// A tile of H blocks, counted on `bar`.
+template <int H>
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int32_t head, int32_t row) {
+#pragma unroll
+  for (int h = 0; h < H; ++h) load_block(dst + h * kBlockBytes, map, bar, 64 * h, head, row);
+}
+
+// Instruction descriptors of kind::f16: bf16 operands, fp32 sums, M = 128.
+__host__ __device__ constexpr uint32_t by_features(uint32_t n) { return ptx::idesc_bf16_f32(kRows, n); }
+__host__ __device__ constexpr uint32_t by_rows(uint32_t n) { return ptx::idesc_bf16_f32(kRows, n) | (1u << 16); }  // B is N-major
+
+// Descriptor of a tile as the right operand with its rows along K: feature blocks
+// kBlockBytes apart (leading offset), groups of eight rows 1024 bytes apart (stride
+// offset), 128-byte swizzle.
+__device__ __forceinline__ uint64_t desc_by_rows(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(kBlockBytes >> 4) << 16) |
+         (static_cast<uint64_t>(1024u >> 4) << 32) | (static_cast<uint64_t>(1u) << 46) | (static_cast<uint64_t>(2u) << 61);
+}
+
+// D (+)= A B for one K = 16 slice with A in tensor memory.
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Scores of two tiles, [128 rows of a, 128 rows of b]: a sum over the features, `slices` times 16.
+template <int H>
+__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b, int slices) {
+  const uint64_t da = ptx::sdesc_k_sw128(a), db = ptx::sdesc_k_sw128(b);
+#pragma unroll
+  for (int s = 0; s < 4 * H; ++s) {
+    if (s < slices) {
+      const uint64_t at = static_cast<uint64_t>((s / 4) * (kBlockBytes >> 4) + (s % 4) * 2);
+      ptx::mma_bf16(d, da + at, db + at, by_features(kRows), s != 0 ? 1u : 0u);
+    }
+  }
+}
+// d [128, width] (+)= weights [128, 128 rows of b] (bf16 pairs in tensor memory) times b.
+__device__ __forceinline__ void mma_weighted(uint32_t d, uint32_t weights, uint32_t b, uint32_t idesc, bool accumulate) {
+  const uint64_t db = desc_by_rows(b);
+#pragma unroll
+  for (int s = 0; s < kRows / 16; ++s)
+    mma_tmem(d, weights + 8 * s, db + static_cast<uint64_t>(s * (2048 >> 4)), idesc, accumulate || s != 0 ? 1u : 0u);
+}
+
+// 32 lanes x 32 consecutive columns: thread t writes lane t.
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+      "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]),
+      "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Bounded wait of a whole warp: one answer for all of its lanes.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
+}
+
+// Place in a ring of SLOTS.
+template <int SLOTS>
+struct RingPlace {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == SLOTS) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// Which of the rows first .. first + 127 of a sequence are there: a bit each.
+// By a whole converged warp; every lane gets all four words.
+__device__ __forceinline__ uint4 rows_there(const Span& s, int first, const uint8_t* __restrict__ mask) {
+  const int lane = threadIdx.x & 31;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = first + 32 * i + lane;
+    w[i] = __ballot_sync(0xFFFFFFFFu, row < s.n && (mask == nullptr || __ldg(mask + s.lo + row) != 0));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Zeros the rows of a tile whose bit is not set, by a whole warp, for the tensor cores to read.
+template <int H>
+__device__ __forceinline__ void zero_rows(uint8_t* tile, const uint4& there) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t w[4] = {there.x, there.y, there.z, there.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (w[i] == 0xFFFFFFFFu) continue;
+    for (int r = lane / 8; r < 32; r += 4) {
+      if (w[i] >> r & 1u) continue;
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        *reinterpret_cast<uint4*>(tile + h * kBlockBytes + (32 * i + r) * 128 + lane % 8 * 16) = make_uint4(0, 0, 0, 0);
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+}
+
+// 32 of a head's features, from fp32, to a contiguous row; or what their rounding leaves (REST).
+template <typename T, bool REST = false>
+__device__ __forceinline__ void store_features(T* row, int first, int dim, bool vec, const uint32_t (&v)[32], float factor) {
+  if (vec && first + 32 <= dim) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        uint32_t u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float x = __uint_as_float(v[i + 2 * k]) * factor, y = __uint_as_float(v[i + 2 * k + 1]) * factor;
+          if constexpr (REST) {
+            x = to_f32(rest_of<T>(x));
+            y = to_f32(rest_of<T>(y));
+          }
+          u[k] = pack_bf16(x, y);
+        }
+        *reinterpret_cast<uint4*>(row + first + i) = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4)
+        *reinterpret_cast<float4*>(row + first + i) =
+            make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
+                        __uint_as_float(v[i + 3]) * factor);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (first + i < dim) {
+        const float x = __uint_as_float(v[i]) * factor;
+        row[first + i] = REST ? rest_of<T>(x) : from_f32<T>(x);
+      }
+  }
+}
+
+}  // namespace attn
+}  // namespace mpm

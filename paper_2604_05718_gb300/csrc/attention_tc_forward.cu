@@ -1,0 +1,531 @@
+// Attention between packed sequences on the tensor cores (bf16): scores, softmax
+// and the weighted sum of the values in one pass over the keys.
+//
+// A block takes 256 queries of one head, two tiles of 128 that share the keys, and
+// streams tiles of 128 keys.  Scores S (fp32) and sums O lie in tensor memory;
+// probabilities P (bf16) take S's place there and are the left operand of O += P V,
+// so that neither leaves the SM.  Roles:
+//   warps 0-3, 4-7  softmax of either tile, a row a thread: maximum, exponentials,
+//                   sum; they write P, and at the end O / sum to global memory
+//   warp 8          issues the products: P0 V, the next S0, P1 V, the next S1, so
+//                   that one tile's products run under the other's softmax
+//   warp 9          finds the work (sequence, tile, head) and loads it by TMA
+//   warp 10         zeros value rows that belong to no key of the sequence: a NaN
+//                   there would survive its weight of 0
+// O is not rescaled at every new maximum: exponents are taken from a maximum that is
+// up to 2^8 behind, and only a row that outgrows that makes its warp rescale (P, bf16,
+// has the range; the sums are fp32).
+#include "attention_tc.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+
+constexpr int kItemRows = 2 * kRows;
+constexpr int kSoftmaxWarps = 8;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kZeroWarp = 10;
+constexpr int kThreads = 11 * 32;
+constexpr int kItems = 3;             // work items known ahead
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kScoreCol = 0, kSumCol = 256;
+constexpr float kBehind = 8.f;        // log2 of how far a row's maximum may be behind
+
+template <int H>
+struct Shape {
+  static constexpr int kTileBytes = H * kBlockBytes;
+  static constexpr int kQueries = H == 1 ? 2 : 1;   // pairs of query tiles
+  static constexpr int kSlots = H == 1 ? 8 : 5;     // tiles of keys or values
+  static constexpr int kSmem = (2 * kQueries + kSlots) * kTileBytes;
+};
+
+// What the roles need of a work item.
+struct Work {
+  int64_t row0;     // first query row
+  int64_t key0;     // first key row of the sequence
+  int rows;         // queries from there on to the sequence's end
+  int keys;         // keys of the sequence
+  int begin, end;   // tiles of keys
+  int head, split;
+  int more;         // 0: the end
+};
+
+struct Control {
+  uint64_t q_full[2], q_empty[2];
+  uint64_t kv_full[8], kv_empty[8], kv_raw[8];
+  uint64_t s_full[2], p_full[2], o_done[2];
+  uint64_t work_full[kItems], work_empty[kItems];
+  uint64_t drain;
+  uint32_t tmem;
+  volatile int failed;
+  Work work[kItems];
+};
+
+template <int H>
+constexpr size_t smem_bytes() {
+  return 1024 + Shape<H>::kSmem + sizeof(Control);
+}
+static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "a block's shared memory");
+
+__device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
+  ctl->failed = 1;
+  report(status, MPM_ERR_DEVICE_TIMEOUT, role);
+}
+
+// Reads the next work item; false after a wait that ran out.
+__device__ __forceinline__ bool next_work(Control* ctl, RingPlace<kItems>& at, Work& w) {
+  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->failed)) return false;
+  w = ctl->work[at.slot];
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
+  at.next();
+  return true;
+}
+
+// Whether a tile of keys has rows that are no keys of the sequence.
+__device__ __forceinline__ bool ragged(int tile, int keys, const uint8_t* mask) {
+  return mask != nullptr || (tile + 1) * kRows > keys;
+}
+
+// Maximum of 32 scores, three at a time.
+__device__ __forceinline__ float max32(const uint32_t (&r)[32], float m) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) m = fmaxf(m, fmaxf(__uint_as_float(r[i]), __uint_as_float(r[i + 1])));
+  return m;
+}
+// Scores whose bit is not set to minus infinity.
+__device__ __forceinline__ void mask32(uint32_t (&r)[32], uint32_t there) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = there >> i & 1u ? r[i] : 0xFF800000u;
+}
+// 2^(s c - base) of 32 scores as bf16 pairs; their sum is added to sum.
+__device__ __forceinline__ void exp32(const uint32_t (&r)[32], float2 c, float2 base, float2& sum, uint32_t* p) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    float2 x = norm::fma(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c, base);
+    x.x = exp2_approx(x.x);
+    x.y = exp2_approx(x.y);
+    sum = norm::add(sum, x);
+    p[i / 2] = pack_bf16(x.x, x.y);
+  }
+}
+
+template <int H>
+__global__ void __launch_bounds__(kThreads, 1)
+    attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v, const AttentionArgs a, bool vec_out) {
+  using W = Shape<H>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
+  Control* ctl = reinterpret_cast<Control*>(smem + W::kSmem);
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
+  volatile int* abort_flag = &ctl->failed;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&ctl->q_full[i], 1);
+      ptx::mbar_init(&ctl->q_empty[i], 1);
+      ptx::mbar_init(&ctl->s_full[i], 1);
+      ptx::mbar_init(&ctl->p_full[i], 4);
+      ptx::mbar_init(&ctl->o_done[i], 1);
+    }
+    for (int i = 0; i < W::kSlots; ++i) {
+      ptx::mbar_init(&ctl->kv_full[i], 1);
+      ptx::mbar_init(&ctl->kv_empty[i], 1);
+      ptx::mbar_init(&ctl->kv_raw[i], 1);
+    }
+    for (int i = 0; i < kItems; ++i) {
+      ptx::mbar_init(&ctl->work_full[i], 1);
+      ptx::mbar_init(&ctl->work_empty[i], kSoftmaxWarps + 2);
+    }
+    ptx::mbar_init(&ctl->drain, 1);
+    ctl->failed = 0;
+    ptx::fence_barrier_init();
+    ptx::prefetch_tensor_map(&map_q);
+    ptx::prefetch_tensor_map(&map_k);
+    ptx::prefetch_tensor_map(&map_v);
+  }
+  if (warp == kMmaWarp) {
+    ptx::tmem_alloc(&ctl->tmem, kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = ctl->tmem;
+  wait_for_previous_grid();
+  allow_next_grid();
+
+  const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
+  const uint32_t ring0 = smem0 + 2 * W::kQueries * W::kTileBytes;
+
+  if (warp == kLoadWarp) {
+    // ---------------- work and loads ----------------
+    if (blockIdx.x == 0 && a.status != nullptr) {
+      for (int side = 0; side < 2; ++side) {
+        const int64_t* off = side == 0 ? a.q_offsets : a.k_offsets;
+        const int64_t rows = side == 0 ? a.q_rows : a.k_rows;
+        if (off == nullptr) continue;
+        for (int b = lane; b <= a.batch; b += 32) {
+          const int64_t v = __ldg(off + b);
+          if ((b == 0 ? v != 0 : v < __ldg(off + b - 1)) || (b == a.batch && v > rows)) report(a.status, MPM_ERR_DEVICE_CHECK, b);
+        }
+      }
+    }
+    RingPlace<kItems> at;
+    RingPlace<W::kQueries> qs;
+    RingPlace<W::kSlots> ks;
+    int q_loads = 0, kv_loads = 0;
+    uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on kv_raw, and that barrier's phase
+    bool ok = true;
+    const int64_t slots = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows), items = slots * a.q_heads * a.splits;
+    for (int64_t it = blockIdx.x;; it += gridDim.x) {
+      Work w{};
+      if (it < items) {
+        const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
+        if (tile.image < 0) continue;
+        const int64_t rest = it / slots;
+        const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
+        w.head = static_cast<int>(rest % a.q_heads);
+        w.split = static_cast<int>(rest / a.q_heads);
+        const Part part = part_of((keys.n + kRows - 1) / kRows, w.split, a.splits);
+        w.row0 = tile.rows.lo + tile.first;
+        w.key0 = keys.lo;
+        w.rows = tile.rows.n - tile.first;
+        w.keys = keys.n;
+        w.begin = part.begin;
+        w.end = part.end;
+        w.more = 1;
+      }
+      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
+        fail(ctl, a.status, 31);
+        break;
+      }
+      if (lane == 0) {
+        ctl->work[at.slot] = w;
+        ptx::mbar_arrive(&ctl->work_full[at.slot]);
+      }
+      __syncwarp();
+      at.next();
+      if (!w.more) break;
+      if (w.begin == w.end) continue;
+      const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
+      if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, abort_flag)) {
+        fail(ctl, a.status, 32);
+        break;
+      }
+      const bool two = w.rows > kRows;
+      if (ptx::elect_one()) {
+        const uint32_t dst = smem0 + qs.slot * 2 * W::kTileBytes;
+        ptx::mbar_arrive_expect_tx(&ctl->q_full[qs.slot], (two ? 2 : 1) * W::kTileBytes);
+        load_rows<H>(dst, &map_q, &ctl->q_full[qs.slot], w.head, row);
+        if (two) load_rows<H>(dst + W::kTileBytes, &map_q, &ctl->q_full[qs.slot], w.head, row + kRows);
+      }
+      __syncwarp();
+      qs.next();
+      ++q_loads;
+      const int kv = w.head / (a.q_heads / a.kv_heads);
+      for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
+        const int t = i / 2;
+        const bool value = i % 2 != 0, raw = value && ragged(t, w.keys, a.mask);
+        if (!warp_wait(&ctl->kv_empty[ks.slot], ks.phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 33);
+          ok = false;
+          break;
+        }
+        uint64_t* bar = raw ? &ctl->kv_raw[ks.slot] : &ctl->kv_full[ks.slot];
+        if (ptx::elect_one()) {
+          ptx::mbar_arrive_expect_tx(bar, W::kTileBytes);
+          load_rows<H>(ring0 + ks.slot * W::kTileBytes, value ? &map_v : &map_k, bar, kv, key + t * kRows);
+        }
+        __syncwarp();
+        const uint32_t bit = 1u << ks.slot;
+        if (raw) raw_phase ^= bit;
+        raw_loaded = raw ? raw_loaded | bit : raw_loaded & ~bit;
+        ks.next();
+        ++kv_loads;
+      }
+      if (!ok) break;
+    }
+    if (ctl->failed) {
+      // Copies under way land before the block ends.  A slot's last load completed phase (number of its loads - 1).
+      for (int s = 0; s < W::kQueries; ++s) {
+        const int n = (q_loads - s + W::kQueries - 1) / W::kQueries;
+        if (n > 0) warp_wait(&ctl->q_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+      }
+      for (int s = 0; s < W::kSlots; ++s) {
+        const int n = (kv_loads - s + W::kSlots - 1) / W::kSlots;
+        if (n <= 0) continue;
+        if (raw_loaded >> s & 1u) warp_wait(&ctl->kv_raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
+        else warp_wait(&ctl->kv_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+      }
+    }
+  } else if (warp == kZeroWarp) {
+    // ---------------- value rows that are no keys ----------------
+    RingPlace<kItems> at;
+    RingPlace<W::kSlots> ks;
+    uint32_t raw_phase = 0;
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 34);
+        break;
+      }
+      if (!w.more) break;
+      const Span keys{w.key0, w.keys};
+      for (int t = w.begin; ok && t < w.end; ++t) {
+        ks.next();
+        if (ragged(t, w.keys, a.mask)) {
+          const uint4 there = rows_there(keys, t * kRows, a.mask);
+          if (!warp_wait(&ctl->kv_raw[ks.slot], raw_phase >> ks.slot & 1u, abort_flag)) {
+            fail(ctl, a.status, 35);
+            ok = false;
+            break;
+          }
+          raw_phase ^= 1u << ks.slot;
+          zero_rows<H>(smem + 2 * W::kQueries * W::kTileBytes + ks.slot * W::kTileBytes, there);
+          if (lane == 0) ptx::mbar_arrive(&ctl->kv_full[ks.slot]);
+          __syncwarp();
+        }
+        ks.next();
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ---------------- products ----------------
+    RingPlace<kItems> at;
+    RingPlace<W::kQueries> qs;
+    RingPlace<W::kSlots> ks;
+    uint32_t p_phase[2] = {0, 0};
+    const int slices = (a.dim + 15) / 16;
+    const uint32_t weighted = by_rows(16 * slices);
+    const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 36);
+        break;
+      }
+      if (!w.more) break;
+      if (w.begin == w.end) continue;
+      const int tiles = w.rows > kRows ? 2 : 1;
+      const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
+      if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag) || !warp_wait(&ctl->kv_full[ks.slot], ks.phase, abort_flag)) {
+        fail(ctl, a.status, 37);
+        break;
+      }
+      ptx::tc_fence_after_sync();
+      if (ptx::elect_one()) {
+        for (int i = 0; i < tiles; ++i) {
+          mma_scores<H>(tmem0 + kScoreCol + i * kRows, q + i * W::kTileBytes, ring0 + ks.slot * W::kTileBytes, slices);
+          ptx::mma_commit(&ctl->s_full[i]);
+        }
+        ptx::mma_commit(&ctl->kv_empty[ks.slot]);
+        if (w.begin + 1 == w.end) ptx::mma_commit(&ctl->q_empty[qs.slot]);
+      }
+      __syncwarp();
+      ks.next();
+      for (int t = w.begin; ok && t < w.end; ++t) {
+        const bool last = t + 1 == w.end;
+        const RingPlace<W::kSlots> value = ks;
+        ks.next();
+        const RingPlace<W::kSlots> key = ks;  // the next tile's
+        if (!warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag) ||
+            (!last && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag))) {
+          fail(ctl, a.status, 38);
+          ok = false;
+          break;
+        }
+        for (int i = 0; i < tiles; ++i) {
+          if (!warp_wait(&ctl->p_full[i], p_phase[i], abort_flag)) {
+            fail(ctl, a.status, 39);
+            ok = false;
+            break;
+          }
+          p_phase[i] ^= 1u;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            mma_weighted(tmem0 + kSumCol + i * kRows, tmem0 + kScoreCol + i * kRows, ring0 + value.slot * W::kTileBytes, weighted,
+                         t != w.begin);
+            ptx::mma_commit(&ctl->o_done[i]);
+            if (!last) {
+              mma_scores<H>(tmem0 + kScoreCol + i * kRows, q + i * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
+              ptx::mma_commit(&ctl->s_full[i]);
+            }
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (ptx::elect_one()) {
+          ptx::mma_commit(&ctl->kv_empty[value.slot]);
+          if (!last) ptx::mma_commit(&ctl->kv_empty[key.slot]);
+          if (t + 2 == w.end) ptx::mma_commit(&ctl->q_empty[qs.slot]);
+        }
+        __syncwarp();
+        if (!last) ks.next();
+      }
+      qs.next();
+    }
+    if (ptx::elect_one()) ptx::mma_commit(&ctl->drain);
+    __syncwarp();
+    ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
+    __syncwarp();
+  } else {
+    // ---------------- softmax ----------------
+    const int tile = warp / 4;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t score = tmem + lanes + kScoreCol + tile * kRows, total = tmem + lanes + kSumCol + tile * kRows;
+    const int r = tile * kRows + (warp & 3) * 32 + lane;  // row within the item
+    const float c = a.scale * kLog2e;
+    RingPlace<kItems> at;
+    uint32_t s_phase = 0, o_phase = 0;  // o_phase: parity of the next product P V to complete
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 40);
+        break;
+      }
+      if (!w.more) break;
+      if (w.rows <= tile * kRows) continue;
+      float top = -INFINITY;  // the maximum that exponents are taken from, log2
+      float2 sum = make_float2(0.f, 0.f);
+      for (int t = w.begin; t < w.end; ++t) {
+        const bool cut = ragged(t, w.keys, a.mask);
+        uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (cut) there = rows_there({w.key0, w.keys}, t * kRows, a.mask);
+        if (!warp_wait(&ctl->s_full[tile], s_phase, abort_flag)) {
+          fail(ctl, a.status, 41);
+          ok = false;
+          break;
+        }
+        s_phase ^= 1u;
+        ptx::tc_fence_after_sync();
+        uint32_t s0[32], s1[32], s2[32], s3[32];
+        ptx::tmem_ld_32x32b_x32(score, s0);
+        ptx::tmem_ld_32x32b_x32(score + 32, s1);
+        ptx::tmem_ld_32x32b_x32(score + 64, s2);
+        ptx::tmem_ld_32x32b_x32(score + 96, s3);
+        ptx::tmem_wait_ld(s0);
+        ptx::tmem_wait_ld(s1);
+        ptx::tmem_wait_ld(s2);
+        ptx::tmem_wait_ld(s3);
+        if (cut) {
+          mask32(s0, there.x);
+          mask32(s1, there.y);
+          mask32(s2, there.z);
+          mask32(s3, there.w);
+        }
+        const float most = fmaxf(top, fmaxf(max32(s1, max32(s0, -INFINITY)), max32(s3, max32(s2, -INFINITY))) * c);
+        if (t == w.begin) {
+          top = most;
+        } else if (__any_sync(0xFFFFFFFFu, most > top + kBehind)) {
+          // O holds tiles up to t - 1 once their product has completed.
+          if (!warp_wait(&ctl->o_done[tile], o_phase ^ 1u, abort_flag)) {
+            fail(ctl, a.status, 42);
+            ok = false;
+            break;
+          }
+          ptx::tc_fence_after_sync();
+          const float f = most == -INFINITY ? 0.f : exp2_approx(top - most);
+          top = most;
+          sum = norm::mul(sum, make_float2(f, f));
+          // Sixteen columns at a time: the scores keep their registers.
+          for (int col = 0; col < a.dim; col += 16) {
+            uint32_t o[16];
+            ptx::tmem_ld_32x32b_x16(total + col, o);
+            ptx::tmem_wait_ld(o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st_x16(total + col, o);
+          }
+        }
+        o_phase ^= 1u;  // of the product of this tile
+        const float base = top == -INFINITY ? 0.f : -top;
+        const float2 c2 = make_float2(c, c), base2 = make_float2(base, base);
+        uint32_t p[32];
+        exp32(s0, c2, base2, sum, p);
+        exp32(s1, c2, base2, sum, p + 16);
+        tmem_st_x32(score, p);
+        exp32(s2, c2, base2, sum, p);
+        exp32(s3, c2, base2, sum, p + 16);
+        tmem_st_x32(score + 32, p);
+        tmem_wait_st();
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&ctl->p_full[tile]);
+      }
+      if (!ok) break;
+      if (w.end > w.begin) {
+        if (!warp_wait(&ctl->o_done[tile], o_phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 43);
+          break;
+        }
+        ptx::tc_fence_after_sync();
+      }
+      const float s = sum.x + sum.y, f = s == 0.f ? 0.f : 1.f / s;
+      const bool live = r < w.rows;
+      const int64_t at_row = (w.row0 + r) * a.q_heads + w.head + (a.splits == 1 ? 0 : w.split * a.q_rows * a.q_heads);
+      for (int col = 0; col < a.dim; col += 32) {
+        uint32_t o[32];
+        if (w.end > w.begin) {
+          ptx::tmem_ld_32x32b_x32(total + col, o);
+          ptx::tmem_wait_ld(o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0;
+        }
+        if (live) {
+          if (a.splits == 1) store_features(static_cast<__nv_bfloat16*>(a.out) + at_row * a.dim, col, a.dim, vec_out, o, f);
+          else store_features(a.partial + at_row * a.dim, col, a.dim, vec_out, o, f);
+          if (a.splits == 1 && a.rest != nullptr)
+            store_features<__nv_bfloat16, true>(static_cast<__nv_bfloat16*>(a.rest) + at_row * a.dim, col, a.dim, vec_out, o, f);
+        }
+        __syncwarp();
+      }
+      ptx::tc_fence_before_sync();
+      float* lse = a.splits == 1 ? a.lse : a.partial_lse;
+      if (live && lse != nullptr) lse[at_row] = (top + log2f(s)) * (a.splits == 1 ? kLn2 : 1.f);
+    }
+  }
+
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int H>
+cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  CUtensorMap q, k, v;
+  if (!map_heads(&q, a.q, a.q_rows, a.q_heads, a.dim)) return cudaErrorInvalidValue;
+  if (a.k_rows == 0) k = v = q;  // never loaded from
+  else if (!map_heads(&k, a.k, a.k_rows, a.kv_heads, a.dim) || !map_heads(&v, a.v, a.k_rows, a.kv_heads, a.dim))
+    return cudaErrorInvalidValue;
+  static std::atomic<uint64_t> attr_done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  const auto kernel = attention_tc_kernel<H>;
+  if (!(attr_done.load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<H>()));
+    if (e != cudaSuccess) return e;
+    attr_done.fetch_or(bit);
+  }
+  const int64_t items = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  const bool vec_out = a.dim % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.rest)) % 16 == 0;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < num_sms ? items : num_sms)), dim3(kThreads), smem_bytes<H>(),
+                          stream, q, k, v, a, vec_out);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  return a.dim <= 64 ? launch<1>(a, num_sms, stream) : launch<2>(a, num_sms, stream);
+}
+
+}  // namespace mpm

@@ -485,7 +485,7 @@ struct Scratch {
 PyObject* cross_attention(PyObject* const* p) {
   const AttentionInputs a(p);
   const OnDevice on(a.device);
-  at::Tensor out, lse;
+  at::Tensor out, lse, rest;
   void* pout;
   if (p[7] == Py_None) {
     out = new_like(*a.q, a.q->sizes(), a.q->scalar_type());
@@ -493,7 +493,10 @@ PyObject* cross_attention(PyObject* const* p) {
   } else {
     pout = buffer(p[7], "out", a.q->scalar_type(), a.device, a.q->sizes());
   }
-  if (truth(p[8])) lse = new_like(*a.q, {a.q->size(0), a.q->size(1)}, at::kFloat);
+  if (truth(p[8])) {
+    lse = new_like(*a.q, {a.q->size(0), a.q->size(1)}, at::kFloat);
+    if (a.dtype == MPM_BF16) rest = new_like(*a.q, a.q->sizes(), at::kBFloat16);
+  }
   const Scratch scratch(p[9],
                         entry.cross_attention_workspace_size(static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0),
                                                              a.q_heads, a.kv_heads, a.dim, a.dtype),
@@ -502,13 +505,14 @@ PyObject* cross_attention(PyObject* const* p) {
         entry.cross_attention(a.q->data_ptr(), a.q->stride(0), a.q->stride(1), a.k->data_ptr(), a.k->stride(0),
                               a.k->stride(1), a.v->data_ptr(), a.v->stride(0), a.v->stride(1), a.q_offsets, a.k_offsets,
                               static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0), a.q_heads, a.kv_heads, a.dim,
-                              a.dtype, a.scale, a.mask, pout, lse.defined() ? static_cast<float*>(lse.data_ptr()) : nullptr,
+                              a.dtype, a.scale, a.mask, pout, rest.defined() ? rest.data_ptr() : nullptr,
+                              lse.defined() ? static_cast<float*>(lse.data_ptr()) : nullptr,
                               scratch.p, scratch.bytes, status_word(p[10], a.device), on.stream));
   written(p[7]);
-  return tuple_of({out.defined() ? wrapped(out) : again(p[7]), wrapped(lse)});
+  return tuple_of({out.defined() ? wrapped(out) : again(p[7]), wrapped(lse), wrapped(rest)});
 }
 
-// cross_attention_backward(<AttentionInputs>, d_out, out, lse, workspace, device_status)
+// cross_attention_backward(<AttentionInputs>, d_out, out, lse, rest, workspace, device_status)
 PyObject* cross_attention_backward(PyObject* const* p) {
   const AttentionInputs a(p);
   const OnDevice on(a.device);
@@ -516,21 +520,22 @@ PyObject* cross_attention_backward(PyObject* const* p) {
   same_kind(*g, "d_out", *a.q);
   if (g->sizes() != a.q->sizes()) value_error("d_out", "must have q's shape");
   const void* out = buffer(p[8], "out", a.q->scalar_type(), a.device, a.q->sizes(), false);
+  const void* rest = buffer(p[10], "stats.rest", at::kBFloat16, a.device, a.q->sizes());
   const int64_t rows_heads[2] = {a.q->size(0), a.q->size(1)};
-  const float* lse = static_cast<float*>(buffer(p[9], "lse", at::kFloat, a.device, rows_heads, false));
+  const float* lse = static_cast<float*>(buffer(p[9], "stats.lse", at::kFloat, a.device, rows_heads, false));
   at::Tensor d_q = new_like(*a.q, a.q->sizes(), a.q->scalar_type());
   at::Tensor d_k = new_like(*a.k, a.k->sizes(), a.k->scalar_type()), d_v = new_like(*a.k, a.k->sizes(), a.k->scalar_type());
-  const Scratch scratch(p[10],
+  const Scratch scratch(p[11],
                         entry.cross_attention_backward_workspace_size(static_cast<int32_t>(a.batch), a.q->size(0),
                                                                       a.k->size(0), a.q_heads, a.kv_heads, a.dim, a.dtype),
                         *a.q);
   check("mpm_cross_attention_backward",
         entry.cross_attention_backward(
             g->data_ptr(), g->stride(0), g->stride(1), a.q->data_ptr(), a.q->stride(0), a.q->stride(1), a.k->data_ptr(),
-            a.k->stride(0), a.k->stride(1), a.v->data_ptr(), a.v->stride(0), a.v->stride(1), out, lse, a.q_offsets,
+            a.k->stride(0), a.k->stride(1), a.v->data_ptr(), a.v->stride(0), a.v->stride(1), out, rest, lse, a.q_offsets,
             a.k_offsets, static_cast<int32_t>(a.batch), a.q->size(0), a.k->size(0), a.q_heads, a.kv_heads, a.dim, a.dtype,
             a.scale, a.mask, d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), scratch.p, scratch.bytes,
-            status_word(p[11], a.device), on.stream));
+            status_word(p[12], a.device), on.stream));
   return tuple_of({wrapped(d_q), wrapped(d_k), wrapped(d_v)});
 }
 
@@ -636,7 +641,7 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"dequantize", fast<dequantize, 5>(), METH_FASTCALL, nullptr},
                          {"matmul", fast<matmul, 10>(), METH_FASTCALL, nullptr},
                          {"cross_attention", fast<cross_attention, 11>(), METH_FASTCALL, nullptr},
-                         {"cross_attention_backward", fast<cross_attention_backward, 12>(), METH_FASTCALL, nullptr},
+                         {"cross_attention_backward", fast<cross_attention_backward, 13>(), METH_FASTCALL, nullptr},
                          {"rotary", fast<rotary, 9>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blocks", "Binding of the encoder-block, attention and rotary entry points of libmpm.so.", -1,

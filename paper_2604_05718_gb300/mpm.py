@@ -83,9 +83,9 @@ def _declare(lib: ctypes.CDLL) -> None:
         "mpm_mxfp4_dequantize": (ctypes.c_int, [P, P, I64, I32, ctypes.c_int, P, I64, P]),
         "mpm_mxfp4_matmul": (ctypes.c_int, [P, P, I64, P, P, I32, I32, P, ctypes.c_int, P, I64, P, P]),
         "mpm_cross_attention": (ctypes.c_int, [P, I64, I64, P, I64, I64, P, I64, I64, P, P, I32, I64, I64, I32, I32, I32,
-                                               ctypes.c_int, F32, P, P, P, P, SZ, P, P]),
+                                               ctypes.c_int, F32, P, P, P, P, P, SZ, P, P]),
         "mpm_cross_attention_workspace_size": (SZ, [I32, I64, I64, I32, I32, I32, ctypes.c_int]),
-        "mpm_cross_attention_backward": (ctypes.c_int, [P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, I32,
+        "mpm_cross_attention_backward": (ctypes.c_int, [P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, P, I32,
                                                         I64, I64, I32, I32, I32, ctypes.c_int, F32, P, P, P, P, P, SZ, P,
                                                         P]),
         "mpm_cross_attention_backward_workspace_size": (SZ, [I32, I64, I64, I32, I32, I32, ctypes.c_int]),

@@ -71,7 +71,8 @@ def attention(q, k, v, d_out, q_offsets, k_offsets, mask, scale, probabilities=N
             ep = es + el + 8 * W
             t = gh @ vh.t()
             delta = (gh * o).sum(1, keepdim=True)
-            ed = (gh.abs() * r.out_bound[rows, h]).sum(1, keepdim=True) + dim * W * (gh.abs() * o.abs()).sum(1, keepdim=True)
+            # delta is taken from the output and what its rounding left.
+            ed = (gh.abs() * (eo + u * u * o.abs())).sum(1, keepdim=True) + dim * W * (gh.abs() * o.abs()).sum(1, keepdim=True)
             ds = p * (t - delta)
             eds = p * ((t - delta).abs() * (ep + 2 * W) + ed + (dim + 2) * W * (gh.abs() @ vh.abs().t())) + pu * ds.abs()
             r.d_q[rows, h] = scale * ds @ kh
