@@ -108,9 +108,11 @@ Plan plan_simt(const Shape& s) {
 }
 
 // The tensor-core kernels' tiles.
-Plan plan_tc(const Shape& s) {
-  const Plan simt = plan_simt(s);
-  return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 1), simt.key_splits};
+Plan plan_tc(const Shape& s) { return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 1), 1}; }
+Plan plan_tc_backward(const Shape& s) {
+  const int64_t group = s.q_heads / s.kv_heads;
+  return {splits_for(s.q_rows, 128, s.q_heads, s.k_rows, 128, s.batch, 1),
+          splits_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, 128, s.batch, 1)};
 }
 // Whether the tensor-core kernels can load a tensor: TMA's addresses and strides are multiples of 16 bytes.
 bool tc_heads(const Heads& x) { return vector_heads(x, 2, 8); }
@@ -129,6 +131,10 @@ size_t backward_bytes(const Shape& s, const Plan& p) {
   return delta_bytes(s) + std::max(part_bytes(p.splits, s.q_rows, s.q_heads, s.dim),
                                    part_bytes(p.key_splits, s.k_rows, s.kv_heads, 2 * s.dim));
 }
+
+// What a caller provides: enough for either kind of kernels, since the shape alone does not tell which runs.
+size_t forward_need(const Shape& s) { return std::max(forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s))); }
+size_t backward_need(const Shape& s) { return std::max(backward_bytes(s, plan_simt(s)), backward_bytes(s, plan_tc_backward(s))); }
 
 mpm::AttentionArgs common_args(const Shape& s, const Heads& q, const Heads& k, const Heads& v, const int64_t* q_offsets,
                                const int64_t* k_offsets, float scale, const uint8_t* mask, int32_t* status) {
@@ -176,13 +182,13 @@ extern "C" {
 size_t mpm_cross_attention_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads,
                                           int32_t head_dim, mpm_dtype dtype) {
   const Shape s{batch, q_rows, k_rows, q_heads, kv_heads, head_dim, dtype};
-  return check_shape(s) != MPM_OK ? 0 : std::max(forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s)));
+  return check_shape(s) != MPM_OK ? 0 : forward_need(s);
 }
 
 size_t mpm_cross_attention_backward_workspace_size(int32_t batch, int64_t q_rows, int64_t k_rows, int32_t q_heads,
                                                    int32_t kv_heads, int32_t head_dim, mpm_dtype dtype) {
   const Shape s{batch, q_rows, k_rows, q_heads, kv_heads, head_dim, dtype};
-  return check_shape(s) != MPM_OK ? 0 : backward_bytes(s, plan_simt(s));
+  return check_shape(s) != MPM_OK ? 0 : backward_need(s);
 }
 
 mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, const void* k,
@@ -206,7 +212,7 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   if (!aligned(out, e) || !aligned(out_rest, e) || !aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
   const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv);
   const Plan plan = tc ? plan_tc(s) : plan_simt(s);
-  const size_t need = forward_bytes(s, plan);
+  const size_t need = forward_need(s);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads;
   if (any_overlap({extent(out, q_values * head_dim * e), extent(out_rest, q_values * head_dim * e), extent(lse, q_values * 4),
@@ -259,8 +265,9 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
   for (const void* p : {out, out_rest, static_cast<const void*>(d_q), static_cast<const void*>(d_k), static_cast<const void*>(d_v)})
     if (!aligned(p, e)) return MPM_ERR_ALIGNMENT;
   if (!aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
-  const Plan plan = plan_simt(s);
-  const size_t need = backward_bytes(s, plan);
+  const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv) && tc_heads(hg);
+  const Plan plan = tc ? plan_tc_backward(s) : plan_simt(s);
+  const size_t need = backward_need(s);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads, k_bytes = static_cast<size_t>(k_rows) * kv_heads * head_dim * e;
   if (any_overlap({extent(d_q, q_values * head_dim * e), extent(d_k, k_bytes), extent(d_v, k_bytes), extent(workspace, need),
@@ -290,7 +297,8 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
           vector_heads(hg, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
   cudaError_t err = mpm::launch_attention_delta(a, dtype == MPM_BF16, sms, on);
-  if (err == cudaSuccess) err = mpm::launch_attention_backward_simt(a, dtype == MPM_BF16, sms, on);
+  if (err == cudaSuccess)
+    err = tc ? mpm::launch_attention_backward_tc(a, sms, on) : mpm::launch_attention_backward_simt(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }
 

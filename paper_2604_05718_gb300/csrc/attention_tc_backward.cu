@@ -1,0 +1,708 @@
+// Gradients of attention between packed sequences on the tensor cores (bf16).
+//
+//   p = exp(s - lse);  ds = p (d_out.v - delta)
+//   d_q = scale sum ds k;  d_k = scale sum ds q;  d_v = sum p d_out
+//
+// Two kernels, each with its sums in tensor memory from its first product to its
+// last: one keeps 128 queries and streams the keys (d_q), the other keeps 128 keys
+// and streams the queries of all heads that share them (d_k, d_v).  The scores and
+// d_out.v are formed in both, seven products where five would do; with five, d_q
+// would be summed across blocks, by atomics whose order changes the result, or
+// through memory (a partial d_q per 128 keys).
+//
+// In both, eight warps turn a tile of scores into ds, a row and 64 columns a thread,
+// and write it over their own columns of d_out.v in tensor memory, where it is the
+// left operand of the sums' products: columns c .. c + 63 become words c .. c + 31.
+// The streamed tiles serve twice, with their features and with their rows along K.
+// Rows that belong to no sequence, and masked keys, are zeroed in shared memory
+// where a sum runs over them, since a NaN survives a weight of 0.
+#include "attention_tc.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+
+constexpr int kWorkWarps = 8;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kZeroWarp = 10, kStatWarp = 11;
+constexpr int kThreads = 12 * 32;
+constexpr int kItems = 3;    // work items known ahead
+constexpr int kStats = 3;    // tiles of queries whose statistics are known ahead
+constexpr uint32_t kTmemCols = 512;
+
+template <int H>
+struct Shape {
+  static constexpr int kTileBytes = H * kBlockBytes;
+  static constexpr int kKept = H == 1 ? 2 : 1;    // pairs of kept tiles
+  static constexpr int kSlots = H == 1 ? 8 : 4;   // streamed tiles
+  static constexpr int kSmem = (2 * kKept + kSlots) * kTileBytes;
+};
+
+struct Work {
+  int64_t row0;     // first kept row
+  int64_t col0;     // first streamed row of the sequence
+  int rows;         // kept rows from there on to the sequence's end
+  int cols;         // streamed rows of the sequence
+  int begin, end;   // streamed tiles; over the group's heads one after the other for d_k, d_v
+  int head, split;
+  int more;         // 0: the end
+};
+
+struct Control {
+  uint64_t kept_full[2], kept_empty[2];
+  uint64_t full[8], empty[8], raw[8];
+  uint64_t s_full, s_free, p_full, sum_done;
+  uint64_t t_full[2], ds_full[2];  // of either place of d_out.v: d_q's products run a tile ahead
+  uint64_t work_full[kItems], work_empty[kItems];
+  uint64_t stat_full[kStats], stat_empty[kStats];
+  uint64_t drain;
+  uint32_t tmem;
+  volatile int failed;
+  Work work[kItems];
+  __align__(16) float lse[kStats][kRows];     // log2, +infinity where there is no query
+  __align__(16) float delta[kStats][kRows];
+};
+
+template <int H>
+constexpr size_t smem_bytes() {
+  return 1024 + Shape<H>::kSmem + sizeof(Control);
+}
+static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "a block's shared memory");
+
+__device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
+  ctl->failed = 1;
+  report(status, MPM_ERR_DEVICE_TIMEOUT, role);
+}
+
+__device__ __forceinline__ bool next_work(Control* ctl, RingPlace<kItems>& at, Work& w) {
+  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->failed)) return false;
+  w = ctl->work[at.slot];
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
+  at.next();
+  return true;
+}
+__device__ __forceinline__ void arrive_warp(uint64_t* bar) {
+  ptx::tc_fence_before_sync();
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(bar);
+}
+
+__device__ __forceinline__ bool ragged(int tile, int rows, const uint8_t* mask) {
+  return mask != nullptr || (tile + 1) * kRows > rows;
+}
+__device__ __forceinline__ float log2_stat(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// Sets a bit's value to `otherwise` where the bit is not set.
+__device__ __forceinline__ void keep32(uint32_t (&r)[32], uint32_t there, uint32_t otherwise) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = there >> i & 1u ? r[i] : otherwise;
+}
+
+// sums (+)= weights x tile, the weights as the warps leave them: 32 words from column 0 and 32 from column 64.
+__device__ __forceinline__ void mma_halves(uint32_t d, uint32_t weights, uint32_t b, uint32_t idesc, bool accumulate) {
+  const uint64_t db = desc_by_rows(b);
+#pragma unroll
+  for (int s = 0; s < kRows / 16; ++s)
+    mma_tmem(d, weights + (s / 4) * 64 + (s % 4) * 8, db + static_cast<uint64_t>(s * (2048 >> 4)), idesc,
+             accumulate || s != 0 ? 1u : 0u);
+}
+
+template <int H>
+__device__ __forceinline__ void init_control(Control* ctl, int work_readers, int stat_readers) {
+  using W = Shape<H>;
+  for (int i = 0; i < W::kKept; ++i) {
+    ptx::mbar_init(&ctl->kept_full[i], 1);
+    ptx::mbar_init(&ctl->kept_empty[i], 1);
+  }
+  for (int i = 0; i < W::kSlots; ++i) {
+    ptx::mbar_init(&ctl->full[i], 1);
+    ptx::mbar_init(&ctl->empty[i], 1);
+    ptx::mbar_init(&ctl->raw[i], 1);
+  }
+  ptx::mbar_init(&ctl->s_full, 1);
+  ptx::mbar_init(&ctl->sum_done, 1);
+  ptx::mbar_init(&ctl->s_free, kWorkWarps);
+  ptx::mbar_init(&ctl->p_full, kWorkWarps);
+  for (int i = 0; i < 2; ++i) {
+    ptx::mbar_init(&ctl->t_full[i], 1);
+    ptx::mbar_init(&ctl->ds_full[i], kWorkWarps);
+  }
+  for (int i = 0; i < kItems; ++i) {
+    ptx::mbar_init(&ctl->work_full[i], 1);
+    ptx::mbar_init(&ctl->work_empty[i], work_readers);
+  }
+  for (int i = 0; i < kStats; ++i) {
+    ptx::mbar_init(&ctl->stat_full[i], 1);
+    ptx::mbar_init(&ctl->stat_empty[i], stat_readers);
+  }
+  ptx::mbar_init(&ctl->drain, 1);
+  ctl->failed = 0;
+  ptx::fence_barrier_init();
+}
+
+// The statistics of 128 queries, by the statistics' warp; false after a wait that ran out.
+__device__ __forceinline__ bool put_stats(Control* ctl, RingPlace<kStats>& at, const AttentionArgs& a, int64_t row0, int rows,
+                                          int head) {
+  const int lane = threadIdx.x & 31;
+  float l[4], d[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = lane + 32 * i;
+    const int64_t p = (row0 + r) * a.q_heads + head;
+    l[i] = r < rows ? log2_stat(__ldg(a.stats + p)) : INFINITY;
+    d[i] = r < rows ? a.delta[p] : 0.f;
+  }
+  if (!warp_wait(&ctl->stat_empty[at.slot], at.phase ^ 1u, &ctl->failed)) return false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    ctl->lse[at.slot][lane + 32 * i] = l[i];
+    ctl->delta[at.slot][lane + 32 * i] = d[i];
+  }
+  __syncwarp();
+  if (lane == 0) ptx::mbar_arrive(&ctl->stat_full[at.slot]);
+  __syncwarp();
+  at.next();
+  return true;
+}
+
+// How a block's loads stand, for the wait before it leaves after a failure.
+template <int H>
+struct Loads {
+  int kept = 0, streamed = 0;
+  uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on raw, and that barrier's phase
+  __device__ __forceinline__ void count(int slot, bool raw) {
+    const uint32_t bit = 1u << slot;
+    if (raw) raw_phase ^= bit;
+    raw_loaded = raw ? raw_loaded | bit : raw_loaded & ~bit;
+    ++streamed;
+  }
+  __device__ __forceinline__ void drain(Control* ctl) const {
+    using W = Shape<H>;
+    for (int s = 0; s < W::kKept; ++s) {
+      const int n = (kept - s + W::kKept - 1) / W::kKept;
+      if (n > 0) warp_wait(&ctl->kept_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+    }
+    for (int s = 0; s < W::kSlots; ++s) {
+      const int n = (streamed - s + W::kSlots - 1) / W::kSlots;
+      if (n <= 0) continue;
+      // full and raw both complete once a use of the slot where the tile was zeroed; full alone otherwise.
+      if (raw_loaded >> s & 1u) warp_wait(&ctl->raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
+      else warp_wait(&ctl->full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+    }
+  }
+};
+
+// d_q: DQ.  Keeps a tile of queries and of d_out, streams keys and values.
+// Otherwise d_k and d_v: keeps keys and values, streams queries and d_out.
+template <int H, bool DQ>
+__global__ void __launch_bounds__(kThreads, 1)
+    attention_tc_backward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                 const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_g,
+                                 const AttentionArgs a, bool vec_out) {
+  using W = Shape<H>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
+  Control* ctl = reinterpret_cast<Control*>(smem + W::kSmem);
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
+  volatile int* abort_flag = &ctl->failed;
+
+  if (threadIdx.x == 0) {
+    init_control<H>(ctl, kWorkWarps + 3, kWorkWarps);
+    ptx::prefetch_tensor_map(&map_q);
+    ptx::prefetch_tensor_map(&map_k);
+    ptx::prefetch_tensor_map(&map_v);
+    ptx::prefetch_tensor_map(&map_g);
+  }
+  if (warp == kMmaWarp) {
+    ptx::tmem_alloc(&ctl->tmem, kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = ctl->tmem;
+  wait_for_previous_grid();
+  allow_next_grid();
+
+  const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
+  constexpr uint32_t kRing = 2 * W::kKept * W::kTileBytes;
+  const uint32_t ring0 = smem0 + kRing;
+  const int group = a.q_heads / a.kv_heads;
+  // Tensor memory: scores, then d_out.v (two of them for d_q), then the sums.
+  const uint32_t score_col = 0, t_col = 128, sum_col = DQ ? 384 : 256;
+
+  if (warp == kLoadWarp) {
+    // ---------------- work and loads ----------------
+    RingPlace<kItems> at;
+    RingPlace<W::kKept> kept;
+    RingPlace<W::kSlots> ring;
+    Loads<H> loads;
+    bool ok = true;
+    const int64_t* off = DQ ? a.q_offsets : a.k_offsets;
+    const int64_t rows = DQ ? a.q_rows : a.k_rows;
+    const int heads = DQ ? a.q_heads : a.kv_heads, splits = DQ ? a.splits : a.key_splits;
+    const int64_t slots = tile_slots<kRows>(off, a.batch, rows), items = slots * heads * splits;
+    for (int64_t it = blockIdx.x;; it += gridDim.x) {
+      Work w{};
+      if (it < items) {
+        const Tile tile = tile_of<kRows>(off, a.batch, rows, it % slots);
+        if (tile.image < 0) continue;
+        const int64_t rest = it / slots;
+        const Span cols = DQ ? span_of(a.k_offsets, tile.image, a.k_rows) : span_of(a.q_offsets, tile.image, a.q_rows);
+        w.head = static_cast<int>(rest % heads);
+        w.split = static_cast<int>(rest / heads);
+        const Part part = part_of((cols.n + kRows - 1) / kRows * (DQ ? 1 : group), w.split, splits);
+        w.row0 = tile.rows.lo + tile.first;
+        w.col0 = cols.lo;
+        w.rows = tile.rows.n - tile.first;
+        w.cols = cols.n;
+        w.begin = part.begin;
+        w.end = part.end;
+        w.more = 1;
+      }
+      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
+        fail(ctl, a.status, 51);
+        break;
+      }
+      if (lane == 0) {
+        ctl->work[at.slot] = w;
+        ptx::mbar_arrive(&ctl->work_full[at.slot]);
+      }
+      __syncwarp();
+      at.next();
+      if (!w.more) break;
+      if (w.begin == w.end) continue;
+      const int row = static_cast<int>(w.row0);
+      if (!warp_wait(&ctl->kept_empty[kept.slot], kept.phase ^ 1u, abort_flag)) {
+        fail(ctl, a.status, 52);
+        break;
+      }
+      if (ptx::elect_one()) {
+        uint64_t* bar = &ctl->kept_full[kept.slot];
+        const uint32_t dst = smem0 + kept.slot * 2 * W::kTileBytes;
+        ptx::mbar_arrive_expect_tx(bar, 2 * W::kTileBytes);
+        load_rows<H>(dst, DQ ? &map_q : &map_k, bar, w.head, row);
+        load_rows<H>(dst + W::kTileBytes, DQ ? &map_g : &map_v, bar, w.head, row);
+      }
+      __syncwarp();
+      kept.next();
+      ++loads.kept;
+      const int tiles = (w.cols + kRows - 1) / kRows;
+      for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
+        const int t = DQ ? i / 2 : i / 2 % tiles, head = DQ ? w.head / group : w.head * group + i / 2 / tiles;
+        const bool second = i % 2 != 0;
+        // Sums run over the keys for d_q, over the queries of both streamed tensors for d_k and d_v.
+        const bool raw = ragged(t, w.cols, DQ ? a.mask : nullptr) && !(DQ && second);
+        if (!warp_wait(&ctl->empty[ring.slot], ring.phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 53);
+          ok = false;
+          break;
+        }
+        uint64_t* bar = raw ? &ctl->raw[ring.slot] : &ctl->full[ring.slot];
+        if (ptx::elect_one()) {
+          ptx::mbar_arrive_expect_tx(bar, W::kTileBytes);
+          load_rows<H>(ring0 + ring.slot * W::kTileBytes, DQ ? (second ? &map_v : &map_k) : (second ? &map_g : &map_q), bar,
+                       head, static_cast<int>(w.col0) + t * kRows);
+        }
+        __syncwarp();
+        loads.count(ring.slot, raw);
+        ring.next();
+      }
+      if (!ok) break;
+    }
+    if (ctl->failed) loads.drain(ctl);
+  } else if (warp == kZeroWarp) {
+    // ---------------- rows that a sum must not see ----------------
+    RingPlace<kItems> at;
+    RingPlace<W::kSlots> ring;
+    uint32_t raw_phase = 0;
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 54);
+        break;
+      }
+      if (!w.more) break;
+      const Span cols{w.col0, w.cols};
+      const int tiles = (w.cols + kRows - 1) / kRows;
+      for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
+        const int t = DQ ? i / 2 : i / 2 % tiles;
+        const uint8_t* mask = DQ ? a.mask : nullptr;
+        if (ragged(t, w.cols, mask) && !(DQ && i % 2 != 0)) {
+          const uint4 there = rows_there(cols, t * kRows, mask);
+          if (!warp_wait(&ctl->raw[ring.slot], raw_phase >> ring.slot & 1u, abort_flag)) {
+            fail(ctl, a.status, 55);
+            ok = false;
+            break;
+          }
+          raw_phase ^= 1u << ring.slot;
+          zero_rows<H>(smem + kRing + ring.slot * W::kTileBytes, there);
+          if (lane == 0) ptx::mbar_arrive(&ctl->full[ring.slot]);
+          __syncwarp();
+        }
+        ring.next();
+      }
+    }
+  } else if (warp == kStatWarp) {
+    // ---------------- statistics of the queries ----------------
+    RingPlace<kItems> at;
+    RingPlace<kStats> stat;
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 56);
+        break;
+      }
+      if (!w.more) break;
+      if (DQ) {
+        if (w.begin != w.end) ok = put_stats(ctl, stat, a, w.row0, w.rows, w.head);
+      } else {
+        const int tiles = (w.cols + kRows - 1) / kRows;
+        for (int i = w.begin; ok && i < w.end; ++i)
+          ok = put_stats(ctl, stat, a, w.col0 + i % tiles * kRows, w.cols - i % tiles * kRows, w.head * group + i / tiles);
+      }
+      if (!ok) fail(ctl, a.status, 57);
+    }
+  } else if (warp == kMmaWarp) {
+    // ---------------- products ----------------
+    RingPlace<kItems> at;
+    RingPlace<W::kKept> kept;
+    RingPlace<W::kSlots> ring;
+    uint32_t free_phase = 1, p_phase = 0, ds_phase[2] = {0, 0};  // the first tile finds the scores' columns free
+    const int slices = (a.dim + 15) / 16;
+    const uint32_t weighted = by_rows(16 * slices);
+    const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 58);
+        break;
+      }
+      if (!w.more) break;
+      if (w.begin == w.end) continue;
+      const uint32_t mine = smem0 + kept.slot * 2 * W::kTileBytes;  // queries and d_out, or keys and values
+      if (!warp_wait(&ctl->kept_full[kept.slot], kept.phase, abort_flag)) {
+        fail(ctl, a.status, 59);
+        break;
+      }
+      // Scores and d_out.v of tile t; `last`: the kept tiles are not read after these.
+      auto scores = [&](const RingPlace<W::kSlots>& x) {
+        if (!warp_wait(&ctl->full[x.slot], x.phase, abort_flag)) return false;
+        if (DQ) {
+          if (!warp_wait(&ctl->s_free, free_phase, abort_flag)) return false;
+          free_phase ^= 1u;
+        }
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
+          mma_scores<H>(tmem0 + score_col, mine, ring0 + x.slot * W::kTileBytes, slices);
+          ptx::mma_commit(&ctl->s_full);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto seconds = [&](const RingPlace<W::kSlots>& y, int t) {
+        if (!warp_wait(&ctl->full[y.slot], y.phase, abort_flag)) return false;
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
+          mma_scores<H>(tmem0 + t_col + (DQ ? (t & 1) * 128 : 0), mine + W::kTileBytes, ring0 + y.slot * W::kTileBytes, slices);
+          ptx::mma_commit(&ctl->t_full[DQ ? t & 1 : 0]);
+          if (DQ) ptx::mma_commit(&ctl->empty[y.slot]);
+          if (t + 1 == w.end) ptx::mma_commit(&ctl->kept_empty[kept.slot]);
+        }
+        __syncwarp();
+        return true;
+      };
+      RingPlace<W::kSlots> x = ring, y = ring;
+      y.next();
+      ok = scores(x) && seconds(y, w.begin);
+      for (int t = w.begin; ok && t < w.end; ++t) {
+        const bool last = t + 1 == w.end;
+        RingPlace<W::kSlots> x1 = y, y1;
+        x1.next();
+        y1 = x1;
+        y1.next();
+        if constexpr (DQ) {
+          if (!last) ok = scores(x1) && seconds(y1, t + 1);
+          const int b = t & 1;
+          ok = ok && warp_wait(&ctl->ds_full[b], b == 0 ? ds_phase[0] : ds_phase[1], abort_flag);
+          if (!ok) break;
+          if (b == 0) ds_phase[0] ^= 1u;
+          else ds_phase[1] ^= 1u;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            mma_halves(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
+            ptx::mma_commit(&ctl->empty[x.slot]);
+            if (last) ptx::mma_commit(&ctl->sum_done);
+          }
+          __syncwarp();
+        } else {
+          ok = warp_wait(&ctl->p_full, p_phase, abort_flag);
+          if (!ok) break;
+          p_phase ^= 1u;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one())
+            mma_halves(tmem0 + sum_col, tmem0 + score_col, ring0 + y.slot * W::kTileBytes, weighted, t != w.begin);
+          __syncwarp();
+          if (!last) ok = scores(x1);
+          ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], abort_flag);
+          if (!ok) break;
+          ds_phase[0] ^= 1u;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            mma_halves(tmem0 + sum_col + 128, tmem0 + t_col, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
+            ptx::mma_commit(&ctl->empty[x.slot]);
+            ptx::mma_commit(&ctl->empty[y.slot]);
+            if (last) ptx::mma_commit(&ctl->sum_done);
+          }
+          __syncwarp();
+          if (!last) ok = seconds(y1, t + 1);
+        }
+        x = x1;
+        y = y1;
+      }
+      if (!ok) {
+        fail(ctl, a.status, 60);
+        break;
+      }
+      ring = x;
+      kept.next();
+    }
+    if (ptx::elect_one()) ptx::mma_commit(&ctl->drain);
+    __syncwarp();
+    ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
+    __syncwarp();
+  } else {
+    // ---------------- scores to ds ----------------
+    const int half = warp / 4;                      // columns 64 half .. + 63 of a tile
+    const int r = (warp & 3) * 32 + lane;           // row of a tile
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t score = tmem + lanes + score_col + half * 64;
+    const float c = a.scale * kLog2e;
+    const float2 c2 = make_float2(c, c);
+    RingPlace<kItems> at;
+    RingPlace<kStats> stat;
+    uint32_t s_phase = 0, t_phases = 0, sum_phase = 0;  // t_phases: a bit for either place of d_out.v
+    Work w;
+    bool ok = true;
+    while (ok) {
+      if (!next_work(ctl, at, w)) {
+        fail(ctl, a.status, 61);
+        break;
+      }
+      if (!w.more) break;
+      float2 base = make_float2(0.f, 0.f), less = base;  // of the thread's query (d_q)
+      if (DQ && w.begin != w.end) {
+        if (!warp_wait(&ctl->stat_full[stat.slot], stat.phase, abort_flag)) {
+          fail(ctl, a.status, 62);
+          break;
+        }
+        base.x = base.y = -ctl->lse[stat.slot][r];
+        less.x = less.y = -ctl->delta[stat.slot][r];
+        arrive_warp(&ctl->stat_empty[stat.slot]);
+        stat.next();
+      }
+      // Of the thread's key (d_k, d_v): all ones, or zeros where there is none.
+      uint32_t keep = 0xFFFFFFFFu;
+      if (!DQ && (r >= w.rows || (a.mask != nullptr && __ldg(a.mask + w.row0 + r) == 0))) keep = 0u;
+      for (int t = w.begin; t < w.end; ++t) {
+        const bool cut = DQ && ragged(t, w.cols, a.mask);
+        uint32_t there[2] = {~0u, ~0u};
+        if (cut) {
+          const uint4 all = rows_there({w.col0, w.cols}, t * kRows, a.mask);
+          there[0] = half == 0 ? all.x : all.z;
+          there[1] = half == 0 ? all.y : all.w;
+        }
+        if (!DQ && !warp_wait(&ctl->stat_full[stat.slot], stat.phase, abort_flag)) {
+          fail(ctl, a.status, 63);
+          ok = false;
+          break;
+        }
+        if (!warp_wait(&ctl->s_full, s_phase, abort_flag)) {
+          fail(ctl, a.status, 64);
+          ok = false;
+          break;
+        }
+        s_phase ^= 1u;
+        ptx::tc_fence_after_sync();
+        uint32_t p[2][32];
+        ptx::tmem_ld_32x32b_x32(score, p[0]);
+        ptx::tmem_ld_32x32b_x32(score + 32, p[1]);
+        ptx::tmem_wait_ld(p[0]);
+        ptx::tmem_wait_ld(p[1]);
+        if (DQ) arrive_warp(&ctl->s_free);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (cut) keep32(p[h], there[h], 0xFF800000u);
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float2 b0 = base, b1 = base;
+            if constexpr (!DQ) {
+              const float4 l = *reinterpret_cast<const float4*>(&ctl->lse[stat.slot][half * 64 + 32 * h + i]);
+              b0 = make_float2(-l.x, -l.y);
+              b1 = make_float2(-l.z, -l.w);
+            }
+            const float2 x = norm::fma(make_float2(__uint_as_float(p[h][i]), __uint_as_float(p[h][i + 1])), c2, b0);
+            const float2 y = norm::fma(make_float2(__uint_as_float(p[h][i + 2]), __uint_as_float(p[h][i + 3])), c2, b1);
+            p[h][i] = __float_as_uint(exp2_approx(x.x));
+            p[h][i + 1] = __float_as_uint(exp2_approx(x.y));
+            p[h][i + 2] = __float_as_uint(exp2_approx(y.x));
+            p[h][i + 3] = __float_as_uint(exp2_approx(y.y));
+          }
+        }
+        if constexpr (!DQ) {
+          uint32_t words[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            words[i] = pack_bf16(__uint_as_float(p[i / 16][2 * i % 32]), __uint_as_float(p[i / 16][2 * i % 32 + 1])) & keep;
+          tmem_st_x32(score, words);
+          tmem_wait_st();
+          arrive_warp(&ctl->p_full);
+        }
+        const int place = DQ ? t & 1 : 0;
+        if (!warp_wait(&ctl->t_full[place], t_phases >> place & 1u, abort_flag)) {
+          fail(ctl, a.status, 65);
+          ok = false;
+          break;
+        }
+        t_phases ^= 1u << place;
+        ptx::tc_fence_after_sync();
+        const uint32_t from = tmem + lanes + t_col + place * 128 + half * 64;
+        uint32_t words[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t d[32];
+          ptx::tmem_ld_32x32b_x32(from + 32 * h, d);
+          ptx::tmem_wait_ld(d);
+          if (cut) keep32(d, there[h], 0u);
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float2 l0 = less, l1 = less;
+            if constexpr (!DQ) {
+              const float4 e = *reinterpret_cast<const float4*>(&ctl->delta[stat.slot][half * 64 + 32 * h + i]);
+              l0 = make_float2(-e.x, -e.y);
+              l1 = make_float2(-e.z, -e.w);
+            }
+            const float2 x = norm::mul(norm::add(make_float2(__uint_as_float(d[i]), __uint_as_float(d[i + 1])), l0),
+                                       make_float2(__uint_as_float(p[h][i]), __uint_as_float(p[h][i + 1])));
+            const float2 y = norm::mul(norm::add(make_float2(__uint_as_float(d[i + 2]), __uint_as_float(d[i + 3])), l1),
+                                       make_float2(__uint_as_float(p[h][i + 2]), __uint_as_float(p[h][i + 3])));
+            words[16 * h + i / 2] = pack_bf16(x.x, x.y) & keep;
+            words[16 * h + i / 2 + 1] = pack_bf16(y.x, y.y) & keep;
+          }
+        }
+        tmem_st_x32(from, words);
+        tmem_wait_st();
+        arrive_warp(&ctl->ds_full[place]);
+        if (!DQ) {
+          arrive_warp(&ctl->stat_empty[stat.slot]);
+          stat.next();
+        }
+      }
+      if (!ok) break;
+      if (w.begin != w.end) {
+        if (!warp_wait(&ctl->sum_done, sum_phase, abort_flag)) {
+          fail(ctl, a.status, 66);
+          break;
+        }
+        sum_phase ^= 1u;
+        ptx::tc_fence_after_sync();
+      }
+      // Features 32 half .. in turns for d_q; one of the two sums a half for d_v and d_k.
+      const bool live = r < w.rows;
+      const int heads = DQ ? a.q_heads : a.kv_heads;
+      const int64_t row = (w.row0 + r) * heads + w.head, rows = (DQ ? a.q_rows : a.k_rows) * heads;
+      const uint32_t sums = tmem + lanes + sum_col + (DQ ? 0 : half * 128);
+      const float f = DQ || half == 1 ? a.scale : 1.f;
+      for (int col = DQ ? 32 * half : 0; col < a.dim; col += DQ ? 64 : 32) {
+        uint32_t v[32];
+        if (w.begin != w.end) {
+          ptx::tmem_ld_32x32b_x32(sums + col, v);
+          ptx::tmem_wait_ld(v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0;
+        }
+        if (live) {
+          if ((DQ ? a.splits : a.key_splits) == 1) {
+            void* out = DQ ? a.d_q : half == 0 ? a.d_v : a.d_k;
+            store_features(static_cast<__nv_bfloat16*>(out) + row * a.dim, col, a.dim, vec_out, v, f);
+          } else {
+            // Parts of d_k, then those of d_v.
+            const int64_t part = w.split + (DQ || half == 1 ? 0 : a.key_splits);
+            store_features(a.partial + (part * rows + row) * a.dim, col, a.dim, vec_out, v, f);
+          }
+        }
+        __syncwarp();
+      }
+      ptx::tc_fence_before_sync();
+    }
+  }
+
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int H, bool DQ>
+cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  CUtensorMap q, k, v, g;
+  // A side without rows is never loaded from.
+  if (a.q_rows > 0 && (!map_heads(&q, a.q, a.q_rows, a.q_heads, a.dim) || !map_heads(&g, a.d_out, a.q_rows, a.q_heads, a.dim)))
+    return cudaErrorInvalidValue;
+  if (a.k_rows > 0 && (!map_heads(&k, a.k, a.k_rows, a.kv_heads, a.dim) || !map_heads(&v, a.v, a.k_rows, a.kv_heads, a.dim)))
+    return cudaErrorInvalidValue;
+  if (a.q_rows == 0) q = g = k;
+  if (a.k_rows == 0) k = v = q;
+  static std::atomic<uint64_t> attr_done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  const auto kernel = attention_tc_backward_kernel<H, DQ>;
+  if (!(attr_done.load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<H>()));
+    if (e != cudaSuccess) return e;
+    attr_done.fetch_or(bit);
+  }
+  const int64_t items = DQ ? tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits
+                           : tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
+  const uintptr_t outs = DQ ? reinterpret_cast<uintptr_t>(a.d_q)
+                            : reinterpret_cast<uintptr_t>(a.d_k) | reinterpret_cast<uintptr_t>(a.d_v);
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < num_sms ? items : num_sms)), dim3(kThreads), smem_bytes<H>(),
+                          stream, q, k, v, g, a, a.dim % 8 == 0 && outs % 16 == 0);
+}
+
+template <int H>
+cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  cudaError_t e = cudaSuccess;
+  if (a.q_rows > 0) {
+    e = launch<H, true>(a, num_sms, stream);
+    if (e == cudaSuccess && a.splits > 1)
+      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, true, num_sms, stream);
+  }
+  if (e == cudaSuccess && a.k_rows > 0) {
+    e = launch<H, false>(a, num_sms, stream);
+    const int64_t each = a.k_rows * a.kv_heads * a.dim;
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, true, num_sms, stream);
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim,
+                               a.d_v, true, num_sms, stream);
+  }
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  return a.dim <= 64 ? backward<1>(a, num_sms, stream) : backward<2>(a, num_sms, stream);
+}
+
+}  // namespace mpm
