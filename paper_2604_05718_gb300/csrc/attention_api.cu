@@ -114,6 +114,27 @@ Plan plan_tc_backward(const Shape& s) {
   return {splits_for(s.q_rows, 128, s.q_heads, s.k_rows, 128, s.batch, 1),
           splits_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, 128, s.batch, 1)};
 }
+// Few queries: blocks of 16 rows, of the heads that share a kv head.  Taken where
+// the sequences' queries are so few on the mean (a longer sequence takes several
+// blocks, which read its keys again).
+struct FewPlan {
+  int queries, cluster, splits;  // queries 0: not taken
+};
+FewPlan plan_few(const Shape& s) {
+  const int64_t group = s.q_heads / s.kv_heads, sequences = std::min<int64_t>(s.batch, s.q_rows);
+  if (s.dtype != MPM_BF16 || s.dim % 8 != 0 || group > 16 || s.q_rows * group > 16 * sequences) return {0, 1, 1};
+  const int queries = static_cast<int>(16 / group);
+  const int64_t items = std::max((s.q_rows + queries - 1) / queries, sequences) * s.kv_heads;
+  const int64_t passes = (s.k_rows / std::max<int64_t>(1, std::min<int64_t>(s.batch, s.k_rows)) + 63) / 64;
+  int cluster = 1;
+  // One round of blocks, of which an SM holds three (head_dim <= 64) or two.
+  const int64_t resident = kSms * (s.dim <= 64 ? 3 : 2);
+  while (cluster < 8 && 2 * cluster <= passes && items * cluster * 2 <= resident) cluster *= 2;
+  int64_t splits = 1;
+  if (cluster == 8 && items * 8 < kSms) splits = std::max<int64_t>(1, std::min({2 * kSms / (items * 8), passes / 16, int64_t{mpm::kAttentionMaxSplits}}));
+  if ((s.q_rows / queries + s.batch) * s.kv_heads * splits * cluster > INT32_MAX) return {0, 1, 1};
+  return {queries, cluster, static_cast<int>(splits)};
+}
 // Whether the tensor-core kernels can load a tensor: TMA's addresses and strides are multiples of 16 bytes.
 bool tc_heads(const Heads& x) { return vector_heads(x, 2, 8); }
 
@@ -133,7 +154,10 @@ size_t backward_bytes(const Shape& s, const Plan& p) {
 }
 
 // What a caller provides: enough for either kind of kernels, since the shape alone does not tell which runs.
-size_t forward_need(const Shape& s) { return std::max(forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s))); }
+size_t forward_need(const Shape& s) {
+  const FewPlan few = plan_few(s);
+  return std::max({forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s)), forward_bytes(s, {few.splits, 1})});
+}
 size_t backward_need(const Shape& s) { return std::max(backward_bytes(s, plan_simt(s)), backward_bytes(s, plan_tc_backward(s))); }
 
 mpm::AttentionArgs common_args(const Shape& s, const Heads& q, const Heads& k, const Heads& v, const int64_t* q_offsets,
@@ -211,7 +235,8 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   if (dtype == MPM_F32 && out_rest != nullptr) return MPM_ERR_UNSUPPORTED;
   if (!aligned(out, e) || !aligned(out_rest, e) || !aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
   const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv);
-  const Plan plan = tc ? plan_tc(s) : plan_simt(s);
+  const FewPlan few = tc ? plan_few(s) : FewPlan{0, 1, 1};
+  const Plan plan = few.queries > 0 ? Plan{few.splits, 1} : tc ? plan_tc(s) : plan_simt(s);
   const size_t need = forward_need(s);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads;
@@ -234,7 +259,9 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   a.partial_lse = a.partial + part_bytes(plan.splits, q_rows, q_heads, head_dim) / sizeof(float);
   a.vec = head_dim % 4 == 0 && vector_heads(hq, e, 4) && vector_heads(hk, e, 4) && vector_heads(hv, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
-  cudaError_t err = tc ? mpm::launch_attention_tc(a, sms, on) : mpm::launch_attention_simt(a, dtype == MPM_BF16, sms, on);
+  cudaError_t err = few.queries > 0 ? mpm::launch_attention_few(a, few.queries, few.cluster, on)
+                    : tc            ? mpm::launch_attention_tc(a, sms, on)
+                                    : mpm::launch_attention_simt(a, dtype == MPM_BF16, sms, on);
   if (err == cudaSuccess && a.splits > 1) err = mpm::launch_attention_join(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }

@@ -55,8 +55,7 @@ struct Tile {
   int first;   // first row of the tile within the sequence
   Span rows;   // the sequence's rows
 };
-template <int T>
-__device__ __forceinline__ Tile tile_of(const int64_t* __restrict__ off, int batch, int64_t rows, int64_t slot) {
+__device__ __forceinline__ Tile tile_of(const int64_t* __restrict__ off, int batch, int64_t rows, int64_t slot, int T) {
   int b = 0;
   int64_t t = slot;
   if (off != nullptr) {
@@ -71,6 +70,10 @@ __device__ __forceinline__ Tile tile_of(const int64_t* __restrict__ off, int bat
   const Span s = span_of(off, b, rows);
   if (t < 0 || t * T >= s.n) return {-1, 0, s};
   return {b, static_cast<int>(t * T), s};
+}
+template <int T>
+__device__ __forceinline__ Tile tile_of(const int64_t* __restrict__ off, int batch, int64_t rows, int64_t slot) {
+  return tile_of(off, batch, rows, slot, T);
 }
 
 // Tiles [begin, end) of `tiles` that part `split` of `splits` takes.

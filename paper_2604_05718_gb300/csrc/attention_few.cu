@@ -1,0 +1,440 @@
+// Attention of a few queries to many keys (bf16): a pooling token, a decoding step,
+// a handful of mask queries.
+//
+// The queries of all heads that share a kv head are the rows of one 16-row operand,
+// so that a key is read once for all of them.  Bound: the bytes of keys and values;
+// the products (mma.sync, 16 x 8 x 16) are a quarter of that time, and a 128-row
+// tensor-core tile would be empty but for these rows.  A lane takes 16 contiguous
+// bytes of a key, four lanes 64, and the features come in that order on both sides
+// (a sum does not mind); its values are 16 bytes of four keys, interleaved in pairs
+// to the operand's layout.  So a lane reads nothing that it has not loaded itself:
+// shared memory is a queue of its own, filled steps ahead by asynchronous copies,
+// and no warp waits for another until the end.
+//
+// Four warps take the 16-key blocks of a block's part in turn, each with a running
+// maximum and sum of its own; maxima are updated only where a score outgrows the
+// last one by 2^8.  The warps' sums are joined in shared memory, those of the up to
+// eight blocks of a cluster, which share a sequence's keys, through distributed
+// shared memory: one launch, no scratch.  Where even eight blocks an item leave SMs
+// idle, items are split again and joined by a second kernel.
+#include <cuda.h>
+
+#include <atomic>
+
+#include "attention_common.cuh"
+#include "pair_ring.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+using pair::cluster_rank;
+using pair::cluster_sync;
+using pair::map_to_rank;
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kRowsM = 16;             // queries times heads of a block
+constexpr int kBlockKeys = 16;         // keys of a step
+constexpr int kPassKeys = kBlockKeys * kWarps;
+constexpr int kMaxCluster = 8;
+constexpr float kBehind = 8.f;
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 load16(const __nv_bfloat16* p, bool there) {
+  return there ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+}
+// 16 bytes to shared memory, zeros where there are none.
+__device__ __forceinline__ void copy16(uint32_t dst, const __nv_bfloat16* p) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const __nv_bfloat16* p, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 read16(uint32_t src) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+  return v;
+}
+__device__ __forceinline__ float remote(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+  return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+  return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+}
+
+// Steps under way: the queues of a block's lanes.
+template <int DP>
+struct Queue {
+  static constexpr int kChunks = DP / 32, kWide = DP / 64;
+  static constexpr int kPieces = 2 * kChunks + 4 * kWide;   // of a lane and step
+  static constexpr int kSteps = DP == 64 ? 4 : 3;
+  static constexpr int kBlocks = DP == 64 ? 3 : 2;          // an SM holds: 192 KB of queues
+  static constexpr int kBytes = kSteps * kPieces * kThreads * 16;
+};
+// What is joined at the end, in the queues' place.
+template <int DP>
+struct Smem {
+  float sums[kWarps][kRowsM][DP];
+  float top[kWarps][kRowsM], total[kWarps][kRowsM];
+  float joined[kRowsM][DP];
+  float joined_top[kRowsM], joined_total[kRowsM];
+};
+
+template <int DP>
+constexpr size_t smem_bytes() {
+  return sizeof(Smem<DP>) > Queue<DP>::kBytes ? sizeof(Smem<DP>) : Queue<DP>::kBytes;
+}
+
+// `queries` queries of `group` heads are a block's rows, row r being query r / group and head r % group.
+template <int DP>
+__global__ void __launch_bounds__(kThreads, Queue<DP>::kBlocks) attention_few_kernel(const AttentionArgs a, int queries, int cluster) {
+  extern __shared__ uint8_t smem_raw[];
+  Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(smem_raw);
+  constexpr int kChunks = DP / 32, kWide = DP / 64;
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {
+    check_offsets(a.q_offsets, a.batch, a.q_rows, a.status);
+    check_offsets(a.k_offsets, a.batch, a.k_rows, a.status);
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c4 = lane & 3;
+  const int group = a.q_heads / a.kv_heads;
+  const int64_t slots = a.q_offsets == nullptr ? (a.q_rows + queries - 1) / queries : a.q_rows / queries + a.batch;
+  // The kv heads of a sequence run side by side: their keys lie in the same rows.
+  const int64_t item = blockIdx.x / cluster, rest = item / a.kv_heads;
+  const int kv = static_cast<int>(item % a.kv_heads), split = static_cast<int>(rest / slots);
+  const Tile tile = tile_of(a.q_offsets, a.batch, a.q_rows, rest % slots, queries);
+  if (tile.image < 0) return;  // as the whole cluster
+  const uint32_t rank = cluster_rank();
+  const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
+  const Part part = part_of((keys.n + kPassKeys - 1) / kPassKeys, split * cluster + static_cast<int>(rank), a.splits * cluster);
+  const int first = part.begin * kPassKeys, last = min(part.end * kPassKeys, keys.n);
+  const int live = min(queries, tile.rows.n - tile.first) * group;  // rows
+
+  // The queries as the left operand.
+  uint32_t q[2 * kChunks][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = g + 8 * h;
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(a.q.p) +
+                             (r < live ? a.q.row * (tile.rows.lo + tile.first + r / group) + a.q.head * (kv * group + r % group) : 0);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      const int d = 32 * i + 8 * c4;
+      const uint4 u = load16(p + d, r < live && d < a.dim);
+      q[2 * i][h] = u.x;
+      q[2 * i][2 + h] = u.y;
+      q[2 * i + 1][h] = u.z;
+      q[2 * i + 1][2 + h] = u.w;
+    }
+  }
+  float o[8 * kWide][4] = {};
+  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+  const float c = a.scale * kLog2e;
+  const __nv_bfloat16* kp = static_cast<const __nv_bfloat16*>(a.k.p) + a.k.row * keys.lo + a.k.head * kv;
+  const __nv_bfloat16* vp = static_cast<const __nv_bfloat16*>(a.v.p) + a.v.row * keys.lo + a.v.head * kv;
+  const uint8_t* mask = a.mask == nullptr ? nullptr : a.mask + keys.lo;
+
+  constexpr int kSteps = Queue<DP>::kSteps, kStepBytes = Queue<DP>::kPieces * 32 * 16;
+  const uint32_t queue = ptx::smem_addr(smem_raw) + warp * kSteps * kStepBytes + lane * 16;
+  // The lane's pieces of a step: 64-byte runs of keys g + {0, 8}, then 16 bytes of
+  // the values of keys 2 c4 + {0, 1, 8, 9}.  Pointers run along, since forming an
+  // address anew takes as many instructions as the rest of the step.
+  const __nv_bfloat16* kl = kp + a.k.row * (first + kBlockKeys * warp + g) + 8 * c4;
+  const __nv_bfloat16* vl = vp + a.v.row * (first + kBlockKeys * warp + 2 * c4) + 8 * g;
+  const int64_t k_step = a.k.row * kPassKeys, v_step = a.v.row * kPassKeys;
+  int ahead = first + kBlockKeys * warp;  // the next step to fill
+  const bool whole = a.dim == DP;
+  auto fill = [&](int place) {
+    const uint32_t dst = queue + place * kStepBytes;
+    if (whole && ahead + kBlockKeys <= last) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) copy16(dst + (n * kChunks + i) * 512, kl + n * 8 * a.k.row + 32 * i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int m = 0; m < kWide; ++m)
+          copy16(dst + (2 * kChunks + i * kWide + m) * 512, vl + ((i & 1) + 8 * (i >> 1)) * a.v.row + 64 * m);
+    } else if (ahead < last) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const bool there = ahead + g + 8 * n < last && 32 * i + 8 * c4 < a.dim;
+          copy16(dst + (n * kChunks + i) * 512, there ? kl + n * 8 * a.k.row + 32 * i : kp, there);
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int m = 0; m < kWide; ++m) {
+          const int e = (i & 1) + 8 * (i >> 1);
+          const bool there = ahead + 2 * c4 + e < last && 64 * m + 8 * g < a.dim;
+          copy16(dst + (2 * kChunks + i * kWide + m) * 512, there ? vl + e * a.v.row + 64 * m : vp, there);
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    kl += k_step;
+    vl += v_step;
+    ahead += kPassKeys;
+  };
+  // Whether keys 2 c4 + {0, 1, 8, 9} of a step are there.
+  auto present = [&](int from) {
+    if (mask == nullptr && from + kBlockKeys <= last) return 15u;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = from + 2 * c4 + (i & 1) + 8 * (i >> 1);
+      bits |= static_cast<uint32_t>(key < last && (mask == nullptr || __ldg(mask + key) != 0)) << i;
+    }
+    return bits;
+  };
+  int at = first + kBlockKeys * warp, place = 0;
+#pragma unroll
+  for (int i = 0; i < kSteps - 1; ++i) fill(i);
+  uint32_t next = present(at);
+  for (; at < last; at += kPassKeys) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kSteps - 2) : "memory");
+    const uint32_t there = next, from = queue + place * kStepBytes;
+    next = present(at + kPassKeys);
+    uint4 kr[2][kChunks], vr[4][kWide];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) kr[n][i] = read16(from + (n * kChunks + i) * 512);
+    float s[2][4] = {}, s1[2][4] = {};  // in two sums each: half as many products wait for one another
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        mma_16816(s[n], q[2 * i], kr[n][i].x, kr[n][i].y);
+        mma_16816(s1[n], q[2 * i + 1], kr[n][i].z, kr[n][i].w);
+      }
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int m = 0; m < kWide; ++m) {
+        vr[i][m] = read16(from + (2 * kChunks + i * kWide + m) * 512);
+        if (there != 15u && !(there >> i & 1u)) vr[i][m] = make_uint4(0, 0, 0, 0);
+      }
+    // The place that was read a step ago is free.
+    fill(place == 0 ? kSteps - 1 : place - 1);
+    if (++place == kSteps) place = 0;
+    // s[n][2 h + e]: row g + 8 h, key 8 n + 2 c4 + e.
+    float most[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float& x = s[n][2 * h + e];
+          if (there != 15u) x = there >> (2 * n + e) & 1u ? x : -INFINITY;
+          most[h] = fmaxf(most[h], x);
+        }
+    most[0] *= c;  // positive: of the largest score the largest product
+    most[1] *= c;
+    if (__any_sync(0xFFFFFFFFu, most[0] > top[0] + kBehind || most[1] > top[1] + kBehind)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float m = fmaxf(top[h], quad_max(most[h]));
+        const float f = m == -INFINITY ? 0.f : ex2(top[h] - m);
+        top[h] = m;
+        sum[h] *= f;
+#pragma unroll
+        for (int j = 0; j < 8 * kWide; ++j) {
+          o[j][2 * h] *= f;
+          o[j][2 * h + 1] *= f;
+        }
+      }
+    }
+    uint32_t p[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float base = top[h] == -INFINITY ? 0.f : -top[h];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float x = ex2(fmaf(s[n][2 * h], c, base)), y = ex2(fmaf(s[n][2 * h + 1], c, base));
+        sum[h] += x + y;
+        p[2 * n + h] = pack(x, y);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < kWide; ++m) {
+      const uint32_t w[4][4] = {{vr[0][m].x, vr[0][m].y, vr[0][m].z, vr[0][m].w},
+                                {vr[1][m].x, vr[1][m].y, vr[1][m].z, vr[1][m].w},
+                                {vr[2][m].x, vr[2][m].y, vr[2][m].z, vr[2][m].w},
+                                {vr[3][m].x, vr[3][m].y, vr[3][m].z, vr[3][m].w}};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t which = j & 1 ? 0x7632u : 0x5410u;
+        mma_16816(o[8 * m + j], p, __byte_perm(w[0][j / 2], w[1][j / 2], which), __byte_perm(w[2][j / 2], w[3][j / 2], which));
+      }
+    }
+  }
+
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();  // the queues' place is taken
+  // o[8 m + j][2 h + e]: row g + 8 h, feature 64 m + 16 c4 + 8 e + j.
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float total = quad_sum(sum[h]);
+    if (c4 == 0) {
+      sm.top[warp][g + 8 * h] = top[h];
+      sm.total[warp][g + 8 * h] = total;
+    }
+#pragma unroll
+    for (int m = 0; m < kWide; ++m)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+          *reinterpret_cast<float4*>(&sm.sums[warp][g + 8 * h][64 * m + 16 * c4 + 8 * e + j]) =
+              make_float4(o[8 * m + j][2 * h + e], o[8 * m + j + 1][2 * h + e], o[8 * m + j + 2][2 * h + e], o[8 * m + j + 3][2 * h + e]);
+  }
+  __syncthreads();
+  for (int r = warp; r < live; r += kWarps) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm.top[w][r]);
+    float f[kWarps], total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      f[w] = sm.top[w][r] == -INFINITY && sm.total[w][r] == 0.f ? 0.f : ex2(sm.top[w][r] - (m == -INFINITY ? 0.f : m));
+      if (m == -INFINITY && sm.total[w][r] != 0.f) f[w] = 1.f;  // NaN without a maximum
+      total = fmaf(f[w], sm.total[w][r], total);
+    }
+#pragma unroll
+    for (int d = lane; d < DP; d += 32) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w)
+        if (f[w] != 0.f) v = fmaf(f[w], sm.sums[w][r][d], v);
+      sm.joined[r][d] = v;
+    }
+    if (lane == 0) {
+      sm.joined_top[r] = m;
+      sm.joined_total[r] = total;
+    }
+  }
+  cluster_sync();
+
+  // Row by row over the cluster's blocks, and over a block's warps.
+  const int64_t all = a.q_rows * a.q_heads;
+  for (int r = static_cast<int>(rank) * kWarps + warp; r < live; r += cluster * kWarps) {
+    // Lane b holds block b's statistics, and then its weight.
+    const float t = lane < cluster ? remote(map_to_rank(ptx::smem_addr(&sm.joined_top[r]), lane)) : -INFINITY;
+    const float n = lane < cluster ? remote(map_to_rank(ptx::smem_addr(&sm.joined_total[r]), lane)) : 0.f;
+    float part_sums[kMaxCluster][DP / 32];
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b)
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+        part_sums[b][i] = b < cluster ? remote(map_to_rank(ptx::smem_addr(&sm.joined[r][lane + 32 * i]), b)) : 0.f;
+    float m = t;
+#pragma unroll
+    for (int d = kMaxCluster / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    m = __shfl_sync(0xFFFFFFFFu, m, 0);
+    const float weight = n == 0.f ? 0.f : m == -INFINITY ? 1.f : ex2(t - m);  // no key there; NaN without a maximum
+    float total = weight * n;
+#pragma unroll
+    for (int d = kMaxCluster / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
+    total = __shfl_sync(0xFFFFFFFFu, total, 0);
+    float v[DP / 32] = {};
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b) {
+      const float f = __shfl_sync(0xFFFFFFFFu, weight, b);
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+        if (f != 0.f) v[i] = fmaf(f, part_sums[b][i], v[i]);
+    }
+    const float f = total == 0.f ? 0.f : 1.f / total;
+    const int64_t row = (tile.rows.lo + tile.first + r / group) * a.q_heads + kv * group + r % group;
+    if (a.splits == 1) {
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + row * a.dim;
+      __nv_bfloat16* left = a.rest == nullptr ? nullptr : static_cast<__nv_bfloat16*>(a.rest) + row * a.dim;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) {
+        if (lane + 32 * i >= a.dim) continue;
+        out[lane + 32 * i] = __float2bfloat16_rn(v[i] * f);
+        if (left != nullptr) left[lane + 32 * i] = rest_of<__nv_bfloat16>(v[i] * f);
+      }
+      if (a.lse != nullptr && lane == 0) a.lse[row] = (m + log2f(total)) * kLn2;
+    } else {
+      float* out = a.partial + (split * all + row) * a.dim;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+        if (lane + 32 * i < a.dim) out[lane + 32 * i] = v[i] * f;
+      if (lane == 0) a.partial_lse[split * all + row] = m + log2f(total);
+    }
+  }
+  cluster_sync();  // no block leaves while another reads its shared memory
+}
+
+template <int DP>
+cudaError_t launch(const AttentionArgs& a, int queries, int cluster, cudaStream_t stream) {
+  const int64_t slots = a.q_offsets == nullptr ? (a.q_rows + queries - 1) / queries : a.q_rows / queries + a.batch;
+  const int64_t blocks = slots * a.kv_heads * a.splits * cluster;
+  static std::atomic<uint64_t> attr_done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  const auto kernel = attention_few_kernel<DP>;
+  if (!(attr_done.load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<DP>()));
+    if (e != cudaSuccess) return e;
+    attr_done.fetch_or(bit);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem_bytes<DP>();
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a, queries, cluster);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_few(const AttentionArgs& a, int queries, int cluster, cudaStream_t stream) {
+  return a.dim <= 64 ? launch<64>(a, queries, cluster, stream) : launch<128>(a, queries, cluster, stream);
+}
+
+}  // namespace mpm
