@@ -323,9 +323,8 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
   a.vec = head_dim % 4 == 0 && vector_heads(hq, e, 4) && vector_heads(hk, e, 4) && vector_heads(hv, e, 4) &&
           vector_heads(hg, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
-  cudaError_t err = mpm::launch_attention_delta(a, dtype == MPM_BF16, sms, on);
-  if (err == cudaSuccess)
-    err = tc ? mpm::launch_attention_backward_tc(a, sms, on) : mpm::launch_attention_backward_simt(a, dtype == MPM_BF16, sms, on);
+  const cudaError_t err =
+      tc ? mpm::launch_attention_backward_tc(a, sms, on) : mpm::launch_attention_backward_simt(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }
 

@@ -87,14 +87,19 @@ __device__ __forceinline__ Part part_of(int tiles, int split, int splits) {
   return {begin, begin + per + (split < extra ? 1 : 0)};
 }
 
-// By all threads of one block of a launch: offsets that are not 0 = off[0] <= .. <= off[batch] <= rows.
-__device__ __forceinline__ void check_offsets(const int64_t* __restrict__ off, int batch, int64_t rows, int32_t* status) {
+// By the threads of one block of a launch, or of one of its warps: reports offsets
+// that are not 0 = off[0] <= .. <= off[batch] <= rows.
+__device__ __forceinline__ void check_offsets(const int64_t* __restrict__ off, int batch, int64_t rows, int32_t* status,
+                                              int first, int step) {
   if (off == nullptr || status == nullptr) return;
-  for (int b = threadIdx.x; b <= batch; b += blockDim.x) {
+  for (int b = first; b <= batch; b += step) {
     const int64_t v = __ldg(off + b);
     const bool bad = b == 0 ? v != 0 : v < __ldg(off + b - 1);
     if (bad || (b == batch && v > rows)) report(status, MPM_ERR_DEVICE_CHECK, b);
   }
+}
+__device__ __forceinline__ void check_offsets(const int64_t* __restrict__ off, int batch, int64_t rows, int32_t* status) {
+  check_offsets(off, batch, rows, status, threadIdx.x, blockDim.x);
 }
 
 }  // namespace attn

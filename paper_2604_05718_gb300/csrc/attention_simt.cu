@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(const Attentio
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) attention_delta_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) attention_delta_kernel(const AttentionArgs a, bool wide) {
   wait_for_previous_grid();
   allow_next_grid();
   if (blockIdx.x == 0) {
@@ -474,6 +474,36 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(const Attenti
   }
   const int lane = threadIdx.x & 31;
   const int64_t live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      // Eight features a lane, eight or sixteen lanes a row and head.
+      const int lanes = a.dim <= 64 ? 8 : 16, d = lane % lanes * 8, each = 32 / lanes;
+      const bool there = d < a.dim;
+      const int64_t step = gridDim.x * int64_t{kThreads} / lanes;
+      for (int64_t first = (blockIdx.x * int64_t{kThreads} + threadIdx.x) / 32 * each; first < live; first += step) {
+        const int64_t r = first + lane / lanes;
+        float v = 0.f;
+        if (there && r < live) {
+          const int64_t row = r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.q_heads) : r / a.q_heads;
+          const uint4 o = ld_stream(reinterpret_cast<const uint4*>(static_cast<const T*>(a.out) + r * a.dim + d));
+          uint4 e = make_uint4(0, 0, 0, 0);
+          if (a.rest != nullptr) e = ld_stream(reinterpret_cast<const uint4*>(static_cast<const T*>(a.rest) + r * a.dim + d));
+          const uint4 g = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.d_out.p) + a.d_out.row * row +
+                                                               a.d_out.head * (r - row * a.q_heads) + d));
+          const norm::F8 fo = norm::widen(o), fe = norm::widen(e), fg = norm::widen(g);
+          float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s = norm::fma(norm::add(fo.p[k], fe.p[k]), fg.p[k], s);
+          v = s.x + s.y;
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1)
+          if (x < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, x);
+        if (d == 0 && r < live) a.delta[r] = v;
+      }
+      return;
+    }
+  }
   for (int64_t r = blockIdx.x * int64_t{kThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kThreads / 32}) {
     const T* o = static_cast<const T*>(a.out) + r * a.dim;
     const T* rest = a.rest == nullptr ? nullptr : static_cast<const T*>(a.rest) + r * a.dim;
@@ -523,9 +553,9 @@ cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
   constexpr size_t smem = sizeof(float) * (4 * Shape<DP>::kMatrix + kScores);
   const int64_t q_items = tile_slots<kTile>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
   const int64_t k_items = tile_slots<kTile>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
-  cudaError_t e = cudaSuccess;
   constexpr bool bf16 = sizeof(T) == 2;
-  if (a.q_rows > 0) {
+  cudaError_t e = launch_attention_delta(a, bf16, num_sms, stream);
+  if (e == cudaSuccess && a.q_rows > 0) {
     e = launch_tiles(attention_simt_dq_kernel<T, DP>, smem, q_items, a, num_sms, stream);
     if (e == cudaSuccess && a.splits > 1)
       e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, bf16, num_sms, stream);
@@ -562,8 +592,10 @@ cudaError_t launch_attention_join(const AttentionArgs& a, bool bf16, int num_sms
 
 cudaError_t launch_attention_delta(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
   const int blocks = blocks_for((a.q_rows * a.q_heads + 7) / 8, int64_t{num_sms} * 8);
-  return bf16 ? launch_dependent(attention_delta_kernel<__nv_bfloat16>, dim3(blocks), dim3(kThreads), 0, stream, a)
-              : launch_dependent(attention_delta_kernel<float>, dim3(blocks), dim3(kThreads), 0, stream, a);
+  const uintptr_t all = reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.rest) | reinterpret_cast<uintptr_t>(a.d_out.p);
+  const bool wide = bf16 && a.dim % 8 == 0 && all % 16 == 0 && a.d_out.row % 8 == 0 && a.d_out.head % 8 == 0;
+  return bf16 ? launch_dependent(attention_delta_kernel<__nv_bfloat16>, dim3(blocks), dim3(kThreads), 0, stream, a, wide)
+              : launch_dependent(attention_delta_kernel<float>, dim3(blocks), dim3(kThreads), 0, stream, a, wide);
 }
 
 cudaError_t launch_attention_sum(const float* parts, int splits, int64_t rows, const int64_t* offsets, int batch, int heads,

@@ -186,39 +186,60 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, const uint4& there) {
   __syncwarp();
 }
 
-// 32 of a head's features, from fp32, to a contiguous row; or what their rounding leaves (REST).
-template <typename T, bool REST = false>
-__device__ __forceinline__ void store_features(T* row, int first, int dim, bool vec, const uint32_t (&v)[32], float factor) {
-  if (vec && first + 32 <= dim) {
-    if constexpr (sizeof(T) == 2) {
+// 32 features of a warp's 32 rows, a row a lane, times a factor a row, to global
+// memory: as bf16, or what that rounding leaves (REST).  They change places in 2 KB
+// of shared memory, so that a store's lanes write whole 64-byte runs of eight rows;
+// lane by lane, 16 bytes of 32 rows at a time, the stores of 1024 rows of 80
+// features took longer than all else.
+constexpr int kStageBytes = 32 * 64;
+template <bool REST>
+__device__ __forceinline__ void store_rows32(__nv_bfloat16* first_row, int64_t pitch, int rows, int col, int dim, bool vec,
+                                             uint8_t* stage, const uint32_t (&v)[32], float factor) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-      for (int i = 0; i < 32; i += 8) {
-        uint32_t u[4];
+  for (int p = 0; p < 4; ++p) {
+    uint32_t u[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float x = __uint_as_float(v[i + 2 * k]) * factor, y = __uint_as_float(v[i + 2 * k + 1]) * factor;
-          if constexpr (REST) {
-            x = to_f32(rest_of<T>(x));
-            y = to_f32(rest_of<T>(y));
-          }
-          u[k] = pack_bf16(x, y);
-        }
-        *reinterpret_cast<uint4*>(row + first + i) = make_uint4(u[0], u[1], u[2], u[3]);
+    for (int k = 0; k < 4; ++k) {
+      float x = __uint_as_float(v[8 * p + 2 * k]) * factor, y = __uint_as_float(v[8 * p + 2 * k + 1]) * factor;
+      if constexpr (REST) {
+        x = to_f32(rest_of<__nv_bfloat16>(x));
+        y = to_f32(rest_of<__nv_bfloat16>(y));
       }
-    } else {
+      u[k] = pack_bf16(x, y);
+    }
+    *reinterpret_cast<uint4*>(stage + lane * 64 + ((p ^ (lane >> 1 & 3)) * 16)) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  __syncwarp();
+  if (vec) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 4)
-        *reinterpret_cast<float4*>(row + first + i) =
-            make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
-                        __uint_as_float(v[i + 3]) * factor);
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + lane / 4, p = lane & 3;
+      if (row < rows && col + 8 * p < dim)
+        *reinterpret_cast<uint4*>(first_row + row * pitch + col + 8 * p) =
+            *reinterpret_cast<const uint4*>(stage + row * 64 + ((p ^ (row >> 1 & 3)) * 16));
     }
   } else {
+    for (int row = 0; row < rows; ++row)
+      if (col + lane < dim)
+        first_row[row * pitch + col + lane] = *reinterpret_cast<const __nv_bfloat16*>(
+            stage + row * 64 + (((lane / 8) ^ (row >> 1 & 3)) * 16) + lane % 8 * 2);
+  }
+  __syncwarp();
+}
+// 32 features of a row to a part's fp32 row.
+__device__ __forceinline__ void store_part32(float* row, int col, int dim, bool vec, const uint32_t (&v)[32], float factor) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (first + i < dim) {
-        const float x = __uint_as_float(v[i]) * factor;
-        row[first + i] = REST ? rest_of<T>(x) : from_f32<T>(x);
-      }
+  for (int i = 0; i < 32; i += 4) {
+    if (vec && col + i < dim) {
+      *reinterpret_cast<float4*>(row + col + i) =
+          make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
+                      __uint_as_float(v[i + 3]) * factor);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + i + e < dim) row[col + i + e] = __uint_as_float(v[i + e]) * factor;
+    }
   }
 }
 

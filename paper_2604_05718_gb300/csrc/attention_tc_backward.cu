@@ -35,7 +35,8 @@ struct Shape {
   static constexpr int kTileBytes = H * kBlockBytes;
   static constexpr int kKept = H == 1 ? 2 : 1;    // pairs of kept tiles
   static constexpr int kSlots = H == 1 ? 8 : 4;   // streamed tiles
-  static constexpr int kSmem = (2 * kKept + kSlots) * kTileBytes;
+  static constexpr int kStage = (2 * kKept + kSlots) * kTileBytes;  // the gradients on their way
+  static constexpr int kSmem = kStage + kWorkWarps * kStageBytes;
 };
 
 struct Work {
@@ -483,6 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t score = tmem + lanes + score_col + half * 64;
     const float c = a.scale * kLog2e;
     const float2 c2 = make_float2(c, c);
+    uint8_t* stage = smem + W::kStage + warp * kStageBytes;
     RingPlace<kItems> at;
     RingPlace<kStats> stat;
     uint32_t s_phase = 0, t_phases = 0, sum_phase = 0;  // t_phases: a bit for either place of d_out.v
@@ -626,15 +628,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = 0;
         }
-        if (live) {
-          if ((DQ ? a.splits : a.key_splits) == 1) {
-            void* out = DQ ? a.d_q : half == 0 ? a.d_v : a.d_k;
-            store_features(static_cast<__nv_bfloat16*>(out) + row * a.dim, col, a.dim, vec_out, v, f);
-          } else {
-            // Parts of d_k, then those of d_v.
-            const int64_t part = w.split + (DQ || half == 1 ? 0 : a.key_splits);
-            store_features(a.partial + (part * rows + row) * a.dim, col, a.dim, vec_out, v, f);
-          }
+        if ((DQ ? a.splits : a.key_splits) == 1) {
+          void* out = DQ ? a.d_q : half == 0 ? a.d_v : a.d_k;
+          store_rows32<false>(static_cast<__nv_bfloat16*>(out) + ((w.row0 + r - lane) * heads + w.head) * a.dim,
+                              static_cast<int64_t>(heads) * a.dim, min(32, w.rows - (r - lane)), col, a.dim, vec_out, stage, v, f);
+        } else if (live) {
+          // Parts of d_k, then those of d_v.
+          const int64_t part = w.split + (DQ || half == 1 ? 0 : a.key_splits);
+          store_part32(a.partial + (part * rows + row) * a.dim, col, a.dim, vec_out, v, f);
         }
         __syncwarp();
       }
@@ -681,8 +682,8 @@ cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
 
 template <int H>
 cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
-  cudaError_t e = cudaSuccess;
-  if (a.q_rows > 0) {
+  cudaError_t e = launch_attention_delta(a, true, num_sms, stream);
+  if (e == cudaSuccess && a.q_rows > 0) {
     e = launch<H, true>(a, num_sms, stream);
     if (e == cudaSuccess && a.splits > 1)
       e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, true, num_sms, stream);

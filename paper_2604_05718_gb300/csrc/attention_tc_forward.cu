@@ -35,8 +35,9 @@ template <int H>
 struct Shape {
   static constexpr int kTileBytes = H * kBlockBytes;
   static constexpr int kQueries = H == 1 ? 2 : 1;   // pairs of query tiles
-  static constexpr int kSlots = H == 1 ? 8 : 5;     // tiles of keys or values
-  static constexpr int kSmem = (2 * kQueries + kSlots) * kTileBytes;
+  static constexpr int kSlots = H == 1 ? 8 : 4;     // tiles of keys or values
+  static constexpr int kStage = (2 * kQueries + kSlots) * kTileBytes;  // the output on its way
+  static constexpr int kSmem = kStage + kSoftmaxWarps * kStageBytes;
 };
 
 // What the roles need of a work item.
@@ -161,16 +162,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kLoadWarp) {
     // ---------------- work and loads ----------------
-    if (blockIdx.x == 0 && a.status != nullptr) {
-      for (int side = 0; side < 2; ++side) {
-        const int64_t* off = side == 0 ? a.q_offsets : a.k_offsets;
-        const int64_t rows = side == 0 ? a.q_rows : a.k_rows;
-        if (off == nullptr) continue;
-        for (int b = lane; b <= a.batch; b += 32) {
-          const int64_t v = __ldg(off + b);
-          if ((b == 0 ? v != 0 : v < __ldg(off + b - 1)) || (b == a.batch && v > rows)) report(a.status, MPM_ERR_DEVICE_CHECK, b);
-        }
-      }
+    if (blockIdx.x == 0) {
+      check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
+      check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
+      __syncwarp();
     }
     RingPlace<kItems> at;
     RingPlace<W::kQueries> qs;
@@ -378,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t score = tmem + lanes + kScoreCol + tile * kRows, total = tmem + lanes + kSumCol + tile * kRows;
     const int r = tile * kRows + (warp & 3) * 32 + lane;  // row within the item
     const float c = a.scale * kLog2e;
+    uint8_t* stage = smem + W::kStage + warp * kStageBytes;
     RingPlace<kItems> at;
     uint32_t s_phase = 0, o_phase = 0;  // o_phase: parity of the next product P V to complete
     Work w;
@@ -466,6 +462,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const float s = sum.x + sum.y, f = s == 0.f ? 0.f : 1.f / s;
       const bool live = r < w.rows;
+      const int warp_rows = min(32, w.rows - (r - lane));
+      const int64_t first = (w.row0 + r - lane) * a.q_heads + w.head, pitch = static_cast<int64_t>(a.q_heads) * a.dim;
       const int64_t at_row = (w.row0 + r) * a.q_heads + w.head + (a.splits == 1 ? 0 : w.split * a.q_rows * a.q_heads);
       for (int col = 0; col < a.dim; col += 32) {
         uint32_t o[32];
@@ -476,11 +474,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = 0;
         }
-        if (live) {
-          if (a.splits == 1) store_features(static_cast<__nv_bfloat16*>(a.out) + at_row * a.dim, col, a.dim, vec_out, o, f);
-          else store_features(a.partial + at_row * a.dim, col, a.dim, vec_out, o, f);
-          if (a.splits == 1 && a.rest != nullptr)
-            store_features<__nv_bfloat16, true>(static_cast<__nv_bfloat16*>(a.rest) + at_row * a.dim, col, a.dim, vec_out, o, f);
+        if (a.splits == 1) {
+          store_rows32<false>(static_cast<__nv_bfloat16*>(a.out) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
+          if (a.rest != nullptr)
+            store_rows32<true>(static_cast<__nv_bfloat16*>(a.rest) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
+        } else if (live) {
+          store_part32(a.partial + at_row * a.dim, col, a.dim, vec_out, o, f);
         }
         __syncwarp();
       }
