@@ -153,6 +153,12 @@ struct RingPlace {
       phase ^= 1u;
     }
   }
+  __device__ __forceinline__ void back() {
+    if (--slot < 0) {
+      slot = SLOTS - 1;
+      phase ^= 1u;
+    }
+  }
 };
 
 // Which of the rows first .. first + 127 of a sequence are there: a bit each.

@@ -25,15 +25,21 @@ using namespace attn;
 constexpr int kItemRows = 2 * kRows;
 constexpr int kSoftmaxWarps = 8;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kZeroWarp = 10;
-constexpr int kThreads = 11 * 32;
+constexpr int kThreads = 12 * 32;   // (the last warp is idle: registers change hands by groups of four)
+constexpr uint32_t kSoftmaxRegs = 200, kOtherRegs = 104;
+static_assert(kSoftmaxWarps * kSoftmaxRegs + 4 * kOtherRegs <= 12 * 168, "what a block is launched with");
 constexpr int kItems = 3;             // work items known ahead
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kScoreCol = 0, kSumCol = 256;
 constexpr float kBehind = 8.f;        // log2 of how far a row's maximum may be behind
 
 template <int H>
 struct Shape {
   static constexpr int kTileBytes = H * kBlockBytes;
+  // Tensor memory: places for scores, 128 columns each, then the sums of either tile.
+  // Three places let a tile's next scores be formed while its last ones are worked on.
+  static constexpr int kPlaces = H == 1 ? 3 : 2;
+  static constexpr uint32_t kSumCol = kPlaces * 128, kSumCols = 64 * H;
+  static_assert(kSumCol + 2 * kSumCols <= kTmemCols, "scores and sums share tensor memory");
   static constexpr int kQueries = H == 1 ? 2 : 1;   // pairs of query tiles
   static constexpr int kSlots = H == 1 ? 8 : 4;     // tiles of keys or values
   static constexpr int kStage = (2 * kQueries + kSlots) * kTileBytes;  // the output on its way
@@ -54,7 +60,11 @@ struct Work {
 struct Control {
   uint64_t q_full[2], q_empty[2];
   uint64_t kv_full[8], kv_empty[8], kv_raw[8];
-  uint64_t s_full[2], p_full[2], o_done[2];
+  // Of a place: the probabilities are there.  Of a query tile and a place: the scores
+  // are there, and their probabilities' product is done.  A barrier's next phase can
+  // complete only after everyone has seen the last one: it takes the place again, and
+  // for that the warps that wait on it have gone past.
+  uint64_t p_full[3], s_full[2][3], o_done[2][3];
   uint64_t work_full[kItems], work_empty[kItems];
   uint64_t drain;
   uint32_t tmem;
@@ -126,9 +136,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&ctl->q_full[i], 1);
       ptx::mbar_init(&ctl->q_empty[i], 1);
-      ptx::mbar_init(&ctl->s_full[i], 1);
+    }
+    for (int i = 0; i < W::kPlaces; ++i) {
       ptx::mbar_init(&ctl->p_full[i], 4);
-      ptx::mbar_init(&ctl->o_done[i], 1);
+      for (int t = 0; t < 2; ++t) {
+        ptx::mbar_init(&ctl->s_full[t][i], 1);
+        ptx::mbar_init(&ctl->o_done[t][i], 1);
+      }
     }
     for (int i = 0; i < W::kSlots; ++i) {
       ptx::mbar_init(&ctl->kv_full[i], 1);
@@ -160,222 +174,237 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t smem0 = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(smem), 0);
   const uint32_t ring0 = smem0 + 2 * W::kQueries * W::kTileBytes;
 
-  if (warp == kLoadWarp) {
-    // ---------------- work and loads ----------------
-    if (blockIdx.x == 0) {
-      check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
-      check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
-      __syncwarp();
-    }
-    RingPlace<kItems> at;
-    RingPlace<W::kQueries> qs;
-    RingPlace<W::kSlots> ks;
-    int q_loads = 0, kv_loads = 0;
-    uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on kv_raw, and that barrier's phase
-    bool ok = true;
-    const int64_t slots = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows), items = slots * a.q_heads * a.splits;
-    for (int64_t it = blockIdx.x;; it += gridDim.x) {
-      Work w{};
-      if (it < items) {
-        const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
-        if (tile.image < 0) continue;
-        const int64_t rest = it / slots;
-        const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
-        w.head = static_cast<int>(rest % a.q_heads);
-        w.split = static_cast<int>(rest / a.q_heads);
-        const Part part = part_of((keys.n + kRows - 1) / kRows, w.split, a.splits);
-        w.row0 = tile.rows.lo + tile.first;
-        w.key0 = keys.lo;
-        w.rows = tile.rows.n - tile.first;
-        w.keys = keys.n;
-        w.begin = part.begin;
-        w.end = part.end;
-        w.more = 1;
+  if (warp >= kSoftmaxWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kLoadWarp) {
+      // ---------------- work and loads ----------------
+      if (blockIdx.x == 0) {
+        check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
+        check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
+        __syncwarp();
       }
-      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
-        fail(ctl, a.status, 31);
-        break;
-      }
-      if (lane == 0) {
-        ctl->work[at.slot] = w;
-        ptx::mbar_arrive(&ctl->work_full[at.slot]);
-      }
-      __syncwarp();
-      at.next();
-      if (!w.more) break;
-      if (w.begin == w.end) continue;
-      const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
-      if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, abort_flag)) {
-        fail(ctl, a.status, 32);
-        break;
-      }
-      const bool two = w.rows > kRows;
-      if (ptx::elect_one()) {
-        const uint32_t dst = smem0 + qs.slot * 2 * W::kTileBytes;
-        ptx::mbar_arrive_expect_tx(&ctl->q_full[qs.slot], (two ? 2 : 1) * W::kTileBytes);
-        load_rows<H>(dst, &map_q, &ctl->q_full[qs.slot], w.head, row);
-        if (two) load_rows<H>(dst + W::kTileBytes, &map_q, &ctl->q_full[qs.slot], w.head, row + kRows);
-      }
-      __syncwarp();
-      qs.next();
-      ++q_loads;
-      const int kv = w.head / (a.q_heads / a.kv_heads);
-      for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
-        const int t = i / 2;
-        const bool value = i % 2 != 0, raw = value && ragged(t, w.keys, a.mask);
-        if (!warp_wait(&ctl->kv_empty[ks.slot], ks.phase ^ 1u, abort_flag)) {
-          fail(ctl, a.status, 33);
-          ok = false;
+      RingPlace<kItems> at;
+      RingPlace<W::kQueries> qs;
+      RingPlace<W::kSlots> ks;
+      int q_loads = 0, kv_loads = 0;
+      uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on kv_raw, and that barrier's phase
+      bool ok = true;
+      const int64_t slots = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows), items = slots * a.q_heads * a.splits;
+      for (int64_t it = blockIdx.x;; it += gridDim.x) {
+        Work w{};
+        if (it < items) {
+          const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
+          if (tile.image < 0) continue;
+          const int64_t rest = it / slots;
+          const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
+          w.head = static_cast<int>(rest % a.q_heads);
+          w.split = static_cast<int>(rest / a.q_heads);
+          const Part part = part_of((keys.n + kRows - 1) / kRows, w.split, a.splits);
+          w.row0 = tile.rows.lo + tile.first;
+          w.key0 = keys.lo;
+          w.rows = tile.rows.n - tile.first;
+          w.keys = keys.n;
+          w.begin = part.begin;
+          w.end = part.end;
+          w.more = 1;
+        }
+        if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 31);
           break;
         }
-        uint64_t* bar = raw ? &ctl->kv_raw[ks.slot] : &ctl->kv_full[ks.slot];
-        if (ptx::elect_one()) {
-          ptx::mbar_arrive_expect_tx(bar, W::kTileBytes);
-          load_rows<H>(ring0 + ks.slot * W::kTileBytes, value ? &map_v : &map_k, bar, kv, key + t * kRows);
+        if (lane == 0) {
+          ctl->work[at.slot] = w;
+          ptx::mbar_arrive(&ctl->work_full[at.slot]);
         }
         __syncwarp();
-        const uint32_t bit = 1u << ks.slot;
-        if (raw) raw_phase ^= bit;
-        raw_loaded = raw ? raw_loaded | bit : raw_loaded & ~bit;
-        ks.next();
-        ++kv_loads;
-      }
-      if (!ok) break;
-    }
-    if (ctl->failed) {
-      // Copies under way land before the block ends.  A slot's last load completed phase (number of its loads - 1).
-      for (int s = 0; s < W::kQueries; ++s) {
-        const int n = (q_loads - s + W::kQueries - 1) / W::kQueries;
-        if (n > 0) warp_wait(&ctl->q_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
-      }
-      for (int s = 0; s < W::kSlots; ++s) {
-        const int n = (kv_loads - s + W::kSlots - 1) / W::kSlots;
-        if (n <= 0) continue;
-        if (raw_loaded >> s & 1u) warp_wait(&ctl->kv_raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
-        else warp_wait(&ctl->kv_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
-      }
-    }
-  } else if (warp == kZeroWarp) {
-    // ---------------- value rows that are no keys ----------------
-    RingPlace<kItems> at;
-    RingPlace<W::kSlots> ks;
-    uint32_t raw_phase = 0;
-    Work w;
-    bool ok = true;
-    while (ok) {
-      if (!next_work(ctl, at, w)) {
-        fail(ctl, a.status, 34);
-        break;
-      }
-      if (!w.more) break;
-      const Span keys{w.key0, w.keys};
-      for (int t = w.begin; ok && t < w.end; ++t) {
-        ks.next();
-        if (ragged(t, w.keys, a.mask)) {
-          const uint4 there = rows_there(keys, t * kRows, a.mask);
-          if (!warp_wait(&ctl->kv_raw[ks.slot], raw_phase >> ks.slot & 1u, abort_flag)) {
-            fail(ctl, a.status, 35);
-            ok = false;
-            break;
-          }
-          raw_phase ^= 1u << ks.slot;
-          zero_rows<H>(smem + 2 * W::kQueries * W::kTileBytes + ks.slot * W::kTileBytes, there);
-          if (lane == 0) ptx::mbar_arrive(&ctl->kv_full[ks.slot]);
-          __syncwarp();
-        }
-        ks.next();
-      }
-    }
-  } else if (warp == kMmaWarp) {
-    // ---------------- products ----------------
-    RingPlace<kItems> at;
-    RingPlace<W::kQueries> qs;
-    RingPlace<W::kSlots> ks;
-    uint32_t p_phase[2] = {0, 0};
-    const int slices = (a.dim + 15) / 16;
-    const uint32_t weighted = by_rows(16 * slices);
-    const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-    Work w;
-    bool ok = true;
-    while (ok) {
-      if (!next_work(ctl, at, w)) {
-        fail(ctl, a.status, 36);
-        break;
-      }
-      if (!w.more) break;
-      if (w.begin == w.end) continue;
-      const int tiles = w.rows > kRows ? 2 : 1;
-      const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
-      if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag) || !warp_wait(&ctl->kv_full[ks.slot], ks.phase, abort_flag)) {
-        fail(ctl, a.status, 37);
-        break;
-      }
-      ptx::tc_fence_after_sync();
-      if (ptx::elect_one()) {
-        for (int i = 0; i < tiles; ++i) {
-          mma_scores<H>(tmem0 + kScoreCol + i * kRows, q + i * W::kTileBytes, ring0 + ks.slot * W::kTileBytes, slices);
-          ptx::mma_commit(&ctl->s_full[i]);
-        }
-        ptx::mma_commit(&ctl->kv_empty[ks.slot]);
-        if (w.begin + 1 == w.end) ptx::mma_commit(&ctl->q_empty[qs.slot]);
-      }
-      __syncwarp();
-      ks.next();
-      for (int t = w.begin; ok && t < w.end; ++t) {
-        const bool last = t + 1 == w.end;
-        const RingPlace<W::kSlots> value = ks;
-        ks.next();
-        const RingPlace<W::kSlots> key = ks;  // the next tile's
-        if (!warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag) ||
-            (!last && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag))) {
-          fail(ctl, a.status, 38);
-          ok = false;
+        at.next();
+        if (!w.more) break;
+        if (w.begin == w.end) continue;
+        const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
+        if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, abort_flag)) {
+          fail(ctl, a.status, 32);
           break;
         }
-        for (int i = 0; i < tiles; ++i) {
-          if (!warp_wait(&ctl->p_full[i], p_phase[i], abort_flag)) {
-            fail(ctl, a.status, 39);
+        const bool two = w.rows > kRows;
+        if (ptx::elect_one()) {
+          const uint32_t dst = smem0 + qs.slot * 2 * W::kTileBytes;
+          ptx::mbar_arrive_expect_tx(&ctl->q_full[qs.slot], (two ? 2 : 1) * W::kTileBytes);
+          load_rows<H>(dst, &map_q, &ctl->q_full[qs.slot], w.head, row);
+          if (two) load_rows<H>(dst + W::kTileBytes, &map_q, &ctl->q_full[qs.slot], w.head, row + kRows);
+        }
+        __syncwarp();
+        qs.next();
+        ++q_loads;
+        const int kv = w.head / (a.q_heads / a.kv_heads);
+        for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
+          const int t = i / 2;
+          const bool value = i % 2 != 0, raw = value && ragged(t, w.keys, a.mask);
+          if (!warp_wait(&ctl->kv_empty[ks.slot], ks.phase ^ 1u, abort_flag)) {
+            fail(ctl, a.status, 33);
             ok = false;
             break;
           }
-          p_phase[i] ^= 1u;
-          ptx::tc_fence_after_sync();
+          uint64_t* bar = raw ? &ctl->kv_raw[ks.slot] : &ctl->kv_full[ks.slot];
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + kSumCol + i * kRows, tmem0 + kScoreCol + i * kRows, ring0 + value.slot * W::kTileBytes, weighted,
-                         t != w.begin);
-            ptx::mma_commit(&ctl->o_done[i]);
-            if (!last) {
-              mma_scores<H>(tmem0 + kScoreCol + i * kRows, q + i * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
-              ptx::mma_commit(&ctl->s_full[i]);
-            }
+            ptx::mbar_arrive_expect_tx(bar, W::kTileBytes);
+            load_rows<H>(ring0 + ks.slot * W::kTileBytes, value ? &map_v : &map_k, bar, kv, key + t * kRows);
           }
           __syncwarp();
+          const uint32_t bit = 1u << ks.slot;
+          if (raw) raw_phase ^= bit;
+          raw_loaded = raw ? raw_loaded | bit : raw_loaded & ~bit;
+          ks.next();
+          ++kv_loads;
         }
         if (!ok) break;
-        if (ptx::elect_one()) {
-          ptx::mma_commit(&ctl->kv_empty[value.slot]);
-          if (!last) ptx::mma_commit(&ctl->kv_empty[key.slot]);
-          if (t + 2 == w.end) ptx::mma_commit(&ctl->q_empty[qs.slot]);
-        }
-        __syncwarp();
-        if (!last) ks.next();
       }
-      qs.next();
+      if (ctl->failed) {
+        // Copies under way land before the block ends.  A slot's last load completed phase (number of its loads - 1).
+        for (int s = 0; s < W::kQueries; ++s) {
+          const int n = (q_loads - s + W::kQueries - 1) / W::kQueries;
+          if (n > 0) warp_wait(&ctl->q_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+        }
+        for (int s = 0; s < W::kSlots; ++s) {
+          const int n = (kv_loads - s + W::kSlots - 1) / W::kSlots;
+          if (n <= 0) continue;
+          if (raw_loaded >> s & 1u) warp_wait(&ctl->kv_raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
+          else warp_wait(&ctl->kv_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+        }
+      }
+    } else if (warp == kZeroWarp) {
+      // ---------------- value rows that are no keys ----------------
+      RingPlace<kItems> at;
+      RingPlace<W::kSlots> ks;
+      uint32_t raw_phase = 0;
+      Work w;
+      bool ok = true;
+      while (ok) {
+        if (!next_work(ctl, at, w)) {
+          fail(ctl, a.status, 34);
+          break;
+        }
+        if (!w.more) break;
+        const Span keys{w.key0, w.keys};
+        for (int t = w.begin; ok && t < w.end; ++t) {
+          ks.next();
+          if (ragged(t, w.keys, a.mask)) {
+            const uint4 there = rows_there(keys, t * kRows, a.mask);
+            if (!warp_wait(&ctl->kv_raw[ks.slot], raw_phase >> ks.slot & 1u, abort_flag)) {
+              fail(ctl, a.status, 35);
+              ok = false;
+              break;
+            }
+            raw_phase ^= 1u << ks.slot;
+            zero_rows<H>(smem + 2 * W::kQueries * W::kTileBytes + ks.slot * W::kTileBytes, there);
+            if (lane == 0) ptx::mbar_arrive(&ctl->kv_full[ks.slot]);
+            __syncwarp();
+          }
+          ks.next();
+        }
+      }
+    } else if (warp == kMmaWarp) {
+      // ---------------- products ----------------
+      // Score tiles are numbered key tile by key tile, query tile by query tile
+      // within; number n lies in place n % kPlaces.  As many are formed ahead as there
+      // are places: n + kPlaces follows the product of n's probabilities, in whose
+      // place it goes (products complete in the order of their issue).
+      RingPlace<kItems> at;
+      RingPlace<W::kQueries> qs;
+      RingPlace<W::kSlots> ring;
+      RingPlace<W::kPlaces> next_place, place;  // of the next scores to form, of the next probabilities to use
+      const int slices = (a.dim + 15) / 16;
+      const uint32_t weighted = by_rows(16 * slices);
+      const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+      Work w;
+      bool ok = true;
+      while (ok) {
+        if (!next_work(ctl, at, w)) {
+          fail(ctl, a.status, 36);
+          break;
+        }
+        if (!w.more) break;
+        if (w.begin == w.end) continue;
+        const int tiles = w.rows > kRows ? 2 : 1, all = (w.end - w.begin) * tiles;
+        const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
+        if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag)) {
+          fail(ctl, a.status, 37);
+          break;
+        }
+        RingPlace<W::kSlots> key = ring, value = ring;
+        value.next();
+        int formed = 0, form_tile = 0;
+        auto form = [&] {
+          if (form_tile == 0 && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag)) return false;
+          ptx::tc_fence_after_sync();
+          ++formed;
+          const bool last_of_key = form_tile + 1 == tiles;
+          if (ptx::elect_one()) {
+            mma_scores<H>(tmem0 + next_place.slot * kRows, q + form_tile * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
+            ptx::mma_commit(&ctl->s_full[form_tile][next_place.slot]);
+            if (last_of_key) ptx::mma_commit(&ctl->kv_empty[key.slot]);
+            if (formed == all) ptx::mma_commit(&ctl->q_empty[qs.slot]);
+          }
+          __syncwarp();
+          next_place.next();
+          if (last_of_key) {
+            key.next();
+            key.next();
+            form_tile = 0;
+          } else {
+            form_tile = 1;
+          }
+          return true;
+        };
+        while (ok && formed < W::kPlaces && formed < all) ok = form();
+        int tile = 0;
+        for (int n = 0; ok && n < all; ++n) {
+          ok = (tile != 0 || warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag)) &&
+               warp_wait(&ctl->p_full[place.slot], place.phase, abort_flag);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const bool last_of_value = tile + 1 == tiles;
+          if (ptx::elect_one()) {
+            mma_weighted(tmem0 + W::kSumCol + tile * W::kSumCols, tmem0 + place.slot * kRows, ring0 + value.slot * W::kTileBytes,
+                         weighted, n >= tiles);
+            ptx::mma_commit(&ctl->o_done[tile][place.slot]);
+            if (last_of_value) ptx::mma_commit(&ctl->kv_empty[value.slot]);
+          }
+          __syncwarp();
+          place.next();
+          if (last_of_value) {
+            value.next();
+            value.next();
+            tile = 0;
+          } else {
+            tile = 1;
+          }
+          if (formed < all) ok = form();
+        }
+        if (!ok) {
+          fail(ctl, a.status, 38);
+          break;
+        }
+        ring = key;
+        qs.next();
+      }
+      if (ptx::elect_one()) ptx::mma_commit(&ctl->drain);
+      __syncwarp();
+      ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
+      __syncwarp();
     }
-    if (ptx::elect_one()) ptx::mma_commit(&ctl->drain);
-    __syncwarp();
-    ptx::mbar_wait(&ctl->drain, 0, nullptr, kWaitNs);
-    __syncwarp();
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     // ---------------- softmax ----------------
     const int tile = warp / 4;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t score = tmem + lanes + kScoreCol + tile * kRows, total = tmem + lanes + kSumCol + tile * kRows;
+    const uint32_t total = tmem + lanes + W::kSumCol + tile * W::kSumCols;
     const int r = tile * kRows + (warp & 3) * 32 + lane;  // row within the item
     const float c = a.scale * kLog2e;
     uint8_t* stage = smem + W::kStage + warp * kStageBytes;
     RingPlace<kItems> at;
-    uint32_t s_phase = 0, o_phase = 0;  // o_phase: parity of the next product P V to complete
+    RingPlace<W::kPlaces> place;  // of the next scores, of either query tile
+    uint32_t phases = 0;          // a bit for each place: the parity of this tile's next scores and product there
+    int last = 0;                 // the place of this tile's last scores
     Work w;
     bool ok = true;
     while (ok) {
@@ -384,20 +413,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       if (!w.more) break;
-      if (w.rows <= tile * kRows) continue;
+      const bool two = w.rows > kRows;
+      if (tile == 1 && !two) {
+        for (int n = (w.end - w.begin) % W::kPlaces; n > 0; --n) place.next();
+        continue;
+      }
+      if (tile == 1 && w.begin != w.end) place.next();
       float top = -INFINITY;  // the maximum that exponents are taken from, log2
       float2 sum = make_float2(0.f, 0.f);
       for (int t = w.begin; t < w.end; ++t) {
         const bool cut = ragged(t, w.keys, a.mask);
         uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
         if (cut) there = rows_there({w.key0, w.keys}, t * kRows, a.mask);
-        if (!warp_wait(&ctl->s_full[tile], s_phase, abort_flag)) {
+        if (!warp_wait(&ctl->s_full[tile][place.slot], phases >> place.slot & 1u, abort_flag)) {
           fail(ctl, a.status, 41);
           ok = false;
           break;
         }
-        s_phase ^= 1u;
+        const int here = place.slot;
         ptx::tc_fence_after_sync();
+        const uint32_t score = tmem + lanes + here * kRows;
+        place.next();
+        if (two) place.next();
         uint32_t s0[32], s1[32], s2[32], s3[32];
         ptx::tmem_ld_32x32b_x32(score, s0);
         ptx::tmem_ld_32x32b_x32(score + 32, s1);
@@ -418,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           top = most;
         } else if (__any_sync(0xFFFFFFFFu, most > top + kBehind)) {
           // O holds tiles up to t - 1 once their product has completed.
-          if (!warp_wait(&ctl->o_done[tile], o_phase ^ 1u, abort_flag)) {
+          if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, abort_flag)) {
             fail(ctl, a.status, 42);
             ok = false;
             break;
@@ -437,7 +474,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st_x16(total + col, o);
           }
         }
-        o_phase ^= 1u;  // of the product of this tile
+        phases ^= 1u << here;
+        last = here;
         const float base = top == -INFINITY ? 0.f : -top;
         const float2 c2 = make_float2(c, c), base2 = make_float2(base, base);
         uint32_t p[32];
@@ -450,11 +488,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_wait_st();
         ptx::tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&ctl->p_full[tile]);
+        if (lane == 0) ptx::mbar_arrive(&ctl->p_full[here]);
       }
       if (!ok) break;
+      if (tile == 1 && w.begin != w.end) place.back();
       if (w.end > w.begin) {
-        if (!warp_wait(&ctl->o_done[tile], o_phase ^ 1u, abort_flag)) {
+        if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, abort_flag)) {
           fail(ctl, a.status, 43);
           break;
         }
