@@ -84,24 +84,59 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
       : "memory");
 }
 
+// Products are issued four at a time: written one by one, what forms their operands
+// took 50 cycles a product, and the issuing warp bounded the kernels (64 x 1024
+// tokens, 12 heads of 64, forward: BEFORE us, AFTER so).
+// D [128, 128] (+)= four K = 16 slices of 64 features of both tiles.
+__device__ __forceinline__ void mma_features4(uint32_t d, uint64_t a, uint64_t b, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, q;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, q;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, q;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(by_features(kRows)), "r"(accumulate), "r"(1u)
+      : "memory");
+}
+// D [128, width] (+)= 64 columns of weights (bf16 pairs in 32 columns of tensor memory) times 64 rows of b.
+__device__ __forceinline__ void mma_rows4(uint32_t d, uint32_t weights, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, q;\n\t"
+      "add.u32 a, %1, 16;\n\tadd.s64 b, %2, 256;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, q;\n\t"
+      "add.u32 a, %1, 24;\n\tadd.s64 b, %2, 384;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, q;\n\t}" ::"r"(d),
+      "r"(weights), "l"(b), "r"(idesc), "r"(accumulate), "r"(1u)
+      : "memory");
+}
 // Scores of two tiles, [128 rows of a, 128 rows of b]: a sum over the features, `slices` times 16.
 template <int H>
 __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b, int slices) {
   const uint64_t da = ptx::sdesc_k_sw128(a), db = ptx::sdesc_k_sw128(b);
 #pragma unroll
-  for (int s = 0; s < 4 * H; ++s) {
-    if (s < slices) {
-      const uint64_t at = static_cast<uint64_t>((s / 4) * (kBlockBytes >> 4) + (s % 4) * 2);
-      ptx::mma_bf16(d, da + at, db + at, by_features(kRows), s != 0 ? 1u : 0u);
+  for (int h = 0; h < H; ++h) {
+    const uint64_t at = static_cast<uint64_t>(h * (kBlockBytes >> 4));
+    if (slices >= 4 * h + 4) {
+      mma_features4(d, da + at, db + at, h != 0 ? 1u : 0u);
+    } else {
+      for (int s = 4 * h; s < slices; ++s)
+        ptx::mma_bf16(d, da + at + (s % 4) * 2, db + at + (s % 4) * 2, by_features(kRows), s != 0 ? 1u : 0u);
     }
   }
 }
-// d [128, width] (+)= weights [128, 128 rows of b] (bf16 pairs in tensor memory) times b.
-__device__ __forceinline__ void mma_weighted(uint32_t d, uint32_t weights, uint32_t b, uint32_t idesc, bool accumulate) {
+// d [128, width] (+)= weights [128, 128 rows of b] times b; `apart`: columns between the weights of rows 0 and 64.
+__device__ __forceinline__ void mma_weighted(uint32_t d, uint32_t weights, uint32_t apart, uint32_t b, uint32_t idesc, bool accumulate) {
   const uint64_t db = desc_by_rows(b);
-#pragma unroll
-  for (int s = 0; s < kRows / 16; ++s)
-    mma_tmem(d, weights + 8 * s, db + static_cast<uint64_t>(s * (2048 >> 4)), idesc, accumulate || s != 0 ? 1u : 0u);
+  mma_rows4(d, weights, db, idesc, accumulate ? 1u : 0u);
+  mma_rows4(d, weights + apart, db + 512, idesc, 1u);
 }
 
 // 32 lanes x 32 consecutive columns: thread t writes lane t.
@@ -232,6 +267,60 @@ __device__ __forceinline__ void store_rows32(__nv_bfloat16* first_row, int64_t p
             stage + row * 64 + (((lane / 8) ^ (row >> 1 & 3)) * 16) + lane % 8 * 2);
   }
   __syncwarp();
+}
+// The same for 16 features, by way of 1 KB.
+constexpr int kStage16Bytes = 32 * 32;
+template <bool REST>
+__device__ __forceinline__ void store_rows16(__nv_bfloat16* first_row, int64_t pitch, int rows, int col, int dim, bool vec,
+                                             uint8_t* stage, const uint32_t (&v)[16], float factor) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    uint32_t u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float x = __uint_as_float(v[8 * p + 2 * k]) * factor, y = __uint_as_float(v[8 * p + 2 * k + 1]) * factor;
+      if constexpr (REST) {
+        x = to_f32(rest_of<__nv_bfloat16>(x));
+        y = to_f32(rest_of<__nv_bfloat16>(y));
+      }
+      u[k] = pack_bf16(x, y);
+    }
+    *reinterpret_cast<uint4*>(stage + lane * 32 + ((p ^ (lane >> 2 & 1)) * 16)) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  __syncwarp();
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 16 * i + lane / 2, p = lane & 1;
+      if (row < rows && col + 8 * p < dim)
+        *reinterpret_cast<uint4*>(first_row + row * pitch + col + 8 * p) =
+            *reinterpret_cast<const uint4*>(stage + row * 32 + ((p ^ (row >> 2 & 1)) * 16));
+    }
+  } else {
+    for (int i = 0; i < 16; ++i) {
+      const int row = 2 * i + lane / 16, e = lane & 15;
+      if (row < rows && col + e < dim)
+        first_row[row * pitch + col + e] =
+            *reinterpret_cast<const __nv_bfloat16*>(stage + row * 32 + (((e / 8) ^ (row >> 2 & 1)) * 16) + e % 8 * 2);
+    }
+  }
+  __syncwarp();
+}
+// 16 features of a row to a part's fp32 row.
+__device__ __forceinline__ void store_part16(float* row, int col, int dim, bool vec, const uint32_t (&v)[16], float factor) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    if (vec && col + i < dim) {
+      *reinterpret_cast<float4*>(row + col + i) =
+          make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
+                      __uint_as_float(v[i + 3]) * factor);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + i + e < dim) row[col + i + e] = __uint_as_float(v[i + e]) * factor;
+    }
+  }
 }
 // 32 features of a row to a part's fp32 row.
 __device__ __forceinline__ void store_part32(float* row, int col, int dim, bool vec, const uint32_t (&v)[32], float factor) {

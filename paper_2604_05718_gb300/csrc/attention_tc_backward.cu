@@ -100,14 +100,7 @@ __device__ __forceinline__ void keep32(uint32_t (&r)[32], uint32_t there, uint32
   for (int i = 0; i < 32; ++i) r[i] = there >> i & 1u ? r[i] : otherwise;
 }
 
-// sums (+)= weights x tile, the weights as the warps leave them: 32 words from column 0 and 32 from column 64.
-__device__ __forceinline__ void mma_halves(uint32_t d, uint32_t weights, uint32_t b, uint32_t idesc, bool accumulate) {
-  const uint64_t db = desc_by_rows(b);
-#pragma unroll
-  for (int s = 0; s < kRows / 16; ++s)
-    mma_tmem(d, weights + (s / 4) * 64 + (s % 4) * 8, db + static_cast<uint64_t>(s * (2048 >> 4)), idesc,
-             accumulate || s != 0 ? 1u : 0u);
-}
+constexpr uint32_t kApart = 64;  // the warps leave their words 64 columns apart, over d_out.v
 
 template <int H>
 __device__ __forceinline__ void init_control(Control* ctl, int work_readers, int stat_readers) {
@@ -435,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           else ds_phase[1] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_halves(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
             ptx::mma_commit(&ctl->empty[x.slot]);
             if (last) ptx::mma_commit(&ctl->sum_done);
           }
@@ -446,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           p_phase ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one())
-            mma_halves(tmem0 + sum_col, tmem0 + score_col, ring0 + y.slot * W::kTileBytes, weighted, t != w.begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + y.slot * W::kTileBytes, weighted, t != w.begin);
           __syncwarp();
           if (!last) ok = scores(x1);
           ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], abort_flag);
@@ -454,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ds_phase[0] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_halves(tmem0 + sum_col + 128, tmem0 + t_col, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
+            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
             ptx::mma_commit(&ctl->empty[x.slot]);
             ptx::mma_commit(&ctl->empty[y.slot]);
             if (last) ptx::mma_commit(&ctl->sum_done);

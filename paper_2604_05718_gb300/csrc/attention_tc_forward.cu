@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tc_fence_after_sync();
           const bool last_of_value = tile + 1 == tiles;
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + W::kSumCol + tile * W::kSumCols, tmem0 + place.slot * kRows, ring0 + value.slot * W::kTileBytes,
+            mma_weighted(tmem0 + W::kSumCol + tile * W::kSumCols, tmem0 + place.slot * kRows, 32, ring0 + value.slot * W::kTileBytes,
                          weighted, n >= tiles);
             ptx::mma_commit(&ctl->o_done[tile][place.slot]);
             if (last_of_value) ptx::mma_commit(&ctl->kv_empty[value.slot]);

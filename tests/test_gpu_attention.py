@@ -346,3 +346,14 @@ def test_gradients_against_differences(mpm):
         # The third derivative's part is h^2 / 6 of it, of the size of the terms' own sum; differences lose 2^-20 / h.
         size = (grad.double().abs() * step.double().abs()).sum()
         assert abs(want - got) <= size * (h * h + 2.0 ** -20 / h), n
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("shape", [(300, 160, 400), (700, 1, 300), (40, 1000, 1100)], ids=["one_or_two_tiles", "any", "many_tiles"])
+def test_many_sequences_a_block(mpm, shape, dim):
+    """More work items than SMs, of one and of two tiles of queries in turn: places and barriers are used over and over."""
+    batch, low, high = shape
+    gen = torch.Generator().manual_seed(batch)
+    q = torch.randint(low, high, (batch,), generator=gen).tolist()
+    k = torch.randint(low, high, (batch,), generator=gen).tolist()
+    run_and_check(mpm, *problem(q, k, 2, 2, dim, torch.bfloat16, masked=0.1 if dim == 128 else 0.0))
