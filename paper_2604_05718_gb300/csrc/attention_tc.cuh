@@ -177,6 +177,14 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
 }
 
+// A value that all lanes hold, in a form that the compiler knows to be uniform: what
+// the products' issuing warp computes with (see ptx::elect_one).
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+// Arrives on the barrier at a shared address when all products issued so far have completed.
+__device__ __forceinline__ void commit_at(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // Place in a ring of SLOTS.
 template <int SLOTS>
 struct RingPlace {

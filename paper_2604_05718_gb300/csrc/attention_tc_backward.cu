@@ -369,6 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int slices = (a.dim + 15) / 16;
     const uint32_t weighted = by_rows(16 * slices);
     const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    const uint32_t bars = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(ctl), 0);
+    auto at_bar = [&](size_t offset, int i) { return bars + static_cast<uint32_t>(offset) + 8u * i; };
     Work w;
     bool ok = true;
     while (ok) {
@@ -377,7 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       if (!w.more) break;
-      if (w.begin == w.end) continue;
+      const int begin = uniform(w.begin), end = uniform(w.end);
+      if (begin == end) continue;
       const uint32_t mine = smem0 + kept.slot * 2 * W::kTileBytes;  // queries and d_out, or keys and values
       if (!warp_wait(&ctl->kept_full[kept.slot], kept.phase, abort_flag)) {
         fail(ctl, a.status, 59);
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) {
           mma_scores<H>(tmem0 + score_col, mine, ring0 + x.slot * W::kTileBytes, slices);
-          ptx::mma_commit(&ctl->s_full);
+          commit_at(at_bar(offsetof(Control, s_full), 0));
         }
         __syncwarp();
         return true;
@@ -403,18 +406,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) {
           mma_scores<H>(tmem0 + t_col + (DQ ? (t & 1) * 128 : 0), mine + W::kTileBytes, ring0 + y.slot * W::kTileBytes, slices);
-          ptx::mma_commit(&ctl->t_full[DQ ? t & 1 : 0]);
-          if (DQ) ptx::mma_commit(&ctl->empty[y.slot]);
-          if (t + 1 == w.end) ptx::mma_commit(&ctl->kept_empty[kept.slot]);
+          commit_at(at_bar(offsetof(Control, t_full), DQ ? t & 1 : 0));
+          if (DQ) commit_at(at_bar(offsetof(Control, empty), y.slot));
+          if (t + 1 == end) commit_at(at_bar(offsetof(Control, kept_empty), kept.slot));
         }
         __syncwarp();
         return true;
       };
       RingPlace<W::kSlots> x = ring, y = ring;
       y.next();
-      ok = scores(x) && seconds(y, w.begin);
-      for (int t = w.begin; ok && t < w.end; ++t) {
-        const bool last = t + 1 == w.end;
+      ok = scores(x) && seconds(y, begin);
+      for (int t = begin; ok && t < end; ++t) {
+        const bool last = t + 1 == end;
         RingPlace<W::kSlots> x1 = y, y1;
         x1.next();
         y1 = x1;
@@ -428,9 +431,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           else ds_phase[1] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
-            ptx::mma_commit(&ctl->empty[x.slot]);
-            if (last) ptx::mma_commit(&ctl->sum_done);
+            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            commit_at(at_bar(offsetof(Control, empty), x.slot));
+            if (last) commit_at(at_bar(offsetof(Control, sum_done), 0));
           }
           __syncwarp();
         } else {
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           p_phase ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one())
-            mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + y.slot * W::kTileBytes, weighted, t != w.begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + y.slot * W::kTileBytes, weighted, t != begin);
           __syncwarp();
           if (!last) ok = scores(x1);
           ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], abort_flag);
@@ -447,10 +450,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           ds_phase[0] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != w.begin);
-            ptx::mma_commit(&ctl->empty[x.slot]);
-            ptx::mma_commit(&ctl->empty[y.slot]);
-            if (last) ptx::mma_commit(&ctl->sum_done);
+            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            commit_at(at_bar(offsetof(Control, empty), x.slot));
+            commit_at(at_bar(offsetof(Control, empty), y.slot));
+            if (last) commit_at(at_bar(offsetof(Control, sum_done), 0));
           }
           __syncwarp();
           if (!last) ok = seconds(y1, t + 1);

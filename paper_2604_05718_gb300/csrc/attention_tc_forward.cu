@@ -315,6 +315,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int slices = (a.dim + 15) / 16;
       const uint32_t weighted = by_rows(16 * slices);
       const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+      const uint32_t bars = __shfl_sync(0xFFFFFFFFu, ptx::smem_addr(ctl), 0);
+      auto at_bar = [&](size_t offset, int i) { return bars + static_cast<uint32_t>(offset) + 8u * i; };
       Work w;
       bool ok = true;
       while (ok) {
@@ -323,8 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         if (!w.more) break;
-        if (w.begin == w.end) continue;
-        const int tiles = w.rows > kRows ? 2 : 1, all = (w.end - w.begin) * tiles;
+        if (uniform(w.begin) == uniform(w.end)) continue;
+        const int tiles = uniform(w.rows > kRows ? 2 : 1), all = uniform(w.end - w.begin) * tiles;
         const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
         if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag)) {
           fail(ctl, a.status, 37);
@@ -340,9 +342,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool last_of_key = form_tile + 1 == tiles;
           if (ptx::elect_one()) {
             mma_scores<H>(tmem0 + next_place.slot * kRows, q + form_tile * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
-            ptx::mma_commit(&ctl->s_full[form_tile][next_place.slot]);
-            if (last_of_key) ptx::mma_commit(&ctl->kv_empty[key.slot]);
-            if (formed == all) ptx::mma_commit(&ctl->q_empty[qs.slot]);
+            commit_at(at_bar(offsetof(Control, s_full), 3 * form_tile + next_place.slot));
+            if (last_of_key) commit_at(at_bar(offsetof(Control, kv_empty), key.slot));
+            if (formed == all) commit_at(at_bar(offsetof(Control, q_empty), qs.slot));
           }
           __syncwarp();
           next_place.next();
@@ -366,8 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (ptx::elect_one()) {
             mma_weighted(tmem0 + W::kSumCol + tile * W::kSumCols, tmem0 + place.slot * kRows, 32, ring0 + value.slot * W::kTileBytes,
                          weighted, n >= tiles);
-            ptx::mma_commit(&ctl->o_done[tile][place.slot]);
-            if (last_of_value) ptx::mma_commit(&ctl->kv_empty[value.slot]);
+            commit_at(at_bar(offsetof(Control, o_done), 3 * tile + place.slot));
+            if (last_of_value) commit_at(at_bar(offsetof(Control, kv_empty), value.slot));
           }
           __syncwarp();
           place.next();
