@@ -21,6 +21,7 @@ namespace {
 using namespace attn;
 
 constexpr int kWarps = 8;
+constexpr int kAtOnce = 3;  // units of a lane
 
 template <typename T>
 struct Vec {
@@ -28,8 +29,7 @@ struct Vec {
   float v[kSize];
 };
 template <typename T>
-__device__ __forceinline__ Vec<T> load_vec(const T* p) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ Vec<T> widen_vec(const uint4& u) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
   Vec<T> r;
 #pragma unroll
@@ -94,6 +94,37 @@ __global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const RotaryArgs a,
   const int head0 = first / units, u0 = first % units, step_head = step / units, step_u = step % units;
   for (int64_t r = blockIdx.x * static_cast<int64_t>(groups) + warp / row_warps; r < live;
        r += gridDim.x * static_cast<int64_t>(groups)) {
+    const T* x = static_cast<const T*>(a.x.p) + r * a.x.row;
+    T* y = static_cast<T*>(a.out) + r * a.out_row;
+    const T* from[kAtOnce];
+    T* to[kAtOnce];
+    int unit[kAtOnce];
+    uint4 lo[kAtOnce], hi[kAtOnce];
+    int head = head0, u = u0;
+    auto load = [&](int i) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        unit[k] = i + k * step < all ? u : -1;
+        from[k] = x + head * a.x.head;
+        to[k] = y + head * a.out_head;
+        if constexpr (VEC) {
+          if (unit[k] >= turned) {
+            lo[k] = *reinterpret_cast<const uint4*>(from[k] + 2 * a.pairs + (u - turned) * S);
+          } else if (unit[k] >= 0) {
+            lo[k] = *reinterpret_cast<const uint4*>(from[k] + u * S);
+            if constexpr (HALVES) hi[k] = *reinterpret_cast<const uint4*>(from[k] + a.pairs + u * S);
+          }
+        }
+        u += step_u;
+        head += step_head;
+        if (u >= units) {
+          u -= units;
+          ++head;
+        }
+      }
+    };
+    // The row's first units are under way while its sines are found.
+    load(first);
     __syncwarp();
     for (int p = lane; p < a.pairs; p += 32) {
       const float at = __ldg(a.positions + r * a.axes + axis[p]);
@@ -104,39 +135,33 @@ __global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const RotaryArgs a,
       table[p] = make_float2(c, a.inverse ? -s : s);
     }
     __syncwarp();
-    const T* x = static_cast<const T*>(a.x.p) + r * a.x.row;
-    T* y = static_cast<T*>(a.out) + r * a.out_row;
-    int head = head0, u = u0;
-    for (int i = first; i < all; i += step) {
-      const T* from = x + head * a.x.head;
-      T* to = y + head * a.out_head;
-      if (u >= turned) {
-        const int at = 2 * a.pairs + (u - turned) * (VEC ? S : 1);
-        if constexpr (VEC) *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(from + at);
-        else to[at] = from[at];
-      } else if constexpr (VEC && HALVES) {
-        Vec<T> lo = load_vec(from + u * S), hi = load_vec(from + a.pairs + u * S);
+    for (int i = first; i < all; i += kAtOnce * step) {
+      if (i != first) load(i);
 #pragma unroll
-        for (int k = 0; k < S; ++k) turn(lo.v[k], hi.v[k], table[u * S + k]);
-        store_vec(to + u * S, lo);
-        store_vec(to + a.pairs + u * S, hi);
-      } else if constexpr (VEC) {
-        Vec<T> v = load_vec(from + u * S);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int n = unit[k];
+        if (n < 0) continue;
+        if (n >= turned) {
+          if constexpr (VEC) *reinterpret_cast<uint4*>(to[k] + 2 * a.pairs + (n - turned) * S) = lo[k];
+          else to[k][2 * a.pairs + n - turned] = from[k][2 * a.pairs + n - turned];
+        } else if constexpr (VEC && HALVES) {
+          Vec<T> v = widen_vec<T>(lo[k]), w = widen_vec<T>(hi[k]);
 #pragma unroll
-        for (int k = 0; k < S / 2; ++k) turn(v.v[2 * k], v.v[2 * k + 1], table[u * (S / 2) + k]);
-        store_vec(to + u * S, v);
-      } else {
-        const int f = HALVES ? u : 2 * u, g = HALVES ? u + a.pairs : 2 * u + 1;
-        float lo = to_f32(from[f]), hi = to_f32(from[g]);
-        turn(lo, hi, table[u]);
-        to[f] = from_f32<T>(lo);
-        to[g] = from_f32<T>(hi);
-      }
-      u += step_u;
-      head += step_head;
-      if (u >= units) {
-        u -= units;
-        ++head;
+          for (int e = 0; e < S; ++e) turn(v.v[e], w.v[e], table[n * S + e]);
+          store_vec(to[k] + n * S, v);
+          store_vec(to[k] + a.pairs + n * S, w);
+        } else if constexpr (VEC) {
+          Vec<T> v = widen_vec<T>(lo[k]);
+#pragma unroll
+          for (int e = 0; e < S / 2; ++e) turn(v.v[2 * e], v.v[2 * e + 1], table[n * (S / 2) + e]);
+          store_vec(to[k] + n * S, v);
+        } else {
+          const int f = HALVES ? n : 2 * n, g = HALVES ? n + a.pairs : 2 * n + 1;
+          float v = to_f32(from[k][f]), w = to_f32(from[k][g]);
+          turn(v, w, table[n]);
+          to[k][f] = from_f32<T>(v);
+          to[k][g] = from_f32<T>(w);
+        }
       }
     }
   }
