@@ -90,29 +90,32 @@ mpm_status check_shape(const Shape& s) {
 
 // How many parts the streamed side of length `stream` (all sequences) is split
 // into, where `rows` rows of the other side, in tiles of `tile`, times `heads` are
-// the work: as many as fill the SMs, each at least a tile.  Lengths are known as
-// means only.
-int splits_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_t stream_tile, int64_t batch, int64_t ways) {
+// the work: as many as fill `ways` blocks an SM, each of `least` tiles or more.
+// Lengths are known as means only.
+int splits_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_t stream_tile, int64_t batch, int64_t ways,
+               int64_t least) {
   const int64_t items = std::max((rows + tile - 1) / tile, std::min(batch, rows)) * heads;
-  if (items == 0 || items * 2 > kSms * ways) return 1;
+  if (items == 0) return 1;
   const int64_t tiles = (stream / std::max<int64_t>(1, std::min(batch, stream)) + stream_tile - 1) / stream_tile;
-  return static_cast<int>(std::max<int64_t>(1, std::min({kSms * ways / items, tiles, int64_t{mpm::kAttentionMaxSplits}})));
+  return static_cast<int>(std::max<int64_t>(1, std::min({kSms * ways / items, tiles / least, int64_t{mpm::kAttentionMaxSplits}})));
 }
 struct Plan {
   int splits, key_splits;
 };
 Plan plan_simt(const Shape& s) {
   const int64_t group = s.q_heads / s.kv_heads;
-  return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 2),
-          splits_for(s.k_rows, 64, s.kv_heads, s.q_rows * group, 64, s.batch, 2)};
+  return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 4, 1),
+          splits_for(s.k_rows, 64, s.kv_heads, s.q_rows * group, 64, s.batch, 4, 1)};
 }
 
-// The tensor-core kernels' tiles.
-Plan plan_tc(const Shape& s) { return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 1), 1}; }
+// The tensor-core kernels' tiles.  A part pays from eight tiles on: parts have to be
+// written and joined (2 x 577 tokens, 16 heads of 64, 13 us forward whole and 25 in
+// two; 8 x 100 queries, 8192 keys, 8 heads: 64 us in two parts, 56 in four).
+Plan plan_tc(const Shape& s) { return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 2, 8), 1}; }
 Plan plan_tc_backward(const Shape& s) {
   const int64_t group = s.q_heads / s.kv_heads;
-  return {splits_for(s.q_rows, 128, s.q_heads, s.k_rows, 128, s.batch, 1),
-          splits_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, 128, s.batch, 1)};
+  return {splits_for(s.q_rows, 128, s.q_heads, s.k_rows, 128, s.batch, 2, 8),
+          splits_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, 128, s.batch, 2, 8)};
 }
 // Few queries: blocks of 16 rows, of the heads that share a kv head.  Taken where
 // the sequences' queries are so few on the mean (a longer sequence takes several

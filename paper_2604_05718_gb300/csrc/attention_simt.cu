@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(kRowThreads) attention_join_kernel(const Atten
     w[0] *= inv;
     w[1] *= inv;
     float v[kAttentionMaxDim / 32] = {};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) {
       const float f = __shfl_sync(0xFFFFFFFFu, s < 32 ? w[0] : w[1], s & 31);
       const float* p = a.partial + (s * all + r) * a.dim;
@@ -553,6 +554,7 @@ __global__ void __launch_bounds__(kRowThreads) attention_sum_kernel(const float*
   const int64_t each = rows * width, live = live_rows(offsets, batch, rows) * width;
   for (int64_t i = blockIdx.x * int64_t{kRowThreads} + threadIdx.x; i < live; i += gridDim.x * int64_t{kRowThreads}) {
     float s = 0.f;
+#pragma unroll 4
     for (int p = 0; p < splits; ++p) s += parts[p * each + i];
     out[i] = from_f32<T>(s);
   }

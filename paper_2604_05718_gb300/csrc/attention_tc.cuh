@@ -276,73 +276,36 @@ __device__ __forceinline__ void store_rows32(__nv_bfloat16* first_row, int64_t p
   }
   __syncwarp();
 }
-// The same for 16 features, by way of 1 KB.
-constexpr int kStage16Bytes = 32 * 32;
-template <bool REST>
-__device__ __forceinline__ void store_rows16(__nv_bfloat16* first_row, int64_t pitch, int rows, int col, int dim, bool vec,
-                                             uint8_t* stage, const uint32_t (&v)[16], float factor) {
+// 32 features of a warp's 32 rows to a part's fp32 rows, by the same way.
+__device__ __forceinline__ void store_part32(float* first_row, int64_t pitch, int rows, int col, int dim, bool vec, uint8_t* stage,
+                                             const uint32_t (&v)[32], float factor) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    uint32_t u[4];
+  for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float x = __uint_as_float(v[8 * p + 2 * k]) * factor, y = __uint_as_float(v[8 * p + 2 * k + 1]) * factor;
-      if constexpr (REST) {
-        x = to_f32(rest_of<__nv_bfloat16>(x));
-        y = to_f32(rest_of<__nv_bfloat16>(y));
+    for (int p = 0; p < 4; ++p) {
+      const float4 u = make_float4(__uint_as_float(v[16 * h + 4 * p]) * factor, __uint_as_float(v[16 * h + 4 * p + 1]) * factor,
+                                   __uint_as_float(v[16 * h + 4 * p + 2]) * factor, __uint_as_float(v[16 * h + 4 * p + 3]) * factor);
+      *reinterpret_cast<float4*>(stage + lane * 64 + ((p ^ (lane >> 1 & 3)) * 16)) = u;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + lane / 4, p = lane & 3, c = col + 16 * h + 4 * p;
+      if (row < rows && c < dim) {
+        const float4 u = *reinterpret_cast<const float4*>(stage + row * 64 + ((p ^ (row >> 1 & 3)) * 16));
+        float* to = first_row + row * pitch + c;
+        if (vec) {
+          *reinterpret_cast<float4*>(to) = u;
+        } else {
+          to[0] = u.x;
+          if (c + 1 < dim) to[1] = u.y;
+          if (c + 2 < dim) to[2] = u.z;
+          if (c + 3 < dim) to[3] = u.w;
+        }
       }
-      u[k] = pack_bf16(x, y);
     }
-    *reinterpret_cast<uint4*>(stage + lane * 32 + ((p ^ (lane >> 2 & 1)) * 16)) = make_uint4(u[0], u[1], u[2], u[3]);
-  }
-  __syncwarp();
-  if (vec) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = 16 * i + lane / 2, p = lane & 1;
-      if (row < rows && col + 8 * p < dim)
-        *reinterpret_cast<uint4*>(first_row + row * pitch + col + 8 * p) =
-            *reinterpret_cast<const uint4*>(stage + row * 32 + ((p ^ (row >> 2 & 1)) * 16));
-    }
-  } else {
-    for (int i = 0; i < 16; ++i) {
-      const int row = 2 * i + lane / 16, e = lane & 15;
-      if (row < rows && col + e < dim)
-        first_row[row * pitch + col + e] =
-            *reinterpret_cast<const __nv_bfloat16*>(stage + row * 32 + (((e / 8) ^ (row >> 2 & 1)) * 16) + e % 8 * 2);
-    }
-  }
-  __syncwarp();
-}
-// 16 features of a row to a part's fp32 row.
-__device__ __forceinline__ void store_part16(float* row, int col, int dim, bool vec, const uint32_t (&v)[16], float factor) {
-#pragma unroll
-  for (int i = 0; i < 16; i += 4) {
-    if (vec && col + i < dim) {
-      *reinterpret_cast<float4*>(row + col + i) =
-          make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
-                      __uint_as_float(v[i + 3]) * factor);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (col + i + e < dim) row[col + i + e] = __uint_as_float(v[i + e]) * factor;
-    }
-  }
-}
-// 32 features of a row to a part's fp32 row.
-__device__ __forceinline__ void store_part32(float* row, int col, int dim, bool vec, const uint32_t (&v)[32], float factor) {
-#pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    if (vec && col + i < dim) {
-      *reinterpret_cast<float4*>(row + col + i) =
-          make_float4(__uint_as_float(v[i]) * factor, __uint_as_float(v[i + 1]) * factor, __uint_as_float(v[i + 2]) * factor,
-                      __uint_as_float(v[i + 3]) * factor);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (col + i + e < dim) row[col + i + e] = __uint_as_float(v[i + e]) * factor;
-    }
+    __syncwarp();
   }
 }
 

@@ -610,7 +610,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tc_fence_after_sync();
       }
       // Features 32 half .. in turns for d_q; one of the two sums a half for d_v and d_k.
-      const bool live = r < w.rows;
       const int heads = DQ ? a.q_heads : a.kv_heads;
       const int64_t row = (w.row0 + r) * heads + w.head, rows = (DQ ? a.q_rows : a.k_rows) * heads;
       const uint32_t sums = tmem + lanes + sum_col + (DQ ? 0 : half * 128);
@@ -628,10 +627,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           void* out = DQ ? a.d_q : half == 0 ? a.d_v : a.d_k;
           store_rows32<false>(static_cast<__nv_bfloat16*>(out) + ((w.row0 + r - lane) * heads + w.head) * a.dim,
                               static_cast<int64_t>(heads) * a.dim, min(32, w.rows - (r - lane)), col, a.dim, vec_out, stage, v, f);
-        } else if (live) {
+        } else {
           // Parts of d_k, then those of d_v.
           const int64_t part = w.split + (DQ || half == 1 ? 0 : a.key_splits);
-          store_part32(a.partial + (part * rows + row) * a.dim, col, a.dim, vec_out, v, f);
+          store_part32(a.partial + (part * rows + row - lane * heads) * a.dim, static_cast<int64_t>(heads) * a.dim,
+                       min(32, w.rows - (r - lane)), col, a.dim, vec_out, stage, v, f);
         }
         __syncwarp();
       }

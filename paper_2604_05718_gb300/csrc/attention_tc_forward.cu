@@ -519,8 +519,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           store_rows32<false>(static_cast<__nv_bfloat16*>(a.out) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
           if (a.rest != nullptr)
             store_rows32<true>(static_cast<__nv_bfloat16*>(a.rest) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
-        } else if (live) {
-          store_part32(a.partial + at_row * a.dim, col, a.dim, vec_out, o, f);
+        } else {
+          store_part32(a.partial + (at_row - lane * a.q_heads) * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
         }
         __syncwarp();
       }
