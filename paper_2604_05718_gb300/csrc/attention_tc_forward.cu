@@ -2,7 +2,9 @@
 // and the weighted sum of the values in one pass over the keys.
 //
 // A block takes 256 queries of one head, two tiles of 128 that share the keys, and
-// streams tiles of 128 keys.  Scores S (fp32) and sums O lie in tensor memory;
+// streams tiles of 128 keys.  A lone tile (a sequence's last, or a short one) takes
+// the place of both, one for the even and one for the odd tiles of keys, whose sums
+// are joined at the end.  Scores S (fp32) and sums O lie in tensor memory;
 // probabilities P (bf16) take S's place there and are the left operand of O += P V,
 // so that neither leaves the SM.  Roles:
 //   warps 0-3, 4-7  softmax of either tile, a row a thread: maximum, exponentials,
@@ -65,11 +67,13 @@ struct Control {
   // complete only after everyone has seen the last one: it takes the place again, and
   // for that the warps that wait on it have gone past.
   uint64_t p_full[3], s_full[2][3], o_done[2][3];
+  uint64_t pair_full, pair_read;  // of a lone query tile's two sums: statistics are there, sums have been read
   uint64_t work_full[kItems], work_empty[kItems];
   uint64_t drain;
   uint32_t tmem;
   volatile int failed;
   Work work[kItems];
+  float top[2][kRows], total[2][kRows];  // of a lone query tile's two sums
 };
 
 template <int H>
@@ -91,6 +95,12 @@ __device__ __forceinline__ bool next_work(Control* ctl, RingPlace<kItems>& at, W
   if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
   at.next();
   return true;
+}
+
+__device__ __forceinline__ void arrive_warp(uint64_t* bar) {
+  ptx::tc_fence_before_sync();
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(bar);
 }
 
 // Whether a tile of keys has rows that are no keys of the sequence.
@@ -153,6 +163,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&ctl->work_full[i], 1);
       ptx::mbar_init(&ctl->work_empty[i], kSoftmaxWarps + 2);
     }
+    ptx::mbar_init(&ctl->pair_full, kSoftmaxWarps);
+    ptx::mbar_init(&ctl->pair_read, kSoftmaxWarps);
     ptx::mbar_init(&ctl->drain, 1);
     ctl->failed = 0;
     ptx::fence_barrier_init();
@@ -305,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kMmaWarp) {
       // ---------------- products ----------------
       // Score tiles are numbered key tile by key tile, query tile by query tile
-      // within; number n lies in place n % kPlaces.  As many are formed ahead as there
+      // within; of a lone query tile the even and the odd key tiles take the two query
+      // tiles' parts.  Number n lies in place n % kPlaces.  As many are formed ahead as there
       // are places: n + kPlaces follows the product of n's probabilities, in whose
       // place it goes (products complete in the order of their issue).
       RingPlace<kItems> at;
@@ -326,7 +339,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!w.more) break;
         if (uniform(w.begin) == uniform(w.end)) continue;
-        const int tiles = uniform(w.rows > kRows ? 2 : 1), all = uniform(w.end - w.begin) * tiles;
+        const bool two = uniform(w.rows > kRows) != 0;
+        const int all = uniform(w.end - w.begin) * (two ? 2 : 1);
         const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
         if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag)) {
           fail(ctl, a.status, 37);
@@ -336,12 +350,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         value.next();
         int formed = 0, form_tile = 0;
         auto form = [&] {
-          if (form_tile == 0 && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag)) return false;
+          if ((form_tile == 0 || !two) && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag)) return false;
           ptx::tc_fence_after_sync();
           ++formed;
-          const bool last_of_key = form_tile + 1 == tiles;
+          const bool last_of_key = form_tile == 1 || !two;
           if (ptx::elect_one()) {
-            mma_scores<H>(tmem0 + next_place.slot * kRows, q + form_tile * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
+            mma_scores<H>(tmem0 + next_place.slot * kRows, q + (two ? form_tile : 0) * W::kTileBytes, ring0 + key.slot * W::kTileBytes, slices);
             commit_at(at_bar(offsetof(Control, s_full), 3 * form_tile + next_place.slot));
             if (last_of_key) commit_at(at_bar(offsetof(Control, kv_empty), key.slot));
             if (formed == all) commit_at(at_bar(offsetof(Control, q_empty), qs.slot));
@@ -351,23 +365,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (last_of_key) {
             key.next();
             key.next();
-            form_tile = 0;
-          } else {
-            form_tile = 1;
           }
+          form_tile ^= 1;
           return true;
         };
         while (ok && formed < W::kPlaces && formed < all) ok = form();
         int tile = 0;
         for (int n = 0; ok && n < all; ++n) {
-          ok = (tile != 0 || warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag)) &&
+          ok = ((tile != 0 && two) || warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag)) &&
                warp_wait(&ctl->p_full[place.slot], place.phase, abort_flag);
           if (!ok) break;
           ptx::tc_fence_after_sync();
-          const bool last_of_value = tile + 1 == tiles;
+          const bool last_of_value = tile == 1 || !two;
           if (ptx::elect_one()) {
             mma_weighted(tmem0 + W::kSumCol + tile * W::kSumCols, tmem0 + place.slot * kRows, 32, ring0 + value.slot * W::kTileBytes,
-                         weighted, n >= tiles);
+                         weighted, n >= 2);
             commit_at(at_bar(offsetof(Control, o_done), 3 * tile + place.slot));
             if (last_of_value) commit_at(at_bar(offsetof(Control, kv_empty), value.slot));
           }
@@ -376,10 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (last_of_value) {
             value.next();
             value.next();
-            tile = 0;
-          } else {
-            tile = 1;
           }
+          tile ^= 1;
           if (formed < all) ok = form();
         }
         if (!ok) {
@@ -400,43 +410,52 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tile = warp / 4;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t total = tmem + lanes + W::kSumCol + tile * W::kSumCols;
-    const int r = tile * kRows + (warp & 3) * 32 + lane;  // row within the item
     const float c = a.scale * kLog2e;
     uint8_t* stage = smem + W::kStage + warp * kStageBytes;
     RingPlace<kItems> at;
-    RingPlace<W::kPlaces> place;  // of the next scores, of either query tile
+    int base = 0;                 // the place of an item's first scores
     uint32_t phases = 0;          // a bit for each place: the parity of this tile's next scores and product there
     int last = 0;                 // the place of this tile's last scores
-    Work w;
+    uint32_t pair_phase = 0;
     bool ok = true;
+    // The item's fields are read again where they are needed: registers are short.
+    auto leave = [&] {
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
+      at.next();
+    };
     while (ok) {
-      if (!next_work(ctl, at, w)) {
+      if (!warp_wait(&ctl->work_full[at.slot], at.phase, abort_flag)) {
         fail(ctl, a.status, 40);
         break;
       }
-      if (!w.more) break;
-      const bool two = w.rows > kRows;
-      if (tile == 1 && !two) {
-        for (int n = (w.end - w.begin) % W::kPlaces; n > 0; --n) place.next();
+      const volatile Work& item = ctl->work[at.slot];
+      if (!item.more) break;
+      // A lone query tile is shared: these warps take its rows against every other key tile.
+      const bool two = item.rows > kRows;
+      const int begin = item.begin, end = item.end, keys = item.keys, tiles = end - begin, step = two ? 1 : 2;
+      int place = (base + tile) % W::kPlaces;
+      base = (base + tiles * (two ? 2 : 1)) % W::kPlaces;
+      if (!two && tile == 1 && tiles <= 1) {
+        leave();
         continue;
       }
-      if (tile == 1 && w.begin != w.end) place.next();
       float top = -INFINITY;  // the maximum that exponents are taken from, log2
       float2 sum = make_float2(0.f, 0.f);
-      for (int t = w.begin; t < w.end; ++t) {
-        const bool cut = ragged(t, w.keys, a.mask);
+      const int from = begin + (two ? 0 : tile);
+      for (int t = from; t < end; t += step) {
+        const bool cut = ragged(t, keys, a.mask);
         uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
-        if (cut) there = rows_there({w.key0, w.keys}, t * kRows, a.mask);
-        if (!warp_wait(&ctl->s_full[tile][place.slot], phases >> place.slot & 1u, abort_flag)) {
+        if (cut) there = rows_there({item.key0, keys}, t * kRows, a.mask);
+        if (!warp_wait(&ctl->s_full[tile][place], phases >> place & 1u, abort_flag)) {
           fail(ctl, a.status, 41);
           ok = false;
           break;
         }
-        const int here = place.slot;
+        const int here = place;
         ptx::tc_fence_after_sync();
         const uint32_t score = tmem + lanes + here * kRows;
-        place.next();
-        if (two) place.next();
+        place += W::kPlaces == 3 ? (place == 0 ? 2 : -1) : 0;  // two on
         uint32_t s0[32], s1[32], s2[32], s3[32];
         ptx::tmem_ld_32x32b_x32(score, s0);
         ptx::tmem_ld_32x32b_x32(score + 32, s1);
@@ -453,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           mask32(s3, there.w);
         }
         const float most = fmaxf(top, fmaxf(max32(s1, max32(s0, -INFINITY)), max32(s3, max32(s2, -INFINITY))) * c);
-        if (t == w.begin) {
+        if (t == from) {
           top = most;
         } else if (__any_sync(0xFFFFFFFFu, most > top + kBehind)) {
           // O holds tiles up to t - 1 once their product has completed.
@@ -478,8 +497,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         phases ^= 1u << here;
         last = here;
-        const float base = top == -INFINITY ? 0.f : -top;
-        const float2 c2 = make_float2(c, c), base2 = make_float2(base, base);
+        const float less = top == -INFINITY ? 0.f : -top;
+        const float2 c2 = make_float2(c, c), base2 = make_float2(less, less);
         uint32_t p[32];
         exp32(s0, c2, base2, sum, p);
         exp32(s1, c2, base2, sum, p + 16);
@@ -493,40 +512,83 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(&ctl->p_full[here]);
       }
       if (!ok) break;
-      if (tile == 1 && w.begin != w.end) place.back();
-      if (w.end > w.begin) {
+      if (from < end) {
         if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, abort_flag)) {
           fail(ctl, a.status, 43);
           break;
         }
         ptx::tc_fence_after_sync();
       }
-      const float s = sum.x + sum.y, f = s == 0.f ? 0.f : 1.f / s;
-      const bool live = r < w.rows;
-      const int warp_rows = min(32, w.rows - (r - lane));
-      const int64_t first = (w.row0 + r - lane) * a.q_heads + w.head, pitch = static_cast<int64_t>(a.q_heads) * a.dim;
-      const int64_t at_row = (w.row0 + r) * a.q_heads + w.head + (a.splits == 1 ? 0 : w.split * a.q_rows * a.q_heads);
-      for (int col = 0; col < a.dim; col += 32) {
+      float s = sum.x + sum.y, f0 = 1.f, f1 = 0.f;  // factors of either sum
+      const bool joined = !two && tiles > 1;
+      if (joined) {
+        const int row = (warp & 3) * 32 + lane;
+        ctl->top[tile][row] = top;
+        ctl->total[tile][row] = s;
+        arrive_warp(&ctl->pair_full);
+        if (!warp_wait(&ctl->pair_full, pair_phase, abort_flag)) {
+          fail(ctl, a.status, 44);
+          break;
+        }
+        ptx::tc_fence_after_sync();
+        const float t0 = ctl->top[0][row], t1 = ctl->top[1][row], s0 = ctl->total[0][row], s1 = ctl->total[1][row];
+        top = fmaxf(t0, t1);
+        // Nothing where there was no key; 1 without a maximum, which is a NaN's row.
+        f0 = s0 == 0.f ? 0.f : top == -INFINITY ? 1.f : exp2_approx(t0 - top);
+        f1 = s1 == 0.f ? 0.f : top == -INFINITY ? 1.f : exp2_approx(t1 - top);
+        s = s0 * f0 + s1 * f1;
+      }
+      const float f = s == 0.f ? 0.f : 1.f / s;
+      f0 *= f;
+      f1 *= f;
+      const int r = (two ? tile : 0) * kRows + (warp & 3) * 32 + lane;  // row within the item
+      const bool live = r < item.rows;
+      const int warp_rows = min(32, item.rows - (r - lane));
+      const int64_t first = (item.row0 + r - lane) * a.q_heads + item.head, pitch = static_cast<int64_t>(a.q_heads) * a.dim;
+      const int64_t at_row = (item.row0 + r) * a.q_heads + item.head + (a.splits == 1 ? 0 : item.split * a.q_rows * a.q_heads);
+      leave();
+      // Joined sums are read, and leave, 32 features by these warps and 32 by the others.
+      for (int col = joined ? 32 * tile : 0; col < a.dim; col += joined ? 64 : 32) {
         uint32_t o[32];
-        if (w.end > w.begin) {
+        if (joined) {
+          uint32_t u[32];
+          ptx::tmem_ld_32x32b_x32(tmem + lanes + W::kSumCol + col, o);
+          ptx::tmem_ld_32x32b_x32(tmem + lanes + W::kSumCol + W::kSumCols + col, u);
+          ptx::tmem_wait_ld(o);
+          ptx::tmem_wait_ld(u);
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            o[i] = __float_as_uint(fmaf(__uint_as_float(o[i]), f0, __uint_as_float(u[i]) * f1));
+        } else if (tiles > 0) {
           ptx::tmem_ld_32x32b_x32(total + col, o);
           ptx::tmem_wait_ld(o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0);
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = 0;
         }
         if (a.splits == 1) {
-          store_rows32<false>(static_cast<__nv_bfloat16*>(a.out) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
+          store_rows32<false>(static_cast<__nv_bfloat16*>(a.out) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, 1.f);
           if (a.rest != nullptr)
-            store_rows32<true>(static_cast<__nv_bfloat16*>(a.rest) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
+            store_rows32<true>(static_cast<__nv_bfloat16*>(a.rest) + first * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, 1.f);
         } else {
-          store_part32(a.partial + (at_row - lane * a.q_heads) * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, f);
+          store_part32(a.partial + (at_row - lane * a.q_heads) * a.dim, pitch, warp_rows, col, a.dim, vec_out, stage, o, 1.f);
         }
         __syncwarp();
       }
       ptx::tc_fence_before_sync();
       float* lse = a.splits == 1 ? a.lse : a.partial_lse;
-      if (live && lse != nullptr) lse[at_row] = (top + log2f(s)) * (a.splits == 1 ? kLn2 : 1.f);
+      if (live && lse != nullptr && (two || tile == 0)) lse[at_row] = (top + log2f(s)) * (a.splits == 1 ? kLn2 : 1.f);
+      if (joined) {
+        // The next item's sums come over these.
+        arrive_warp(&ctl->pair_read);
+        if (!warp_wait(&ctl->pair_read, pair_phase, abort_flag)) {
+          fail(ctl, a.status, 45);
+          break;
+        }
+        pair_phase ^= 1u;
+      }
     }
   }
 

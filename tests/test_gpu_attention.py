@@ -137,11 +137,13 @@ def test_masks(mpm, lengths, masked, dim, dtype):
         assert (lse[:sum(lengths[0])] == -math.inf).all() and (grads.d_q[:sum(lengths[0])] == 0).all()
 
 
-def test_a_whole_tile_that_is_masked(mpm):
-    t, g, off, _ = problem([140], [700], 2, 2, 64, torch.bfloat16)
+@pytest.mark.parametrize("queries", [20, 100, 140, 300])
+@pytest.mark.parametrize("which", [(0, 1, 4), (0, 2, 4), (1, 3, 5), (0, 1, 2, 3, 4)])
+def test_whole_tiles_that_are_masked(mpm, which, queries):
+    t, g, off, _ = problem([queries], [700], 2, 2, 64, torch.bfloat16)
     mask = torch.ones(700, dtype=torch.bool, device=DEV)
-    mask[:256] = False
-    mask[512:640] = False
+    for tile in which:
+        mask[128 * tile:128 * tile + 128] = False
     t["k"][~mask], t["v"][~mask] = float("nan"), float("nan")
     run_and_check(mpm, t, g, off, mask)
 
