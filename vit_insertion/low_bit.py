@@ -6,7 +6,10 @@ the library's encoder-block operators:
     matmul_mxfp4 with weights that are laid out in 4 bits once;
   - every residual addition, its gate (a vector of features per branch, as
     LayerScale has) and the norm before the next block is one block_norm.
-Embedding, attention, GELU and the dense head are PyTorch's.
+Embedding, GELU and the dense head are PyTorch's, and so is attention unless
+``attention="packed"`` asks for the library's, which takes queries, keys and values
+as they lie in the joint projection.  ``rotary=True`` turns queries and keys by the
+patches' rows and columns on the grid; a merged token has the mean of its patches'.
 
 ``tune_last_gate`` fits the last branch's gate to the full model's features by
 gradient descent: what merging and 4 bits shift, feature by feature.
@@ -37,11 +40,17 @@ EPS = 1e-5  # torch's layer norm, which the full model calls without one
 class LowBitViT(ViT):
     """ViT with MXFP4 linear layers and fused norms; same constructor and seed, same weights before rounding."""
 
-    def __init__(self, cfg, device, dtype=torch.bfloat16, seed: int = 0):
+    def __init__(self, cfg, device, dtype=torch.bfloat16, seed: int = 0, *, attention: str = "torch", rotary: bool = False):
         super().__init__(cfg, device, dtype, seed)
         import paper_2604_05718_gb300 as ops
 
-        self.ops = ops
+        if attention not in ("torch", "packed"):
+            raise ValueError("attention must be 'torch' or 'packed'")
+        self.ops, self.packed = ops, attention == "packed"
+        # Pairs of features that turn with the row and with the column.
+        pairs = cfg.dim // cfg.heads // 2
+        self.sections = (pairs // 2, pairs - pairs // 2)
+        self.frequencies = ops.rotary_frequencies(self.sections, 100.0, self.device) if rotary else None
         for p in self.blocks:
             for name in LINEARS:
                 p[name] = ops.quantize_mxfp4(p.pop(name + "_w"))
@@ -69,12 +78,39 @@ class LowBitViT(ViT):
         """Layer norm of a stream that no branch is added to: at the start and behind a merge."""
         return F.layer_norm(x, (self.cfg.dim,), weight.to(x.dtype), bias.to(x.dtype), eps=EPS)
 
-    def branches(self, x: torch.Tensor, h: torch.Tensor, p: dict, cu: torch.Tensor, max_len: int):
+    def attend(self, qkv: torch.Tensor, starts: torch.Tensor, max_len: int, at: torch.Tensor | None) -> torch.Tensor:
+        """Attention within each image: qkv [S, 3 heads, Dh] (turned in place by positions `at`) -> [S, dim]."""
+        heads = self.cfg.heads
+        if at is not None:
+            both = qkv[:, :2 * heads]
+            self.ops.rotary(both, at, self.frequencies, self.sections, out=both, device_status=self.status)
+        q, k, v = (qkv[:, i * heads:(i + 1) * heads] for i in range(3))
+        if self.packed:
+            a, _ = self.ops.cross_attention(q, k, v, q_offsets=starts, k_offsets=starts, device_status=self.status)
+        else:
+            a = varlen_attention(q.contiguous(), k.contiguous(), v.contiguous(), starts.to(torch.int32), max_len)
+        return a.reshape(qkv.shape[0], self.cfg.dim)
+
+    def grid_positions(self, b: int) -> torch.Tensor:
+        """Rows and columns of all patches, float32 [B * N, 2], counted from 1: special tokens are at 0."""
+        g = self.cfg.grid
+        n = torch.arange(g * g, device=self.device)
+        return torch.stack([n // g + 1, n % g + 1], dim=1).float().repeat(b, 1)
+
+    def merged_positions(self, at: torch.Tensor, off: torch.Tensor, m: torch.Tensor, off1: torch.Tensor, total: int):
+        """Positions after a merge: the mean over the tokens that map m took together."""
+        rows = torch.arange(at.shape[0], device=at.device)
+        to = off1[torch.searchsorted(off[1:], rows, right=True)] + m[:at.shape[0]]
+        total_at = torch.zeros(total, 2, device=at.device).index_add_(0, to, at)
+        return total_at / torch.zeros(total, 1, device=at.device).index_add_(0, to, torch.ones_like(at[:, :1]))
+
+    def branches(self, x: torch.Tensor, h: torch.Tensor, p: dict, starts: torch.Tensor, max_len: int,
+                 at: torch.Tensor | None = None):
         """One block from the stream x and its norm h: (stream after attention, output of the MLP branch)."""
         cfg = self.cfg
         s = x.shape[0]
-        qkv = self.linear(h, p, "qkv").view(s, 3, cfg.heads, cfg.dim // cfg.heads)
-        a = varlen_attention(*(qkv[:, i].contiguous() for i in range(3)), cu, max_len).reshape(s, cfg.dim)
+        qkv = self.linear(h, p, "qkv").view(s, 3 * cfg.heads, cfg.dim // cfg.heads)
+        a = self.attend(qkv, starts, max_len, at)
         x, h, _ = self.ops.block_norm(self.linear(a, p, "proj"), x, norm="layer", gate=p["gate1"], pre_weight=p["ln2_w"],
                                       pre_bias=p["ln2_b"], eps=EPS, device_status=self.status)
         return x, self.linear(F.gelu(self.linear(h, p, "fc1")), p, "fc2")
@@ -89,6 +125,9 @@ class LowBitViT(ViT):
         maps = []
         points = set(cfg.insert_at if insert_at is None else insert_at) if mpm is not None else set()
         h = None
+        at = None if self.frequencies is None else self.grid_positions(b)
+        zeros = torch.zeros(b * e, 2, device=self.device)
+        turned = None if at is None else self.join(zeros, at, off)
         for i, p in enumerate(self.blocks):
             if i in points:
                 specials, patches = self.split(x, off)
@@ -96,13 +135,16 @@ class LowBitViT(ViT):
                 off1_host = off1.cpu()                       # the merged length decides the next shapes
                 longest = int((off1_host[1:] - off1_host[:-1]).max())
                 maps.append((m, off))
+                if at is not None:
+                    at = self.merged_positions(at, off, m, off1, int(off1_host[-1]))
+                    turned = self.join(zeros, at, off1)
                 off = off1
                 x = self.join(specials, merged[:int(off1_host[-1])], off)
                 h = None
             if h is None:
                 h = self.norm(x, p["ln1_w"], p["ln1_b"])
-            cu = (off + e * torch.arange(b + 1, device=self.device)).to(torch.int32)
-            x, y = self.branches(x, h, p, cu, longest + e)
+            starts = off + e * torch.arange(b + 1, device=self.device)
+            x, y = self.branches(x, h, p, starts, longest + e, turned)
             if i + 1 == len(self.blocks):
                 return x, y, maps, off
             # The next block's norm comes with the addition, unless a merge changes the rows in between.
@@ -180,15 +222,19 @@ def main() -> int:
     cfg = VIT_CONFIGS[args.model]
     images = synthetic_images(args.batch, cfg.image, cfg.patch, args.seed, dev)
     full, low = ViT(cfg, dev, seed=args.seed), LowBitViT(cfg, dev, seed=args.seed)
+    packed = LowBitViT(cfg, dev, seed=args.seed, attention="packed")
     ws = mpm.new_workspace(args.batch * cfg.tokens, args.batch, cfg.dim, torch.bfloat16, dev)
     with torch.inference_mode():
         want = full.forward(images)
         ms = {"full": timed(lambda: full.forward(images), args.steps, args.warmup),
               "merged": timed(lambda: full.forward(images, mpm=mpm, workspace=ws), args.steps, args.warmup),
               "low_bit": timed(lambda: low.forward(images), args.steps, args.warmup),
-              "low_bit_merged": timed(lambda: low.forward(images, mpm=mpm, workspace=ws), args.steps, args.warmup)}
+              "low_bit_merged": timed(lambda: low.forward(images, mpm=mpm, workspace=ws), args.steps, args.warmup),
+              "low_bit_packed": timed(lambda: packed.forward(images), args.steps, args.warmup),
+              "low_bit_packed_merged": timed(lambda: packed.forward(images, mpm=mpm, workspace=ws), args.steps, args.warmup)}
         got = low.forward(images, mpm=mpm, workspace=ws)
         low.check_status()
+        packed.check_status()
         likeness = F.cosine_similarity(got.float(), want.float(), dim=1).mean().item()
     print(json.dumps({"metric": "ViT encoder + dense head, 4-bit linear layers and fused norms", "model": cfg.name,
                       "batch": args.batch, "ms": ms, "fps": {k: args.batch / v * 1e3 for k, v in ms.items()},
