@@ -172,10 +172,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+// How a block's roles give up.  A role may wait for as long as a work item takes,
+// and that is as long as its sequence: 20 us are allowed for each of its tiles, ten
+// times what they take.
+struct Bounds {
+  volatile int failed;  // a wait ran out somewhere
+  uint32_t limit_us;
+  __device__ __forceinline__ void init(const AttentionArgs& a) {
+    const uint64_t rows = static_cast<uint64_t>(a.q_rows) * (a.q_heads / a.kv_heads) + static_cast<uint64_t>(a.k_rows);
+    const uint64_t us = kWaitNs / 1000 + rows / kRows * 20;
+    failed = 0;
+    limit_us = us < 0xFFFFFFFFu ? static_cast<uint32_t>(us) : 0xFFFFFFFFu;
+  }
+};
 // Bounded wait of a whole warp: one answer for all of its lanes.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag, kWaitNs));
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, Bounds* bounds) {
+  bool done = ptx::mbar_try_wait(bar, parity);
+  if (!done) done = ptx::mbar_wait(bar, parity, &bounds->failed, static_cast<uint64_t>(bounds->limit_us) * 1000);
+  return __all_sync(0xFFFFFFFFu, done);
 }
+// The wait for copies under way, at a block's end.
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) { ptx::mbar_wait(bar, parity, nullptr, kWaitNs); }
 
 // A value that all lanes hold, in a form that the compiler knows to be uniform: what
 // the products' issuing warp computes with (see ptx::elect_one).

@@ -58,7 +58,7 @@ struct Control {
   uint64_t stat_full[kStats], stat_empty[kStats];
   uint64_t drain;
   uint32_t tmem;
-  volatile int failed;
+  Bounds bounds;
   Work work[kItems];
   __align__(16) float lse[kStats][kRows];     // log2, +infinity where there is no query
   __align__(16) float delta[kStats][kRows];
@@ -71,12 +71,12 @@ constexpr size_t smem_bytes() {
 static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "a block's shared memory");
 
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
-  ctl->failed = 1;
+  ctl->bounds.failed = 1;
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
 }
 
 __device__ __forceinline__ bool next_work(Control* ctl, RingPlace<kItems>& at, Work& w) {
-  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->failed)) return false;
+  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->bounds)) return false;
   w = ctl->work[at.slot];
   __syncwarp();
   if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
@@ -131,7 +131,6 @@ __device__ __forceinline__ void init_control(Control* ctl, int work_readers, int
     ptx::mbar_init(&ctl->stat_empty[i], stat_readers);
   }
   ptx::mbar_init(&ctl->drain, 1);
-  ctl->failed = 0;
   ptx::fence_barrier_init();
 }
 
@@ -147,7 +146,7 @@ __device__ __forceinline__ bool put_stats(Control* ctl, RingPlace<kStats>& at, c
     l[i] = r < rows ? log2_stat(__ldg(a.stats + p)) : INFINITY;
     d[i] = r < rows ? a.delta[p] : 0.f;
   }
-  if (!warp_wait(&ctl->stat_empty[at.slot], at.phase ^ 1u, &ctl->failed)) return false;
+  if (!warp_wait(&ctl->stat_empty[at.slot], at.phase ^ 1u, &ctl->bounds)) return false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     ctl->lse[at.slot][lane + 32 * i] = l[i];
@@ -160,7 +159,7 @@ __device__ __forceinline__ bool put_stats(Control* ctl, RingPlace<kStats>& at, c
   return true;
 }
 
-// How a block's loads stand, for the wait before it leaves after a failure.
+// How a block's loads stand, for the wait before it leaves: a role may have given up while they were under way.
 template <int H>
 struct Loads {
   int kept = 0, streamed = 0;
@@ -175,14 +174,14 @@ struct Loads {
     using W = Shape<H>;
     for (int s = 0; s < W::kKept; ++s) {
       const int n = (kept - s + W::kKept - 1) / W::kKept;
-      if (n > 0) warp_wait(&ctl->kept_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+      if (n > 0) drain_wait(&ctl->kept_full[s], static_cast<uint32_t>(n - 1) & 1u);
     }
     for (int s = 0; s < W::kSlots; ++s) {
       const int n = (streamed - s + W::kSlots - 1) / W::kSlots;
       if (n <= 0) continue;
       // full and raw both complete once a use of the slot where the tile was zeroed; full alone otherwise.
-      if (raw_loaded >> s & 1u) warp_wait(&ctl->raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
-      else warp_wait(&ctl->full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+      if (raw_loaded >> s & 1u) drain_wait(&ctl->raw[s], (raw_phase >> s & 1u) ^ 1u);
+      else drain_wait(&ctl->full[s], static_cast<uint32_t>(n - 1) & 1u);
     }
   }
 };
@@ -199,10 +198,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
   Control* ctl = reinterpret_cast<Control*>(smem + W::kSmem);
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
-  volatile int* abort_flag = &ctl->failed;
+  Bounds* bounds = &ctl->bounds;
 
   if (threadIdx.x == 0) {
     init_control<H>(ctl, kWorkWarps + 3, kWorkWarps);
+    ctl->bounds.init(a);
     ptx::prefetch_tensor_map(&map_q);
     ptx::prefetch_tensor_map(&map_k);
     ptx::prefetch_tensor_map(&map_v);
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         w.end = part.end;
         w.more = 1;
       }
-      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
+      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
         fail(ctl, a.status, 51);
         break;
       }
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!w.more) break;
       if (w.begin == w.end) continue;
       const int row = static_cast<int>(w.row0);
-      if (!warp_wait(&ctl->kept_empty[kept.slot], kept.phase ^ 1u, abort_flag)) {
+      if (!warp_wait(&ctl->kept_empty[kept.slot], kept.phase ^ 1u, bounds)) {
         fail(ctl, a.status, 52);
         break;
       }
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool second = i % 2 != 0;
         // Sums run over the keys for d_q, over the queries of both streamed tensors for d_k and d_v.
         const bool raw = ragged(t, w.cols, DQ ? a.mask : nullptr) && !(DQ && second);
-        if (!warp_wait(&ctl->empty[ring.slot], ring.phase ^ 1u, abort_flag)) {
+        if (!warp_wait(&ctl->empty[ring.slot], ring.phase ^ 1u, bounds)) {
           fail(ctl, a.status, 53);
           ok = false;
           break;
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
     }
-    if (ctl->failed) loads.drain(ctl);
+    loads.drain(ctl);
   } else if (warp == kZeroWarp) {
     // ---------------- rows that a sum must not see ----------------
     RingPlace<kItems> at;
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint8_t* mask = DQ ? a.mask : nullptr;
         if (ragged(t, w.cols, mask) && !(DQ && i % 2 != 0)) {
           const uint4 there = rows_there(cols, t * kRows, mask);
-          if (!warp_wait(&ctl->raw[ring.slot], raw_phase >> ring.slot & 1u, abort_flag)) {
+          if (!warp_wait(&ctl->raw[ring.slot], raw_phase >> ring.slot & 1u, bounds)) {
             fail(ctl, a.status, 55);
             ok = false;
             break;
@@ -382,15 +382,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int begin = uniform(w.begin), end = uniform(w.end);
       if (begin == end) continue;
       const uint32_t mine = smem0 + kept.slot * 2 * W::kTileBytes;  // queries and d_out, or keys and values
-      if (!warp_wait(&ctl->kept_full[kept.slot], kept.phase, abort_flag)) {
+      if (!warp_wait(&ctl->kept_full[kept.slot], kept.phase, bounds)) {
         fail(ctl, a.status, 59);
         break;
       }
       // Scores and d_out.v of tile t; `last`: the kept tiles are not read after these.
       auto scores = [&](const RingPlace<W::kSlots>& x) {
-        if (!warp_wait(&ctl->full[x.slot], x.phase, abort_flag)) return false;
+        if (!warp_wait(&ctl->full[x.slot], x.phase, bounds)) return false;
         if (DQ) {
-          if (!warp_wait(&ctl->s_free, free_phase, abort_flag)) return false;
+          if (!warp_wait(&ctl->s_free, free_phase, bounds)) return false;
           free_phase ^= 1u;
         }
         ptx::tc_fence_after_sync();
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       auto seconds = [&](const RingPlace<W::kSlots>& y, int t) {
-        if (!warp_wait(&ctl->full[y.slot], y.phase, abort_flag)) return false;
+        if (!warp_wait(&ctl->full[y.slot], y.phase, bounds)) return false;
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) {
           mma_scores<H>(tmem0 + t_col + (DQ ? (t & 1) * 128 : 0), mine + W::kTileBytes, ring0 + y.slot * W::kTileBytes, slices);
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (DQ) {
           if (!last) ok = scores(x1) && seconds(y1, t + 1);
           const int b = t & 1;
-          ok = ok && warp_wait(&ctl->ds_full[b], b == 0 ? ds_phase[0] : ds_phase[1], abort_flag);
+          ok = ok && warp_wait(&ctl->ds_full[b], b == 0 ? ds_phase[0] : ds_phase[1], bounds);
           if (!ok) break;
           if (b == 0) ds_phase[0] ^= 1u;
           else ds_phase[1] ^= 1u;
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         } else {
-          ok = warp_wait(&ctl->p_full, p_phase, abort_flag);
+          ok = warp_wait(&ctl->p_full, p_phase, bounds);
           if (!ok) break;
           p_phase ^= 1u;
           ptx::tc_fence_after_sync();
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + y.slot * W::kTileBytes, weighted, t != begin);
           __syncwarp();
           if (!last) ok = scores(x1);
-          ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], abort_flag);
+          ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], bounds);
           if (!ok) break;
           ds_phase[0] ^= 1u;
           ptx::tc_fence_after_sync();
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!w.more) break;
       float2 base = make_float2(0.f, 0.f), less = base;  // of the thread's query (d_q)
       if (DQ && w.begin != w.end) {
-        if (!warp_wait(&ctl->stat_full[stat.slot], stat.phase, abort_flag)) {
+        if (!warp_wait(&ctl->stat_full[stat.slot], stat.phase, bounds)) {
           fail(ctl, a.status, 62);
           break;
         }
@@ -514,12 +514,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           there[0] = half == 0 ? all.x : all.z;
           there[1] = half == 0 ? all.y : all.w;
         }
-        if (!DQ && !warp_wait(&ctl->stat_full[stat.slot], stat.phase, abort_flag)) {
+        if (!DQ && !warp_wait(&ctl->stat_full[stat.slot], stat.phase, bounds)) {
           fail(ctl, a.status, 63);
           ok = false;
           break;
         }
-        if (!warp_wait(&ctl->s_full, s_phase, abort_flag)) {
+        if (!warp_wait(&ctl->s_full, s_phase, bounds)) {
           fail(ctl, a.status, 64);
           ok = false;
           break;
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           arrive_warp(&ctl->p_full);
         }
         const int place = DQ ? t & 1 : 0;
-        if (!warp_wait(&ctl->t_full[place], t_phases >> place & 1u, abort_flag)) {
+        if (!warp_wait(&ctl->t_full[place], t_phases >> place & 1u, bounds)) {
           fail(ctl, a.status, 65);
           ok = false;
           break;
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (w.begin != w.end) {
-        if (!warp_wait(&ctl->sum_done, sum_phase, abort_flag)) {
+        if (!warp_wait(&ctl->sum_done, sum_phase, bounds)) {
           fail(ctl, a.status, 66);
           break;
         }

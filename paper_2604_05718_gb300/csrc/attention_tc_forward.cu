@@ -71,7 +71,7 @@ struct Control {
   uint64_t work_full[kItems], work_empty[kItems];
   uint64_t drain;
   uint32_t tmem;
-  volatile int failed;
+  Bounds bounds;
   Work work[kItems];
   float top[2][kRows], total[2][kRows];  // of a lone query tile's two sums
 };
@@ -83,13 +83,13 @@ constexpr size_t smem_bytes() {
 static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "a block's shared memory");
 
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
-  ctl->failed = 1;
+  ctl->bounds.failed = 1;
   report(status, MPM_ERR_DEVICE_TIMEOUT, role);
 }
 
 // Reads the next work item; false after a wait that ran out.
 __device__ __forceinline__ bool next_work(Control* ctl, RingPlace<kItems>& at, Work& w) {
-  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->failed)) return false;
+  if (!warp_wait(&ctl->work_full[at.slot], at.phase, &ctl->bounds)) return false;
   w = ctl->work[at.slot];
   __syncwarp();
   if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&ctl->work_empty[at.slot]);
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
   Control* ctl = reinterpret_cast<Control*>(smem + W::kSmem);
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
-  volatile int* abort_flag = &ctl->failed;
+  Bounds* bounds = &ctl->bounds;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(&ctl->pair_full, kSoftmaxWarps);
     ptx::mbar_init(&ctl->pair_read, kSoftmaxWarps);
     ptx::mbar_init(&ctl->drain, 1);
-    ctl->failed = 0;
+    ctl->bounds.init(a);
     ptx::fence_barrier_init();
     ptx::prefetch_tensor_map(&map_q);
     ptx::prefetch_tensor_map(&map_k);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           w.end = part.end;
           w.more = 1;
         }
-        if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, abort_flag)) {
+        if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
           fail(ctl, a.status, 31);
           break;
         }
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!w.more) break;
         if (w.begin == w.end) continue;
         const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
-        if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, abort_flag)) {
+        if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, bounds)) {
           fail(ctl, a.status, 32);
           break;
         }
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 2 * w.begin; i < 2 * w.end; ++i) {
           const int t = i / 2;
           const bool value = i % 2 != 0, raw = value && ragged(t, w.keys, a.mask);
-          if (!warp_wait(&ctl->kv_empty[ks.slot], ks.phase ^ 1u, abort_flag)) {
+          if (!warp_wait(&ctl->kv_empty[ks.slot], ks.phase ^ 1u, bounds)) {
             fail(ctl, a.status, 33);
             ok = false;
             break;
@@ -270,17 +270,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) break;
       }
-      if (ctl->failed) {
-        // Copies under way land before the block ends.  A slot's last load completed phase (number of its loads - 1).
+      {
+        // Copies under way land before the block ends, whoever may have given up.  A slot's last load completed phase (number of its loads - 1).
         for (int s = 0; s < W::kQueries; ++s) {
           const int n = (q_loads - s + W::kQueries - 1) / W::kQueries;
-          if (n > 0) warp_wait(&ctl->q_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+          if (n > 0) drain_wait(&ctl->q_full[s], static_cast<uint32_t>(n - 1) & 1u);
         }
         for (int s = 0; s < W::kSlots; ++s) {
           const int n = (kv_loads - s + W::kSlots - 1) / W::kSlots;
           if (n <= 0) continue;
-          if (raw_loaded >> s & 1u) warp_wait(&ctl->kv_raw[s], (raw_phase >> s & 1u) ^ 1u, nullptr);
-          else warp_wait(&ctl->kv_full[s], static_cast<uint32_t>(n - 1) & 1u, nullptr);
+          if (raw_loaded >> s & 1u) drain_wait(&ctl->kv_raw[s], (raw_phase >> s & 1u) ^ 1u);
+          else drain_wait(&ctl->kv_full[s], static_cast<uint32_t>(n - 1) & 1u);
         }
       }
     } else if (warp == kZeroWarp) {
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ks.next();
           if (ragged(t, w.keys, a.mask)) {
             const uint4 there = rows_there(keys, t * kRows, a.mask);
-            if (!warp_wait(&ctl->kv_raw[ks.slot], raw_phase >> ks.slot & 1u, abort_flag)) {
+            if (!warp_wait(&ctl->kv_raw[ks.slot], raw_phase >> ks.slot & 1u, bounds)) {
               fail(ctl, a.status, 35);
               ok = false;
               break;
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool two = uniform(w.rows > kRows) != 0;
         const int all = uniform(w.end - w.begin) * (two ? 2 : 1);
         const uint32_t q = smem0 + qs.slot * 2 * W::kTileBytes;
-        if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, abort_flag)) {
+        if (!warp_wait(&ctl->q_full[qs.slot], qs.phase, bounds)) {
           fail(ctl, a.status, 37);
           break;
         }
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         value.next();
         int formed = 0, form_tile = 0;
         auto form = [&] {
-          if ((form_tile == 0 || !two) && !warp_wait(&ctl->kv_full[key.slot], key.phase, abort_flag)) return false;
+          if ((form_tile == 0 || !two) && !warp_wait(&ctl->kv_full[key.slot], key.phase, bounds)) return false;
           ptx::tc_fence_after_sync();
           ++formed;
           const bool last_of_key = form_tile == 1 || !two;
@@ -372,8 +372,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         while (ok && formed < W::kPlaces && formed < all) ok = form();
         int tile = 0;
         for (int n = 0; ok && n < all; ++n) {
-          ok = ((tile != 0 && two) || warp_wait(&ctl->kv_full[value.slot], value.phase, abort_flag)) &&
-               warp_wait(&ctl->p_full[place.slot], place.phase, abort_flag);
+          ok = ((tile != 0 && two) || warp_wait(&ctl->kv_full[value.slot], value.phase, bounds)) &&
+               warp_wait(&ctl->p_full[place.slot], place.phase, bounds);
           if (!ok) break;
           ptx::tc_fence_after_sync();
           const bool last_of_value = tile == 1 || !two;
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       at.next();
     };
     while (ok) {
-      if (!warp_wait(&ctl->work_full[at.slot], at.phase, abort_flag)) {
+      if (!warp_wait(&ctl->work_full[at.slot], at.phase, bounds)) {
         fail(ctl, a.status, 40);
         break;
       }
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool cut = ragged(t, keys, a.mask);
         uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
         if (cut) there = rows_there({item.key0, keys}, t * kRows, a.mask);
-        if (!warp_wait(&ctl->s_full[tile][place], phases >> place & 1u, abort_flag)) {
+        if (!warp_wait(&ctl->s_full[tile][place], phases >> place & 1u, bounds)) {
           fail(ctl, a.status, 41);
           ok = false;
           break;
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           top = most;
         } else if (__any_sync(0xFFFFFFFFu, most > top + kBehind)) {
           // O holds tiles up to t - 1 once their product has completed.
-          if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, abort_flag)) {
+          if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, bounds)) {
             fail(ctl, a.status, 42);
             ok = false;
             break;
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (from < end) {
-        if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, abort_flag)) {
+        if (!warp_wait(&ctl->o_done[tile][last], (phases >> last & 1u) ^ 1u, bounds)) {
           fail(ctl, a.status, 43);
           break;
         }
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ctl->top[tile][row] = top;
         ctl->total[tile][row] = s;
         arrive_warp(&ctl->pair_full);
-        if (!warp_wait(&ctl->pair_full, pair_phase, abort_flag)) {
+        if (!warp_wait(&ctl->pair_full, pair_phase, bounds)) {
           fail(ctl, a.status, 44);
           break;
         }
@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (joined) {
         // The next item's sums come over these.
         arrive_warp(&ctl->pair_read);
-        if (!warp_wait(&ctl->pair_read, pair_phase, abort_flag)) {
+        if (!warp_wait(&ctl->pair_read, pair_phase, bounds)) {
           fail(ctl, a.status, 45);
           break;
         }
