@@ -94,6 +94,11 @@ __device__ __forceinline__ bool ragged(int tile, int rows, const uint8_t* mask) 
 }
 __device__ __forceinline__ float log2_stat(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
+// What rounding x to the packed pair left, as a pair.
+__device__ __forceinline__ uint32_t pack_rest(uint32_t rounded, float2 x) {
+  const float2 r = norm::add(x, make_float2(-__uint_as_float(rounded << 16), -__uint_as_float(rounded & 0xFFFF0000u)));
+  return pack_bf16(r.x, r.y);
+}
 // Sets a bit's value to `otherwise` where the bit is not set.
 __device__ __forceinline__ void keep32(uint32_t (&r)[32], uint32_t there, uint32_t otherwise) {
 #pragma unroll
@@ -101,6 +106,7 @@ __device__ __forceinline__ void keep32(uint32_t (&r)[32], uint32_t there, uint32
 }
 
 constexpr uint32_t kApart = 64;  // the warps leave their words 64 columns apart, over d_out.v
+constexpr uint32_t kRest = 32;   // and behind them what their rounding left
 
 template <int H>
 __device__ __forceinline__ void init_control(Control* ctl, int work_readers, int stat_readers) {
@@ -431,7 +437,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           else ds_phase[1] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128 + kRest, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + t_col + (t & 1) * 128, kApart, ring0 + x.slot * W::kTileBytes, weighted, true);
             commit_at(at_bar(offsetof(Control, empty), x.slot));
             if (last) commit_at(at_bar(offsetof(Control, sum_done), 0));
           }
@@ -450,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           ds_phase[0] ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one()) {
-            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col + kRest, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
+            mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, true);
             commit_at(at_bar(offsetof(Control, empty), x.slot));
             commit_at(at_bar(offsetof(Control, empty), y.slot));
             if (last) commit_at(at_bar(offsetof(Control, sum_done), 0));
@@ -569,12 +577,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         t_phases ^= 1u << place;
         ptx::tc_fence_after_sync();
         const uint32_t from = tmem + lanes + t_col + place * 128 + half * 64;
-        uint32_t words[32];
+        // ds as the sum of two bf16 values: rounded to one, its error would be d_q's and d_k's
+        // largest by far where keys have much in common (its sum over them is 0, that of the
+        // roundings is not).
+        uint32_t both[2][32];
+        ptx::tmem_ld_32x32b_x32(from, both[0]);
+        ptx::tmem_ld_32x32b_x32(from + 32, both[1]);
+        ptx::tmem_wait_ld(both[0]);
+        ptx::tmem_wait_ld(both[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t d[32];
-          ptx::tmem_ld_32x32b_x32(from + 32 * h, d);
-          ptx::tmem_wait_ld(d);
+          uint32_t (&d)[32] = both[h];
+          uint32_t words[16], rest[16];
           if (cut) keep32(d, there[h], 0u);
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
@@ -588,11 +602,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                                        make_float2(__uint_as_float(p[h][i]), __uint_as_float(p[h][i + 1])));
             const float2 y = norm::mul(norm::add(make_float2(__uint_as_float(d[i + 2]), __uint_as_float(d[i + 3])), l1),
                                        make_float2(__uint_as_float(p[h][i + 2]), __uint_as_float(p[h][i + 3])));
-            words[16 * h + i / 2] = pack_bf16(x.x, x.y) & keep;
-            words[16 * h + i / 2 + 1] = pack_bf16(y.x, y.y) & keep;
+            words[i / 2] = pack_bf16(x.x, x.y) & keep;
+            words[i / 2 + 1] = pack_bf16(y.x, y.y) & keep;
+            rest[i / 2] = pack_rest(words[i / 2], x) & keep;
+            rest[i / 2 + 1] = pack_rest(words[i / 2 + 1], y) & keep;
           }
+          tmem_st_x16(from + 16 * h, words);
+          tmem_st_x16(from + kRest + 16 * h, rest);
         }
-        tmem_st_x32(from, words);
         tmem_wait_st();
         arrive_warp(&ctl->ds_full[place]);
         if (!DQ) {
