@@ -538,7 +538,8 @@ MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_sca
  *                 against d_q as sequences get longer
  *   lse           optional float [q_rows, q_heads], for the backward pass
  *   workspace     mpm_cross_attention_workspace_size(..) bytes, 256-byte aligned
- *                 (NULL where that is 0)
+ *                 (NULL where that is 0); calls that may run at the same time,
+ *                 graphs among them, have one each
  *   device_status optional int32 [2] device word: offsets that are not
  *                 0 = off[0] <= ... <= off[batch] <= rows are reported as
  *                 MPM_ERR_DEVICE_CHECK (detail = index), a wait in a kernel that
@@ -547,8 +548,10 @@ MPM_API mpm_status mpm_mxfp4_matmul(const uint8_t* a_codes, const uint8_t* a_sca
  * Rows and heads of a tensor must not overlap: with several of them, either
  * stride is at least head_dim, and one at least what the other dimension spans.
  * Buffers need only the alignment of their elements; 16-byte aligned rows and
- * heads of bf16 run on the tensor cores (products of bf16 values, probabilities
- * rounded to bf16), all else, fp32 among it, in fp32 on the CUDA cores.
+ * heads of bf16 run as products of bf16 values (probabilities rounded to bf16,
+ * score gradients as the sum of two), all else, fp32 among it, as products of two
+ * tf32 values a factor, as good as fp32's to 2^-21 of a product.  Infinities and
+ * values within 2^-12 of the largest fp32 end as NaN there.
  * Statistics and sums are fp32, taken in a fixed order: the same call gives the
  * same bits.  1 <= head_dim <= MPM_ATTENTION_MAX_HEAD_DIM, kv_heads divides
  * q_heads, scale > 0.  An output, the workspace or the status word over an input

@@ -45,8 +45,8 @@ struct AttentionArgs {
   bool vec;                  // four elements of any row can be loaded at once
 };
 
-cudaError_t launch_attention_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
-cudaError_t launch_attention_backward_simt(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
+cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
+cudaError_t launch_attention_backward_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 // bf16 whose rows and heads are 16-byte aligned, on the tensor cores.
 cudaError_t launch_attention_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream);
 // bf16, 16-byte aligned, head_dim a multiple of 8: blocks of `queries` queries, `cluster` blocks a sequence.

@@ -102,10 +102,12 @@ int splits_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_
 struct Plan {
   int splits, key_splits;
 };
-Plan plan_simt(const Shape& s) {
-  const int64_t group = s.q_heads / s.kv_heads;
-  return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 4, 1),
-          splits_for(s.k_rows, 64, s.kv_heads, s.q_rows * group, 64, s.batch, 4, 1)};
+// The fp32 kernels' tiles: streamed ones of 64 rows, their own of 64 too, but for gradients of wide heads.
+Plan plan_f32(const Shape& s) { return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 4, 1), 1}; }
+Plan plan_f32_backward(const Shape& s) {
+  const int64_t group = s.q_heads / s.kv_heads, tile = s.dim <= 64 ? 64 : 128, ways = s.dim <= 64 ? 4 : 2;
+  return {splits_for(s.q_rows, tile, s.q_heads, s.k_rows, 64, s.batch, ways, 1),
+          splits_for(s.k_rows, tile, s.kv_heads, s.q_rows * group, 64, s.batch, ways, 1)};
 }
 
 // The tensor-core kernels' tiles.  A part pays from eight tiles on: parts have to be
@@ -159,9 +161,9 @@ size_t backward_bytes(const Shape& s, const Plan& p) {
 // What a caller provides: enough for either kind of kernels, since the shape alone does not tell which runs.
 size_t forward_need(const Shape& s) {
   const FewPlan few = plan_few(s);
-  return std::max({forward_bytes(s, plan_simt(s)), forward_bytes(s, plan_tc(s)), forward_bytes(s, {few.splits, 1})});
+  return std::max({forward_bytes(s, plan_f32(s)), forward_bytes(s, plan_tc(s)), forward_bytes(s, {few.splits, 1})});
 }
-size_t backward_need(const Shape& s) { return std::max(backward_bytes(s, plan_simt(s)), backward_bytes(s, plan_tc_backward(s))); }
+size_t backward_need(const Shape& s) { return std::max(backward_bytes(s, plan_f32_backward(s)), backward_bytes(s, plan_tc_backward(s))); }
 
 mpm::AttentionArgs common_args(const Shape& s, const Heads& q, const Heads& k, const Heads& v, const int64_t* q_offsets,
                                const int64_t* k_offsets, float scale, const uint8_t* mask, int32_t* status) {
@@ -239,7 +241,7 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   if (!aligned(out, e) || !aligned(out_rest, e) || !aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
   const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv);
   const FewPlan few = tc ? plan_few(s) : FewPlan{0, 1, 1};
-  const Plan plan = few.queries > 0 ? Plan{few.splits, 1} : tc ? plan_tc(s) : plan_simt(s);
+  const Plan plan = few.queries > 0 ? Plan{few.splits, 1} : tc ? plan_tc(s) : plan_f32(s);
   const size_t need = forward_need(s);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads;
@@ -264,7 +266,7 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
   cudaError_t err = few.queries > 0 ? mpm::launch_attention_few(a, few.queries, few.cluster, on)
                     : tc            ? mpm::launch_attention_tc(a, sms, on)
-                                    : mpm::launch_attention_simt(a, dtype == MPM_BF16, sms, on);
+                                    : mpm::launch_attention_f32(a, dtype == MPM_BF16, sms, on);
   if (err == cudaSuccess && a.splits > 1) err = mpm::launch_attention_join(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }
@@ -296,7 +298,7 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
     if (!aligned(p, e)) return MPM_ERR_ALIGNMENT;
   if (!aligned(lse, 4)) return MPM_ERR_ALIGNMENT;
   const bool tc = dtype == MPM_BF16 && tc_heads(hq) && tc_heads(hk) && tc_heads(hv) && tc_heads(hg);
-  const Plan plan = tc ? plan_tc_backward(s) : plan_simt(s);
+  const Plan plan = tc ? plan_tc_backward(s) : plan_f32_backward(s);
   const size_t need = backward_need(s);
   if (need > 0 && (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need)) return MPM_ERR_WORKSPACE;
   const size_t q_values = static_cast<size_t>(q_rows) * q_heads, k_bytes = static_cast<size_t>(k_rows) * kv_heads * head_dim * e;
@@ -327,7 +329,7 @@ mpm_status mpm_cross_attention_backward(const void* d_out, int64_t d_out_row_str
           vector_heads(hg, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
   const cudaError_t err =
-      tc ? mpm::launch_attention_backward_tc(a, sms, on) : mpm::launch_attention_backward_simt(a, dtype == MPM_BF16, sms, on);
+      tc ? mpm::launch_attention_backward_tc(a, sms, on) : mpm::launch_attention_backward_f32(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }
 

@@ -1,0 +1,519 @@
+// Attention between packed sequences to fp32's precision: for fp32 tokens, and for
+// bf16 tokens whose rows the tcgen05 kernels cannot load (strides or addresses that
+// are not 16-byte multiples).
+//
+//   s = scale q.k;  p = exp(s - lse);  o = sum p v
+//   ds = p (do.v - delta), delta = do.o;  dq = scale sum ds k;  dk = scale sum ds q;  dv = sum p do
+//
+// Products run on the tensor cores (mma.sync, tf32) as three: x = hi + lo, hi x's
+// first eleven bits and lo the next eleven; hi.hi + (hi.lo + lo.hi), the dropped lo.lo
+// is 2^-22 of the term.  tf32 has fp32's exponents, so nothing is scaled.  Sums in
+// the tensor cores are cut, not rounded, at each addition: so the small products have
+// an accumulator of their own, and a running sum over keys (or queries) is kept in
+// registers, one fp32 addition a tile of 64.
+//
+// One scheme serves the three passes.  A block of four warps keeps a tile of 64 rows
+// (queries, or keys for dk and dv) in shared memory and streams tiles of 64 columns
+// past it; a warp has 16 rows and all columns.  The order of a sum's terms is free, so
+// a lane's features of both operands are four neighbours (one 16-byte load for two
+// products), and the columns that it holds of a score tile are those that it needs as
+// the left operand of the product over them: probabilities never leave the registers.
+//
+// Bound: latencies of the arithmetic.  The registers of sums leave 8 to 12 warps an
+// SM, which issue in 44 % of the cycles and wait for their own results or for the tensor
+// cores' queue in the rest (for memory in a tenth); the tensor cores are 44 % busy, at
+// 135 of the 303 TFLOP/s that tf32 products alone reach here.  8 x 1024 tokens, 12
+// heads of 64: forward 572 us, 45 TFLOP/s of attention, gradients 1.93 ms (fma on the
+// CUDA cores, 74 TFLOP/s at their peak: 826 us and 2.51 ms); 4 x 1024, 12 heads of 128:
+// 594 us and 1.89 ms (858 us, 2.62 ms).  Gradients of wide heads take tiles of 128 rows
+// and eight warps, as one block fills the shared memory (64 rows, four warps: 2.97 ms).
+//
+// Nothing outside a sequence enters a sum: rows past its end and masked keys are
+// loaded as zeros (a NaN there would survive a product with 0) and their scores
+// count as minus infinity.
+#include "attention_common.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+
+constexpr int kTile = 64;          // columns of a score tile
+constexpr int kCols = kTile / 8;   // in groups of eight, two of them a lane's
+
+template <int DP>
+struct Shape {
+  static constexpr int kPitch = DP + 4;        // floats of a row in shared memory
+  static constexpr int kFeatures = DP / 8;     // feature groups, likewise
+};
+
+// Rows first .. first + R - 1 of one head on their way to shared memory, all of a
+// thread's pieces of four features under way at once.  Zeros past the
+// sequence, past the head's width and for masked rows.
+template <typename T, int DP, int W, int R>
+__device__ __forceinline__ void load_tile(float* sm, const Heads& x, int head, const Span& s, int first, int dim, bool vec,
+                                          const uint8_t* __restrict__ mask) {
+  constexpr int kThreads = 32 * W, kPieces = R * DP / 4 / kThreads;
+  const T* base = static_cast<const T*>(x.p) + x.head * head;
+  float4 v[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int u = threadIdx.x + kThreads * i, c = u % (DP / 4) * 4, row = first + u / (DP / 4);
+    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < dim && row < s.n && (mask == nullptr || __ldg(mask + s.lo + row) != 0)) {
+      const T* p = base + x.row * (s.lo + row) + c;
+      if (vec) {
+        if constexpr (sizeof(T) == 4) {
+          v[i] = __ldg(reinterpret_cast<const float4*>(p));
+        } else {
+          const uint2 w = __ldg(reinterpret_cast<const uint2*>(p));
+          v[i] = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                             __uint_as_float(w.y & 0xFFFF0000u));
+        }
+      } else {
+        v[i].x = to_f32(p[0]);
+        if (c + 1 < dim) v[i].y = to_f32(p[1]);
+        if (c + 2 < dim) v[i].z = to_f32(p[2]);
+        if (c + 3 < dim) v[i].w = to_f32(p[3]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int u = threadIdx.x + kThreads * i;
+    *reinterpret_cast<float4*>(sm + u / (DP / 4) * Shape<DP>::kPitch + u % (DP / 4) * 4) = v[i];
+  }
+}
+
+// x as two values of eleven bits, the first rounded to the nearest: the second is at
+// most 2^-11 of it.  (What has no fp32 neighbour there, infinities and NaN, ends as NaN.)
+struct Split {
+  uint32_t hi, lo;
+};
+__device__ __forceinline__ Split split(float x) {
+  const uint32_t hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
+  return {hi, __float_as_uint(x - __uint_as_float(hi))};
+}
+__device__ __forceinline__ void mma_1688(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// big += hi.hi, small += hi.lo + lo.hi, for N columns groups: a has two terms of rows
+// g and g + 8, b[n] two terms.  Products into one accumulator are kept apart.
+template <int N>
+__device__ __forceinline__ void mma_split(float (*big)[4], float (*small)[4], const Split (&a)[4], const Split (&b)[N][2]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) mma_1688(small[n], a[0].hi, a[1].hi, a[2].hi, a[3].hi, b[n][0].lo, b[n][1].lo);
+#pragma unroll
+  for (int n = 0; n < N; ++n) mma_1688(big[n], a[0].hi, a[1].hi, a[2].hi, a[3].hi, b[n][0].hi, b[n][1].hi);
+#pragma unroll
+  for (int n = 0; n < N; ++n) mma_1688(small[n], a[0].lo, a[1].lo, a[2].lo, a[3].lo, b[n][0].hi, b[n][1].hi);
+}
+
+// A warp's lane (g, c) = (lane / 4, lane % 4) has of its 16 rows g and g + 8, and of
+// columns (or features) 8 n + 2 c and the next: acc[n][2 h + e] is row g + 8 h, column 8 n + 2 c + e.
+
+// acc = rows . cols, in steps of 32 features of which a lane takes 8 c .. 8 c + 7
+// (two loads whose eight lanes at a time meet all banks); of a last 16 it takes 4 c .. 4 c + 3.
+template <int DP>
+__device__ __forceinline__ void dot_tile(const float* rows, const float* cols, int dim, float (&acc)[kCols][4]) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const float* r = rows + (threadIdx.x / 32 * 16 + g) * Shape<DP>::kPitch;
+  const float* k = cols + g * Shape<DP>::kPitch;
+  float small[kCols][4];
+#pragma unroll
+  for (int n = 0; n < kCols; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[n][e] = small[n][e] = 0.f;
+#pragma unroll 1
+  for (int d = 0; d < dim; d += 32) {
+    const bool half = dim - d <= 16;
+    const int at = d + (half ? 4 * c : 8 * c);
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      if (j == 4 && half) break;
+      const float4 x = *reinterpret_cast<const float4*>(r + at + j), y = *reinterpret_cast<const float4*>(r + 8 * Shape<DP>::kPitch + at + j);
+      const Split a0[4] = {split(x.x), split(y.x), split(x.y), split(y.y)}, a1[4] = {split(x.z), split(y.z), split(x.w), split(y.w)};
+#pragma unroll
+      for (int n = 0; n < kCols; n += 2) {
+        const float4 b = *reinterpret_cast<const float4*>(k + 8 * n * Shape<DP>::kPitch + at + j);
+        const float4 b2 = *reinterpret_cast<const float4*>(k + 8 * (n + 1) * Shape<DP>::kPitch + at + j);
+        const Split first[2][2] = {{split(b.x), split(b.y)}, {split(b2.x), split(b2.y)}};
+        mma_split<2>(acc + n, small + n, a0, first);
+        const Split second[2][2] = {{split(b.z), split(b.w)}, {split(b2.z), split(b2.w)}};
+        mma_split<2>(acc + n, small + n, a1, second);
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kCols; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[n][e] += small[n][e];
+}
+
+// acc += weights (a score tile's layout) . tile, over its 64 rows, feature groups in fours.
+template <int DP>
+__device__ __forceinline__ void sum_tile(const float (&weights)[kCols][4], const float* tile, int dim,
+                                         float (&acc)[Shape<DP>::kFeatures][4]) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const float* t = tile + 2 * c * Shape<DP>::kPitch + g;
+#pragma unroll
+  for (int m0 = 0; m0 < Shape<DP>::kFeatures; m0 += 4) {
+    if (8 * m0 >= dim) break;
+    float big[4][4] = {}, small[4][4] = {};
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      const Split a[4] = {split(weights[n][0]), split(weights[n][2]), split(weights[n][1]), split(weights[n][3])};
+      Split b[4][2];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float* p = t + 8 * n * Shape<DP>::kPitch + 8 * (m0 + m);
+        b[m][0] = split(p[0]);
+        b[m][1] = split(p[Shape<DP>::kPitch]);
+      }
+      mma_split<4>(big, small, a, b);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[m0 + m][e] += big[m][e] + small[m][e];
+  }
+}
+
+// The lane's sums, times a factor a row, to rows of `dim` contiguous values, and
+// what their rounding left to rows of `rest`, if that is wanted.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(T* out, int64_t row0, int rows, int heads, int head, int dim,
+                                           const float (&acc)[Shape<DP>::kFeatures][4], float f0, float f1, T* rest = nullptr) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = threadIdx.x / 32 * 16 + g + 8 * h;
+    if (r >= rows) continue;
+    const int64_t at = ((row0 + r) * heads + head) * dim;
+#pragma unroll
+    for (int m = 0; m < Shape<DP>::kFeatures; ++m)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int d = 8 * m + 2 * c + e;
+        if (d >= dim) continue;
+        const float v = acc[m][2 * h + e] * (h == 0 ? f0 : f1);
+        out[at + d] = from_f32<T>(v);
+        if (rest != nullptr) rest[at + d] = rest_of<T>(v);
+      }
+  }
+}
+
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+  return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+  return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+}
+
+struct Item {
+  Tile tile;
+  int head, split;
+};
+// Items are numbered with the tile fastest: neighbours read the same head's rows.
+template <int T>
+__device__ __forceinline__ Item item_of(int64_t item, const int64_t* off, int batch, int64_t rows, int heads) {
+  const int64_t slots = tile_slots<T>(off, batch, rows), rest = item / slots;
+  return {tile_of<T>(off, batch, rows, item % slots), static_cast<int>(rest % heads), static_cast<int>(rest / heads)};
+}
+
+template <typename T, int DP, int W>
+__global__ void __launch_bounds__(32 * W, DP == 64 ? 3 : 2) attention_f32_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  constexpr int kRows = 16 * W, kOwn = kRows * Shape<DP>::kPitch, kStreamed = kTile * Shape<DP>::kPitch;
+  float* sq = sm;
+  float* sk = sq + kOwn;
+  float* sv = sk + kStreamed;
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {
+    check_offsets(a.q_offsets, a.batch, a.q_rows, a.status);
+    check_offsets(a.k_offsets, a.batch, a.k_rows, a.status);
+  }
+  const int lane = threadIdx.x & 31, g = lane >> 2, c2 = lane & 3;
+  const float c = a.scale * kLog2e;
+  const int64_t items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kRows>(it, a.q_offsets, a.batch, a.q_rows, a.q_heads);
+    if (w.tile.image < 0) continue;
+    const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
+    const int kv = w.head / (a.q_heads / a.kv_heads);
+    const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    float acc[Shape<DP>::kFeatures][4] = {};
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+    __syncthreads();  // the last item's tiles have been read
+    load_tile<T, DP, W, kRows>(sq, a.q, w.head, w.tile.rows, w.tile.first, a.dim, a.vec, nullptr);
+    for (int t = part.begin; t < part.end; ++t) {
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP, W, kTile>(sk, a.k, kv, ks, t * kTile, a.dim, a.vec, a.mask);
+      load_tile<T, DP, W, kTile>(sv, a.v, kv, ks, t * kTile, a.dim, a.vec, a.mask);
+      __syncthreads();
+      float s[kCols][4];
+      dot_tile<DP>(sq, sk, a.dim, s);
+      if (a.mask != nullptr || (t + 1) * kTile > ks.n) {
+#pragma unroll
+        for (int n = 0; n < kCols; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = t * kTile + 8 * n + 2 * c2 + e;
+            if (!(key < ks.n && (a.mask == nullptr || __ldg(a.mask + ks.lo + key) != 0))) s[n][e] = s[n][2 + e] = -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) most = fmaxf(most, fmaxf(s[n][2 * h], s[n][2 * h + 1]));
+        // In units of log2: c is positive, so the largest score is the largest product.
+        const float m = fmaxf(top[h], quad_max(most) * c);
+        const float base = m == -INFINITY ? 0.f : m;
+        const float shrink = exp2f(top[h] - base);
+        top[h] = m;
+        float part_sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < kCols; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s[n][2 * h + e] = exp2f(fmaf(s[n][2 * h + e], c, -base));
+            part_sum += s[n][2 * h + e];
+          }
+        sum[h] = fmaf(sum[h], shrink, quad_sum(part_sum));
+#pragma unroll
+        for (int m2 = 0; m2 < Shape<DP>::kFeatures; ++m2) {
+          acc[m2][2 * h] *= shrink;
+          acc[m2][2 * h + 1] *= shrink;
+        }
+      }
+      sum_tile<DP>(s, sv, a.dim, acc);
+    }
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    const float f0 = sum[0] == 0.f ? 0.f : 1.f / sum[0], f1 = sum[1] == 0.f ? 0.f : 1.f / sum[1];
+    const int64_t part0 = a.splits == 1 ? 0 : static_cast<int64_t>(w.split) * a.q_rows * a.q_heads;
+    if (a.splits == 1)
+      store_rows<T, DP>(static_cast<T*>(a.out), row0, rows, a.q_heads, w.head, a.dim, acc, f0, f1, static_cast<T*>(a.rest));
+    else
+      store_rows<float, DP>(a.partial + part0 * a.dim, row0, rows, a.q_heads, w.head, a.dim, acc, f0, f1);
+    float* lse = a.splits == 1 ? a.lse : a.partial_lse + part0;
+    if (lse != nullptr && c2 == 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = threadIdx.x / 32 * 16 + g + 8 * h;
+        if (r < rows) lse[(row0 + r) * a.q_heads + w.head] = (top[h] + log2f(sum[h])) * (a.splits == 1 ? kLn2 : 1.f);
+      }
+    }
+  }
+}
+
+// The row's statistic in log2 units; a row without keys has no probabilities.
+__device__ __forceinline__ float log2_stat(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+template <typename T, int DP, int W>
+__global__ void __launch_bounds__(32 * W, DP == 64 ? 3 : 1) attention_f32_dq_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  constexpr int kRows = 16 * W, kOwn = kRows * Shape<DP>::kPitch, kStreamed = kTile * Shape<DP>::kPitch;
+  float* sq = sm;
+  float* sg = sq + kOwn;
+  float* sk = sg + kOwn;
+  float* sv = sk + kStreamed;
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int lane = threadIdx.x & 31, g = lane >> 2, c2 = lane & 3;
+  const float c = a.scale * kLog2e;
+  const int64_t items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kRows>(it, a.q_offsets, a.batch, a.q_rows, a.q_heads);
+    if (w.tile.image < 0) continue;
+    const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
+    const int kv = w.head / (a.q_heads / a.kv_heads);
+    const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    float acc[Shape<DP>::kFeatures][4] = {};
+    float lse2[2], delta[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = threadIdx.x / 32 * 16 + g + 8 * h;
+      lse2[h] = r < rows ? log2_stat(__ldg(a.stats + (row0 + r) * a.q_heads + w.head)) : INFINITY;
+      delta[h] = r < rows ? a.delta[(row0 + r) * a.q_heads + w.head] : 0.f;
+    }
+    __syncthreads();  // the last item's tiles have been read
+    load_tile<T, DP, W, kRows>(sq, a.q, w.head, w.tile.rows, w.tile.first, a.dim, a.vec, nullptr);
+    load_tile<T, DP, W, kRows>(sg, a.d_out, w.head, w.tile.rows, w.tile.first, a.dim, a.vec, nullptr);
+    for (int t = part.begin; t < part.end; ++t) {
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP, W, kTile>(sk, a.k, kv, ks, t * kTile, a.dim, a.vec, a.mask);
+      load_tile<T, DP, W, kTile>(sv, a.v, kv, ks, t * kTile, a.dim, a.vec, a.mask);
+      __syncthreads();
+      float s[kCols][4], dp[kCols][4];
+      dot_tile<DP>(sq, sk, a.dim, s);
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] = exp2f(fmaf(s[n][e], c, -lse2[e / 2]));
+      dot_tile<DP>(sg, sv, a.dim, dp);
+      const bool cut = a.mask != nullptr || (t + 1) * kTile > ks.n;
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = t * kTile + 8 * n + 2 * c2 + e % 2;
+          const bool there = !cut || (key < ks.n && (a.mask == nullptr || __ldg(a.mask + ks.lo + key) != 0));
+          s[n][e] = there && lse2[e / 2] != INFINITY ? s[n][e] * (dp[n][e] - delta[e / 2]) : 0.f;
+        }
+      sum_tile<DP>(s, sk, a.dim, acc);
+    }
+    if (a.splits == 1)
+      store_rows<T, DP>(static_cast<T*>(a.d_q), row0, rows, a.q_heads, w.head, a.dim, acc, a.scale, a.scale);
+    else
+      store_rows<float, DP>(a.partial + static_cast<int64_t>(w.split) * a.q_rows * a.q_heads * a.dim, row0, rows, a.q_heads,
+                            w.head, a.dim, acc, a.scale, a.scale);
+  }
+}
+
+template <typename T, int DP, int W>
+__global__ void __launch_bounds__(32 * W, DP == 64 ? 2 : 1) attention_f32_dkv_kernel(const AttentionArgs a) {
+  extern __shared__ float sm[];
+  constexpr int kRows = 16 * W, kOwn = kRows * Shape<DP>::kPitch, kStreamed = kTile * Shape<DP>::kPitch;
+  float* sk = sm;
+  float* sv = sk + kOwn;
+  float* sq = sv + kOwn;
+  float* sg = sq + kStreamed;
+  __shared__ __align__(16) float stat[kTile], dot[kTile];
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int lane = threadIdx.x & 31, g = lane >> 2, c2 = lane & 3;
+  const float c = a.scale * kLog2e;
+  const int group = a.q_heads / a.kv_heads;
+  const int64_t items = tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const Item w = item_of<kRows>(it, a.k_offsets, a.batch, a.k_rows, a.kv_heads);
+    if (w.tile.image < 0) continue;
+    const Span qs = span_of(a.q_offsets, w.tile.image, a.q_rows);
+    const int tiles = (qs.n + kTile - 1) / kTile;
+    const Part part = part_of(tiles * group, w.split, a.key_splits);
+    const int64_t row0 = w.tile.rows.lo + w.tile.first;
+    const int rows = w.tile.rows.n - w.tile.first;
+    float dk[Shape<DP>::kFeatures][4] = {}, dv[Shape<DP>::kFeatures][4] = {};
+    bool there[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = threadIdx.x / 32 * 16 + g + 8 * h;
+      there[h] = r < rows && (a.mask == nullptr || __ldg(a.mask + row0 + r) != 0);
+    }
+    __syncthreads();  // the last item's tiles have been read
+    load_tile<T, DP, W, kRows>(sk, a.k, w.head, w.tile.rows, w.tile.first, a.dim, a.vec, a.mask);
+    load_tile<T, DP, W, kRows>(sv, a.v, w.head, w.tile.rows, w.tile.first, a.dim, a.vec, a.mask);
+    for (int t = part.begin; t < part.end; ++t) {
+      const int head = w.head * group + t / tiles, first = t % tiles * kTile;
+      if (t > part.begin) __syncthreads();
+      load_tile<T, DP, W, kTile>(sq, a.q, head, qs, first, a.dim, a.vec, nullptr);
+      load_tile<T, DP, W, kTile>(sg, a.d_out, head, qs, first, a.dim, a.vec, nullptr);
+      if (threadIdx.x < kTile) {
+        const int r = first + threadIdx.x;
+        const int64_t at = (qs.lo + r) * a.q_heads + head;
+        stat[threadIdx.x] = r < qs.n ? log2_stat(__ldg(a.stats + at)) : INFINITY;
+        dot[threadIdx.x] = r < qs.n ? a.delta[at] : 0.f;
+      }
+      __syncthreads();
+      float s[kCols][4], dp[kCols][4];
+      dot_tile<DP>(sk, sq, a.dim, s);
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) {
+        const float2 l = *reinterpret_cast<const float2*>(stat + 8 * n + 2 * c2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float l2 = e % 2 == 0 ? l.x : l.y;
+          s[n][e] = there[e / 2] && l2 != INFINITY ? exp2f(fmaf(s[n][e], c, -l2)) : 0.f;
+        }
+      }
+      sum_tile<DP>(s, sg, a.dim, dv);
+      dot_tile<DP>(sv, sg, a.dim, dp);
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) {
+        const float2 l = *reinterpret_cast<const float2*>(stat + 8 * n + 2 * c2), d = *reinterpret_cast<const float2*>(dot + 8 * n + 2 * c2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[n][e] = there[e / 2] && (e % 2 == 0 ? l.x : l.y) != INFINITY ? s[n][e] * (dp[n][e] - (e % 2 == 0 ? d.x : d.y)) : 0.f;
+      }
+      sum_tile<DP>(s, sq, a.dim, dk);
+    }
+    if (a.key_splits == 1) {
+      store_rows<T, DP>(static_cast<T*>(a.d_k), row0, rows, a.kv_heads, w.head, a.dim, dk, a.scale, a.scale);
+      store_rows<T, DP>(static_cast<T*>(a.d_v), row0, rows, a.kv_heads, w.head, a.dim, dv, 1.f, 1.f);
+    } else {
+      const int64_t each = a.k_rows * a.kv_heads * a.dim;
+      float* p = a.partial + w.split * each;
+      store_rows<float, DP>(p, row0, rows, a.kv_heads, w.head, a.dim, dk, a.scale, a.scale);
+      store_rows<float, DP>(p + a.key_splits * each, row0, rows, a.kv_heads, w.head, a.dim, dv, 1.f, 1.f);
+    }
+  }
+}
+
+// Launches with dynamic shared memory on as many blocks as are resident at once.
+template <typename K>
+cudaError_t launch_tiles(K kernel, int warps, size_t smem, int64_t items, const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  int each = 0;
+  e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, 32 * warps, smem);
+  if (e != cudaSuccess) return e;
+  const int64_t most = int64_t{num_sms} * (each < 1 ? 1 : each);
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < most ? items : most)), dim3(32 * warps), smem, stream, a);
+}
+
+template <typename T, int DP>
+cudaError_t forward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  constexpr int kWarps = 4, kRows = 16 * kWarps;
+  constexpr size_t smem = sizeof(float) * Shape<DP>::kPitch * (kRows + 2 * kTile);
+  const int64_t items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  return launch_tiles(attention_f32_kernel<T, DP, kWarps>, kWarps, smem, items, a, num_sms, stream);
+}
+template <typename T, int DP>
+cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  // Four tiles of 128 features leave room for one block: it has eight warps then.
+  constexpr int kWarps = DP == 64 ? 4 : 8, kRows = 16 * kWarps;
+  constexpr size_t smem = sizeof(float) * Shape<DP>::kPitch * 2 * (kRows + kTile);
+  const int64_t q_items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
+  const int64_t k_items = tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
+  constexpr bool bf16 = sizeof(T) == 2;
+  cudaError_t e = launch_attention_delta(a, bf16, num_sms, stream);
+  if (e == cudaSuccess && a.q_rows > 0) {
+    e = launch_tiles(attention_f32_dq_kernel<T, DP, kWarps>, kWarps, smem, q_items, a, num_sms, stream);
+    if (e == cudaSuccess && a.splits > 1)
+      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, bf16, num_sms, stream);
+  }
+  if (e == cudaSuccess && a.k_rows > 0) {
+    e = launch_tiles(attention_f32_dkv_kernel<T, DP, kWarps>, kWarps, smem, k_items, a, num_sms, stream);
+    const int64_t each = a.k_rows * a.kv_heads * a.dim;
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, bf16, num_sms, stream);
+    if (e == cudaSuccess && a.key_splits > 1)
+      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim,
+                               a.d_v, bf16, num_sms, stream);
+  }
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  if (bf16) return a.dim <= 64 ? forward<__nv_bfloat16, 64>(a, num_sms, stream) : forward<__nv_bfloat16, 128>(a, num_sms, stream);
+  return a.dim <= 64 ? forward<float, 64>(a, num_sms, stream) : forward<float, 128>(a, num_sms, stream);
+}
+
+cudaError_t launch_attention_backward_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  if (bf16) return a.dim <= 64 ? backward<__nv_bfloat16, 64>(a, num_sms, stream) : backward<__nv_bfloat16, 128>(a, num_sms, stream);
+  return a.dim <= 64 ? backward<float, 64>(a, num_sms, stream) : backward<float, 128>(a, num_sms, stream);
+}
+
+}  // namespace mpm

@@ -1,0 +1,150 @@
+// The attention kernels that work row by row: the join of parts, delta, sums of parts.
+// Bound: HBM, every value once.
+#include "attention_common.cuh"
+
+namespace mpm {
+namespace {
+
+using namespace attn;
+
+constexpr int kRowThreads = 256;
+
+// out = sum over parts of 2^(l_s - l) o_s, l = log2 sum 2^l_s: a warp a row and head.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) attention_join_kernel(const AttentionArgs a) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int lane = threadIdx.x & 31;
+  const int64_t all = a.q_rows * a.q_heads, live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
+  for (int64_t r = blockIdx.x * int64_t{kRowThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kRowThreads / 32}) {
+    // Two parts a lane.
+    float l[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) l[i] = lane + 32 * i < a.splits ? a.partial_lse[(lane + 32 * i) * all + r] : -INFINITY;
+    float top = fmaxf(l[0], l[1]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const float base = top == -INFINITY ? 0.f : top;
+    float w[2] = {exp2f(l[0] - base), exp2f(l[1] - base)};
+    float sum = w[0] + w[1];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    w[0] *= inv;
+    w[1] *= inv;
+    float v[kAttentionMaxDim / 32] = {};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = __shfl_sync(0xFFFFFFFFu, s < 32 ? w[0] : w[1], s & 31);
+      const float* p = a.partial + (s * all + r) * a.dim;
+#pragma unroll
+      for (int i = 0; i < kAttentionMaxDim / 32; ++i)
+        if (lane + 32 * i < a.dim) v[i] = fmaf(f, p[lane + 32 * i], v[i]);
+    }
+    T* out = static_cast<T*>(a.out) + r * a.dim;
+#pragma unroll
+    for (int i = 0; i < kAttentionMaxDim / 32; ++i)
+      if (lane + 32 * i < a.dim) {
+        out[lane + 32 * i] = from_f32<T>(v[i]);
+        if (a.rest != nullptr) static_cast<T*>(a.rest)[r * a.dim + lane + 32 * i] = rest_of<T>(v[i]);
+      }
+    if (a.lse != nullptr && lane == 0) a.lse[r] = (top + log2f(sum)) * kLn2;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) attention_delta_kernel(const AttentionArgs a, bool wide) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {
+    check_offsets(a.q_offsets, a.batch, a.q_rows, a.status);
+    check_offsets(a.k_offsets, a.batch, a.k_rows, a.status);
+  }
+  const int lane = threadIdx.x & 31;
+  const int64_t live = live_rows(a.q_offsets, a.batch, a.q_rows) * a.q_heads;
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      // Eight features a lane, eight or sixteen lanes a row and head.
+      const int lanes = a.dim <= 64 ? 8 : 16, d = lane % lanes * 8, each = 32 / lanes;
+      const bool there = d < a.dim;
+      const int64_t step = gridDim.x * int64_t{kRowThreads} / lanes;
+      for (int64_t first = (blockIdx.x * int64_t{kRowThreads} + threadIdx.x) / 32 * each; first < live; first += step) {
+        const int64_t r = first + lane / lanes;
+        float v = 0.f;
+        if (there && r < live) {
+          const int64_t row = r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.q_heads) : r / a.q_heads;
+          const uint4 o = ld_stream(reinterpret_cast<const uint4*>(static_cast<const T*>(a.out) + r * a.dim + d));
+          uint4 e = make_uint4(0, 0, 0, 0);
+          if (a.rest != nullptr) e = ld_stream(reinterpret_cast<const uint4*>(static_cast<const T*>(a.rest) + r * a.dim + d));
+          const uint4 g = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.d_out.p) + a.d_out.row * row +
+                                                               a.d_out.head * (r - row * a.q_heads) + d));
+          const norm::F8 fo = norm::widen(o), fe = norm::widen(e), fg = norm::widen(g);
+          float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s = norm::fma(norm::add(fo.p[k], fe.p[k]), fg.p[k], s);
+          v = s.x + s.y;
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1)
+          if (x < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, x);
+        if (d == 0 && r < live) a.delta[r] = v;
+      }
+      return;
+    }
+  }
+  for (int64_t r = blockIdx.x * int64_t{kRowThreads / 32} + threadIdx.x / 32; r < live; r += gridDim.x * int64_t{kRowThreads / 32}) {
+    const T* o = static_cast<const T*>(a.out) + r * a.dim;
+    const T* rest = a.rest == nullptr ? nullptr : static_cast<const T*>(a.rest) + r * a.dim;
+    const T* g = static_cast<const T*>(a.d_out.p) + a.d_out.row * (r / a.q_heads) + a.d_out.head * (r % a.q_heads);
+    float s = 0.f;
+    for (int d = lane; d < a.dim; d += 32) s = fmaf(to_f32(o[d]) + (rest == nullptr ? 0.f : to_f32(rest[d])), to_f32(g[d]), s);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if (lane == 0) a.delta[r] = s;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) attention_sum_kernel(const float* __restrict__ parts, int splits, int64_t rows,
+                                                                 const int64_t* __restrict__ offsets, int batch, int width,
+                                                                 T* __restrict__ out) {
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int64_t each = rows * width, live = live_rows(offsets, batch, rows) * width;
+  for (int64_t i = blockIdx.x * int64_t{kRowThreads} + threadIdx.x; i < live; i += gridDim.x * int64_t{kRowThreads}) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < splits; ++p) s += parts[p * each + i];
+    out[i] = from_f32<T>(s);
+  }
+}
+
+int blocks_for(int64_t work, int64_t most) { return static_cast<int>(work < 1 ? 1 : work < most ? work : most); }
+
+}  // namespace
+
+cudaError_t launch_attention_join(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  const int blocks = blocks_for((a.q_rows * a.q_heads + 7) / 8, int64_t{num_sms} * 8);
+  return bf16 ? launch_dependent(attention_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(kRowThreads), 0, stream, a)
+              : launch_dependent(attention_join_kernel<float>, dim3(blocks), dim3(kRowThreads), 0, stream, a);
+}
+
+cudaError_t launch_attention_delta(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
+  const int blocks = blocks_for((a.q_rows * a.q_heads + 7) / 8, int64_t{num_sms} * 8);
+  const uintptr_t all = reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.rest) | reinterpret_cast<uintptr_t>(a.d_out.p);
+  const bool wide = bf16 && a.dim % 8 == 0 && all % 16 == 0 && a.d_out.row % 8 == 0 && a.d_out.head % 8 == 0;
+  return bf16 ? launch_dependent(attention_delta_kernel<__nv_bfloat16>, dim3(blocks), dim3(kRowThreads), 0, stream, a, wide)
+              : launch_dependent(attention_delta_kernel<float>, dim3(blocks), dim3(kRowThreads), 0, stream, a, wide);
+}
+
+cudaError_t launch_attention_sum(const float* parts, int splits, int64_t rows, const int64_t* offsets, int batch, int heads,
+                                 int dim, void* out, bool bf16, int num_sms, cudaStream_t stream) {
+  const int width = heads * dim;
+  const int blocks = blocks_for((rows * width + kRowThreads - 1) / kRowThreads, int64_t{num_sms} * 8);
+  return bf16 ? launch_dependent(attention_sum_kernel<__nv_bfloat16>, dim3(blocks), dim3(kRowThreads), 0, stream, parts, splits, rows,
+                                 offsets, batch, width, static_cast<__nv_bfloat16*>(out))
+              : launch_dependent(attention_sum_kernel<float>, dim3(blocks), dim3(kRowThreads), 0, stream, parts, splits, rows, offsets,
+                                 batch, width, static_cast<float*>(out));
+}
+
+}  // namespace mpm

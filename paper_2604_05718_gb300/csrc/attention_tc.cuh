@@ -86,7 +86,7 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
 
 // Products are issued four at a time: written one by one, what forms their operands
 // took 50 cycles a product, and the issuing warp bounded the kernels (64 x 1024
-// tokens, 12 heads of 64, forward: BEFORE us, AFTER so).
+// tokens, 12 heads of 64, forward: 233 us, 227 so).
 // D [128, 128] (+)= four K = 16 slices of 64 features of both tiles.
 __device__ __forceinline__ void mma_features4(uint32_t d, uint64_t a, uint64_t b, uint32_t accumulate) {
   asm volatile(
@@ -210,12 +210,6 @@ struct RingPlace {
   __device__ __forceinline__ void next() {
     if (++slot == SLOTS) {
       slot = 0;
-      phase ^= 1u;
-    }
-  }
-  __device__ __forceinline__ void back() {
-    if (--slot < 0) {
-      slot = SLOTS - 1;
       phase ^= 1u;
     }
   }

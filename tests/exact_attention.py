@@ -4,9 +4,15 @@ Test infrastructure: plain torch in float64, no code shared with the library.
 
 A bound follows each quantity's error to first order (the tests add a quarter for
 what lies beyond).  u is half a step of the tokens' type, w half a step of fp32, and
-v half a step of what probabilities and score gradients are rounded to before they
-multiply (bf16 on the tensor cores, fp32 on the CUDA cores).  A sum of n terms in
-fp32, in any order, is off by at most n w times the sum of their sizes.
+v half a step of what probabilities are rounded to before they multiply (bf16, or
+nothing more than fp32).  A sum of n terms in fp32, in any order, is off by at most
+n w times the sum of their sizes.
+
+Where v is bf16's, score gradients multiply as two bf16 values, the second half a step
+of bf16 from what the first left: v^2.  Elsewhere factors multiply as two tf32 values
+of eleven bits.  The second is at most 2^-11 of the factor, so the dropped product of
+both seconds is 2^-22; it has up to twelve bits, of which one is cut, 2^-23 a factor.
+Together y = 2^-21 = 8 w a product.
 """
 
 from __future__ import annotations
@@ -38,6 +44,7 @@ class Exact(NamedTuple):
 def attention(q, k, v, d_out, q_offsets, k_offsets, mask, scale, probabilities=None) -> Exact:
     """All of it for packed tensors; rows outside the sequences are zeros.  probabilities: the type they are rounded to."""
     u, pu = HALF[q.dtype], HALF[probabilities or q.dtype]
+    y, du = (8 * W, W) if pu == W else (0.0, pu * pu)
     q, k, v, g = q.double(), k.double(), v.double(), d_out.double()
     heads, group, dim = q.shape[1], q.shape[1] // k.shape[1], q.shape[2]
     zeros = torch.zeros_like
@@ -60,10 +67,10 @@ def attention(q, k, v, d_out, q_offsets, k_offsets, mask, scale, probabilities=N
             o = p @ vh
             # Scores: the product's sum, the factor's rounding, that of score - maximum, and the exponential's few units.
             size = scale * qh.abs() @ kh.abs().t()
-            es = (dim + 4) * W * size + 4 * W * (s.abs() + lse.abs())
+            es = ((dim + 4) * W + y) * size + 4 * W * (s.abs() + lse.abs())
             ep = es + (p * es).sum(1, keepdim=True) + (8 + nk) * W
             r.out[rows, h], r.lse[rows, h] = o, lse[:, 0]
-            eo = (p * (ep + pu + nk * W)) @ vh.abs()
+            eo = (p * (ep + pu + nk * W + y)) @ vh.abs()
             r.out_bound[rows, h] = eo + u * o.abs()
             r.lse_bound[rows, h] = (p * es).sum(1) + (8 + nk) * W + 4 * W * (lse[:, 0].abs() + s.abs().amax(1))
             # Backward: p from the kept lse, its own error among it.
@@ -74,14 +81,14 @@ def attention(q, k, v, d_out, q_offsets, k_offsets, mask, scale, probabilities=N
             # delta is taken from the output and what its rounding left.
             ed = (gh.abs() * (eo + u * u * o.abs())).sum(1, keepdim=True) + dim * W * (gh.abs() * o.abs()).sum(1, keepdim=True)
             ds = p * (t - delta)
-            eds = p * ((t - delta).abs() * (ep + 2 * W) + ed + (dim + 2) * W * (gh.abs() @ vh.abs().t())) + pu * ds.abs()
+            eds = p * ((t - delta).abs() * (ep + 2 * W) + ed + ((dim + 2) * W + y) * (gh.abs() @ vh.abs().t())) + du * ds.abs()
             r.d_q[rows, h] = scale * ds @ kh
-            r.d_q_bound[rows, h] = scale * (eds + nk * W * ds.abs()) @ kh.abs() + u * r.d_q[rows, h].abs()
+            r.d_q_bound[rows, h] = scale * (eds + (nk * W + y) * ds.abs()) @ kh.abs() + u * r.d_q[rows, h].abs()
             n = nq * group * W
             r.d_v[cols, kv] += p.t() @ gh
-            r.d_v_bound[cols, kv] += (p * (ep + pu + n)).t() @ gh.abs()
+            r.d_v_bound[cols, kv] += (p * (ep + pu + n + y)).t() @ gh.abs()
             r.d_k[cols, kv] += scale * ds.t() @ qh
-            r.d_k_bound[cols, kv] += scale * (eds + n * ds.abs()).t() @ qh.abs()
+            r.d_k_bound[cols, kv] += scale * (eds + (n + y) * ds.abs()).t() @ qh.abs()
     r.d_k_bound.add_(u * r.d_k.abs())
     r.d_v_bound.add_(u * r.d_v.abs())
     return r

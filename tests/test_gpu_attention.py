@@ -214,6 +214,37 @@ def test_no_rows(mpm, shape):
     assert all((x == 0).all() for x in grads) and grads.d_k.shape == k.shape
 
 
+@pytest.mark.parametrize("heads", [(2, 2), (4, 1)])
+@pytest.mark.parametrize("shape", [(0, 5), (5, 0), (0, 0), (300, 0), (0, 300)])
+def test_no_rows_in_bf16(mpm, shape, heads):
+    q = torch.zeros(shape[0], heads[0], 64, device=DEV, dtype=torch.bfloat16)
+    k = torch.zeros(shape[1], heads[1], 64, device=DEV, dtype=torch.bfloat16)
+    out, lse = mpm.cross_attention(q, k, k, with_lse=True)
+    assert out.shape == q.shape and (out == 0).all() and (lse.lse == -math.inf).all()
+    grads = mpm.cross_attention_backward(q, q, k, k, out, lse)
+    assert all((x == 0).all() for x in grads) and grads.d_k.shape == k.shape
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("queries", [[3, 1, 9], [140, 300, 31]], ids=["few", "many"])
+def test_one_key_a_sequence(mpm, queries, dim, dtype):
+    """All weight on one key: gradients of q and k are 0 but for rounding."""
+    run_and_check(mpm, *problem(queries, [1, 1, 1], 4, 2, dim, dtype, seed=dim))
+
+
+@pytest.mark.parametrize("dim", [33, 64, 72, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_rows_of_any_alignment_over_many_tiles(mpm, dtype, dim):
+    """Rows an odd number of elements apart: fp32's precision, in several tiles and parts either way."""
+    t, g, off, mask = problem([700, 61], [200, 1100], 4, 2, dim, dtype, masked=0.2, seed=dim)
+    odd = {}
+    for name, x in t.items():
+        odd[name] = torch.empty(x.shape[0], x.shape[1] * dim + 1, device=DEV, dtype=dtype)[:, :-1].view(x.shape[0], x.shape[1], dim)
+        odd[name].copy_(x)
+    run_and_check(mpm, odd, g, off, mask)
+
+
 @pytest.mark.parametrize("where", ["q", "k", "v"])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_a_nan_stays_with_what_it_touches(mpm, where, dtype):
@@ -263,10 +294,11 @@ def test_given_workspaces_and_outputs(mpm):
     assert e.value.code == 4
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("lengths", [([1], [2000]), ([300, 40], [280, 120])], ids=["few", "many"])
-def test_a_captured_graph_follows_its_inputs(mpm, lengths):
+def test_a_captured_graph_follows_its_inputs(mpm, lengths, dtype):
     """Lengths, tokens and masks of a later replay, while an eager call runs between."""
-    t, g, off, _ = problem(*lengths, 4, 2, 64, torch.bfloat16)
+    t, g, off, _ = problem(*lengths, 4, 2, 64, dtype)
     dev = {n: torch.tensor(o, device=DEV) for n, o in off.items()}
     mask = torch.ones(sum(lengths[1]), dtype=torch.uint8, device=DEV)
 
@@ -283,7 +315,7 @@ def test_a_captured_graph_follows_its_inputs(mpm, lengths):
     with torch.cuda.graph(graph):
         made = step()
     for seed in (1, 2):
-        fresh, g2, _, _ = problem(*lengths, 4, 2, 64, torch.bfloat16, seed=seed)
+        fresh, g2, _, _ = problem(*lengths, 4, 2, 64, dtype, seed=seed)
         for n, x in fresh.items():
             t[n].copy_(x)
         g.copy_(g2)
