@@ -131,10 +131,21 @@ FewPlan plan_few(const Shape& s) {
   const int queries = static_cast<int>(16 / group);
   const int64_t items = std::max((s.q_rows + queries - 1) / queries, sequences) * s.kv_heads;
   const int64_t passes = (s.k_rows / std::max<int64_t>(1, std::min<int64_t>(s.batch, s.k_rows)) + 63) / 64;
-  int cluster = 1;
-  // One round of blocks, of which an SM holds three (head_dim <= 64) or two.
+  // Of the blocks, of which an SM holds three (head_dim <= 64) or two, the rounds times
+  // their length in passes, where starting and joining takes about five: 192 items of 256
+  // passes alone leave the second round of SMs a third full (347 us; by threes 303, by
+  // fours 292), 768 items of 14 passes are best left whole (43 us; in twos 55, in eights
+  // 130).  Clusters of five and seven do not fill the GPCs (128 items: by sevens 227, by
+  // fours 202, by twos 208).
   const int64_t resident = kSms * (s.dim <= 64 ? 3 : 2);
-  while (cluster < 8 && 2 * cluster <= passes && items * cluster * 2 <= resident) cluster *= 2;
+  int cluster = 1;
+  int64_t least = INT64_MAX;
+  for (const int c : {1, 2, 3, 4, 6, 8}) {
+    const int64_t cost = (items * c + resident - 1) / resident * ((passes + c - 1) / c + 5);
+    if (c > std::max<int64_t>(1, passes) || cost >= least) continue;
+    least = cost;
+    cluster = c;
+  }
   int64_t splits = 1;
   if (cluster == 8 && items * 8 < kSms) splits = std::max<int64_t>(1, std::min({2 * kSms / (items * 8), passes / 16, int64_t{mpm::kAttentionMaxSplits}}));
   if ((s.q_rows / queries + s.batch) * s.kv_heads * splits * cluster > INT32_MAX) return {0, 1, 1};
