@@ -23,6 +23,7 @@ namespace attn {
 constexpr int kRows = 128;                  // rows of a tile
 constexpr int kBlockBytes = kRows * 128;    // 64 features of a tile
 constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr int64_t kMaxBlocks = INT32_MAX;
 
 // Tokens as (feature, head, row); boxes of 64 features of one head of 128 rows.
 inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
@@ -201,6 +202,74 @@ __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, 
 __device__ __forceinline__ void commit_at(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+
+// Work items are the grid's blocks: a block that runs takes the places of blocks that
+// have not started yet, one after another, so that SMs whose items were short do more
+// of them.  An item's result does not depend on who does it.
+struct Claims {
+  uint4 answer[2];
+  uint64_t bar[2];
+};
+// By one warp, converged.
+struct ClaimedItems {
+  Claims* claims;
+  int64_t item, items;
+  uint32_t asked = 0, answered = 0;
+  bool more;
+  __device__ __forceinline__ ClaimedItems(Claims* c, int64_t n) : claims(c), item(blockIdx.x), items(n), more(item < n) {}
+  // Asks for the block after this item's; the answer is read by next().
+  __device__ __forceinline__ void ask() {
+    if (asked != answered) return;
+    const uint32_t i = asked++ & 1u;
+    if ((threadIdx.x & 31) == 0) {
+      // The answer's last value has been read.
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      ptx::mbar_arrive_expect_tx(&claims->bar[i], 16);
+      asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                       ptx::smem_addr(&claims->answer[i])),
+                   "r"(ptx::smem_addr(&claims->bar[i]))
+                   : "memory");
+    }
+    __syncwarp();
+  }
+  // On to the next item, if there is one; false after a wait that ran out.
+  __device__ __forceinline__ bool next(Bounds* bounds) {
+    if (item + gridDim.x < items) {  // more items than a grid can have blocks
+      item += gridDim.x;
+      return true;
+    }
+    ask();
+    if (!warp_wait(&claims->bar[answered & 1u], answered >> 1 & 1u, bounds)) return false;
+    take();
+    return true;
+  }
+  // Before the block leaves: an answer under way has come, and after a failure nobody starts on what is left.
+  __device__ __forceinline__ void finish(Bounds* bounds) {
+    while (asked != answered || (bounds->failed && more)) {
+      ask();
+      if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(&claims->bar[answered & 1u], answered >> 1 & 1u, nullptr, kWaitNs))) return;
+      take();
+    }
+  }
+
+ private:
+  __device__ __forceinline__ void take() {
+    int32_t first;
+    asm volatile(
+        "{\n\t.reg .b128 a;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+        "ld.shared.b128 a, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+        "mov.b32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, a;\n\t}"
+        : "=r"(first)
+        : "r"(ptx::smem_addr(&claims->answer[answered & 1u]))
+        : "memory");
+    first = __shfl_sync(0xFFFFFFFFu, first, 0);
+    ++answered;
+    more = first >= 0;
+    if (more) item = first;
+  }
+};
 
 // Place in a ring of SLOTS.
 template <int SLOTS>

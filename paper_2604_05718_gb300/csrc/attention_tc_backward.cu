@@ -58,7 +58,7 @@ struct Work {
   int more;         // 0: the end
 };
 
-struct Control {
+struct alignas(16) Control {
   uint64_t kept_full[2], kept_empty[2];
   uint64_t full[8], empty[8], raw[8];
   uint64_t s_full, s_free, p_full, sum_done;
@@ -68,6 +68,7 @@ struct Control {
   uint64_t drain;
   uint32_t tmem;
   Bounds bounds;
+  Claims claims;
   Work work[kItems];
   __align__(16) float lse[kStats][kRows];     // log2, +infinity where there is no query
   __align__(16) float delta[kStats][kRows];
@@ -146,6 +147,7 @@ __device__ __forceinline__ void init_control(Control* ctl, int work_readers, int
     ptx::mbar_init(&ctl->stat_empty[i], stat_readers);
   }
   ptx::mbar_init(&ctl->drain, 1);
+  for (int i = 0; i < 2; ++i) ptx::mbar_init(&ctl->claims.bar[i], 1);
   ptx::fence_barrier_init();
 }
 
@@ -252,11 +254,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t rows = DQ ? a.q_rows : a.k_rows;
     const int heads = DQ ? a.q_heads : a.kv_heads, splits = DQ ? a.splits : a.key_splits;
     const int64_t slots = tile_slots<kRows>(off, a.batch, rows), items = slots * heads * splits;
-    for (int64_t it = blockIdx.x;; it += gridDim.x) {
+    ClaimedItems claimed(&ctl->claims, items);
+    for (;;) {
       Work w{};
-      if (it < items) {
+      if (claimed.more) {
+        const int64_t it = claimed.item;
+        claimed.ask();
         const Tile tile = tile_of<kRows>(off, a.batch, rows, it % slots);
-        if (tile.image < 0) continue;
+        if (tile.image < 0) {
+          if (claimed.next(bounds)) continue;
+          fail(ctl, a.status, 50);
+          break;
+        }
         const int64_t rest = it / slots;
         const Span cols = DQ ? span_of(a.k_offsets, tile.image, a.k_rows) : span_of(a.q_offsets, tile.image, a.q_rows);
         w.head = static_cast<int>(rest % heads);
@@ -281,7 +290,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       at.next();
       if (!w.more) break;
-      if (w.begin == w.end) continue;
+      if (w.begin == w.end) {
+        if (claimed.next(bounds)) continue;
+        fail(ctl, a.status, 50);
+        break;
+      }
       const int row = static_cast<int>(w.row0);
       if (!warp_wait(&ctl->kept_empty[kept.slot], kept.phase ^ 1u, bounds)) {
         fail(ctl, a.status, 52);
@@ -319,7 +332,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         ring.next();
       }
       if (!ok) break;
+      if (!claimed.next(bounds)) {
+        fail(ctl, a.status, 50);
+        break;
+      }
     }
+    claimed.finish(bounds);
     loads.drain(ctl);
   } else if (warp == kZeroWarp) {
     // ---------------- rows that a sum must not see ----------------
@@ -698,7 +716,7 @@ cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
                            : tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
   const uintptr_t outs = DQ ? reinterpret_cast<uintptr_t>(a.d_q)
                             : reinterpret_cast<uintptr_t>(a.d_k) | reinterpret_cast<uintptr_t>(a.d_v);
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < num_sms ? items : num_sms)), dim3(kThreads), smem_bytes<H>(),
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < kMaxBlocks ? items : kMaxBlocks)), dim3(kThreads), smem_bytes<H>(),
                           stream, q, k, v, g, a, a.dim % 8 == 0 && outs % 16 == 0);
 }
 

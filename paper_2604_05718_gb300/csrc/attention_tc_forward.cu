@@ -63,7 +63,7 @@ struct Work {
   int more;         // 0: the end
 };
 
-struct Control {
+struct alignas(16) Control {
   uint64_t q_full[2], q_empty[2];
   uint64_t kv_full[8], kv_empty[8], kv_raw[8];
   // Of a place: the probabilities are there.  Of a query tile and a place: the scores
@@ -76,6 +76,7 @@ struct Control {
   uint64_t drain;
   uint32_t tmem;
   Bounds bounds;
+  Claims claims;
   Work work[kItems];
   float top[2][kRows], total[2][kRows];  // of a lone query tile's two sums
 };
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(&ctl->pair_full, kSoftmaxWarps);
     ptx::mbar_init(&ctl->pair_read, kSoftmaxWarps);
     ptx::mbar_init(&ctl->drain, 1);
+    for (int i = 0; i < 2; ++i) ptx::mbar_init(&ctl->claims.bar[i], 1);
     ctl->bounds.init(a);
     ptx::fence_barrier_init();
     ptx::prefetch_tensor_map(&map_q);
@@ -194,23 +196,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kLoadWarp) {
       // ---------------- work and loads ----------------
-      if (blockIdx.x == 0) {
-        check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
-        check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
-        __syncwarp();
-      }
+      const int64_t slots = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows), items = slots * a.q_heads * a.splits;
+      ClaimedItems claimed(&ctl->claims, items);
       RingPlace<kItems> at;
       RingPlace<W::kQueries> qs;
       RingPlace<W::kSlots> ks;
       int q_loads = 0, kv_loads = 0;
       uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on kv_raw, and that barrier's phase
       bool ok = true;
-      const int64_t slots = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows), items = slots * a.q_heads * a.splits;
-      for (int64_t it = blockIdx.x;; it += gridDim.x) {
+      for (;;) {
         Work w{};
-        if (it < items) {
+        if (claimed.more) {
+          const int64_t it = claimed.item;
+          claimed.ask();
+          if (it == 0) {
+            check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
+            check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
+            __syncwarp();
+          }
           const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
-          if (tile.image < 0) continue;
+          if (tile.image < 0) {
+            if (claimed.next(bounds)) continue;
+            fail(ctl, a.status, 30);
+            break;
+          }
           const int64_t rest = it / slots;
           const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
           w.head = static_cast<int>(rest % a.q_heads);
@@ -235,7 +244,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         at.next();
         if (!w.more) break;
-        if (w.begin == w.end) continue;
+        if (w.begin == w.end) {
+          if (claimed.next(bounds)) continue;
+          fail(ctl, a.status, 30);
+          break;
+        }
         const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
         if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, bounds)) {
           fail(ctl, a.status, 32);
@@ -273,7 +286,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++kv_loads;
         }
         if (!ok) break;
+        if (!claimed.next(bounds)) {
+          fail(ctl, a.status, 30);
+          break;
+        }
       }
+      claimed.finish(bounds);
       {
         // Copies under way land before the block ends, whoever may have given up.  A slot's last load completed phase (number of its loads - 1).
         for (int s = 0; s < W::kQueries; ++s) {
@@ -624,7 +642,7 @@ cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
   }
   const int64_t items = tile_slots<kItemRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
   const bool vec_out = a.dim % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.rest)) % 16 == 0;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < num_sms ? items : num_sms)), dim3(kThreads), smem_bytes<H>(),
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < kMaxBlocks ? items : kMaxBlocks)), dim3(kThreads), smem_bytes<H>(),
                           stream, q, k, v, a, vec_out);
 }
 
