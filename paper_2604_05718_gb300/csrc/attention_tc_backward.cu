@@ -255,16 +255,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int heads = DQ ? a.q_heads : a.kv_heads, splits = DQ ? a.splits : a.key_splits;
     const int64_t slots = tile_slots<kRows>(off, a.batch, rows), items = slots * heads * splits;
     ClaimedItems claimed(&ctl->claims, items);
-    for (;;) {
+    for (bool fresh = true;; fresh = false) {
+      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
+        fail(ctl, a.status, 51);
+        break;
+      }
       Work w{};
-      if (claimed.more) {
+      bool got = fresh || claimed.next(bounds);
+      while (got && claimed.more) {
         const int64_t it = claimed.item;
-        claimed.ask();
         const Tile tile = tile_of<kRows>(off, a.batch, rows, it % slots);
         if (tile.image < 0) {
-          if (claimed.next(bounds)) continue;
-          fail(ctl, a.status, 50);
-          break;
+          got = claimed.next(bounds);
+          continue;
         }
         const int64_t rest = it / slots;
         const Span cols = DQ ? span_of(a.k_offsets, tile.image, a.k_rows) : span_of(a.q_offsets, tile.image, a.q_rows);
@@ -278,9 +281,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         w.begin = part.begin;
         w.end = part.end;
         w.more = 1;
+        break;
       }
-      if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
-        fail(ctl, a.status, 51);
+      if (!got) {
+        fail(ctl, a.status, 50);
         break;
       }
       if (lane == 0) {
@@ -290,11 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       at.next();
       if (!w.more) break;
-      if (w.begin == w.end) {
-        if (claimed.next(bounds)) continue;
-        fail(ctl, a.status, 50);
-        break;
-      }
+      if (w.begin == w.end) continue;
       const int row = static_cast<int>(w.row0);
       if (!warp_wait(&ctl->kept_empty[kept.slot], kept.phase ^ 1u, bounds)) {
         fail(ctl, a.status, 52);
@@ -332,10 +332,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         ring.next();
       }
       if (!ok) break;
-      if (!claimed.next(bounds)) {
-        fail(ctl, a.status, 50);
-        break;
-      }
     }
     claimed.finish(bounds);
     loads.drain(ctl);

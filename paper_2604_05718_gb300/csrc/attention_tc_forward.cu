@@ -204,11 +204,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       int q_loads = 0, kv_loads = 0;
       uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on kv_raw, and that barrier's phase
       bool ok = true;
-      for (;;) {
+      for (bool fresh = true;; fresh = false) {
+        if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
+          fail(ctl, a.status, 31);
+          break;
+        }
         Work w{};
-        if (claimed.more) {
+        bool got = fresh || claimed.next(bounds);
+        while (got && claimed.more) {
           const int64_t it = claimed.item;
-          claimed.ask();
           if (it == 0) {
             check_offsets(a.q_offsets, a.batch, a.q_rows, a.status, lane, 32);
             check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
@@ -216,9 +220,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
           if (tile.image < 0) {
-            if (claimed.next(bounds)) continue;
-            fail(ctl, a.status, 30);
-            break;
+            got = claimed.next(bounds);
+            continue;
           }
           const int64_t rest = it / slots;
           const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
@@ -232,9 +235,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           w.begin = part.begin;
           w.end = part.end;
           w.more = 1;
+          break;
         }
-        if (!warp_wait(&ctl->work_empty[at.slot], at.phase ^ 1u, bounds)) {
-          fail(ctl, a.status, 31);
+        if (!got) {
+          fail(ctl, a.status, 30);
           break;
         }
         if (lane == 0) {
@@ -244,11 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         at.next();
         if (!w.more) break;
-        if (w.begin == w.end) {
-          if (claimed.next(bounds)) continue;
-          fail(ctl, a.status, 30);
-          break;
-        }
+        if (w.begin == w.end) continue;
         const int row = static_cast<int>(w.row0), key = static_cast<int>(w.key0);
         if (!warp_wait(&ctl->q_empty[qs.slot], qs.phase ^ 1u, bounds)) {
           fail(ctl, a.status, 32);
@@ -286,10 +286,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++kv_loads;
         }
         if (!ok) break;
-        if (!claimed.next(bounds)) {
-          fail(ctl, a.status, 30);
-          break;
-        }
       }
       claimed.finish(bounds);
       {
