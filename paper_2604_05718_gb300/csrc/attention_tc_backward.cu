@@ -264,15 +264,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool got = fresh || claimed.next(bounds);
       while (got && claimed.more) {
         const int64_t it = claimed.item;
-        const Tile tile = tile_of<kRows>(off, a.batch, rows, it % slots);
+        const Tile tile = tile_of<kRows>(off, a.batch, rows, it / heads % slots);
         if (tile.image < 0) {
           got = claimed.next(bounds);
           continue;
         }
-        const int64_t rest = it / slots;
         const Span cols = DQ ? span_of(a.k_offsets, tile.image, a.k_rows) : span_of(a.q_offsets, tile.image, a.q_rows);
-        w.head = static_cast<int>(rest % heads);
-        w.split = static_cast<int>(rest / heads);
+        w.head = static_cast<int>(it % heads);
+        w.split = static_cast<int>(it / heads / slots);
         const Part part = part_of((cols.n + kRows - 1) / kRows * (DQ ? 1 : group), w.split, splits);
         w.row0 = tile.rows.lo + tile.first;
         w.col0 = cols.lo;

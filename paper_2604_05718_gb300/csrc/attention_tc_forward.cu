@@ -218,15 +218,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             check_offsets(a.k_offsets, a.batch, a.k_rows, a.status, lane, 32);
             __syncwarp();
           }
-          const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it % slots);
+          const Tile tile = tile_of<kItemRows>(a.q_offsets, a.batch, a.q_rows, it / a.q_heads % slots);
           if (tile.image < 0) {
             got = claimed.next(bounds);
             continue;
           }
-          const int64_t rest = it / slots;
           const Span keys = span_of(a.k_offsets, tile.image, a.k_rows);
-          w.head = static_cast<int>(rest % a.q_heads);
-          w.split = static_cast<int>(rest / a.q_heads);
+          w.head = static_cast<int>(it % a.q_heads);
+          w.split = static_cast<int>(it / a.q_heads / slots);
           const Part part = part_of((keys.n + kRows - 1) / kRows, w.split, a.splits);
           w.row0 = tile.rows.lo + tile.first;
           w.key0 = keys.lo;
