@@ -45,10 +45,10 @@ struct AttentionArgs {
   bool vec;                  // four elements of any row can be loaded at once
 };
 
-cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
+cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, cudaStream_t stream);
 cudaError_t launch_attention_backward_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 // bf16 whose rows and heads are 16-byte aligned, on the tensor cores.
-cudaError_t launch_attention_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream);
+cudaError_t launch_attention_tc(const AttentionArgs& a, cudaStream_t stream);
 // bf16, 16-byte aligned, head_dim a multiple of 8: blocks of `queries` queries, `cluster` blocks a sequence.
 cudaError_t launch_attention_few(const AttentionArgs& a, int queries, int cluster, cudaStream_t stream);
 cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream);

@@ -110,14 +110,39 @@ Plan plan_f32_backward(const Shape& s) {
           splits_for(s.k_rows, tile, s.kv_heads, s.q_rows * group, 64, s.batch, ways, 1)};
 }
 
-// The tensor-core kernels' tiles.  A part pays from eight tiles on: parts have to be
-// written and joined (2 x 577 tokens, 16 heads of 64, 13 us forward whole and 25 in
-// two; 8 x 100 queries, 8192 keys, 8 heads: 64 us in two parts, 56 in four).
-Plan plan_tc(const Shape& s) { return {splits_for(s.q_rows, 256, s.q_heads, s.k_rows, 128, s.batch, 2, 8), 1}; }
+// Parts of the tensor-core kernels' streamed side: the rounds of items over the SMs
+// times an item's length, and what writing and joining the parts costs, `launches` of
+// 4 us and every part's fp32 rows there and back at 4 TB/s.  A part has eight tiles
+// or more.  us of a tile: what the kernels take at head widths of 64 to 128.  (Against
+// as many parts as fill two blocks an SM: 4096 tokens, 8 heads of 128 forward whole 56
+// us, in two 72; 2 x 5000 and 1999 tokens, 8 heads of 128 on 2, gradients with keys in
+// three parts 782 us, whole 901; 24 x 100 queries, 1024 to 4096 keys, 8 heads of 32
+// whole 29 us, in two 38.)
+int parts_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_t batch, double tile_us, int launches,
+              int64_t values) {
+  const int64_t items = std::max((rows + tile - 1) / tile, std::min(batch, rows)) * heads;
+  const int64_t tiles = (stream / std::max<int64_t>(1, std::min(batch, stream)) + 127) / 128;
+  int best = 1;
+  double least = 0;
+  for (int parts = 1; parts == 1 || (parts <= mpm::kAttentionMaxSplits && parts * 8 <= tiles); ++parts) {
+    const int64_t rounds = (items * parts + kSms - 1) / kSms;
+    double us = static_cast<double>(rounds) * (static_cast<double>((tiles + parts - 1) / parts) * tile_us + 2);
+    if (parts > 1) us += 4 * launches + 2e-6 * static_cast<double>(values) * parts;
+    if (parts > 1 && us >= least) continue;
+    least = us;
+    best = parts;
+  }
+  return best;
+}
+Plan plan_tc(const Shape& s) {
+  // Of a lone tile of queries the even and the odd tiles of keys run side by side.
+  const double tile_us = s.q_rows <= int64_t{128} * s.batch ? 0.7 : 1.4;
+  return {parts_for(s.q_rows, 256, s.q_heads, s.k_rows, s.batch, tile_us, 1, s.q_rows * s.q_heads * s.dim), 1};
+}
 Plan plan_tc_backward(const Shape& s) {
   const int64_t group = s.q_heads / s.kv_heads;
-  return {splits_for(s.q_rows, 128, s.q_heads, s.k_rows, 128, s.batch, 2, 8),
-          splits_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, 128, s.batch, 2, 8)};
+  return {parts_for(s.q_rows, 128, s.q_heads, s.k_rows, s.batch, 1.6, 1, s.q_rows * s.q_heads * s.dim),
+          parts_for(s.k_rows, 128, s.kv_heads, s.q_rows * group, s.batch, 1.6, 2, 2 * s.k_rows * s.kv_heads * s.dim)};
 }
 // Few queries: blocks of 16 rows, of the heads that share a kv head.  Taken where
 // the sequences' queries are so few on the mean (a longer sequence takes several
@@ -276,8 +301,8 @@ mpm_status mpm_cross_attention(const void* q, int64_t q_row_stride, int64_t q_he
   a.vec = head_dim % 4 == 0 && vector_heads(hq, e, 4) && vector_heads(hk, e, 4) && vector_heads(hv, e, 4);
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
   cudaError_t err = few.queries > 0 ? mpm::launch_attention_few(a, few.queries, few.cluster, on)
-                    : tc            ? mpm::launch_attention_tc(a, sms, on)
-                                    : mpm::launch_attention_f32(a, dtype == MPM_BF16, sms, on);
+                    : tc            ? mpm::launch_attention_tc(a, on)
+                                    : mpm::launch_attention_f32(a, dtype == MPM_BF16, on);
   if (err == cudaSuccess && a.splits > 1) err = mpm::launch_attention_join(a, dtype == MPM_BF16, sms, on);
   return status_of(err);
 }

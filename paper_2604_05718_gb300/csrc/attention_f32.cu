@@ -21,11 +21,11 @@
 //
 // Bound: latencies of the arithmetic.  The registers of sums leave 8 to 12 warps an
 // SM, which issue in 44 % of the cycles and wait for their own results or for the tensor
-// cores' queue in the rest (for memory in a tenth); the tensor cores are 44 % busy, at
-// 135 of the 303 TFLOP/s that tf32 products alone reach here.  8 x 1024 tokens, 12
-// heads of 64: forward 572 us, 45 TFLOP/s of attention, gradients 1.93 ms (fma on the
+// cores' queue in the rest (for memory in a tenth); the tensor cores are half busy, at
+// 150 of the 303 TFLOP/s that tf32 products alone reach here.  8 x 1024 tokens, 12
+// heads of 64: forward 511 us, 50 TFLOP/s of attention, gradients 1.77 ms (fma on the
 // CUDA cores, 74 TFLOP/s at their peak: 826 us and 2.51 ms); 4 x 1024, 12 heads of 128:
-// 594 us and 1.89 ms (858 us, 2.62 ms).  Gradients of wide heads take tiles of 128 rows
+// 568 us and 1.91 ms (858 us, 2.62 ms).  Gradients of wide heads take tiles of 128 rows
 // and eight warps, as one block fills the shared memory (64 rows, four warps: 2.97 ms).
 //
 // Nothing outside a sequence enters a sum: rows past its end and masked keys are
@@ -459,24 +459,22 @@ __global__ void __launch_bounds__(32 * W, DP == 64 ? 2 : 1) attention_f32_dkv_ke
   }
 }
 
-// Launches with dynamic shared memory on as many blocks as are resident at once.
+// A block an item, as items differ in length: blocks that stay on their SM and take
+// items in turn lose a tenth and more (8 x 1024 tokens, 12 heads of 64: 577 us, 511 so;
+// 64 queries, 8192 keys, 8 heads: 70, 51).
 template <typename K>
-cudaError_t launch_tiles(K kernel, int warps, size_t smem, int64_t items, const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch_tiles(K kernel, int warps, size_t smem, int64_t items, const AttentionArgs& a, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  int each = 0;
-  e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, 32 * warps, smem);
-  if (e != cudaSuccess) return e;
-  const int64_t most = int64_t{num_sms} * (each < 1 ? 1 : each);
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < most ? items : most)), dim3(32 * warps), smem, stream, a);
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < INT32_MAX ? items : INT32_MAX)), dim3(32 * warps), smem, stream, a);
 }
 
 template <typename T, int DP>
-cudaError_t forward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t forward(const AttentionArgs& a, cudaStream_t stream) {
   constexpr int kWarps = 4, kRows = 16 * kWarps;
   constexpr size_t smem = sizeof(float) * Shape<DP>::kPitch * (kRows + 2 * kTile);
   const int64_t items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
-  return launch_tiles(attention_f32_kernel<T, DP, kWarps>, kWarps, smem, items, a, num_sms, stream);
+  return launch_tiles(attention_f32_kernel<T, DP, kWarps>, kWarps, smem, items, a, stream);
 }
 template <typename T, int DP>
 cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
@@ -488,12 +486,12 @@ cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
   constexpr bool bf16 = sizeof(T) == 2;
   cudaError_t e = launch_attention_delta(a, bf16, num_sms, stream);
   if (e == cudaSuccess && a.q_rows > 0) {
-    e = launch_tiles(attention_f32_dq_kernel<T, DP, kWarps>, kWarps, smem, q_items, a, num_sms, stream);
+    e = launch_tiles(attention_f32_dq_kernel<T, DP, kWarps>, kWarps, smem, q_items, a, stream);
     if (e == cudaSuccess && a.splits > 1)
       e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, bf16, num_sms, stream);
   }
   if (e == cudaSuccess && a.k_rows > 0) {
-    e = launch_tiles(attention_f32_dkv_kernel<T, DP, kWarps>, kWarps, smem, k_items, a, num_sms, stream);
+    e = launch_tiles(attention_f32_dkv_kernel<T, DP, kWarps>, kWarps, smem, k_items, a, stream);
     const int64_t each = a.k_rows * a.kv_heads * a.dim;
     if (e == cudaSuccess && a.key_splits > 1)
       e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, bf16, num_sms, stream);
@@ -506,9 +504,9 @@ cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {
-  if (bf16) return a.dim <= 64 ? forward<__nv_bfloat16, 64>(a, num_sms, stream) : forward<__nv_bfloat16, 128>(a, num_sms, stream);
-  return a.dim <= 64 ? forward<float, 64>(a, num_sms, stream) : forward<float, 128>(a, num_sms, stream);
+cudaError_t launch_attention_f32(const AttentionArgs& a, bool bf16, cudaStream_t stream) {
+  if (bf16) return a.dim <= 64 ? forward<__nv_bfloat16, 64>(a, stream) : forward<__nv_bfloat16, 128>(a, stream);
+  return a.dim <= 64 ? forward<float, 64>(a, stream) : forward<float, 128>(a, stream);
 }
 
 cudaError_t launch_attention_backward_f32(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream) {

@@ -175,13 +175,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // How a block's roles give up.  A role may wait for as long as a work item takes,
 // and that is as long as its sequence: 20 us are allowed for each of its tiles, ten
-// times what they take.
+// times what they take.  So are places of sequences without rows, passed at some us each.
 struct Bounds {
   volatile int failed;  // a wait ran out somewhere
   uint32_t limit_us;
   __device__ __forceinline__ void init(const AttentionArgs& a) {
     const uint64_t rows = static_cast<uint64_t>(a.q_rows) * (a.q_heads / a.kv_heads) + static_cast<uint64_t>(a.k_rows);
-    const uint64_t us = kWaitNs / 1000 + rows / kRows * 20;
+    const uint64_t empty = static_cast<uint64_t>(a.batch) * a.q_heads * (a.splits > a.key_splits ? a.splits : a.key_splits);
+    const uint64_t us = kWaitNs / 1000 + rows / kRows * 20 + empty / 16;
     failed = 0;
     limit_us = us < 0xFFFFFFFFu ? static_cast<uint32_t>(us) : 0xFFFFFFFFu;
   }

@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int H, bool DQ>
-cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch(const AttentionArgs& a, cudaStream_t stream) {
   CUtensorMap q, k, v, g;
   // A side without rows is never loaded from.
   if (a.q_rows > 0 && (!map_heads(&q, a.q, a.q_rows, a.q_heads, a.dim) || !map_heads(&g, a.d_out, a.q_rows, a.q_heads, a.dim)))
@@ -719,12 +719,12 @@ template <int H>
 cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
   cudaError_t e = launch_attention_delta(a, true, num_sms, stream);
   if (e == cudaSuccess && a.q_rows > 0) {
-    e = launch<H, true>(a, num_sms, stream);
+    e = launch<H, true>(a, stream);
     if (e == cudaSuccess && a.splits > 1)
       e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, true, num_sms, stream);
   }
   if (e == cudaSuccess && a.k_rows > 0) {
-    e = launch<H, false>(a, num_sms, stream);
+    e = launch<H, false>(a, stream);
     const int64_t each = a.k_rows * a.kv_heads * a.dim;
     if (e == cudaSuccess && a.key_splits > 1)
       e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, true, num_sms, stream);

@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int H>
-cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch(const AttentionArgs& a, cudaStream_t stream) {
   CUtensorMap q, k, v;
   if (!map_heads(&q, a.q, a.q_rows, a.q_heads, a.dim)) return cudaErrorInvalidValue;
   if (a.k_rows == 0) k = v = q;  // never loaded from
@@ -643,8 +643,8 @@ cudaError_t launch(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_attention_tc(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
-  return a.dim <= 64 ? launch<1>(a, num_sms, stream) : launch<2>(a, num_sms, stream);
+cudaError_t launch_attention_tc(const AttentionArgs& a, cudaStream_t stream) {
+  return a.dim <= 64 ? launch<1>(a, stream) : launch<2>(a, stream);
 }
 
 }  // namespace mpm
