@@ -56,9 +56,15 @@ cudaError_t launch_attention_backward_tc(const AttentionArgs& a, int num_sms, cu
 cudaError_t launch_attention_join(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 // delta from out and d_out.
 cudaError_t launch_attention_delta(const AttentionArgs& a, bool bf16, int num_sms, cudaStream_t stream);
-// Sums of parts: `values` per part, rounded once to out.
+// What parts are parts of: sequences in tiles of `tile` rows, `times` over.
+struct Streamed {
+  const int64_t* offsets;
+  int64_t rows;
+  int tile, times;
+};
+// Sums of the parts that a row's sequence has, rounded once to out.
 cudaError_t launch_attention_sum(const float* parts, int splits, int64_t rows, const int64_t* offsets, int batch, int heads,
-                                 int dim, void* out, bool bf16, int num_sms, cudaStream_t stream);
+                                 int dim, const Streamed& streamed, void* out, bool bf16, int num_sms, cudaStream_t stream);
 
 struct RotaryArgs {
   Heads x;

@@ -88,26 +88,28 @@ mpm_status check_shape(const Shape& s) {
   return MPM_OK;
 }
 
-// How many parts the streamed side of length `stream` (all sequences) is split
-// into, where `rows` rows of the other side, in tiles of `tile`, times `heads` are
-// the work: as many as fill `ways` blocks an SM, each of `least` tiles or more.
-// Lengths are known as means only.
-int splits_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_t stream_tile, int64_t batch, int64_t ways,
-               int64_t least) {
+// How many parts the fp32 kernels' streamed side of length `stream` (all sequences)
+// is split into, where `rows` rows of the other side, in tiles of `tile`, times `heads`
+// are the work: as many as fill `ways` blocks an SM, a tile of 64 each in a sequence of
+// four times the mean length, which is all that is known.  A shorter sequence's last
+// parts are not there and cost next to nothing (4 sequences of 1 to 785 keys, 6 heads:
+// forward and gradients 70 us, with as many parts as the mean has tiles 114).
+int splits_for(int64_t rows, int64_t tile, int64_t heads, int64_t stream, int64_t batch, int64_t ways) {
   const int64_t items = std::max((rows + tile - 1) / tile, std::min(batch, rows)) * heads;
   if (items == 0) return 1;
-  const int64_t tiles = (stream / std::max<int64_t>(1, std::min(batch, stream)) + stream_tile - 1) / stream_tile;
-  return static_cast<int>(std::max<int64_t>(1, std::min({kSms * ways / items, tiles / least, int64_t{mpm::kAttentionMaxSplits}})));
+  const int64_t mean = (stream / std::max<int64_t>(1, std::min(batch, stream)) + 63) / 64;
+  const int64_t most = mean <= 1 ? mean : std::min((stream + 63) / 64, 4 * mean);
+  return static_cast<int>(std::max<int64_t>(1, std::min({kSms * ways / items, most, int64_t{mpm::kAttentionMaxSplits}})));
 }
 struct Plan {
   int splits, key_splits;
 };
 // The fp32 kernels' tiles: streamed ones of 64 rows, their own of 64 too, but for gradients of wide heads.
-Plan plan_f32(const Shape& s) { return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, 64, s.batch, 4, 1), 1}; }
+Plan plan_f32(const Shape& s) { return {splits_for(s.q_rows, 64, s.q_heads, s.k_rows, s.batch, 4), 1}; }
 Plan plan_f32_backward(const Shape& s) {
   const int64_t group = s.q_heads / s.kv_heads, tile = s.dim <= 64 ? 64 : 128, ways = s.dim <= 64 ? 4 : 2;
-  return {splits_for(s.q_rows, tile, s.q_heads, s.k_rows, 64, s.batch, ways, 1),
-          splits_for(s.k_rows, tile, s.kv_heads, s.q_rows * group, 64, s.batch, ways, 1)};
+  return {splits_for(s.q_rows, tile, s.q_heads, s.k_rows, s.batch, ways),
+          splits_for(s.k_rows, tile, s.kv_heads, s.q_rows * group, s.batch, ways)};
 }
 
 // Parts of the tensor-core kernels' streamed side: the rounds of items over the SMs

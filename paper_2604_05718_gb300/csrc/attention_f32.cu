@@ -248,6 +248,12 @@ __global__ void __launch_bounds__(32 * W, DP == 64 ? 3 : 2) attention_f32_kernel
     const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
     const int kv = w.head / (a.q_heads / a.kv_heads);
     const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    if (part.begin == part.end && a.splits > 1) {  // a part that is not there
+      const int64_t rows = w.tile.rows.n - w.tile.first, row0 = w.tile.rows.lo + w.tile.first;
+      for (int r = threadIdx.x; r < kRows && r < rows; r += 32 * W)
+        a.partial_lse[static_cast<int64_t>(w.split) * a.q_rows * a.q_heads + (row0 + r) * a.q_heads + w.head] = -INFINITY;
+      continue;
+    }
     float acc[Shape<DP>::kFeatures][4] = {};
     float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
     __syncthreads();  // the last item's tiles have been read
@@ -336,6 +342,7 @@ __global__ void __launch_bounds__(32 * W, DP == 64 ? 3 : 1) attention_f32_dq_ker
     const Span ks = span_of(a.k_offsets, w.tile.image, a.k_rows);
     const int kv = w.head / (a.q_heads / a.kv_heads);
     const Part part = part_of((ks.n + kTile - 1) / kTile, w.split, a.splits);
+    if (part.begin == part.end && a.splits > 1) continue;
     const int64_t row0 = w.tile.rows.lo + w.tile.first;
     const int rows = w.tile.rows.n - w.tile.first;
     float acc[Shape<DP>::kFeatures][4] = {};
@@ -401,6 +408,7 @@ __global__ void __launch_bounds__(32 * W, DP == 64 ? 2 : 1) attention_f32_dkv_ke
     const Span qs = span_of(a.q_offsets, w.tile.image, a.q_rows);
     const int tiles = (qs.n + kTile - 1) / kTile;
     const Part part = part_of(tiles * group, w.split, a.key_splits);
+    if (part.begin == part.end && a.key_splits > 1) continue;
     const int64_t row0 = w.tile.rows.lo + w.tile.first;
     const int rows = w.tile.rows.n - w.tile.first;
     float dk[Shape<DP>::kFeatures][4] = {}, dv[Shape<DP>::kFeatures][4] = {};
@@ -484,19 +492,20 @@ cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
   const int64_t q_items = tile_slots<kRows>(a.q_offsets, a.batch, a.q_rows) * a.q_heads * a.splits;
   const int64_t k_items = tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
   constexpr bool bf16 = sizeof(T) == 2;
+  const Streamed keys{a.k_offsets, a.k_rows, kTile, 1}, queries{a.q_offsets, a.q_rows, kTile, a.q_heads / a.kv_heads};
   cudaError_t e = launch_attention_delta(a, bf16, num_sms, stream);
   if (e == cudaSuccess && a.q_rows > 0) {
     e = launch_tiles(attention_f32_dq_kernel<T, DP, kWarps>, kWarps, smem, q_items, a, stream);
     if (e == cudaSuccess && a.splits > 1)
-      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, bf16, num_sms, stream);
+      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, keys, a.d_q, bf16, num_sms, stream);
   }
   if (e == cudaSuccess && a.k_rows > 0) {
     e = launch_tiles(attention_f32_dkv_kernel<T, DP, kWarps>, kWarps, smem, k_items, a, stream);
     const int64_t each = a.k_rows * a.kv_heads * a.dim;
     if (e == cudaSuccess && a.key_splits > 1)
-      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, bf16, num_sms, stream);
+      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, queries, a.d_k, bf16, num_sms, stream);
     if (e == cudaSuccess && a.key_splits > 1)
-      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim,
+      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, queries,
                                a.d_v, bf16, num_sms, stream);
   }
   return e;

@@ -33,8 +33,11 @@ __global__ void __launch_bounds__(kRowThreads) attention_join_kernel(const Atten
     w[0] *= inv;
     w[1] *= inv;
     float v[kAttentionMaxDim / 32] = {};
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
+    // Up to the last part with a weight: those that a short sequence does not have come behind it and were not written.
+    const uint32_t low = __ballot_sync(0xFFFFFFFFu, w[0] != 0.f), high = __ballot_sync(0xFFFFFFFFu, w[1] != 0.f);
+    const int there = high != 0 ? 64 - __clz(high) : 32 - __clz(low);
+#pragma unroll 8
+    for (int s = 0; s < there; ++s) {
       const float f = __shfl_sync(0xFFFFFFFFu, s < 32 ? w[0] : w[1], s & 31);
       const float* p = a.partial + (s * all + r) * a.dim;
 #pragma unroll
@@ -104,18 +107,39 @@ __global__ void __launch_bounds__(kRowThreads) attention_delta_kernel(const Atte
   }
 }
 
-template <typename T>
+// N values a thread.
+template <typename T, int N>
 __global__ void __launch_bounds__(kRowThreads) attention_sum_kernel(const float* __restrict__ parts, int splits, int64_t rows,
                                                                  const int64_t* __restrict__ offsets, int batch, int width,
-                                                                 T* __restrict__ out) {
+                                                                 const Streamed streamed, T* __restrict__ out) {
   wait_for_previous_grid();
   allow_next_grid();
   const int64_t each = rows * width, live = live_rows(offsets, batch, rows) * width;
-  for (int64_t i = blockIdx.x * int64_t{kRowThreads} + threadIdx.x; i < live; i += gridDim.x * int64_t{kRowThreads}) {
-    float s = 0.f;
+  for (int64_t i = (blockIdx.x * int64_t{kRowThreads} + threadIdx.x) * N; i < live; i += gridDim.x * int64_t{kRowThreads} * N) {
+    const int64_t row = i <= UINT32_MAX ? static_cast<uint32_t>(i) / static_cast<uint32_t>(width) : i / width;
+    int b = 0;
+    for (int hi = offsets == nullptr ? 0 : batch - 1; b < hi;) {
+      const int mid = (b + hi + 1) >> 1;
+      if (__ldg(offsets + mid) <= row) b = mid; else hi = mid - 1;
+    }
+    // Parts without a tile were not written; they come last.
+    const int n = span_of(streamed.offsets, b, streamed.rows).n, tiles = (n + streamed.tile - 1) / streamed.tile * streamed.times;
+    const int there = tiles < splits ? tiles : splits;
+    float s[N] = {};
 #pragma unroll 4
-    for (int p = 0; p < splits; ++p) s += parts[p * each + i];
-    out[i] = from_f32<T>(s);
+    for (int p = 0; p < there; ++p) {
+      if constexpr (N == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(parts + p * each + i);
+        s[0] += v.x;
+        s[1] += v.y;
+        s[2] += v.z;
+        s[3] += v.w;
+      } else {
+        s[0] += parts[p * each + i];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) out[i + e] = from_f32<T>(s[e]);
   }
 }
 
@@ -138,13 +162,20 @@ cudaError_t launch_attention_delta(const AttentionArgs& a, bool bf16, int num_sm
 }
 
 cudaError_t launch_attention_sum(const float* parts, int splits, int64_t rows, const int64_t* offsets, int batch, int heads,
-                                 int dim, void* out, bool bf16, int num_sms, cudaStream_t stream) {
+                                 int dim, const Streamed& streamed, void* out, bool bf16, int num_sms, cudaStream_t stream) {
   const int width = heads * dim;
-  const int blocks = blocks_for((rows * width + kRowThreads - 1) / kRowThreads, int64_t{num_sms} * 8);
-  return bf16 ? launch_dependent(attention_sum_kernel<__nv_bfloat16>, dim3(blocks), dim3(kRowThreads), 0, stream, parts, splits, rows,
-                                 offsets, batch, width, static_cast<__nv_bfloat16*>(out))
-              : launch_dependent(attention_sum_kernel<float>, dim3(blocks), dim3(kRowThreads), 0, stream, parts, splits, rows, offsets,
-                                 batch, width, static_cast<float*>(out));
+  // Parts start at multiples of 256 bytes of the workspace, of rows * width values each.
+  const bool fours = width % 4 == 0;
+  const int blocks = blocks_for((rows * width / (fours ? 4 : 1) + kRowThreads - 1) / kRowThreads, int64_t{num_sms} * 8);
+  const auto launch = [&](auto kernel, auto* to) {
+    return launch_dependent(kernel, dim3(blocks), dim3(kRowThreads), 0, stream, parts, splits, rows, offsets, batch, width, streamed, to);
+  };
+  if (bf16) {
+    auto* to = static_cast<__nv_bfloat16*>(out);
+    return fours ? launch(attention_sum_kernel<__nv_bfloat16, 4>, to) : launch(attention_sum_kernel<__nv_bfloat16, 1>, to);
+  }
+  auto* to = static_cast<float*>(out);
+  return fours ? launch(attention_sum_kernel<float, 4>, to) : launch(attention_sum_kernel<float, 1>, to);
 }
 
 }  // namespace mpm

@@ -653,6 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t row = (w.row0 + r) * heads + w.head, rows = (DQ ? a.q_rows : a.k_rows) * heads;
       const uint32_t sums = tmem + lanes + sum_col + (DQ ? 0 : half * 128);
       const float f = DQ || half == 1 ? a.scale : 1.f;
+      if (w.begin == w.end && (DQ ? a.splits : a.key_splits) > 1) continue;  // a part that is not there
       for (int col = DQ ? 32 * half : 0; col < a.dim; col += DQ ? 64 : 32) {
         uint32_t v[32];
         if (w.begin != w.end) {
@@ -717,19 +718,20 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t stream) {
 
 template <int H>
 cudaError_t backward(const AttentionArgs& a, int num_sms, cudaStream_t stream) {
+  const Streamed keys{a.k_offsets, a.k_rows, kRows, 1}, queries{a.q_offsets, a.q_rows, kRows, a.q_heads / a.kv_heads};
   cudaError_t e = launch_attention_delta(a, true, num_sms, stream);
   if (e == cudaSuccess && a.q_rows > 0) {
     e = launch<H, true>(a, stream);
     if (e == cudaSuccess && a.splits > 1)
-      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, a.d_q, true, num_sms, stream);
+      e = launch_attention_sum(a.partial, a.splits, a.q_rows, a.q_offsets, a.batch, a.q_heads, a.dim, keys, a.d_q, true, num_sms, stream);
   }
   if (e == cudaSuccess && a.k_rows > 0) {
     e = launch<H, false>(a, stream);
     const int64_t each = a.k_rows * a.kv_heads * a.dim;
     if (e == cudaSuccess && a.key_splits > 1)
-      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, a.d_k, true, num_sms, stream);
+      e = launch_attention_sum(a.partial, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, queries, a.d_k, true, num_sms, stream);
     if (e == cudaSuccess && a.key_splits > 1)
-      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim,
+      e = launch_attention_sum(a.partial + a.key_splits * each, a.key_splits, a.k_rows, a.k_offsets, a.batch, a.kv_heads, a.dim, queries,
                                a.d_v, true, num_sms, stream);
   }
   return e;

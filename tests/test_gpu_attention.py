@@ -295,6 +295,26 @@ def test_given_workspaces_and_outputs(mpm):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [([100, 17, 1, 64], [785, 197, 1, 0]), ([4000, 1, 0, 5], [3000, 2, 77, 400]), ([1, 1, 1], [9000, 3, 0])],
+                         ids=["short", "long", "one"])
+def test_nothing_is_read_that_was_not_written(mpm, lengths, dtype):
+    """Workspaces full of NaN, where the sequences have unlike numbers of parts."""
+    t, g, off, _ = problem(*lengths, 4, 2, 64, dtype)
+    dev = {n: torch.tensor(o, device=DEV) for n, o in off.items()}
+    out, stats = mpm.cross_attention(**t, with_lse=True, **dev)
+    grads = mpm.cross_attention_backward(g, t["q"], t["k"], t["v"], out, stats, **dev)
+    ws, back = (mpm.cross_attention_workspace(t["q"], t["k"], batch=len(lengths[0]), backward=b) for b in (False, True))
+    for w in (ws, back):
+        if w is not None:
+            w.fill_(255)  # NaN in every type
+    again, _ = mpm.cross_attention(**t, workspace=ws, **dev)
+    assert torch.equal(out, again)
+    dirty = mpm.cross_attention_backward(g, t["q"], t["k"], t["v"], out, stats, workspace=back, **dev)
+    assert all(torch.equal(a, b) for a, b in zip(grads, dirty))
+    run_and_check(mpm, t, g, off, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("lengths", [([1], [2000]), ([300, 40], [280, 120])], ids=["few", "many"])
 def test_a_captured_graph_follows_its_inputs(mpm, lengths, dtype):
     """Lengths, tokens and masks of a later replay, while an eager call runs between."""
