@@ -19,8 +19,8 @@
 // 64: 640 us in one, 756 in two).
 //
 // Bound: the softmax warps' issue and the products, about even.  4 x 4096 queries, 8192
-// keys, 16 heads of 128 on 4: 3.10 ms, 887 TFLOP/s (of the formulas' five products);
-// 64 x 849 tokens, 12 heads of 64: 756 us, 470.
+// keys, 16 heads of 128 on 4: 3.11 ms, 870 TFLOP/s (of the formulas' five products);
+// 64 x 820 to 877 tokens, 12 heads of 64: 715 us, 500.
 //
 // The streamed tiles serve twice, with their features and with their rows along K.
 // Rows that belong to no sequence, and masked keys, are zeroed in shared memory
