@@ -19,8 +19,8 @@
 // 64: 640 us in one, 756 in two).
 //
 // Bound: the softmax warps' issue and the products, about even.  4 x 4096 queries, 8192
-// keys, 16 heads of 128 on 4: 3.11 ms, 870 TFLOP/s (of the formulas' five products);
-// 64 x 820 to 877 tokens, 12 heads of 64: 715 us, 500.
+// keys, 16 heads of 128 on 4: 2.83 ms, 960 TFLOP/s (of the formulas' five products);
+// 64 x 820 to 877 tokens, 12 heads of 64: 718 us, 490.
 //
 // The streamed tiles serve twice, with their features and with their rows along K.
 // Rows that belong to no sequence, and masked keys, are zeroed in shared memory
@@ -39,11 +39,16 @@ constexpr int kItems = 3;    // work items known ahead
 constexpr int kStats = 3;    // tiles of queries whose statistics are known ahead
 constexpr uint32_t kTmemCols = 512;
 
-template <int H>
+template <int H, bool DQ>
 struct Shape {
   static constexpr int kTileBytes = H * kBlockBytes;
   static constexpr int kKept = H == 1 ? 2 : 1;    // pairs of kept tiles
-  static constexpr int kSlots = H == 1 ? 8 : 4;   // streamed tiles
+  // Streamed tiles, keys or queries in one ring and values or d_out in the other.  d_q's
+  // keys serve the scores and, a tile later, the sums; its values only d_out.v.  (Two
+  // places for either: 4 x 4096 queries, 8192 keys, 16 heads of 128 on 4, all gradients
+  // 3.11 ms, 2.83 so.)
+  static constexpr int kFirsts = H == 1 ? 4 : DQ ? 3 : 2, kSeconds = H == 1 ? 4 : DQ ? 1 : 2;
+  static constexpr int kSlots = kFirsts + kSeconds;
   static constexpr int kStage = (2 * kKept + kSlots) * kTileBytes;  // the gradients on their way
   static constexpr int kSmem = kStage + kWorkWarps * kStageBytes;
 };
@@ -74,11 +79,12 @@ struct alignas(16) Control {
   __align__(16) float delta[kStats][kRows];
 };
 
-template <int H>
+template <int H, bool DQ>
 constexpr size_t smem_bytes() {
-  return 1024 + Shape<H>::kSmem + sizeof(Control);
+  return 1024 + Shape<H, DQ>::kSmem + sizeof(Control);
 }
-static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "a block's shared memory");
+static_assert(smem_bytes<1, true>() <= 227 * 1024 && smem_bytes<2, true>() <= 227 * 1024 && smem_bytes<2, false>() <= 227 * 1024,
+              "a block's shared memory");
 
 __device__ __forceinline__ void fail(Control* ctl, int32_t* status, int32_t role) {
   ctl->bounds.failed = 1;
@@ -118,9 +124,8 @@ __device__ __forceinline__ void keep32(uint32_t (&r)[32], uint32_t there, uint32
 constexpr uint32_t kApart = 64;  // the warps leave their words 64 columns apart, over d_out.v
 constexpr uint32_t kRest = 32;   // and behind them what their rounding left
 
-template <int H>
+template <typename W>
 __device__ __forceinline__ void init_control(Control* ctl, int work_readers, int stat_readers) {
-  using W = Shape<H>;
   for (int i = 0; i < W::kKept; ++i) {
     ptx::mbar_init(&ctl->kept_full[i], 1);
     ptx::mbar_init(&ctl->kept_empty[i], 1);
@@ -177,24 +182,25 @@ __device__ __forceinline__ bool put_stats(Control* ctl, RingPlace<kStats>& at, c
 }
 
 // How a block's loads stand, for the wait before it leaves: a role may have given up while they were under way.
-template <int H>
+template <typename W>
 struct Loads {
-  int kept = 0, streamed = 0;
+  int kept = 0, firsts = 0, seconds = 0;
   uint32_t raw_loaded = 0, raw_phase = 0;  // per slot: whether its last load is counted on raw, and that barrier's phase
   __device__ __forceinline__ void count(int slot, bool raw) {
     const uint32_t bit = 1u << slot;
     if (raw) raw_phase ^= bit;
     raw_loaded = raw ? raw_loaded | bit : raw_loaded & ~bit;
-    ++streamed;
+    if (slot < W::kFirsts) ++firsts;
+    else ++seconds;
   }
   __device__ __forceinline__ void drain(Control* ctl) const {
-    using W = Shape<H>;
     for (int s = 0; s < W::kKept; ++s) {
       const int n = (kept - s + W::kKept - 1) / W::kKept;
       if (n > 0) drain_wait(&ctl->kept_full[s], static_cast<uint32_t>(n - 1) & 1u);
     }
     for (int s = 0; s < W::kSlots; ++s) {
-      const int n = (streamed - s + W::kSlots - 1) / W::kSlots;
+      const int n = s < W::kFirsts ? (firsts - s + W::kFirsts - 1) / W::kFirsts
+                                   : (seconds - (s - W::kFirsts) + W::kSeconds - 1) / W::kSeconds;
       if (n <= 0) continue;
       // full and raw both complete once a use of the slot where the tile was zeroed; full alone otherwise.
       if (raw_loaded >> s & 1u) drain_wait(&ctl->raw[s], (raw_phase >> s & 1u) ^ 1u);
@@ -210,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     attention_tc_backward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_g,
                                  const AttentionArgs a, bool vec_out) {
-  using W = Shape<H>;
+  using W = Shape<H, DQ>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
   Control* ctl = reinterpret_cast<Control*>(smem + W::kSmem);
@@ -218,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   Bounds* bounds = &ctl->bounds;
 
   if (threadIdx.x == 0) {
-    init_control<H>(ctl, kWorkWarps + 3, kWorkWarps);
+    init_control<W>(ctl, kWorkWarps + 3, kWorkWarps);
     ctl->bounds.init(a);
     ptx::prefetch_tensor_map(&map_q);
     ptx::prefetch_tensor_map(&map_k);
@@ -247,8 +253,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------- work and loads ----------------
     RingPlace<kItems> at;
     RingPlace<W::kKept> kept;
-    RingPlace<W::kSlots> ring;
-    Loads<H> loads;
+    RingPlace<W::kFirsts> firsts;
+    RingPlace<W::kSeconds> seconds;
+    Loads<W> loads;
     bool ok = true;
     const int64_t* off = DQ ? a.q_offsets : a.k_offsets;
     const int64_t rows = DQ ? a.q_rows : a.k_rows;
@@ -315,20 +322,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool second = i % 2 != 0;
         // Sums run over the keys for d_q, over the queries of both streamed tensors for d_k and d_v.
         const bool raw = ragged(t, w.cols, DQ ? a.mask : nullptr) && !(DQ && second);
-        if (!warp_wait(&ctl->empty[ring.slot], ring.phase ^ 1u, bounds)) {
+        const int slot = second ? W::kFirsts + seconds.slot : firsts.slot;
+        if (!warp_wait(&ctl->empty[slot], (second ? seconds.phase : firsts.phase) ^ 1u, bounds)) {
           fail(ctl, a.status, 53);
           ok = false;
           break;
         }
-        uint64_t* bar = raw ? &ctl->raw[ring.slot] : &ctl->full[ring.slot];
+        uint64_t* bar = raw ? &ctl->raw[slot] : &ctl->full[slot];
         if (ptx::elect_one()) {
           ptx::mbar_arrive_expect_tx(bar, W::kTileBytes);
-          load_rows<H>(ring0 + ring.slot * W::kTileBytes, DQ ? (second ? &map_v : &map_k) : (second ? &map_g : &map_q), bar,
+          load_rows<H>(ring0 + slot * W::kTileBytes, DQ ? (second ? &map_v : &map_k) : (second ? &map_g : &map_q), bar,
                        head, static_cast<int>(w.col0) + t * kRows);
         }
         __syncwarp();
-        loads.count(ring.slot, raw);
-        ring.next();
+        loads.count(slot, raw);
+        if (second) seconds.next();
+        else firsts.next();
       }
       if (!ok) break;
     }
@@ -337,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == kZeroWarp) {
     // ---------------- rows that a sum must not see ----------------
     RingPlace<kItems> at;
-    RingPlace<W::kSlots> ring;
+    RingPlace<W::kFirsts> firsts;
+    RingPlace<W::kSeconds> seconds;
     uint32_t raw_phase = 0;
     Work w;
     bool ok = true;
@@ -353,18 +363,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int t = DQ ? i / 2 : i / 2 % tiles;
         const uint8_t* mask = DQ ? a.mask : nullptr;
         if (ragged(t, w.cols, mask) && !(DQ && i % 2 != 0)) {
+          const int slot = i % 2 != 0 ? W::kFirsts + seconds.slot : firsts.slot;
           const uint4 there = rows_there(cols, t * kRows, mask);
-          if (!warp_wait(&ctl->raw[ring.slot], raw_phase >> ring.slot & 1u, bounds)) {
+          if (!warp_wait(&ctl->raw[slot], raw_phase >> slot & 1u, bounds)) {
             fail(ctl, a.status, 55);
             ok = false;
             break;
           }
-          raw_phase ^= 1u << ring.slot;
-          zero_rows<H>(smem + kRing + ring.slot * W::kTileBytes, there);
-          if (lane == 0) ptx::mbar_arrive(&ctl->full[ring.slot]);
+          raw_phase ^= 1u << slot;
+          zero_rows<H>(smem + kRing + slot * W::kTileBytes, there);
+          if (lane == 0) ptx::mbar_arrive(&ctl->full[slot]);
           __syncwarp();
         }
-        ring.next();
+        if (i % 2 != 0) seconds.next();
+        else firsts.next();
       }
     }
   } else if (warp == kStatWarp) {
@@ -392,7 +404,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------- products ----------------
     RingPlace<kItems> at;
     RingPlace<W::kKept> kept;
-    RingPlace<W::kSlots> ring;
+    RingPlace<W::kFirsts> x;    // of the tile whose sums come next
+    RingPlace<W::kSeconds> y;
     uint32_t free_phase = 1, p_phase = 0, ds_phase[2] = {0, 0};  // the first tile finds the scores' columns free
     const int slices = (a.dim + 15) / 16;
     const uint32_t weighted = by_rows(16 * slices);
@@ -415,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       // Scores and d_out.v of tile t; `last`: the kept tiles are not read after these.
-      auto scores = [&](const RingPlace<W::kSlots>& x) {
+      auto scores = [&](const RingPlace<W::kFirsts>& x) {
         if (!warp_wait(&ctl->full[x.slot], x.phase, bounds)) return false;
         if (DQ) {
           if (!warp_wait(&ctl->s_free, free_phase, bounds)) return false;
@@ -429,26 +442,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         return true;
       };
-      auto seconds = [&](const RingPlace<W::kSlots>& y, int t) {
-        if (!warp_wait(&ctl->full[y.slot], y.phase, bounds)) return false;
+      auto seconds = [&](const RingPlace<W::kSeconds>& y, int t) {
+        if (!warp_wait(&ctl->full[W::kFirsts + y.slot], y.phase, bounds)) return false;
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) {
-          mma_scores<H>(tmem0 + t_col + (DQ ? (t & 1) * 128 : 0), mine + W::kTileBytes, ring0 + y.slot * W::kTileBytes, slices);
+          mma_scores<H>(tmem0 + t_col + (DQ ? (t & 1) * 128 : 0), mine + W::kTileBytes, ring0 + (W::kFirsts + y.slot) * W::kTileBytes, slices);
           commit_at(at_bar(offsetof(Control, t_full), DQ ? t & 1 : 0));
-          if (DQ) commit_at(at_bar(offsetof(Control, empty), y.slot));
+          if (DQ) commit_at(at_bar(offsetof(Control, empty), W::kFirsts + y.slot));
           if (t + 1 == end) commit_at(at_bar(offsetof(Control, kept_empty), kept.slot));
         }
         __syncwarp();
         return true;
       };
-      RingPlace<W::kSlots> x = ring, y = ring;
-      y.next();
       ok = scores(x) && seconds(y, begin);
       for (int t = begin; ok && t < end; ++t) {
         const bool last = t + 1 == end;
-        RingPlace<W::kSlots> x1 = y, y1;
+        RingPlace<W::kFirsts> x1 = x;
+        RingPlace<W::kSeconds> y1 = y;
         x1.next();
-        y1 = x1;
         y1.next();
         if constexpr (DQ) {
           if (!last) ok = scores(x1) && seconds(y1, t + 1);
@@ -471,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           p_phase ^= 1u;
           ptx::tc_fence_after_sync();
           if (ptx::elect_one())
-            mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + y.slot * W::kTileBytes, weighted, t != begin);
+            mma_weighted(tmem0 + sum_col, tmem0 + score_col, kApart, ring0 + (W::kFirsts + y.slot) * W::kTileBytes, weighted, t != begin);
           __syncwarp();
           if (!last) ok = scores(x1);
           ok = ok && warp_wait(&ctl->ds_full[0], ds_phase[0], bounds);
@@ -482,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col + kRest, kApart, ring0 + x.slot * W::kTileBytes, weighted, t != begin);
             mma_weighted(tmem0 + sum_col + 128, tmem0 + t_col, kApart, ring0 + x.slot * W::kTileBytes, weighted, true);
             commit_at(at_bar(offsetof(Control, empty), x.slot));
-            commit_at(at_bar(offsetof(Control, empty), y.slot));
+            commit_at(at_bar(offsetof(Control, empty), W::kFirsts + y.slot));
             if (last) commit_at(at_bar(offsetof(Control, sum_done), 0));
           }
           __syncwarp();
@@ -495,7 +506,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         fail(ctl, a.status, 60);
         break;
       }
-      ring = x;
       kept.next();
     }
     if (ptx::elect_one()) ptx::mma_commit(&ctl->drain);
@@ -704,7 +714,7 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t stream) {
   const uint64_t bit = 1ull << (dev & 63);
   const auto kernel = attention_tc_backward_kernel<H, DQ>;
   if (!(attr_done.load() & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<H>()));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<H, DQ>()));
     if (e != cudaSuccess) return e;
     attr_done.fetch_or(bit);
   }
@@ -712,7 +722,7 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t stream) {
                            : tile_slots<kRows>(a.k_offsets, a.batch, a.k_rows) * a.kv_heads * a.key_splits;
   const uintptr_t outs = DQ ? reinterpret_cast<uintptr_t>(a.d_q)
                             : reinterpret_cast<uintptr_t>(a.d_k) | reinterpret_cast<uintptr_t>(a.d_v);
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < kMaxBlocks ? items : kMaxBlocks)), dim3(kThreads), smem_bytes<H>(),
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(items < kMaxBlocks ? items : kMaxBlocks)), dim3(kThreads), smem_bytes<H, DQ>(),
                           stream, q, k, v, g, a, a.dim % 8 == 0 && outs % 16 == 0);
 }
 
