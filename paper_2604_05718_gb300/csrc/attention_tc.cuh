@@ -246,7 +246,7 @@ struct ClaimedItems {
   }
   // Before the block leaves: an answer under way has come, and after a failure nobody starts on what is left.
   __device__ __forceinline__ void finish(Bounds* bounds) {
-    while (asked != answered || (bounds->failed && more)) {
+    while (asked != answered || (__any_sync(0xFFFFFFFFu, bounds->failed != 0) && more)) {
       ask();
       if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(&claims->bar[answered & 1u], answered >> 1 & 1u, nullptr, kWaitNs))) return;
       take();
